@@ -83,6 +83,59 @@ dipaco_status dipaco_k_attention_bwd(int32_t dtype, const void* qkv, const void*
                                      void* dqkv, float* dsum, float* colsum_out, float* colsum_scratch, int32_t B,
                                      int32_t S, int32_t H, int32_t dh, void* stream);
 
+/* Causal softmax attention with a sliding window and sinks.  Position i of a document sees position j where j <= i and
+ * (j > i - window or j < sinks): the last `window` positions, itself included, and the first `sinks` of the document.
+ * window >= 1 (one that covers the sequence is plain causal attention), sinks >= 0.
+ *   qkv [B*S, (H + 2*H_kv)*dh], row = q | k | v; H is a multiple of H_kv, and query head h reads key and value head
+ *   h / (H / H_kv).  dh in {32, 64, 128}.  o [B*S, H*dh];  lse fp32 [B, H, S] = log of the sum of exp(q_i.k_j / sqrt(dh))
+ *   over the positions that i sees.
+ *   lengths: NULL, or device int32 [B]: document b is the first lengths[b] of its S rows (taken as 0 below 0, as S above).
+ *   Rows behind it are padding: they are not read, whatever they hold, and o, lse and dqkv are written 0 there.
+ * A value that is not finite reaches exactly the rows that see it.  B * S < 2^31, H * S <= 2^25,
+ * (H + 2*H_kv) * dh <= 2^20.  Results are bit-reproducible. */
+dipaco_status dipaco_k_attention_window_fwd(int32_t dtype, const void* qkv, const int32_t* lengths, void* o, float* lse,
+                                            int32_t B, int32_t S, int32_t H, int32_t H_kv, int32_t dh, int32_t window,
+                                            int32_t sinks, void* stream);
+
+/* Gradient of the above: d_o [B*S, H*dh] -> dqkv [B*S, (H + 2*H_kv)*dh], from the o and lse that it left; the gradients of a
+ * key or value head are the sums over the query heads that read it.  dsum: fp32 scratch of 2 * B * H * S128 floats,
+ * S128 = S rounded up to a multiple of 128.  dqkv must not overlap the inputs. */
+dipaco_status dipaco_k_attention_window_bwd(int32_t dtype, const void* qkv, const int32_t* lengths, const void* o,
+                                            const void* d_o, const float* lse, void* dqkv, float* dsum, int32_t B, int32_t S,
+                                            int32_t H, int32_t H_kv, int32_t dh, int32_t window, int32_t sinks, void* stream);
+
+/* A paged cache of keys and values, for documents that are read or written in pieces.
+ *   cache      dtype [n_pages, 2, H_kv, page_size, dh], keys then values; page_size in {16, 32, 64, 128, 256}.
+ *   pages      device int32 [B, pages_per_doc]: position p of document b is slot p % page_size of page
+ *              pages[b, p / page_size].  An entry outside [0, n_pages) is no page: nothing is written for its positions and
+ *              nobody sees them (pages that a window has left behind can be handed back).  Documents may share pages that
+ *              are only read; a page that a call writes to belongs to one document.
+ *   qkv        the new tokens, [T, (H + 2*H_kv)*dh], row = q | k | v.
+ *   row_start  device int32 [B + 1], not decreasing, 0 .. T: rows row_start[b] .. row_start[b+1] - 1 are the new tokens
+ *              of document b, none or more.  Rows behind row_start[B] belong to nobody.
+ *   cache_len  device int32 [B]: positions that document b had in front of them: its first new token is position
+ *              cache_len[b].  All of these are read on the device: a captured graph follows their values.
+ * T * H <= 2^25, B <= 2^20, pages_per_doc * page_size <= 2^28.
+ * dipaco_k_cache_append writes the new tokens' keys and values into the pages. */
+dipaco_status dipaco_k_cache_append(int32_t dtype, const void* qkv, const int32_t* row_start, const int32_t* cache_len,
+                                    const int32_t* pages, void* cache, int32_t T, int32_t B, int32_t H, int32_t H_kv,
+                                    int32_t dh, int32_t n_pages, int32_t page_size, int32_t pages_per_doc, void* stream);
+
+/* Attention of the new tokens over the cache that they have been appended to (same row_start and cache_len), with the window
+ * and sinks of dipaco_k_attention_window_fwd over positions: chunk by chunk, or token by token, the rows of that call.
+ *   o [T, H*dh];  lse fp32 [T, H] or NULL.  A row that sees nothing (its pages are gone): o = 0, lse = -inf.  Rows of nobody
+ *   are left as they were.  max_new: no document has more new tokens in this call (rows beyond it are left as they were).
+ * workspace: device, >= dipaco_k_attention_paged_workspace_bytes(...) (0 = invalid shape), contents undefined before and
+ * after; calls that may overlap in time, captured ones included, need one each.  A value that is not finite reaches exactly
+ * the rows that see it.  Results are bit-reproducible; those of one row may differ in rounding with the other rows of the call. */
+size_t dipaco_k_attention_paged_workspace_bytes(int32_t T, int32_t B, int32_t max_new, int32_t H, int32_t H_kv, int32_t dh,
+                                                int32_t page_size, int32_t pages_per_doc);
+dipaco_status dipaco_k_attention_paged(int32_t dtype, const void* qkv, const int32_t* row_start, const int32_t* cache_len,
+                                       const int32_t* pages, const void* cache, void* o, float* lse, int32_t T, int32_t B,
+                                       int32_t max_new, int32_t H, int32_t H_kv, int32_t dh, int32_t n_pages,
+                                       int32_t page_size, int32_t pages_per_doc, int32_t window, int32_t sinks,
+                                       void* workspace, size_t workspace_bytes, void* stream);
+
 /* Measurement aid, no part of the method: register-only loops that show how the matrix cores and the vector ALU of a
  * SIMD share instruction issue (the inner loops of the attention kernels are priced with it).  One workgroup of
  * 256 * waves_per_simd threads per compute unit (256 workgroups) runs `iters` iterations of

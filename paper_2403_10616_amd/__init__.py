@@ -100,6 +100,11 @@ _SIGS = {
     "dipaco_k_attention_fwd": (C.c_int, [C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32,
                                          C.c_int32, C.c_void_p]),
     "dipaco_k_attention_bwd": (C.c_int, [C.c_int32] + [C.c_void_p] * 8 + [C.c_int32] * 4 + [C.c_void_p]),
+    "dipaco_k_attention_window_fwd": (C.c_int, [C.c_int32] + [C.c_void_p] * 4 + [C.c_int32] * 7 + [C.c_void_p]),
+    "dipaco_k_attention_window_bwd": (C.c_int, [C.c_int32] + [C.c_void_p] * 7 + [C.c_int32] * 7 + [C.c_void_p]),
+    "dipaco_k_cache_append": (C.c_int, [C.c_int32] + [C.c_void_p] * 5 + [C.c_int32] * 8 + [C.c_void_p]),
+    "dipaco_k_attention_paged_workspace_bytes": (C.c_size_t, [C.c_int32] * 8),
+    "dipaco_k_attention_paged": (C.c_int, [C.c_int32] + [C.c_void_p] * 7 + [C.c_int32] * 11 + [C.c_void_p, C.c_size_t, C.c_void_p]),
 }
 
 EXPORTS = tuple(_SIGS)
@@ -439,3 +444,35 @@ def dipaco_k_attention_bwd(dtype: int, qkv, o, d_o, lse, dqkv, dsum, B: int, S: 
                            colsum_out=None, colsum_scratch=None):
     _check(load().dipaco_k_attention_bwd(dtype, _ptr(qkv), _ptr(o), _ptr(d_o), _ptr(lse), _ptr(dqkv), _ptr(dsum),
                                          _ptr(colsum_out), _ptr(colsum_scratch), B, S, H, dh, _stream(stream)))
+
+
+def dipaco_k_attention_window_fwd(dtype: int, qkv, lengths, o, lse, B: int, S: int, H: int, H_kv: int, dh: int, window: int,
+                                  sinks: int, stream=None):
+    _check(load().dipaco_k_attention_window_fwd(dtype, _ptr(qkv), _ptr(lengths), _ptr(o), _ptr(lse), B, S, H, H_kv, dh, window,
+                                                sinks, _stream(stream)))
+
+
+def dipaco_k_attention_window_bwd(dtype: int, qkv, lengths, o, d_o, lse, dqkv, dsum, B: int, S: int, H: int, H_kv: int, dh: int,
+                                  window: int, sinks: int, stream=None):
+    _check(load().dipaco_k_attention_window_bwd(dtype, _ptr(qkv), _ptr(lengths), _ptr(o), _ptr(d_o), _ptr(lse), _ptr(dqkv),
+                                                _ptr(dsum), B, S, H, H_kv, dh, window, sinks, _stream(stream)))
+
+
+def dipaco_k_cache_append(dtype: int, qkv, row_start, cache_len, pages, cache, T: int, B: int, H: int, H_kv: int, dh: int,
+                          n_pages: int, page_size: int, pages_per_doc: int, stream=None):
+    _check(load().dipaco_k_cache_append(dtype, _ptr(qkv), _ptr(row_start), _ptr(cache_len), _ptr(pages), _ptr(cache), T, B, H,
+                                        H_kv, dh, n_pages, page_size, pages_per_doc, _stream(stream)))
+
+
+def dipaco_k_attention_paged_workspace_bytes(T: int, B: int, max_new: int, H: int, H_kv: int, dh: int, page_size: int,
+                                             pages_per_doc: int) -> int:
+    return int(load().dipaco_k_attention_paged_workspace_bytes(T, B, max_new, H, H_kv, dh, page_size, pages_per_doc))
+
+
+def dipaco_k_attention_paged(dtype: int, qkv, row_start, cache_len, pages, cache, o, lse, T: int, B: int, max_new: int, H: int,
+                             H_kv: int, dh: int, n_pages: int, page_size: int, pages_per_doc: int, window: int, sinks: int,
+                             workspace, stream=None):
+    _check(load().dipaco_k_attention_paged(dtype, _ptr(qkv), _ptr(row_start), _ptr(cache_len), _ptr(pages), _ptr(cache), _ptr(o),
+                                           _ptr(lse), T, B, max_new, H, H_kv, dh, n_pages, page_size, pages_per_doc, window,
+                                           sinks, _ptr(workspace), workspace.numel() * workspace.element_size(),
+                                           _stream(stream)))

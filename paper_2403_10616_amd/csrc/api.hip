@@ -376,6 +376,43 @@ static dipaco_status check_ptr(const void* p, const char* name) {
   return DIPACO_OK;
 }
 
+// ---- window and paged attention --------------------------------------------------------------------------
+static dipaco_status check_heads(int32_t dtype, int32_t H, int32_t H_kv, int32_t dh) {
+  if (dtype != DIPACO_F32 && dtype != DIPACO_BF16) return fail(DIPACO_EINVAL, "dtype must be DIPACO_F32 or DIPACO_BF16");
+  if (H < 1 || H_kv < 1) return fail(DIPACO_EINVAL, "H and H_kv must be positive");
+  if (H % H_kv != 0) return fail(DIPACO_ESHAPE, "H must be a multiple of H_kv");
+  if (dh != 32 && dh != 64 && dh != 128) return fail(DIPACO_ESHAPE, "d_head must be 32, 64 or 128");
+  if ((int64_t)(H + 2 * (int64_t)H_kv) * dh > (1 << 20)) return fail(DIPACO_ESHAPE, "a row of q | k | v may hold 2^20 elements");
+  return DIPACO_OK;
+}
+static dipaco_status check_window(int32_t window, int32_t sinks) {
+  if (window < 1 || sinks < 0) return fail(DIPACO_EINVAL, "window >= 1 and sinks >= 0 required");
+  return DIPACO_OK;
+}
+static dipaco_status check_padded(int32_t B, int32_t S, int32_t H) {
+  if (B < 1 || S < 1) return fail(DIPACO_EINVAL, "B and S must be positive");
+  if ((int64_t)B * S >= (1LL << 31) || (int64_t)H * S > (1LL << 25)) return fail(DIPACO_ESHAPE, "B * S < 2^31 and H * S <= 2^25 required");
+  return DIPACO_OK;
+}
+
+static dipaco_status check_cache(int32_t T, int32_t B, int32_t H, int32_t n_pages, int32_t page_size, int32_t pages_per_doc) {
+  if (T < 0 || B < 1 || n_pages < 1 || pages_per_doc < 1) return fail(DIPACO_EINVAL, "T >= 0, B >= 1, n_pages >= 1 and pages_per_doc >= 1 required");
+  if (page_size != 16 && page_size != 32 && page_size != 64 && page_size != 128 && page_size != 256)
+    return fail(DIPACO_ESHAPE, "page_size must be 16, 32, 64, 128 or 256");
+  if ((int64_t)T * H > (1LL << 25) || B > (1 << 20)) return fail(DIPACO_ESHAPE, "T * H <= 2^25 and B <= 2^20 required");
+  if ((int64_t)pages_per_doc * page_size > (1 << 28)) return fail(DIPACO_ESHAPE, "a document may hold 2^28 positions");
+  return DIPACO_OK;
+}
+template <typename T>
+static PagedArgs<T> paged_args(const void* qkv, const int32_t* row_start, const int32_t* cache_len, const int32_t* pages, const void* cache, void* o,
+                               float* lse, int32_t rows, int32_t B, int32_t max_new, int32_t H, int32_t H_kv, int32_t n_pages, int32_t page_size,
+                               int32_t pages_per_doc, Window w) {
+  int shift = 4;
+  while ((1 << shift) < page_size) ++shift;
+  return {static_cast<const T*>(qkv), row_start, cache_len, pages, const_cast<T*>(static_cast<const T*>(cache)), static_cast<T*>(o), lse, rows, B,
+          max_new, H, H_kv, n_pages, shift, pages_per_doc, w};
+}
+
 }  // namespace dipaco
 
 // ==========================================================================================================
@@ -1067,6 +1104,85 @@ dipaco_status dipaco_k_attention_bwd(int32_t dtype, const void* qkv, const void*
              : launch_attention_bwd<float>(static_cast<const float*>(qkv), static_cast<const float*>(o),
                                            static_cast<const float*>(d_o), lse, static_cast<float*>(dqkv), dsum, colsum_out,
                                            colsum_scratch, B, S, H, dh, st, nullptr, true);
+}
+
+// ---- window and paged attention --------------------------------------------------------------------------
+dipaco_status dipaco_k_attention_window_fwd(int32_t dtype, const void* qkv, const int32_t* lengths, void* o, float* lse, int32_t B, int32_t S,
+                                            int32_t H, int32_t H_kv, int32_t dh, int32_t window, int32_t sinks, void* stream) {
+  TRY(check_heads(dtype, H, H_kv, dh));
+  TRY(check_window(window, sinks));
+  TRY(check_padded(B, S, H));
+  TRY(check_ptr(qkv, "qkv")); TRY(check_ptr(o, "o")); TRY(check_ptr(lse, "lse"));
+  if (lengths) TRY(check_ptr(lengths, "lengths"));
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const Window w{window, sinks};
+  return dtype == DIPACO_BF16
+             ? launch_window_fwd<bf16>(static_cast<const bf16*>(qkv), lengths, static_cast<bf16*>(o), lse, B, S, H, H_kv, dh, w, st)
+             : launch_window_fwd<float>(static_cast<const float*>(qkv), lengths, static_cast<float*>(o), lse, B, S, H, H_kv, dh, w, st);
+}
+
+dipaco_status dipaco_k_attention_window_bwd(int32_t dtype, const void* qkv, const int32_t* lengths, const void* o, const void* d_o, const float* lse,
+                                            void* dqkv, float* dsum, int32_t B, int32_t S, int32_t H, int32_t H_kv, int32_t dh, int32_t window,
+                                            int32_t sinks, void* stream) {
+  TRY(check_heads(dtype, H, H_kv, dh));
+  TRY(check_window(window, sinks));
+  TRY(check_padded(B, S, H));
+  TRY(check_ptr(qkv, "qkv")); TRY(check_ptr(o, "o")); TRY(check_ptr(d_o, "d_o")); TRY(check_ptr(lse, "lse"));
+  TRY(check_ptr(dqkv, "dqkv")); TRY(check_ptr(dsum, "dsum"));
+  if (lengths) TRY(check_ptr(lengths, "lengths"));
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const Window w{window, sinks};
+  return dtype == DIPACO_BF16
+             ? launch_window_bwd<bf16>(static_cast<const bf16*>(qkv), lengths, static_cast<const bf16*>(o), static_cast<const bf16*>(d_o), lse,
+                                       static_cast<bf16*>(dqkv), dsum, B, S, H, H_kv, dh, w, st)
+             : launch_window_bwd<float>(static_cast<const float*>(qkv), lengths, static_cast<const float*>(o), static_cast<const float*>(d_o), lse,
+                                        static_cast<float*>(dqkv), dsum, B, S, H, H_kv, dh, w, st);
+}
+
+dipaco_status dipaco_k_cache_append(int32_t dtype, const void* qkv, const int32_t* row_start, const int32_t* cache_len, const int32_t* pages,
+                                    void* cache, int32_t T, int32_t B, int32_t H, int32_t H_kv, int32_t dh, int32_t n_pages, int32_t page_size,
+                                    int32_t pages_per_doc, void* stream) {
+  TRY(check_heads(dtype, H, H_kv, dh));
+  TRY(check_cache(T, B, H, n_pages, page_size, pages_per_doc));
+  if (T == 0) return DIPACO_OK;
+  TRY(check_ptr(qkv, "qkv")); TRY(check_ptr(row_start, "row_start")); TRY(check_ptr(cache_len, "cache_len")); TRY(check_ptr(pages, "pages"));
+  TRY(check_ptr(cache, "cache"));
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const Window all{1, 0};
+  return dtype == DIPACO_BF16
+             ? launch_cache_append(paged_args<bf16>(qkv, row_start, cache_len, pages, cache, nullptr, nullptr, T, B, T, H, H_kv, n_pages, page_size,
+                                                    pages_per_doc, all), dh, st)
+             : launch_cache_append(paged_args<float>(qkv, row_start, cache_len, pages, cache, nullptr, nullptr, T, B, T, H, H_kv, n_pages, page_size,
+                                                     pages_per_doc, all), dh, st);
+}
+
+size_t dipaco_k_attention_paged_workspace_bytes(int32_t T, int32_t B, int32_t max_new, int32_t H, int32_t H_kv, int32_t dh, int32_t page_size,
+                                                int32_t pages_per_doc) {
+  if (check_heads(DIPACO_F32, H, H_kv, dh) != DIPACO_OK || check_cache(T, B, H, 1, page_size, pages_per_doc) != DIPACO_OK || max_new < 0) return 0;
+  return paged_workspace_bytes(T, B, max_new, H, H_kv, dh, page_size, pages_per_doc);
+}
+
+dipaco_status dipaco_k_attention_paged(int32_t dtype, const void* qkv, const int32_t* row_start, const int32_t* cache_len, const int32_t* pages,
+                                       const void* cache, void* o, float* lse, int32_t T, int32_t B, int32_t max_new, int32_t H, int32_t H_kv,
+                                       int32_t dh, int32_t n_pages, int32_t page_size, int32_t pages_per_doc, int32_t window, int32_t sinks,
+                                       void* workspace, size_t workspace_bytes, void* stream) {
+  TRY(check_heads(dtype, H, H_kv, dh));
+  TRY(check_cache(T, B, H, n_pages, page_size, pages_per_doc));
+  TRY(check_window(window, sinks));
+  if (max_new < 0) return fail(DIPACO_EINVAL, "max_new >= 0 required");
+  if (T == 0 || max_new == 0) return DIPACO_OK;
+  TRY(check_ptr(qkv, "qkv")); TRY(check_ptr(row_start, "row_start")); TRY(check_ptr(cache_len, "cache_len")); TRY(check_ptr(pages, "pages"));
+  TRY(check_ptr(cache, "cache")); TRY(check_ptr(o, "o")); TRY(check_ptr(workspace, "workspace"));
+  if (lse) TRY(check_ptr(lse, "lse"));
+  if (workspace_bytes < paged_workspace_bytes(T, B, max_new, H, H_kv, dh, page_size, pages_per_doc))
+    return fail(DIPACO_EWORKSPACE, "workspace smaller than dipaco_k_attention_paged_workspace_bytes");
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const Window w{window, sinks};
+  return dtype == DIPACO_BF16
+             ? launch_attention_paged(paged_args<bf16>(qkv, row_start, cache_len, pages, cache, o, lse, T, B, max_new, H, H_kv, n_pages, page_size,
+                                                       pages_per_doc, w), dh, workspace, st)
+             : launch_attention_paged(paged_args<float>(qkv, row_start, cache_len, pages, cache, o, lse, T, B, max_new, H, H_kv, n_pages, page_size,
+                                                        pages_per_doc, w), dh, workspace, st);
 }
 
 }  // extern "C"

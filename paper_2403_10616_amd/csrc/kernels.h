@@ -3,6 +3,8 @@
 #include <algorithm>
 
 #include "common.h"
+#include "paged.h"
+#include "visible.h"
 
 namespace dipaco {
 
@@ -298,5 +300,19 @@ dipaco_status launch_attention_bwd_f32(const float* qkv, const float* o, const f
 // bf16 kernels: 0: a workgroup takes a long and a short block of the causal triangle; 1: one block per workgroup, longest first
 void set_attention_single_block(int on);
 int attention_single_block();
+
+// ---- attention_window.hip: window and sinks over packed q | k | v rows, H query heads on H_kv key heads -------
+// lengths (nullable): rows of each document; what lies behind them is not read, and 0 is written there
+template <typename T>
+dipaco_status launch_window_fwd(const T* qkv, const int* lengths, T* o, float* lse, int B, int S, int H, int H_kv, int dh, Window w, hipStream_t s);
+// dsum: fp32 scratch of 2 * B * H * roundup(S, 128) floats
+template <typename T>
+dipaco_status launch_window_bwd(const T* qkv, const int* lengths, const T* o, const T* d_o, const float* lse, T* dqkv, float* dsum, int B, int S, int H,
+                                int H_kv, int dh, Window w, hipStream_t s);
+
+// ---- paged.hip ---------------------------------------------------------------------------------------
+template <typename T> dipaco_status launch_cache_append(const PagedArgs<T>& a, int dh, hipStream_t s);
+size_t paged_workspace_bytes(int T_rows, int B, int max_new, int H, int H_kv, int dh, int page_size, int pages_per_doc);
+template <typename T> dipaco_status launch_attention_paged(const PagedArgs<T>& a, int dh, void* workspace, hipStream_t s);
 
 }  // namespace dipaco
