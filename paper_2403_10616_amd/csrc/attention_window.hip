@@ -7,6 +7,8 @@
 //
 // One wave per row and head.  The forward pass and dQ take 64 visible keys at a time: a lane forms one key's score, then the wave adds the
 // values with the lanes on the head's columns.  dK / dV do the same over the rows that see a key.
+#include <type_traits>
+
 #include "kernels.h"
 #include "visible.h"
 
@@ -160,6 +162,7 @@ __global__ void __launch_bounds__(256) window_dkv_rows(const T* __restrict__ qkv
 
 template <int DH, typename T>
 dipaco_status fwd(const T* qkv, const int* lengths, T* o, float* lse, int B, int S, int H, int H_kv, Window w, hipStream_t s) {
+  if constexpr (std::is_same<T, bf16>::value) return launch_window_fwd_mfma<DH>(qkv, lengths, o, lse, B, S, H, H_kv, w, s);
   window_fwd_rows<DH, T><<<dim3((S + 3) / 4, H, B), 256, 0, s>>>(qkv, lengths, o, lse, S, H, H_kv, w);
   DIPACO_LAUNCH_CHECK();
   return DIPACO_OK;

@@ -310,6 +310,10 @@ template <typename T>
 dipaco_status launch_window_bwd(const T* qkv, const int* lengths, const T* o, const T* d_o, const float* lse, T* dqkv, float* dsum, int B, int S, int H,
                                 int H_kv, int dh, Window w, hipStream_t s);
 
+// attention_window_mfma.hip: bf16, matrix cores
+template <int DH>
+dipaco_status launch_window_fwd_mfma(const bf16* qkv, const int* lengths, bf16* o, float* lse, int B, int S, int H, int H_kv, Window w, hipStream_t s);
+
 // ---- paged.hip ---------------------------------------------------------------------------------------
 template <typename T> dipaco_status launch_cache_append(const PagedArgs<T>& a, int dh, hipStream_t s);
 size_t paged_workspace_bytes(int T_rows, int B, int max_new, int H, int H_kv, int dh, int page_size, int pages_per_doc);

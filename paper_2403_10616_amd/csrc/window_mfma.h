@@ -1,0 +1,173 @@
+// bf16 attention under a sliding window with sinks on the matrix cores: the pieces that the forward pass over a padded batch
+// (attention_window_mfma.hip) and the one over a paged cache (paged_mfma.hip) share.
+//
+// Tiles, fragments and the order of contraction are those of attention_mfma.h: S^T = K.Q^T, so that a query's softmax state is a lane's and
+// the probabilities are the next product's operand without leaving registers.  New here is which tiles are read: a workgroup walks
+// the tiles of the sinks, then those of its rows' windows (TileList); a wave takes of each tile the halves of 32 keys that any of
+// its 32 rows sees, and applies the mask only where some pair of the half is hidden.
+//
+// Probabilities are rounded to bf16 where the second product multiplies them (2^-8 of each, the size of the output's own rounding);
+// their sum is taken in fp32 before that, so that lse keeps fp32's digits.
+#pragma once
+#include "attention_mfma.h"
+#include "visible.h"
+
+namespace dipaco {
+
+namespace {
+
+// The tiles of 64 keys that rows at positions lo .. hi see: the first `front` of the document, then `first` to that of position hi
+struct TileList {
+  int front, first, count;
+  __device__ __forceinline__ TileList(const Window& w, int lo, int hi) {
+    const int near = w.near_from(lo);
+    first = near >> 6;
+    front = min((min(w.sinks, near) + 63) >> 6, first);
+    count = front + (hi >> 6) + 1 - first;
+  }
+  __device__ __forceinline__ int at(int t) const { return t < front ? t : first + t - front; }
+};
+
+// max of three, NaN ignored.  As an instruction of its own: fmaxf has the compiler quiet every operand first, one more instruction an element.
+// The operands must not come straight from a matrix instruction: see max_of.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+// The maximum of N score tiles.  The first maximum is the compiler's (median with +inf), which waits for the matrix instructions that wrote
+// the tiles; the others depend on it.
+template <int N> __device__ __forceinline__ float max_of(const f32x16 (&st)[N]) {
+  float mx = __builtin_amdgcn_fmed3f(st[0][0], st[N - 1][15], INFINITY);
+  if constexpr (N == 2) {
+#pragma unroll
+    for (int e = 0; e < 15; ++e) mx = max3(mx, st[0][e + 1], st[1][e]);
+  } else {
+#pragma unroll
+    for (int e = 1; e < 15; e += 2) mx = max3(mx, st[0][e], st[0][e + 1]);
+  }
+  return mx;
+}
+
+// a wave's rows: their first and last position (none: hi < lo)
+struct RowSpan { int lo, hi; };
+enum Seen { NONE = 0, SOME = 1, ALL_PAIRS = 2 };
+// what rows of the span see of the 32 keys from k0 on (wave-uniform)
+__device__ __forceinline__ int seen_half(const Window& w, const RowSpan& r, int k0) {
+  if (k0 > r.hi || (k0 + 31 < w.near_from(r.lo) && k0 >= w.sinks)) return NONE;
+  return k0 + 31 <= r.lo && (k0 >= w.near_from(r.hi) || k0 + 31 < w.sinks) ? ALL_PAIRS : SOME;
+}
+
+// One query row a lane pair: reference exponent, half row sum, O^T
+template <int DH> struct SoftmaxRow {
+  f32x16 o[DH / 32];
+  float m, m_neg, l;   // m_neg = -m, 0 while nothing has been seen
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int dt = 0; dt < DH / 32; ++dt) zero(o[dt]);
+    m = -INFINITY;
+    m_neg = 0.f;
+    l = 0.f;
+  }
+};
+
+// NT halves of 32 keys from k0 on.  k_, v_: the halves' first row in LDS.  masked: some pair may be hidden.  holes: bit per 16 keys that nobody sees
+template <int DH, int NT>
+__device__ __forceinline__ void attend_half(SoftmaxRow<DH>& x, const uint4 (&qf)[DH / 16], const char* k_, const char* v_, const FragOff& fo, const TrOff& to,
+                                            int k0, bool masked, int holes, int pos, int near, int sinks, int lane) {
+  constexpr int KS = DH / 16, DT = DH / 32;
+  f32x16 st[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) zero(st[t]);
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+    for (int t = 0; t < NT; ++t) st[t] = mfma16(row_frag(k_, fo, ks, t), qf[ks], st[t]);
+  if (masked) {   // wave-uniform
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int key = k0 + 32 * t + acc_row(e, lane);
+        const bool hole = (holes >> (2 * t + (e >> 3))) & 1;
+        st[t][e] = !hole && key <= pos && (key >= near || key < sinks) ? st[t][e] : -INFINITY;
+      }
+  }
+  const float sc = score_scale<DH>() * LOG2E;
+  float mx = max_of(st);
+  mx = fmaxf(mx, __shfl_xor(mx, 32, WAVE));
+  // the reference may lag behind the running maximum by 2^8 (attention_mfma.h); rows that have seen nothing keep 0 for it
+  const float mn = fmaxf(x.m, mx * sc);
+  if (__builtin_amdgcn_ballot_w64(mn > x.m + 8.0f) != 0) {   // wave-uniform
+    const float corr = mn == x.m ? 1.f : __builtin_amdgcn_exp2f(x.m - mn);
+    x.l *= corr;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x.o[dt][e] *= corr;
+    x.m = mn;
+    x.m_neg = mn == -INFINITY ? 0.f : -mn;
+  }
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) st[t][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[t][e], sc, x.m_neg));
+#pragma unroll
+    for (int e = 0; e < 16; e += 2) { s0 += st[t][e]; s1 += st[t][e + 1]; }
+    x.l += s0 + s1;
+    const uint4 p0 = pack8<0>(st[t]), p1 = pack8<8>(st[t]);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+      x.o[dt] = mfma16(tr_read(v_, to, dt, 2 * t), p0, x.o[dt]);
+      x.o[dt] = mfma16(tr_read(v_, to, dt, 2 * t + 1), p1, x.o[dt]);
+    }
+  }
+}
+// a tile of 64 keys: both halves in one go where both are seen, else the one that is
+template <int DH>
+__device__ __forceinline__ void attend_tile(SoftmaxRow<DH>& x, const uint4 (&qf)[DH / 16], const char* k_, const char* v_, const FragOff& fo, const TrOff& to,
+                                            int k0, int holes, const Window& w, const RowSpan& span, int pos, int near, int lane) {
+  const int a = holes == 15 ? NONE : seen_half(w, span, k0), b = holes == 15 ? NONE : seen_half(w, span, k0 + 32);
+  if (a != NONE && b != NONE)
+    attend_half<DH, 2>(x, qf, k_, v_, fo, to, k0, a + b != 2 * ALL_PAIRS || holes, holes, pos, near, w.sinks, lane);
+  else if (a != NONE || b != NONE) {
+    const int half = a != NONE ? 0 : 1;
+    attend_half<DH, 1>(x, qf, k_ + 4096 * half, v_ + 4096 * half, fo, to, k0 + 32 * half, a + b != ALL_PAIRS || holes, holes >> (2 * half), pos, near,
+                       w.sinks, lane);
+  }
+}
+
+__device__ __forceinline__ bool bits_not_finite(float v) { return (__builtin_bit_cast(uint32_t, v) & 0x7f800000u) == 0x7f800000u; }
+
+// Keys and values of one document and head in packed rows ld elements apart
+template <int DH> struct RowTiles {
+  const bf16 *k, *v;
+  int ld, rows;
+  uint32_t off[2];
+  __device__ __forceinline__ RowTiles(const bf16* k, const bf16* v, int ld, int rows, int wave, int lane) : k(k), v(v), ld(ld), rows(rows) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) off[i] = (uint32_t)(loader_row(i, wave, lane) * ld * 2) + loader_column_bytes<DH>(i, wave, lane);
+  }
+  // this wave's loads of a tile into a stage: rows behind the document's last one re-read it (they are hidden from every row)
+  __device__ __forceinline__ void issue(int tile, int wave, int lane, uint32_t stage_addr) const {
+    constexpr int NP = panels<DH>();
+    const int row0 = tile * 64;
+    const bf16* const b0 = k + (long)row0 * ld;
+    const bf16* const b1 = v + (long)row0 * ld;
+    uint32_t at[2] = {off[0], off[1]};
+    if (row0 + 64 > rows) {   // wave-uniform
+#pragma unroll
+      for (int i = 0; i < 2; ++i) at[i] = (uint32_t)(min(loader_row(i, wave, lane), rows - 1 - row0) * ld * 2) + loader_column_bytes<DH>(i, wave, lane);
+    }
+#pragma unroll
+    for (int i = 0; i < 4 * NP; ++i) {
+      const int second = i / (2 * NP), panel = (i >> 1) % NP;   // compile-time
+      load16_to_lds_at((second ? b1 : b0) + 64 * panel, at[i & 1], stage_addr + (uint32_t)((wave + 4 * i) * 1024));
+    }
+  }
+};
+
+}  // namespace
+
+}  // namespace dipaco
