@@ -1115,7 +1115,7 @@ dipaco_status dipaco_k_attention_window_fwd(int32_t dtype, const void* qkv, cons
   TRY(check_ptr(qkv, "qkv")); TRY(check_ptr(o, "o")); TRY(check_ptr(lse, "lse"));
   if (lengths) TRY(check_ptr(lengths, "lengths"));
   hipStream_t st = static_cast<hipStream_t>(stream);
-  const Window w{window, sinks};
+  const Window w{std::min(window, S), std::min(sinks, S)};
   return dtype == DIPACO_BF16
              ? launch_window_fwd<bf16>(static_cast<const bf16*>(qkv), lengths, static_cast<bf16*>(o), lse, B, S, H, H_kv, dh, w, st)
              : launch_window_fwd<float>(static_cast<const float*>(qkv), lengths, static_cast<float*>(o), lse, B, S, H, H_kv, dh, w, st);
@@ -1131,7 +1131,7 @@ dipaco_status dipaco_k_attention_window_bwd(int32_t dtype, const void* qkv, cons
   TRY(check_ptr(dqkv, "dqkv")); TRY(check_ptr(dsum, "dsum"));
   if (lengths) TRY(check_ptr(lengths, "lengths"));
   hipStream_t st = static_cast<hipStream_t>(stream);
-  const Window w{window, sinks};
+  const Window w{std::min(window, S), std::min(sinks, S)};
   return dtype == DIPACO_BF16
              ? launch_window_bwd<bf16>(static_cast<const bf16*>(qkv), lengths, static_cast<const bf16*>(o), static_cast<const bf16*>(d_o), lse,
                                        static_cast<bf16*>(dqkv), dsum, B, S, H, H_kv, dh, w, st)
@@ -1177,7 +1177,8 @@ dipaco_status dipaco_k_attention_paged(int32_t dtype, const void* qkv, const int
   if (workspace_bytes < paged_workspace_bytes(T, B, max_new, H, H_kv, dh, page_size, pages_per_doc))
     return fail(DIPACO_EWORKSPACE, "workspace smaller than dipaco_k_attention_paged_workspace_bytes");
   hipStream_t st = static_cast<hipStream_t>(stream);
-  const Window w{window, sinks};
+  const int most = pages_per_doc * page_size + T;   // positions
+  const Window w{std::min(window, most), std::min(sinks, most)};
   return dtype == DIPACO_BF16
              ? launch_attention_paged(paged_args<bf16>(qkv, row_start, cache_len, pages, cache, o, lse, T, B, max_new, H, H_kv, n_pages, page_size,
                                                        pages_per_doc, w), dh, workspace, st)

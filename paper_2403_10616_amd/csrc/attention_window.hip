@@ -170,6 +170,7 @@ dipaco_status fwd(const T* qkv, const int* lengths, T* o, float* lse, int B, int
 template <int DH, typename T>
 dipaco_status bwd(const T* qkv, const int* lengths, const T* o, const T* d_o, const float* lse, T* dqkv, float* dsum, int B, int S, int H, int H_kv,
                   Window w, hipStream_t s) {
+  if constexpr (std::is_same<T, bf16>::value) return launch_window_bwd_mfma<DH>(qkv, lengths, o, d_o, lse, dqkv, dsum, B, S, H, H_kv, w, s);
   const int S128 = (S + 127) / 128 * 128;
   window_stats<DH, T><<<dim3(S128 / 4, H, B), 256, 0, s>>>(o, d_o, lengths, dsum, S, S128, H);
   DIPACO_LAUNCH_CHECK();

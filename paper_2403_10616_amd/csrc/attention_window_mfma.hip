@@ -41,7 +41,7 @@ __global__ void __launch_bounds__(AT_THREADS, DH == 128 ? 2 : 3) window_fwd_mfma
     const TrOff to = tr_offsets(lane);
     const uint32_t smem_addr = (uint32_t)(uintptr_t)wf_smem;
     const bf16* const k = base + (a.H + hk) * DH;
-    const RowTiles<DH> src(k, k + a.H_kv * DH, ld, rows, wave, lane);
+    const RowTiles<DH> src(k, k + a.H_kv * DH, ld, ld, rows, wave, lane);
     const TileList tiles(a.w, q0, min(q0 + 127, rows - 1));
     src.issue(tiles.at(0), wave, lane, smem_addr);
     auto tile = [&](auto CUR, int t) {
@@ -62,7 +62,7 @@ __global__ void __launch_bounds__(AT_THREADS, DH == 128 ? 2 : 3) window_fwd_mfma
       const VisibleList vis(a.w, q);
 #pragma unroll 1
       for (int t = 0; t < vis.count; ++t) {
-        const bf16* kr = src.k + (long)vis.at(t) * ld;
+        const bf16* kr = src.t0 + (long)vis.at(t) * ld;
         plain::add_row(x.o, __builtin_amdgcn_exp2f(__builtin_fmaf(plain::dot<DH>(qrow, kr), sc, x.m_neg)), kr + a.H_kv * DH, h);
       }
     }
@@ -75,6 +75,305 @@ __global__ void __launch_bounds__(AT_THREADS, DH == 128 ? 2 : 3) window_fwd_mfma
     store_transposed_out(out, x.o, h, q_out < rows ? 1.0f / x.l : 0.f);
     if (h == 0) lse[(long)bh * a.S + q_out] = q_out < rows ? (x.m + __builtin_amdgcn_logf(x.l)) * LN2 : 0.f;   // v_log_f32 is log2
   }
+}
+
+// ---- backward: D = rowsum(dO * O) and -lse log2(e) of every row, in rows padded to whole blocks of 128 -----------------------------
+// Behind a document D is 0 and -lse log2(e) is -inf (probability 0), so that the blocks below need no bounds check.
+template <int DH>
+__global__ void __launch_bounds__(AT_THREADS) window_stats_mfma(WindowArgs a, const bf16* __restrict__ o, const bf16* __restrict__ d_o,
+                                                               const float* __restrict__ lse, float* __restrict__ dsum) {
+  constexpr int LANES = DH / 8, ROWS = AT_THREADS / LANES;   // lanes of a row, rows of a workgroup at a time
+  const int n_bh = a.B * a.H, nqb = (a.S + 127) / 128, bh = blockIdx.x / nqb, qb = blockIdx.x - bh * nqb, b = bh / a.H, hd = bh - b * a.H;
+  const int c = 8 * (threadIdx.x % LANES), rows = document_rows(a.lengths, b, a.S);
+  const long Sp = (long)nqb * 128;
+#pragma unroll
+  for (int i = 0; i < 128 / ROWS; ++i) {
+    const int q = qb * 128 + ROWS * i + threadIdx.x / LANES;
+    float D = 0.f;
+    if (q < rows) {
+      const size_t at = (((size_t)b * a.S + q) * a.H + hd) * DH + c;
+      float x[8], y[8];
+      load_vec16(o + at, x);
+      load_vec16(d_o + at, y);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) D = __builtin_fmaf(x[e], y[e], D);
+    }
+#pragma unroll
+    for (int m = 1; m < LANES; m <<= 1) D += __shfl_xor(D, m, WAVE);
+    if (threadIdx.x % LANES == 0) {
+      dsum[bh * Sp + q] = D;
+      dsum[(n_bh + bh) * Sp + q] = q < rows ? -lse[(long)bh * a.S + q] * LOG2E : -INFINITY;
+    }
+  }
+}
+
+// acc^T[dt] += (tile^T)[columns 32 dt .., the 32 rows from `tile` on] . src
+template <int DT> __device__ __forceinline__ void mma_transposed_half(f32x16 (&acc)[DT], const char* tile, const TrOff& to, const f32x16& src) {
+  const uint4 p0 = pack8<0>(src), p1 = pack8<8>(src);
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) {
+    acc[dt] = mfma16(tr_read(tile, to, dt, 0), p0, acc[dt]);
+    acc[dt] = mfma16(tr_read(tile, to, dt, 1), p1, acc[dt]);
+  }
+}
+
+// ---- backward, dQ: 128 queries of a head ---------------------------------------------------------------------------
+template <int DH> __device__ __forceinline__ void window_dq(const WindowArgs& a, const bf16* __restrict__ d_o, const float* __restrict__ dsum,
+                                                            bf16* __restrict__ dqkv, int bh, int qb, char* smem) {
+  constexpr int KS = DH / 16, DT = DH / 32, TILE_BYTES = tile_bytes<DH>();
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, h = lane >> 5;
+  const int b = bh / a.H, hd = bh - b * a.H, hk = hd / (a.H / a.H_kv), q0 = qb * 128, q = q0 + 32 * wave + r;
+  const int rows = document_rows(a.lengths, b, a.S), ld = (a.H + 2 * a.H_kv) * DH;
+  const long Sp = (a.S + 127) / 128 * 128L;
+  const bf16* const base = a.qkv + (long)b * a.S * ld;
+  const bf16* const qrow = base + (long)q * ld + hd * DH;
+  const bf16* const grow = d_o + (((long)b * a.S + q) * a.H + hd) * DH;
+  const RowSpan span{q0 + 32 * wave, q0 + 32 * wave < rows ? min(q0 + 32 * wave + 31, rows - 1) : -1};
+  const int near = a.w.near_from(q);
+  const float sc = score_scale<DH>() * LOG2E;
+  f32x16 dq[DT];
+  plain::clear(dq);
+  if (q0 < rows) {
+    uint4 qf[KS], gf[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      qf[ks] = q < rows ? *reinterpret_cast<const uint4*>(qrow + 8 * (2 * ks + h)) : make_uint4(0, 0, 0, 0);
+      gf[ks] = q < rows ? *reinterpret_cast<const uint4*>(grow + 8 * (2 * ks + h)) : make_uint4(0, 0, 0, 0);
+    }
+    const float D = dsum[bh * Sp + q], nlse2 = dsum[((long)a.B * a.H + bh) * Sp + q];
+    const FragOff fo = frag_offsets(lane);
+    const TrOff to = tr_offsets(lane);
+    const uint32_t smem_addr = (uint32_t)(uintptr_t)smem;
+    const bf16* const k = base + (a.H + hk) * DH;
+    const RowTiles<DH> src(k, k + a.H_kv * DH, ld, ld, rows, wave, lane);
+    const TileList tiles(a.w, q0, min(q0 + 127, rows - 1));
+    src.issue(tiles.at(0), wave, lane, smem_addr);
+    for (int t = 0, cur = 0; t < tiles.count; ++t, cur ^= 1) {
+      wait_vmcnt<0>();
+      __syncthreads();   // tile t is in LDS, and nobody still reads the other stage
+      if (t + 1 < tiles.count) src.issue(tiles.at(t + 1), wave, lane, smem_addr + (1 - cur) * 2 * TILE_BYTES);
+      const int k0 = tiles.at(t) * 64;
+      const char* k_ = smem + cur * 2 * TILE_BYTES;
+      const char* v_ = k_ + TILE_BYTES;
+      auto halves = [&](auto NTc, int half, bool masked) {
+        constexpr int NT = decltype(NTc)::value;
+        f32x16 st[NT], dp[NT];
+#pragma unroll
+        for (int i = 0; i < NT; ++i) { zero(st[i]); zero(dp[i]); }
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+          for (int i = 0; i < NT; ++i) {
+            st[i] = mfma16(row_frag(k_ + 4096 * half, fo, ks, i), qf[ks], st[i]);
+            dp[i] = mfma16(row_frag(v_ + 4096 * half, fo, ks, i), gf[ks], dp[i]);
+          }
+#pragma unroll
+        for (int i = 0; i < NT; ++i)   // dS^T without the factor 1 / sqrt(d_head), which dQ gets when it is stored
+#pragma unroll
+          for (int e = 0; e < 16; ++e) st[i][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[i][e], sc, nlse2)) * (dp[i][e] - D);
+        if (masked) {
+#pragma unroll
+          for (int i = 0; i < NT; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const int key = k0 + 32 * (half + i) + acc_row(e, lane);
+              if (key > q || (key < near && key >= a.w.sinks)) st[i][e] = 0.f;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < NT; ++i) mma_transposed_half(dq, k_ + 4096 * (half + i), to, st[i]);
+      };
+      const int s0 = seen_half(a.w, span, k0), s1 = seen_half(a.w, span, k0 + 32);
+      if (s0 != NONE && s1 != NONE) halves(std::integral_constant<int, 2>{}, 0, s0 + s1 != 2 * ALL_PAIRS);
+      else if (s0 != NONE || s1 != NONE) halves(std::integral_constant<int, 1>{}, s0 != NONE ? 0 : 1, s0 + s1 != ALL_PAIRS);
+    }
+    if (__any(q < rows && plain::not_finite(dq)) && q < rows) {
+      plain::clear(dq);
+      const VisibleList vis(a.w, q);
+#pragma unroll 1
+      for (int t = 0; t < vis.count; ++t) {
+        const bf16* kr = k + (long)vis.at(t) * ld;
+        plain::add_row(dq, __builtin_amdgcn_exp2f(__builtin_fmaf(plain::dot<DH>(qrow, kr), sc, nlse2)) * (plain::dot<DH>(grow, kr + a.H_kv * DH) - D), kr, h);
+      }
+    }
+  }
+  int q_out = q;
+  asm volatile("" : "+v"(q_out));
+  if (q_out < a.S) {
+    if (q_out >= rows) plain::clear(dq);
+    store_transposed_out(dqkv + ((long)b * a.S + q_out) * ld + hd * DH, dq, h, score_scale<DH>());
+  }
+}
+
+// ---- backward, dK and dV ------------------------------------------------------------------------------------------
+// Keys: 128 of a key head, 32 a wave, over the queries of every head of the group that see them under the window alone; the stages hold 64
+// queries.  Sinks are seen by all queries behind them, a multiple of what the other keys take, so a workgroup takes only 32 of them (SINKS):
+// its waves share the stage, two of them on each half of it, one for dV and one for dK, and the halves' sums meet at the end.
+template <int DH> constexpr int window_dkv_stage() { return 2 * tile_bytes<DH>() + 2 * 64 * (int)sizeof(float); }   // Q | dO | -lse log2(e) | D
+
+template <int DH, bool SINKS>
+__device__ __forceinline__ void window_dkv(const WindowArgs& a, const bf16* __restrict__ d_o, const float* __restrict__ dsum, bf16* __restrict__ dqkv, int b, int hk,
+                                           int k0, char* smem) {
+  constexpr int KS = DH / 16, DT = DH / 32, TILE_BYTES = tile_bytes<DH>(), STAGE = window_dkv_stage<DH>();
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, h = lane >> 5;
+  const int rows = document_rows(a.lengths, b, a.S), ld = (a.H + 2 * a.H_kv) * DH, G = a.H / a.H_kv;
+  const int sinks = rows <= a.w.window ? 0 : min(a.w.sinks, rows);   // a window that covers the document leaves the sinks nothing of their own
+  if (SINKS && k0 >= sinks) return;
+  const int kw0 = k0 + (SINKS ? 0 : 32 * wave), key = kw0 + r;
+  const long Sp = (a.S + 127) / 128 * 128L;
+  const bf16* const base = a.qkv + (long)b * a.S * ld;
+  const bf16* const krow = base + (long)key * ld + (a.H + hk) * DH;
+  // positions that see the wave's keys, and this lane's key
+  const int last = SINKS ? rows - 1 : min(rows - 1, kw0 + 31 + a.w.window - 1);
+  const int key_last = SINKS ? rows - 1 : min(rows - 1, key + a.w.window - 1);
+  const bool idle = kw0 >= rows || (!SINKS && kw0 + 31 < sinks);
+  const float sc = score_scale<DH>() * LOG2E;
+  f32x16 dk[DT], dv[DT];
+  plain::clear(dk);
+  plain::clear(dv);
+  if (k0 < rows && (SINKS || k0 + 127 >= sinks)) {
+    uint4 kf[KS], vf[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      kf[ks] = key < rows ? *reinterpret_cast<const uint4*>(krow + 8 * (2 * ks + h)) : make_uint4(0, 0, 0, 0);
+      vf[ks] = key < rows ? *reinterpret_cast<const uint4*>(krow + a.H_kv * DH + 8 * (2 * ks + h)) : make_uint4(0, 0, 0, 0);
+    }
+    FragOff fo = frag_offsets(lane);
+    TrOff to = tr_offsets(lane);
+    const uint32_t smem_addr = (uint32_t)(uintptr_t)smem;
+    const int block_last = SINKS ? rows - 1 : min(rows - 1, k0 + 127 + a.w.window - 1);
+    const int first = k0 >> 6, n_tiles = (block_last >> 6) + 1 - first, steps = G * n_tiles;
+    const int head0 = b * a.H + hk * G;
+    RowTiles<DH, true> src(base + hk * G * DH, d_o + ((long)b * a.S * a.H + hk * G) * DH, ld, a.H * DH, rows, wave, lane);
+    // statistics of a tile's 64 queries: waves 0 and 2 fetch -lse log2(e), waves 1 and 3 fetch D
+    const float* stat = dsum + ((wave & 1 ? 0 : (long)a.B * a.H) + head0) * Sp + lane;
+    const uint32_t stat_dst = 2 * TILE_BYTES + (wave & 1 ? 256 : 0);
+    int next_tile = first;
+    auto issue = [&](int stage) {   // the next step's tile: the heads of the group one after the other
+      src.issue(next_tile, wave, lane, smem_addr + stage * STAGE);
+      load4_to_lds(stat + next_tile * 64, smem_addr + stage * STAGE + stat_dst);
+      if (++next_tile == first + n_tiles) {
+        next_tile = first;
+        src.t0 += DH;
+        src.t1 += DH;
+        stat += Sp;
+      }
+    };
+    issue(0);
+    for (int n = 0, qt = first, cur = 0; n < steps; ++n, cur ^= 1) {
+      wait_vmcnt<0>();
+      __syncthreads();
+      if (n + 1 < steps) issue(1 - cur);
+      const int q0 = qt * 64;
+      if (++qt == first + n_tiles) qt = first;
+      const char* q_ = smem + cur * STAGE;
+      const char* g_ = q_ + TILE_BYTES;
+      const float* nlse2s = reinterpret_cast<const float*>(q_ + 2 * TILE_BYTES);
+      const float* Ds = nlse2s + 64;
+#pragma unroll
+      for (int i = 0; i < (SINKS ? 1 : 2); ++i) {
+        const int t = SINKS ? wave & 1 : i, qh = q0 + 32 * t;   // 32 queries
+        if (idle || qh + 31 < kw0 || qh > last) continue;       // wave-uniform
+        if constexpr (DH == 128) rederive_offsets(fo, to);
+        f32x16 st, dp;
+        zero(st); zero(dp);
+        const bool want_v = !SINKS || wave < 2, want_k = !SINKS || wave >= 2;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          st = mfma16(row_frag(q_ + 4096 * t, fo, ks, 0), kf[ks], st);
+          if (want_k) dp = mfma16(row_frag(g_ + 4096 * t, fo, ks, 0), vf[ks], dp);
+        }
+        // accumulator elements 4g .. 4g + 3 are queries 8g + 4h + (0..3) of the half: their statistics are 16 contiguous bytes
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const float4 Lq = *reinterpret_cast<const float4*>(nlse2s + 32 * t + 8 * g + 4 * h);
+          const float4 Dv = *reinterpret_cast<const float4*>(Ds + 32 * t + 8 * g + 4 * h);
+          const float Ls[4] = {Lq.x, Lq.y, Lq.z, Lq.w}, Dd[4] = {Dv.x, Dv.y, Dv.z, Dv.w};
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int e = 4 * g + j;
+            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(st[e], sc, Ls[j]));
+            st[e] = p;
+            dp[e] = p * (dp[e] - Dd[j]);   // dS without 1 / sqrt(d_head), which dK gets when it is stored
+          }
+        }
+        if (qh < kw0 + 31 || (!SINKS && qh + 31 > kw0 + a.w.window - 1)) {   // wave-uniform: some pair is hidden
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int q = qh + acc_row(e, lane);
+            if (q < key || q > key_last) { st[e] = 0.f; dp[e] = 0.f; }
+          }
+        }
+        if (want_v) mma_transposed_half(dv, g_ + 4096 * t, to, st);
+        if (want_k) mma_transposed_half(dk, q_ + 4096 * t, to, dp);
+      }
+    }
+    if constexpr (SINKS) {   // the odd waves hand their half of the queries over; then wave 2 its dK to wave 0
+      constexpr int PER = 16 * DT * WAVE;
+      static_assert(3 * PER * 4 <= 2 * STAGE, "the sums fit in the stages");
+      float* const at = reinterpret_cast<float*>(smem);
+      __syncthreads();
+      if (wave == 1) hand_over(dv, at, lane);
+      if (wave == 3) hand_over(dk, at + PER, lane);
+      __syncthreads();
+      if (wave == 0) take_over(dv, at, 1.f, 1.f, lane);
+      if (wave == 2) {
+        take_over(dk, at + PER, 1.f, 1.f, lane);
+        hand_over(dk, at + 2 * PER, lane);
+      }
+      __syncthreads();
+      if (wave != 0) return;
+      take_over(dk, at + 2 * PER, 0.f, 1.f, lane);
+    }
+    if (__any(key < rows && (plain::not_finite(dk) || plain::not_finite(dv))) && key < rows) {
+      plain::clear(dk);
+      plain::clear(dv);
+#pragma unroll 1
+      for (int g = 0; g < G; ++g) {
+        const float* const D = dsum + (long)(head0 + g) * Sp;
+        const float* const L = D + (long)a.B * a.H * Sp;
+#pragma unroll 1
+        for (int i = key; i <= key_last; ++i) {
+          const bf16* qr = base + (long)i * ld + (hk * G + g) * DH;
+          const bf16* gr = d_o + (((long)b * a.S + i) * a.H + hk * G + g) * DH;
+          const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(plain::dot<DH>(qr, krow), sc, L[i]));
+          plain::add_row(dv, p, gr, h);
+          plain::add_row(dk, p * (plain::dot<DH>(gr, krow + a.H_kv * DH) - D[i]), qr, h);
+        }
+      }
+    }
+  }
+  int key_out = key;
+  asm volatile("" : "+v"(key_out));
+  if (key_out < a.S && (SINKS ? key_out < sinks : key_out >= sinks)) {
+    if (key_out >= rows) { plain::clear(dk); plain::clear(dv); }
+    bf16* const out = dqkv + ((long)b * a.S + key_out) * ld + (a.H + hk) * DH;
+    store_transposed_out(out, dk, h, score_scale<DH>());
+    store_transposed_out(out + a.H_kv * DH, dv, h, 1.0f);
+  }
+}
+
+// One launch: the sinks' workgroups, which take longest, then those of dK / dV, then dQ's
+template <int DH>
+__global__ void __launch_bounds__(AT_THREADS, 2) window_bwd_mfma(WindowArgs a, const bf16* __restrict__ d_o, const float* __restrict__ dsum, bf16* __restrict__ dqkv,
+                                                                 int sink_blocks) {
+  extern __shared__ __attribute__((aligned(16))) char wb_smem[];
+  const int n_kv = a.B * a.H_kv, nb = (a.S + 127) / 128;
+  int i = blockIdx.x;
+  if (i < sink_blocks * n_kv) {
+    const int s = i / n_kv, bk = i - s * n_kv, b = bk / a.H_kv;
+    window_dkv<DH, true>(a, d_o, dsum, dqkv, b, bk - b * a.H_kv, 32 * s, wb_smem);
+    return;
+  }
+  i -= sink_blocks * n_kv;
+  if (i < n_kv * nb) {
+    const int kb = i / n_kv, bk = i - kb * n_kv, b = bk / a.H_kv;
+    window_dkv<DH, false>(a, d_o, dsum, dqkv, b, bk - b * a.H_kv, 128 * kb, wb_smem);
+    return;
+  }
+  i -= n_kv * nb;
+  const int n_bh = a.B * a.H, qb = i / n_bh;
+  window_dq<DH>(a, d_o, dsum, dqkv, i - qb * n_bh, nb - 1 - qb, wb_smem);
 }
 
 }  // namespace
@@ -91,5 +390,26 @@ dipaco_status launch_window_fwd_mfma(const bf16* qkv, const int* lengths, bf16* 
 template dipaco_status launch_window_fwd_mfma<32>(const bf16*, const int*, bf16*, float*, int, int, int, int, Window, hipStream_t);
 template dipaco_status launch_window_fwd_mfma<64>(const bf16*, const int*, bf16*, float*, int, int, int, int, Window, hipStream_t);
 template dipaco_status launch_window_fwd_mfma<128>(const bf16*, const int*, bf16*, float*, int, int, int, int, Window, hipStream_t);
+
+
+template <int DH>
+dipaco_status launch_window_bwd_mfma(const bf16* qkv, const int* lengths, const bf16* o, const bf16* d_o, const float* lse, bf16* dqkv, float* dsum, int B, int S,
+                                     int H, int H_kv, Window w, hipStream_t s) {
+  constexpr int LDS = 2 * window_dkv_stage<DH>();
+  static_assert(LDS >= 4 * tile_bytes<DH>(), "dQ's stages fit");
+  static std::atomic<unsigned long long> lds_set{0};
+  if (dipaco_status st = ensure_dynamic_lds(reinterpret_cast<const void*>(window_bwd_mfma<DH>), LDS, lds_set)) return st;
+  const WindowArgs a{qkv, lengths, B, S, H, H_kv, w};
+  const int nb = (S + 127) / 128, sink_blocks = w.window >= S ? 0 : (std::min(w.sinks, S) + 31) / 32;
+  window_stats_mfma<DH><<<B * H * nb, AT_THREADS, 0, s>>>(a, o, d_o, lse, dsum);
+  DIPACO_LAUNCH_CHECK();
+  window_bwd_mfma<DH><<<B * H_kv * (sink_blocks + nb) + B * H * nb, AT_THREADS, LDS, s>>>(a, d_o, dsum, dqkv, sink_blocks);
+  DIPACO_LAUNCH_CHECK();
+  return DIPACO_OK;
+}
+template dipaco_status launch_window_bwd_mfma<32>(const bf16*, const int*, const bf16*, const bf16*, const float*, bf16*, float*, int, int, int, int, Window, hipStream_t);
+template dipaco_status launch_window_bwd_mfma<64>(const bf16*, const int*, const bf16*, const bf16*, const float*, bf16*, float*, int, int, int, int, Window, hipStream_t);
+template dipaco_status launch_window_bwd_mfma<128>(const bf16*, const int*, const bf16*, const bf16*, const float*, bf16*, float*, int, int, int, int, Window,
+                                                   hipStream_t);
 
 }  // namespace dipaco

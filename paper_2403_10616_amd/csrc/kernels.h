@@ -313,6 +313,9 @@ dipaco_status launch_window_bwd(const T* qkv, const int* lengths, const T* o, co
 // attention_window_mfma.hip: bf16, matrix cores
 template <int DH>
 dipaco_status launch_window_fwd_mfma(const bf16* qkv, const int* lengths, bf16* o, float* lse, int B, int S, int H, int H_kv, Window w, hipStream_t s);
+template <int DH>
+dipaco_status launch_window_bwd_mfma(const bf16* qkv, const int* lengths, const bf16* o, const bf16* d_o, const float* lse, bf16* dqkv, float* dsum, int B, int S,
+                                     int H, int H_kv, Window w, hipStream_t s);
 
 // ---- paged.hip ---------------------------------------------------------------------------------------
 template <typename T> dipaco_status launch_cache_append(const PagedArgs<T>& a, int dh, hipStream_t s);

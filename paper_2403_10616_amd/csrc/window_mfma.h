@@ -140,30 +140,33 @@ __device__ __forceinline__ void attend_tile(SoftmaxRow<DH>& x, const uint4 (&qf)
 
 __device__ __forceinline__ bool bits_not_finite(float v) { return (__builtin_bit_cast(uint32_t, v) & 0x7f800000u) == 0x7f800000u; }
 
-// Keys and values of one document and head in packed rows ld elements apart
-template <int DH> struct RowTiles {
-  const bf16 *k, *v;
-  int ld, rows;
-  uint32_t off[2];
-  __device__ __forceinline__ RowTiles(const bf16* k, const bf16* v, int ld, int rows, int wave, int lane) : k(k), v(v), ld(ld), rows(rows) {
+// Two operands' rows of one document and head (keys and values; queries and output gradients), ld0 and ld1 elements apart
+template <int DH, bool TWO_STRIDES = false> struct RowTiles {
+  const bf16 *t0, *t1;
+  int ld0, ld1, rows;
+  uint32_t off[TWO_STRIDES ? 4 : 2];
+  __device__ __forceinline__ uint32_t offset(int i, int row) const { return (uint32_t)(row * (i < 2 ? ld0 : ld1) * 2); }
+  __device__ __forceinline__ RowTiles(const bf16* t0, const bf16* t1, int ld0, int ld1, int rows, int wave, int lane)
+      : t0(t0), t1(t1), ld0(ld0), ld1(ld1), rows(rows) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) off[i] = (uint32_t)(loader_row(i, wave, lane) * ld * 2) + loader_column_bytes<DH>(i, wave, lane);
+    for (int i = 0; i < (TWO_STRIDES ? 4 : 2); ++i) off[i] = offset(i, loader_row(i & 1, wave, lane)) + loader_column_bytes<DH>(i & 1, wave, lane);
   }
-  // this wave's loads of a tile into a stage: rows behind the document's last one re-read it (they are hidden from every row)
+  // this wave's loads of a tile of 64 rows into a stage: rows behind the document's last one re-read it (callers give them no weight)
   __device__ __forceinline__ void issue(int tile, int wave, int lane, uint32_t stage_addr) const {
     constexpr int NP = panels<DH>();
     const int row0 = tile * 64;
-    const bf16* const b0 = k + (long)row0 * ld;
-    const bf16* const b1 = v + (long)row0 * ld;
-    uint32_t at[2] = {off[0], off[1]};
+    const bf16* const b0 = t0 + (long)row0 * ld0;
+    const bf16* const b1 = t1 + (long)row0 * ld1;
+    uint32_t at[4] = {off[0], off[1], off[TWO_STRIDES ? 2 : 0], off[TWO_STRIDES ? 3 : 1]};
     if (row0 + 64 > rows) {   // wave-uniform
 #pragma unroll
-      for (int i = 0; i < 2; ++i) at[i] = (uint32_t)(min(loader_row(i, wave, lane), rows - 1 - row0) * ld * 2) + loader_column_bytes<DH>(i, wave, lane);
+      for (int i = 0; i < 4; ++i)
+        at[i] = offset(i, min(loader_row(i & 1, wave, lane), rows - 1 - row0)) + loader_column_bytes<DH>(i & 1, wave, lane);
     }
 #pragma unroll
     for (int i = 0; i < 4 * NP; ++i) {
       const int second = i / (2 * NP), panel = (i >> 1) % NP;   // compile-time
-      load16_to_lds_at((second ? b1 : b0) + 64 * panel, at[i & 1], stage_addr + (uint32_t)((wave + 4 * i) * 1024));
+      load16_to_lds_at((second ? b1 : b0) + 64 * panel, at[2 * second + (i & 1)], stage_addr + (uint32_t)((wave + 4 * i) * 1024));
     }
   }
 };
