@@ -410,7 +410,7 @@ static PagedArgs<T> paged_args(const void* qkv, const int32_t* row_start, const 
   int shift = 4;
   while ((1 << shift) < page_size) ++shift;
   return {static_cast<const T*>(qkv), row_start, cache_len, pages, const_cast<T*>(static_cast<const T*>(cache)), static_cast<T*>(o), lse, rows, B,
-          max_new, H, H_kv, n_pages, shift, pages_per_doc, w};
+          max_new, H, H_kv, n_pages, shift, pages_per_doc, w, 1, 1, nullptr};
 }
 
 }  // namespace dipaco
@@ -1159,7 +1159,7 @@ dipaco_status dipaco_k_cache_append(int32_t dtype, const void* qkv, const int32_
 size_t dipaco_k_attention_paged_workspace_bytes(int32_t T, int32_t B, int32_t max_new, int32_t H, int32_t H_kv, int32_t dh, int32_t page_size,
                                                 int32_t pages_per_doc) {
   if (check_heads(DIPACO_F32, H, H_kv, dh) != DIPACO_OK || check_cache(T, B, H, 1, page_size, pages_per_doc) != DIPACO_OK || max_new < 0) return 0;
-  return paged_workspace_bytes(T, B, max_new, H, H_kv, dh, page_size, pages_per_doc);
+  return paged_workspace_bytes(T, H, dh, page_size, pages_per_doc);
 }
 
 dipaco_status dipaco_k_attention_paged(int32_t dtype, const void* qkv, const int32_t* row_start, const int32_t* cache_len, const int32_t* pages,
@@ -1174,7 +1174,7 @@ dipaco_status dipaco_k_attention_paged(int32_t dtype, const void* qkv, const int
   TRY(check_ptr(qkv, "qkv")); TRY(check_ptr(row_start, "row_start")); TRY(check_ptr(cache_len, "cache_len")); TRY(check_ptr(pages, "pages"));
   TRY(check_ptr(cache, "cache")); TRY(check_ptr(o, "o")); TRY(check_ptr(workspace, "workspace"));
   if (lse) TRY(check_ptr(lse, "lse"));
-  if (workspace_bytes < paged_workspace_bytes(T, B, max_new, H, H_kv, dh, page_size, pages_per_doc))
+  if (workspace_bytes < paged_workspace_bytes(T, H, dh, page_size, pages_per_doc))
     return fail(DIPACO_EWORKSPACE, "workspace smaller than dipaco_k_attention_paged_workspace_bytes");
   hipStream_t st = static_cast<hipStream_t>(stream);
   const int most = pages_per_doc * page_size + T;   // positions

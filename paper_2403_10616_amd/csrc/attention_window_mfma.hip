@@ -42,7 +42,7 @@ __global__ void __launch_bounds__(AT_THREADS, DH == 128 ? 2 : 3) window_fwd_mfma
     const uint32_t smem_addr = (uint32_t)(uintptr_t)wf_smem;
     const bf16* const k = base + (a.H + hk) * DH;
     const RowTiles<DH> src(k, k + a.H_kv * DH, ld, ld, rows, wave, lane);
-    const TileList tiles(a.w, q0, min(q0 + 127, rows - 1));
+    const TileList<6> tiles(a.w, q0, min(q0 + 127, rows - 1));
     src.issue(tiles.at(0), wave, lane, smem_addr);
     auto tile = [&](auto CUR, int t) {
       constexpr int cur = decltype(CUR)::value;
@@ -50,7 +50,7 @@ __global__ void __launch_bounds__(AT_THREADS, DH == 128 ? 2 : 3) window_fwd_mfma
       __syncthreads();   // tile t is in LDS, and nobody still reads the other stage
       if (t + 1 < tiles.count) src.issue(tiles.at(t + 1), wave, lane, smem_addr + (1 - cur) * 2 * TILE_BYTES);
       const char* k_ = wf_smem + cur * 2 * TILE_BYTES;
-      attend_tile<DH>(x, qf, k_, k_ + TILE_BYTES, fo, to, tiles.at(t) * 64, 0, a.w, span, q, near, lane);
+      attend_tile<DH>(x, qf, k_, k_ + TILE_BYTES, fo, to, tiles.at(t) * 64, 0, a.w, span, false, q, near, lane);
     };
     for (int t = 0; t < tiles.count; t += 2) {
       tile(std::integral_constant<int, 0>{}, t);
@@ -59,11 +59,13 @@ __global__ void __launch_bounds__(AT_THREADS, DH == 128 ? 2 : 3) window_fwd_mfma
     x.l += __shfl_xor(x.l, 32, WAVE);
     if (__any(q < rows && plain::not_finite(x.o)) && q < rows) {
       plain::clear(x.o);
-      const VisibleList vis(a.w, q);
+      int q_again = q;
+      asm volatile("" : "+v"(q_again));   // formed anew, not kept through the loop
+      const VisibleList vis(a.w, q_again);
 #pragma unroll 1
       for (int t = 0; t < vis.count; ++t) {
         const bf16* kr = src.t0 + (long)vis.at(t) * ld;
-        plain::add_row(x.o, __builtin_amdgcn_exp2f(__builtin_fmaf(plain::dot<DH>(qrow, kr), sc, x.m_neg)), kr + a.H_kv * DH, h);
+        plain::add_row(x.o, __builtin_amdgcn_exp2f(__builtin_fmaf(plain::dot<DH>(base + (long)q_again * ld + hd * DH, kr), sc, x.m_neg)), kr + a.H_kv * DH, h);
       }
     }
   }
@@ -146,7 +148,7 @@ template <int DH> __device__ __forceinline__ void window_dq(const WindowArgs& a,
     const uint32_t smem_addr = (uint32_t)(uintptr_t)smem;
     const bf16* const k = base + (a.H + hk) * DH;
     const RowTiles<DH> src(k, k + a.H_kv * DH, ld, ld, rows, wave, lane);
-    const TileList tiles(a.w, q0, min(q0 + 127, rows - 1));
+    const TileList<6> tiles(a.w, q0, min(q0 + 127, rows - 1));
     src.issue(tiles.at(0), wave, lane, smem_addr);
     for (int t = 0, cur = 0; t < tiles.count; ++t, cur ^= 1) {
       wait_vmcnt<0>();

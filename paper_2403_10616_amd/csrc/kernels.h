@@ -319,7 +319,10 @@ dipaco_status launch_window_bwd_mfma(const bf16* qkv, const int* lengths, const 
 
 // ---- paged.hip ---------------------------------------------------------------------------------------
 template <typename T> dipaco_status launch_cache_append(const PagedArgs<T>& a, int dh, hipStream_t s);
-size_t paged_workspace_bytes(int T_rows, int B, int max_new, int H, int H_kv, int dh, int page_size, int pages_per_doc);
-template <typename T> dipaco_status launch_attention_paged(const PagedArgs<T>& a, int dh, void* workspace, hipStream_t s);
+size_t paged_workspace_bytes(int T_rows, int H, int dh, int page_size, int pages_per_doc);
+template <typename T> dipaco_status launch_attention_paged(PagedArgs<T> a, int dh, void* workspace, hipStream_t s);
+// paged_mfma.hip: bf16, matrix cores
+template <int DH> dipaco_status launch_paged_narrow_mfma(const PagedArgs<bf16>& a, hipStream_t s);
+template <int DH> dipaco_status launch_paged_wide_mfma(const PagedArgs<bf16>& a, int blocks, hipStream_t s);
 
 }  // namespace dipaco

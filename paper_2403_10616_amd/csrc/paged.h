@@ -1,11 +1,34 @@
-// The paged cache of keys and values, and the rows of new tokens that are read from and attend to it.
+// The paged cache of keys and values, the rows of new tokens that attend to it, and how their work is cut.
 //
 // cache: [n_pages][2][H_kv][page_size][dh], keys then values; position p of document b sits in page pages[b * pages_per_doc + p /
 // page_size], slot p % page_size.  A head's share of a page is contiguous: page_size x dh elements, 2 KB for 16 positions of 64 bf16.
+//
+// The query heads that read one key head, G of them, are rows of one product: row R of a document's n G packed rows is token R / G, head
+// R % G of the group.  A workgroup takes a block of packed rows of a document and a key head, and a part ("split") of the keys that these see:
+//   narrow: a document of up to 32 packed rows is one block; its workgroup's waves take the keys in turn, each with a ring of its own.
+//   wide:   128 packed rows, 32 a wave; the waves share the keys' tiles.
+// A split's sums go to the workspace, and paged_join adds them; a block whose keys are one split's writes its rows itself.
 #pragma once
 #include "visible.h"
 
 namespace dipaco {
+
+// Tiles of 2^SHIFT keys that rows at positions lo .. hi see: the first `front` of the document, then `first` to that of position hi
+template <int SHIFT> struct TileList {
+  int front, first, count;
+  __device__ __forceinline__ TileList() : front(0), first(0), count(0) {}
+  __device__ __forceinline__ TileList(const Window& w, int lo, int hi) {
+    const int near = w.near_from(lo);
+    first = min(near >> SHIFT, (hi >> SHIFT) + 1);   // hi lies in front of the window only where a document outgrows its table
+    front = min((min(w.sinks, near) + (1 << SHIFT) - 1) >> SHIFT, first);
+    count = front + (hi >> SHIFT) + 1 - first;
+  }
+  __device__ __forceinline__ int at(int t) const { return t < front ? t : first + t - front; }
+};
+
+constexpr int NARROW_ROWS = 32, WIDE_ROWS = 128;
+constexpr int SPLIT_KEYS = 512;   // a split has at least so many keys
+constexpr int PAGED_MOST_SPLITS = 64, PAGED_NARROW_GROUPS = 512, PAGED_WIDE_GROUPS = 512;   // splits, and the workgroups that they are to make
 
 template <typename T> struct PagedArgs {
   const T* qkv;              // [T rows, (H + 2 H_kv) dh]
@@ -17,7 +40,10 @@ template <typename T> struct PagedArgs {
   float* lse;                // [T rows, H], or null
   int T_rows, B, max_new, H, H_kv, n_pages, page_shift, pages_per_doc;
   Window w;
+  int narrow_splits, wide_splits;
+  float* part;               // [splits][T rows][H] x (dh sums, then in an array of its own reference exponent and sum)
 
+  __device__ __forceinline__ int group() const { return H / H_kv; }
   __device__ __forceinline__ int capacity() const { return pages_per_doc << page_shift; }
   __device__ __forceinline__ int cached(int b) const { return min(max(cache_len[b], 0), capacity()); }
   // the page of a position, or -1 where the table holds none
@@ -31,6 +57,36 @@ template <typename T> struct PagedArgs {
     return ((((long)page * 2 * H_kv + hk) << page_shift) + slot) * DH;
   }
   template <int DH> __device__ __forceinline__ long value_from_key() const { return ((long)H_kv << page_shift) * DH; }
+  template <int DH> __device__ __forceinline__ float* part_sums(int split, long row, int head) const { return part + (((long)split * T_rows + row) * H + head) * DH; }
+  template <int DH> __device__ __forceinline__ float2* part_state(int splits, int split, long row, int head) const {
+    return reinterpret_cast<float2*>(part + (long)splits * T_rows * H * DH) + ((long)split * T_rows + row) * H + head;
+  }
+};
+
+// A block of packed rows of one document: which rows, the tiles that they see, and how many of these a split takes
+template <int SHIFT> struct PagedBlock {
+  int b, row0, rows, packed0, packed, pos0, last;   // rows row0 .. of the call, `rows` of them; packed rows packed0 .. of `packed`; position of row 0; last one
+  int lo, hi;                                       // positions of the block's first and last row
+  TileList<SHIFT> tiles;
+  int per, used;                                    // tiles a split, splits that have any
+  template <typename T> __device__ __forceinline__ PagedBlock(const PagedArgs<T>& a, int b, int block, int block_rows, int splits) : b(b) {
+    const RowRange r = ragged_rows(a.row_start, b, a.T_rows);
+    row0 = r.first;
+    rows = min(r.count, a.max_new);
+    packed = rows * a.group();
+    packed0 = block * block_rows;
+    pos0 = a.cached(b);
+    last = min(pos0 + rows, a.capacity()) - 1;
+    per = used = lo = hi = 0;
+    if (packed0 >= packed) return;
+    lo = pos0 + packed0 / a.group();
+    hi = pos0 + (min(packed, packed0 + block_rows) - 1) / a.group();
+    if (last < 0) return;
+    tiles = TileList<SHIFT>(a.w, lo, min(hi, last));
+    if (tiles.count <= 0) { tiles.count = 0; return; }
+    per = max((tiles.count + splits - 1) / splits, SPLIT_KEYS >> SHIFT);
+    used = (tiles.count + per - 1) / per;
+  }
 };
 
 }  // namespace dipaco

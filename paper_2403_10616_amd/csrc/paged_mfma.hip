@@ -1,0 +1,355 @@
+// bf16 attention of new tokens over a paged cache on the matrix cores (paged.h: how the work is cut; window_mfma.h: the arithmetic of a tile).
+//
+// Keys and values go from their pages straight into LDS, eight rows of one page a load.  The table's entries are fetched 64 at a time, a lane
+// each: a load's page is then a wave-uniform value, and the loop waits for the table once in 16 tiles (wide) or 32 halves (narrow).
+// What a load must not read (positions behind the document's last one, pages that the table does not name) is replaced by the last position's row,
+// which nobody gives weight there.
+#include "kernels.h"
+#include "window_mfma.h"
+
+namespace dipaco {
+
+namespace {
+
+// v, the same in every lane, in scalar registers
+__device__ __forceinline__ const char* uniform(const char* v) {
+  const uint64_t a = (uint64_t)v;
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)a), hi = __builtin_amdgcn_readfirstlane((uint32_t)(a >> 32));
+  return reinterpret_cast<const char*>(((uint64_t)hi << 32) | lo);
+}
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return __builtin_amdgcn_readfirstlane(v); }
+
+// where a document's keys of one head lie
+template <int DH> struct PagePlace {
+  const char* base;          // keys of this head in page 0
+  long page_bytes, value_bytes;
+  int b, shift, last;
+  long safe;                 // the last position's key, from base
+  __device__ __forceinline__ PagePlace(const PagedArgs<bf16>& a, int b, int hk, int last) : b(b), shift(a.page_shift), last(last) {
+    base = reinterpret_cast<const char*>(a.cache + a.template key_offset<DH>(0, hk, 0));
+    page_bytes = ((long)2 * a.H_kv << shift) * DH * 2;
+    value_bytes = a.template value_from_key<DH>() * 2;
+    const int page = a.page_of(b, last);
+    safe = page < 0 ? 0 : page * page_bytes + (last & ((1 << shift) - 1)) * DH * 2;
+  }
+  __device__ __forceinline__ long at(int page, int pos) const { return page * page_bytes + (long)((pos & ((1 << shift) - 1)) * DH * 2); }
+};
+
+// A row of the block: which, where its query lies and what it sees
+template <int DH> struct PagedRow {
+  bool valid;
+  long row;
+  int head, pos, near;
+  const bf16* q;
+  __device__ __forceinline__ PagedRow(const PagedArgs<bf16>& a, int R, int packed, int row0, int pos0, int hk) {
+    const int G = a.group(), token = R / G;
+    valid = R < packed;
+    row = row0 + token;
+    head = hk * G + R - token * G;
+    pos = pos0 + token;
+    near = a.w.near_from(pos);
+    q = a.qkv + row * (a.H + 2 * a.H_kv) * DH + head * DH;
+  }
+  __device__ __forceinline__ void load(uint4 (&qf)[DH / 16], int h) const {
+#pragma unroll
+    for (int ks = 0; ks < DH / 16; ++ks) qf[ks] = valid ? *reinterpret_cast<const uint4*>(q + 8 * (2 * ks + h)) : make_uint4(0, 0, 0, 0);
+  }
+};
+// o of a row over the keys k0 .. k0 + n - 1 that it sees, pair by pair: x.o += ...
+template <int DH>
+__device__ __forceinline__ void add_seen(SoftmaxRow<DH>& x, const PagedArgs<bf16>& a, const PagePlace<DH>& at, const PagedRow<DH>& row, int k0, int n, int h) {
+  const float sc = score_scale<DH>() * LOG2E;
+#pragma unroll 1
+  for (int key = k0; key < k0 + n; ++key) {
+    const int page = key > at.last ? -1 : a.page_of(at.b, key);
+    if (page < 0 || key > row.pos || (key < row.near && key >= a.w.sinks)) continue;
+    const char* const k = at.base + at.at(page, key);
+    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(plain::dot<DH>(row.q, reinterpret_cast<const bf16*>(k)), sc, x.m_neg));
+    plain::add_row(x.o, p, reinterpret_cast<const bf16*>(k + at.value_bytes), h);
+  }
+}
+
+// the document and block of the i-th wide block of the call (-1: there are fewer); the whole wave
+__device__ __forceinline__ int find_wide_block(const PagedArgs<bf16>& a, int& i, int lane) {
+  for (int b0 = 0; b0 < a.B; b0 += 64) {
+    int n = 0;
+    if (b0 + lane < a.B) {
+      const int packed = min(ragged_rows(a.row_start, b0 + lane, a.T_rows).count, a.max_new) * a.group();
+      n = packed > NARROW_ROWS ? (packed + WIDE_ROWS - 1) / WIDE_ROWS : 0;
+    }
+    int upto = n;   // blocks of documents b0 .. b0 + lane
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int before = __shfl_up(upto, d, WAVE);
+      if (lane >= d) upto += before;
+    }
+    const int all = __builtin_amdgcn_readlane(upto, 63);
+    if (i < all) {
+      const unsigned long long before = __builtin_amdgcn_ballot_w64(upto <= i);
+      const int at = __builtin_popcountll(before);
+      i -= at ? __builtin_amdgcn_readlane(upto, at - 1) : 0;
+      return b0 + at;
+    }
+    i -= all;
+  }
+  return -1;
+}
+
+// ---- wide ----------------------------------------------------------------------------------------------------------
+template <int DH>
+__global__ void __launch_bounds__(AT_THREADS, 2) paged_wide_mfma(PagedArgs<bf16> a, int blocks) {
+  constexpr int KS = DH / 16, NP = panels<DH>(), TILE_BYTES = tile_bytes<DH>();
+  extern __shared__ __attribute__((aligned(16))) char pw_smem[];   // [stage][K | V]
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, h = lane >> 5;
+  const int item = blockIdx.x / blocks, hk = item % a.H_kv, split = item / a.H_kv;
+  int block = blockIdx.x - item * blocks;
+  const int b = __builtin_amdgcn_readfirstlane(find_wide_block(a, block, lane));
+  if (b < 0) return;
+  const PagedBlock<6> blk(a, b, __builtin_amdgcn_readfirstlane(block), WIDE_ROWS, a.wide_splits);
+  const int t0 = split * blk.per, n_tiles = min(blk.tiles.count - t0, blk.per);
+  if (split >= max(blk.used, 1)) return;
+  const int G = a.group(), r0 = blk.packed0 + 32 * wave;
+  int R = r0 + r;
+  const int pos = blk.pos0 + R / G, near = a.w.near_from(pos);
+  const RowSpan span{blk.pos0 + r0 / G, r0 < blk.packed ? blk.pos0 + (min(r0 + 31, blk.packed - 1)) / G : -1};
+  SoftmaxRow<DH> x;
+  x.clear();
+  if (n_tiles > 0) {
+    uint4 qf[KS];
+    PagedRow<DH>(a, R, blk.packed, blk.row0, blk.pos0, hk).load(qf, h);
+    const FragOff fo = frag_offsets(lane);
+    const TrOff to = tr_offsets(lane);
+    const uint32_t smem_addr = (uint32_t)(uintptr_t)pw_smem;
+    const PagePlace<DH> at(a, b, hk, blk.last);
+    const uint32_t col = loader_column_bytes<DH>(0, wave, lane), off = (uint32_t)((lane >> 3) * DH * 2) + col;   // the same for both row groups of a wave
+    int ids = 0;   // lane 4 (t % 16) + g: the page of rows 16 g .. of tile t
+    auto issue = [&](int t, int stage) -> int {
+      const int tile = blk.tiles.at(t0 + t), row0 = tile * 64;
+      if ((t & 15) == 0) ids = a.page_of(b, min(blk.tiles.at(t0 + min(t + (lane >> 2), n_tiles - 1)) * 64 + 16 * (lane & 3), at.last));
+      const int l0 = 4 * (t & 15);
+      const int holes = (int)((__builtin_amdgcn_ballot_w64(ids < 0) >> l0) & 15);
+      const uint32_t dst = uniform(smem_addr + stage * 2 * TILE_BYTES + wave * 1024);
+      if (holes == 0 && row0 + 63 <= at.last) {   // wave-uniform
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int rows8 = row0 + 8 * (wave + 4 * i);
+          const char* const k = uniform(at.base + at.at(__builtin_amdgcn_readlane(ids, l0 + ((wave + 4 * i) >> 1)), rows8));
+          const char* const v = uniform(k + at.value_bytes);
+#pragma unroll
+          for (int p = 0; p < NP; ++p) {
+            load16_to_lds_at(k + 128 * p, off, dst + i * 4096 + p * PANEL_BYTES);
+            load16_to_lds_at(v + 128 * p, off, dst + i * 4096 + TILE_BYTES + p * PANEL_BYTES);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int pos = row0 + 8 * (wave + 4 * i) + (lane >> 3);
+          const int id = __shfl(ids, l0 + ((wave + 4 * i) >> 1), WAVE);
+          const char* const k = at.base + (id < 0 || pos > at.last ? at.safe : at.at(id, pos)) + col;
+#pragma unroll
+          for (int p = 0; p < NP; ++p) {
+            load16_to_lds(k + 128 * p, dst + i * 4096 + p * PANEL_BYTES);
+            load16_to_lds(k + at.value_bytes + 128 * p, dst + i * 4096 + TILE_BYTES + p * PANEL_BYTES);
+          }
+        }
+      }
+      return holes;
+    };
+    int holes = issue(0, 0);
+    for (int t = 0; t < n_tiles; ++t) {
+      wait_vmcnt<0>();
+      __syncthreads();
+      const int mine = holes;
+      if (t + 1 < n_tiles) holes = issue(t + 1, (t + 1) & 1);
+      const char* k_ = pw_smem + (t & 1) * 2 * TILE_BYTES;
+      // a position behind the table's end holds no key: rows there see up to the last one that does
+      attend_tile<DH>(x, qf, k_, k_ + TILE_BYTES, fo, to, blk.tiles.at(t0 + t) * 64, mine, a.w, span, blk.hi > at.last, min(pos, at.last), near, lane);
+    }
+    x.l += __shfl_xor(x.l, 32, WAVE);
+    asm volatile("" : "+v"(R));   // what follows is formed anew, not kept through the loop
+    const PagedRow<DH> row(a, R, blk.packed, blk.row0, blk.pos0, hk);
+    if (__any(row.valid && plain::not_finite(x.o)) && row.valid) {
+      plain::clear(x.o);
+      for (int t = 0; t < n_tiles; ++t) add_seen<DH>(x, a, at, row, blk.tiles.at(t0 + t) * 64, 64, h);
+    }
+  }
+  asm volatile("" : "+v"(R));
+  const PagedRow<DH> row(a, R, blk.packed, blk.row0, blk.pos0, hk);
+  if (!row.valid) return;
+  if (blk.used <= 1) {
+    store_transposed_out(a.o + (row.row * a.H + row.head) * DH, x.o, h, x.m == -INFINITY ? 0.f : 1.0f / x.l);
+    if (a.lse && h == 0) a.lse[row.row * a.H + row.head] = (x.m + __builtin_amdgcn_logf(x.l)) * LN2;   // v_log_f32 is log2; -inf where nothing is seen
+  } else {
+    float* const sums = a.template part_sums<DH>(split, row.row, row.head);
+#pragma unroll
+    for (int dt = 0; dt < DH / 32; ++dt)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<float4*>(sums + 32 * dt + 8 * g + 4 * h) = make_float4(x.o[dt][4 * g], x.o[dt][4 * g + 1], x.o[dt][4 * g + 2], x.o[dt][4 * g + 3]);
+    if (h == 0) *a.template part_state<DH>(a.wide_splits, split, row.row, row.head) = make_float2(x.m, x.l);
+  }
+}
+
+// ---- narrow --------------------------------------------------------------------------------------------------------
+template <int DH> constexpr int narrow_stages() { return DH == 128 ? 2 : 4; }
+template <int DH> constexpr int narrow_stage() { return panels<DH>() * PANEL_BYTES; }   // 32 rows of K and V: a panel holds K's, then V's
+template <int DH> constexpr int narrow_lds() { return 4 * narrow_stages<DH>() * narrow_stage<DH>(); }
+
+template <int DH>
+__global__ void __launch_bounds__(AT_THREADS, 1) paged_narrow_mfma(PagedArgs<bf16> a) {
+  constexpr int KS = DH / 16, DT = DH / 32, NP = panels<DH>(), NS = narrow_stages<DH>(), STAGE = narrow_stage<DH>(), LPW = 8 * NP;
+  extern __shared__ __attribute__((aligned(16))) char pn_smem[];   // [wave][stage]
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, h = lane >> 5;
+  const int item = blockIdx.x / a.narrow_splits, split = blockIdx.x - item * a.narrow_splits, b = item / a.H_kv, hk = item - b * a.H_kv;
+  const PagedBlock<5> blk(a, b, 0, NARROW_ROWS, a.narrow_splits);
+  if (blk.packed == 0 || blk.packed > NARROW_ROWS || split >= max(blk.used, 1)) return;
+  const int t0 = split * blk.per, end = min(t0 + blk.per, blk.tiles.count), n = (end - t0 - wave + 3) >> 2;   // this wave's halves: t0 + wave, + 4, ..
+  const PagedRow<DH> row(a, r, blk.packed, blk.row0, blk.pos0, hk);
+  const RowSpan span{blk.lo, blk.hi};
+  SoftmaxRow<DH> x;
+  x.clear();
+  if (n > 0) {
+    const FragOff fo = frag_offsets(lane);
+    const TrOff to = tr_offsets(lane);
+    char* const ring = pn_smem + wave * NS * STAGE;
+    const uint32_t ring_addr = (uint32_t)(uintptr_t)ring;
+    const PagePlace<DH> at(a, b, hk, blk.last);
+    uint32_t col[2], off[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      int c = (lane & 7) ^ swz64(8 * i + (lane >> 3));
+      if (DH == 32) c &= 3;
+      col[i] = (uint32_t)(c * 16);
+      off[i] = (uint32_t)((lane >> 3) * DH * 2) + col[i];
+    }
+    int ids = 0;   // lane 2 (t % 32) + g: the page of rows 16 g .. of this wave's half t
+    auto half_at = [&](int t) { return blk.tiles.at(t0 + wave + 4 * t) * 32; };
+    auto holes_of = [&](unsigned long long none, int t) { return (int)((none >> (2 * (t & 31))) & 3); };
+    unsigned long long none = 0;   // which of the lanes' pages are none; of the 32 halves before as well
+    unsigned long long none_before = 0;
+    auto issue = [&](int t) {
+      const int row0 = half_at(t);
+      if ((t & 31) == 0) {
+        ids = a.page_of(b, min(half_at(min(t + (lane >> 1), n - 1)) + 16 * (lane & 1), at.last));
+        none_before = none;
+        none = __builtin_amdgcn_ballot_w64(ids < 0);
+      }
+      const int l0 = 2 * (t & 31);
+      const uint32_t dst = uniform(ring_addr + (t % NS) * STAGE);
+      if (holes_of(none, t) == 0 && row0 + 31 <= at.last) {   // wave-uniform
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const char* const k = uniform(at.base + at.at(__builtin_amdgcn_readlane(ids, l0 + (i >> 1)), row0 + 8 * i));
+          const char* const v = uniform(k + at.value_bytes);
+#pragma unroll
+          for (int p = 0; p < NP; ++p) {
+            load16_to_lds_at(k + 128 * p, off[i & 1], dst + i * 1024 + p * PANEL_BYTES);
+            load16_to_lds_at(v + 128 * p, off[i & 1], dst + i * 1024 + 4096 + p * PANEL_BYTES);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int pos = row0 + 8 * i + (lane >> 3), id = __shfl(ids, l0 + (i >> 1), WAVE);
+          const char* const k = at.base + (id < 0 || pos > at.last ? at.safe : at.at(id, pos)) + col[i & 1];
+#pragma unroll
+          for (int p = 0; p < NP; ++p) {
+            load16_to_lds(k + 128 * p, dst + i * 1024 + p * PANEL_BYTES);
+            load16_to_lds(k + at.value_bytes + 128 * p, dst + i * 1024 + 4096 + p * PANEL_BYTES);
+          }
+        }
+      }
+    };
+#pragma unroll
+    for (int t = 0; t < NS - 1; ++t)
+      if (t < n) issue(t);
+    uint4 qf[KS];
+    row.load(qf, h);
+    for (int t = 0; t < n; ++t) {
+      // half t has landed: the loads behind it are those of the next NS - 2 halves (the query's, issued among the first, only make this wait longer)
+      wait_stages_but<LPW>(min(NS - 2, n - 1 - t));
+      asm volatile("" ::: "memory");
+      if (t + NS - 1 < n) issue(t + NS - 1);   // into the stage of half t - 1, whose reads its products have waited for
+      const int k0 = half_at(t), holes = holes_of((t >> 5) == ((min(t + NS - 1, n - 1)) >> 5) ? none : none_before, t);
+      const int s = holes == 3 ? NONE : seen_half(a.w, span, k0);
+      const char* k_ = ring + (t % NS) * STAGE;
+      if (s != NONE)
+        attend_half<DH, 1>(x, qf, k_, k_ + 4096, fo, to, k0, s != ALL_PAIRS || holes || blk.hi > at.last, holes, min(row.pos, at.last), row.near, a.w.sinks, lane);
+      asm volatile("" ::: "memory");
+    }
+    x.l += __shfl_xor(x.l, 32, WAVE);
+    if (__any(row.valid && plain::not_finite(x.o)) && row.valid) {
+      plain::clear(x.o);
+      for (int t = 0; t < n; ++t) add_seen<DH>(x, a, at, row, half_at(t), 32, h);
+    }
+  }
+  // the four waves' sums meet in LDS: wave w adds accumulator elements 4w .. 4w + 3 of every 32 columns
+  constexpr int PER = 16 * DT * WAVE;
+  static_assert((4 * PER + 2 * 4 * WAVE) * 4 <= narrow_lds<DH>(), "the sums fit in the rings");
+  float* const sums = reinterpret_cast<float*>(pn_smem);
+  float2* const state = reinterpret_cast<float2*>(sums + 4 * PER);
+  __syncthreads();   // the rings have been read
+  hand_over(x.o, sums + wave * PER, lane);
+  state[wave * WAVE + lane] = make_float2(x.m, x.l);
+  __syncthreads();
+  if (!row.valid) return;
+  float2 st[4];
+#pragma unroll
+  for (int w = 0; w < 4; ++w) st[w] = state[w * WAVE + lane];
+  const float m = fmaxf(fmaxf(st[0].x, st[1].x), fmaxf(st[2].x, st[3].x));
+  float c[4], l = 0.f;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    c[w] = st[w].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st[w].x - m);
+    l = __builtin_fmaf(st[w].y, c[w], l);
+  }
+  const bool whole = blk.used <= 1;
+  const float scale = !whole ? 1.f : m == -INFINITY ? 0.f : 1.0f / l;
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) {
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float4 p = *reinterpret_cast<const float4*>(sums + w * PER + ((dt * 4 + wave) * WAVE + lane) * 4);
+      v.x = __builtin_fmaf(p.x, c[w], v.x); v.y = __builtin_fmaf(p.y, c[w], v.y); v.z = __builtin_fmaf(p.z, c[w], v.z); v.w = __builtin_fmaf(p.w, c[w], v.w);
+    }
+    const int at = 32 * dt + 8 * wave + 4 * h;
+    if (whole) {
+      const bf16x4 out = {(bf16)(v.x * scale), (bf16)(v.y * scale), (bf16)(v.z * scale), (bf16)(v.w * scale)};
+      *reinterpret_cast<bf16x4*>(a.o + (row.row * a.H + row.head) * DH + at) = out;
+    } else {
+      *reinterpret_cast<float4*>(a.template part_sums<DH>(split, row.row, row.head) + at) = v;
+    }
+  }
+  if (wave == 0 && h == 0) {
+    if (!whole) *a.template part_state<DH>(a.narrow_splits, split, row.row, row.head) = make_float2(m, l);
+    else if (a.lse) a.lse[row.row * a.H + row.head] = (m + __builtin_amdgcn_logf(l)) * LN2;
+  }
+}
+
+}  // namespace
+
+template <int DH> dipaco_status launch_paged_narrow_mfma(const PagedArgs<bf16>& a, hipStream_t s) {
+  static std::atomic<unsigned long long> lds_set{0};
+  if (dipaco_status st = ensure_dynamic_lds(reinterpret_cast<const void*>(paged_narrow_mfma<DH>), narrow_lds<DH>(), lds_set)) return st;
+  paged_narrow_mfma<DH><<<a.B * a.H_kv * a.narrow_splits, AT_THREADS, narrow_lds<DH>(), s>>>(a);
+  DIPACO_LAUNCH_CHECK();
+  return DIPACO_OK;
+}
+template <int DH> dipaco_status launch_paged_wide_mfma(const PagedArgs<bf16>& a, int blocks, hipStream_t s) {
+  constexpr int LDS = 4 * tile_bytes<DH>();
+  static std::atomic<unsigned long long> lds_set{0};
+  if (dipaco_status st = ensure_dynamic_lds(reinterpret_cast<const void*>(paged_wide_mfma<DH>), LDS, lds_set)) return st;
+  paged_wide_mfma<DH><<<blocks * a.H_kv * a.wide_splits, AT_THREADS, LDS, s>>>(a, blocks);
+  DIPACO_LAUNCH_CHECK();
+  return DIPACO_OK;
+}
+template dipaco_status launch_paged_narrow_mfma<32>(const PagedArgs<bf16>&, hipStream_t);
+template dipaco_status launch_paged_narrow_mfma<64>(const PagedArgs<bf16>&, hipStream_t);
+template dipaco_status launch_paged_narrow_mfma<128>(const PagedArgs<bf16>&, hipStream_t);
+template dipaco_status launch_paged_wide_mfma<32>(const PagedArgs<bf16>&, int, hipStream_t);
+template dipaco_status launch_paged_wide_mfma<64>(const PagedArgs<bf16>&, int, hipStream_t);
+template dipaco_status launch_paged_wide_mfma<128>(const PagedArgs<bf16>&, int, hipStream_t);
+
+}  // namespace dipaco

@@ -10,23 +10,11 @@
 // their sum is taken in fp32 before that, so that lse keeps fp32's digits.
 #pragma once
 #include "attention_mfma.h"
-#include "visible.h"
+#include "paged.h"
 
 namespace dipaco {
 
 namespace {
-
-// The tiles of 64 keys that rows at positions lo .. hi see: the first `front` of the document, then `first` to that of position hi
-struct TileList {
-  int front, first, count;
-  __device__ __forceinline__ TileList(const Window& w, int lo, int hi) {
-    const int near = w.near_from(lo);
-    first = near >> 6;
-    front = min((min(w.sinks, near) + 63) >> 6, first);
-    count = front + (hi >> 6) + 1 - first;
-  }
-  __device__ __forceinline__ int at(int t) const { return t < front ? t : first + t - front; }
-};
 
 // max of three, NaN ignored.  As an instruction of its own: fmaxf has the compiler quiet every operand first, one more instruction an element.
 // The operands must not come straight from a matrix instruction: see max_of.
@@ -124,16 +112,16 @@ __device__ __forceinline__ void attend_half(SoftmaxRow<DH>& x, const uint4 (&qf)
     }
   }
 }
-// a tile of 64 keys: both halves in one go where both are seen, else the one that is
+// a tile of 64 keys: both halves in one go where both are seen, else the one that is.  masked: the mask is needed whatever the span says
 template <int DH>
 __device__ __forceinline__ void attend_tile(SoftmaxRow<DH>& x, const uint4 (&qf)[DH / 16], const char* k_, const char* v_, const FragOff& fo, const TrOff& to,
-                                            int k0, int holes, const Window& w, const RowSpan& span, int pos, int near, int lane) {
-  const int a = holes == 15 ? NONE : seen_half(w, span, k0), b = holes == 15 ? NONE : seen_half(w, span, k0 + 32);
+                                            int k0, int holes, const Window& w, const RowSpan& span, bool masked, int pos, int near, int lane) {
+  const int a = (holes & 3) == 3 ? NONE : seen_half(w, span, k0), b = holes >> 2 == 3 ? NONE : seen_half(w, span, k0 + 32);
   if (a != NONE && b != NONE)
-    attend_half<DH, 2>(x, qf, k_, v_, fo, to, k0, a + b != 2 * ALL_PAIRS || holes, holes, pos, near, w.sinks, lane);
+    attend_half<DH, 2>(x, qf, k_, v_, fo, to, k0, masked || a + b != 2 * ALL_PAIRS || holes, holes, pos, near, w.sinks, lane);
   else if (a != NONE || b != NONE) {
     const int half = a != NONE ? 0 : 1;
-    attend_half<DH, 1>(x, qf, k_ + 4096 * half, v_ + 4096 * half, fo, to, k0 + 32 * half, a + b != ALL_PAIRS || holes, holes >> (2 * half), pos, near,
+    attend_half<DH, 1>(x, qf, k_ + 4096 * half, v_ + 4096 * half, fo, to, k0 + 32 * half, masked || a + b != ALL_PAIRS || holes, holes >> (2 * half), pos, near,
                        w.sinks, lane);
   }
 }
