@@ -115,7 +115,7 @@ dipaco_status dipaco_k_attention_window_bwd(int32_t dtype, const void* qkv, cons
  *              of document b, none or more.  Rows behind row_start[B] belong to nobody.
  *   cache_len  device int32 [B]: positions that document b had in front of them: its first new token is position
  *              cache_len[b].  All of these are read on the device: a captured graph follows their values.
- * T * H <= 2^25, B <= 2^20, pages_per_doc * page_size <= 2^28.
+ * T <= 2^23, T * H <= 2^25, B <= 2^20, B * H <= 2^22, pages_per_doc * page_size <= 2^28.
  * dipaco_k_cache_append writes the new tokens' keys and values into the pages. */
 dipaco_status dipaco_k_cache_append(int32_t dtype, const void* qkv, const int32_t* row_start, const int32_t* cache_len,
                                     const int32_t* pages, void* cache, int32_t T, int32_t B, int32_t H, int32_t H_kv,

@@ -399,7 +399,8 @@ static dipaco_status check_cache(int32_t T, int32_t B, int32_t H, int32_t n_page
   if (T < 0 || B < 1 || n_pages < 1 || pages_per_doc < 1) return fail(DIPACO_EINVAL, "T >= 0, B >= 1, n_pages >= 1 and pages_per_doc >= 1 required");
   if (page_size != 16 && page_size != 32 && page_size != 64 && page_size != 128 && page_size != 256)
     return fail(DIPACO_ESHAPE, "page_size must be 16, 32, 64, 128 or 256");
-  if ((int64_t)T * H > (1LL << 25) || B > (1 << 20)) return fail(DIPACO_ESHAPE, "T * H <= 2^25 and B <= 2^20 required");
+  if (T > (1 << 23) || (int64_t)T * H > (1LL << 25) || B > (1 << 20) || (int64_t)B * H > (1LL << 22))
+    return fail(DIPACO_ESHAPE, "T <= 2^23, T * H <= 2^25, B <= 2^20 and B * H <= 2^22 required");
   if ((int64_t)pages_per_doc * page_size > (1 << 28)) return fail(DIPACO_ESHAPE, "a document may hold 2^28 positions");
   return DIPACO_OK;
 }

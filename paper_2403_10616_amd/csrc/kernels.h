@@ -316,13 +316,21 @@ dipaco_status launch_window_fwd_mfma(const bf16* qkv, const int* lengths, bf16* 
 template <int DH>
 dipaco_status launch_window_bwd_mfma(const bf16* qkv, const int* lengths, const bf16* o, const bf16* d_o, const float* lse, bf16* dqkv, float* dsum, int B, int S,
                                      int H, int H_kv, Window w, hipStream_t s);
+// attention_window_f32.hip
+template <int DH>
+dipaco_status launch_window_fwd_f32(const float* qkv, const int* lengths, float* o, float* lse, int B, int S, int H, int H_kv, Window w, hipStream_t s);
+template <int DH>
+dipaco_status launch_window_bwd_f32(const float* qkv, const int* lengths, const float* o, const float* d_o, const float* lse, float* dqkv, float* dsum, int B,
+                                    int S, int H, int H_kv, Window w, hipStream_t s);
 
 // ---- paged.hip ---------------------------------------------------------------------------------------
 template <typename T> dipaco_status launch_cache_append(const PagedArgs<T>& a, int dh, hipStream_t s);
 size_t paged_workspace_bytes(int T_rows, int H, int dh, int page_size, int pages_per_doc);
 template <typename T> dipaco_status launch_attention_paged(PagedArgs<T> a, int dh, void* workspace, hipStream_t s);
-// paged_mfma.hip: bf16, matrix cores
-template <int DH> dipaco_status launch_paged_narrow_mfma(const PagedArgs<bf16>& a, hipStream_t s);
-template <int DH> dipaco_status launch_paged_wide_mfma(const PagedArgs<bf16>& a, int blocks, hipStream_t s);
+// paged_mfma.hip (bf16), paged_f32.hip
+template <int DH> dipaco_status launch_paged_narrow(const PagedArgs<bf16>& a, hipStream_t s);
+template <int DH> dipaco_status launch_paged_wide(const PagedArgs<bf16>& a, int blocks, hipStream_t s);
+template <int DH> dipaco_status launch_paged_narrow(const PagedArgs<float>& a, hipStream_t s);
+template <int DH> dipaco_status launch_paged_wide(const PagedArgs<float>& a, int blocks, hipStream_t s);
 
 }  // namespace dipaco

@@ -5,8 +5,8 @@
 //
 // The query heads that read one key head, G of them, are rows of one product: row R of a document's n G packed rows is token R / G, head
 // R % G of the group.  A workgroup takes a block of packed rows of a document and a key head, and a part ("split") of the keys that these see:
-//   narrow: a document of up to 32 packed rows is one block; its workgroup's waves take the keys in turn, each with a ring of its own.
-//   wide:   128 packed rows, 32 a wave; the waves share the keys' tiles.
+//   narrow: a document of up to 32 packed rows (fp32: 16) is one block; its workgroup's waves take the keys in turn.
+//   wide:   128 packed rows, 32 a wave (fp32: 64, 16 a wave); the waves share the keys' tiles.
 // A split's sums go to the workspace, and paged_join adds them; a block whose keys are one split's writes its rows itself.
 #pragma once
 #include "visible.h"
@@ -26,7 +26,9 @@ template <int SHIFT> struct TileList {
   __device__ __forceinline__ int at(int t) const { return t < front ? t : first + t - front; }
 };
 
-constexpr int NARROW_ROWS = 32, WIDE_ROWS = 128;
+// packed rows of a block, and log2 of the keys of a tile
+template <typename T> struct PagedCut { static constexpr int NARROW_ROWS = 32, NARROW_SHIFT = 5, WIDE_ROWS = 128, WIDE_SHIFT = 6; };
+template <> struct PagedCut<float> { static constexpr int NARROW_ROWS = 16, NARROW_SHIFT = 6, WIDE_ROWS = 64, WIDE_SHIFT = 5; };
 constexpr int SPLIT_KEYS = 512;   // a split has at least so many keys
 constexpr int PAGED_MOST_SPLITS = 64, PAGED_NARROW_GROUPS = 512, PAGED_WIDE_GROUPS = 512;   // splits, and the workgroups that they are to make
 
@@ -88,5 +90,31 @@ template <int SHIFT> struct PagedBlock {
     used = (tiles.count + per - 1) / per;
   }
 };
+
+// the document and block of the i-th wide block of the call (-1: there are fewer); the whole wave
+template <typename T> __device__ __forceinline__ int find_wide_block(const PagedArgs<T>& a, int& i, int lane) {
+  for (int b0 = 0; b0 < a.B; b0 += 64) {
+    int n = 0;
+    if (b0 + lane < a.B) {
+      const int packed = min(ragged_rows(a.row_start, b0 + lane, a.T_rows).count, a.max_new) * a.group();
+      n = packed > PagedCut<T>::NARROW_ROWS ? (packed + PagedCut<T>::WIDE_ROWS - 1) / PagedCut<T>::WIDE_ROWS : 0;
+    }
+    int upto = n;   // blocks of documents b0 .. b0 + lane
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int before = __shfl_up(upto, d, WAVE);
+      if (lane >= d) upto += before;
+    }
+    const int all = __builtin_amdgcn_readlane(upto, 63);
+    if (i < all) {
+      const unsigned long long before = __builtin_amdgcn_ballot_w64(upto <= i);
+      const int at = __builtin_popcountll(before);
+      i -= at ? __builtin_amdgcn_readlane(upto, at - 1) : 0;
+      return b0 + at;
+    }
+    i -= all;
+  }
+  return -1;
+}
 
 }  // namespace dipaco

@@ -4,7 +4,8 @@
 // loads: its document, the document's length, the page) and, for whole chunks, by the bytes.
 //
 // Attention: row r of document b is position cache_len[b] + r - row_start[b] and sees what a position sees under the window
-// (visible.h), among the positions whose page the table holds.  One wave per row and head, 64 keys at a time.
+// (visible.h), among the positions whose page the table holds.  paged.h says how a call is cut into workgroups; here are the plan and the launch
+// that adds what was split.
 #include <type_traits>
 
 #include "kernels.h"
@@ -34,67 +35,6 @@ __global__ void __launch_bounds__(256) cache_append_rows(PagedArgs<T> a, int dh)
   }
 }
 
-template <int DH> constexpr float head_scale() { return DH == 32 ? 0.17677669529663689f : DH == 64 ? 0.125f : 0.088388347648318447f; }
-
-template <int DH, typename T> __device__ __forceinline__ float row_dot(const T* a, const T* b) {
-  constexpr int VEC = Vec16<T>::N;
-  float s = 0.f;
-  for (int c = 0; c < DH; c += VEC) {
-    float x[VEC], y[VEC];
-    load_vec16(a + c, x);
-    load_vec16(b + c, y);
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) s = __builtin_fmaf(x[e], y[e], s);
-  }
-  return s;
-}
-
-template <int DH, typename T>
-__global__ void __launch_bounds__(256) paged_rows(PagedArgs<T> a) {
-  const int lane = threadIdx.x & 63, row = blockIdx.x * 4 + (threadIdx.x >> 6), h = blockIdx.y, hk = h / (a.H / a.H_kv);
-  if (row >= a.T_rows) return;
-  const int b = find_document(a.row_start, a.B, row, lane);
-  const RowRange r = ragged_rows(a.row_start, b, a.T_rows);
-  if (row < r.first || row >= r.first + min(r.count, a.max_new)) return;
-  const int pos = a.cached(b) + row - r.first;
-  const T* const q = a.qkv + (long)row * (a.H + 2 * a.H_kv) * DH + h * DH;
-  float acc[2] = {0.f, 0.f}, m = -INFINITY, l = 0.f;
-  const VisibleList vis(a.w, pos);
-  for (int t0 = 0; t0 < vis.count; t0 += 64) {
-    const int n = min(64, vis.count - t0), j = vis.at(t0 + lane);
-    const int page = lane < n ? a.page_of(b, j) : -1;
-    const long at = page < 0 ? 0 : a.template key_offset<DH>(page, hk, j & ((1 << a.page_shift) - 1));
-    const float s = page < 0 ? -INFINITY : row_dot<DH>(q, a.cache + at) * head_scale<DH>();
-    const float mn = fmaxf(m, wave_max(s));
-    if (mn == -INFINITY) continue;   // nothing seen so far
-    const float corr = expf(m - mn), p = expf(s - mn);
-    m = mn;
-    l = l * corr + wave_sum(p);
-    acc[0] *= corr;
-    acc[1] *= corr;
-    for (int t = 0; t < n; ++t) {
-      if (__builtin_amdgcn_readlane(page, t) < 0) continue;
-      const float pt = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, p), t));
-      const long from = __shfl(at, t, WAVE) + a.template value_from_key<DH>();
-#pragma unroll
-      for (int c = 0; c < (DH == 128 ? 2 : 1); ++c)
-        if (DH >= 64 || lane < DH) acc[c] = __builtin_fmaf(pt, to_f32(a.cache[from + lane + 64 * c]), acc[c]);
-    }
-  }
-  T* const out = a.o + ((long)row * a.H + h) * DH;
-  const float scale = m == -INFINITY ? 0.f : 1.f / l;
-#pragma unroll
-  for (int c = 0; c < (DH == 128 ? 2 : 1); ++c)
-    if (DH >= 64 || lane < DH) out[lane + 64 * c] = from_f32<T>(acc[c] * scale);
-  if (a.lse && lane == 0) a.lse[(long)row * a.H + h] = m == -INFINITY ? -INFINITY : m + logf(l);
-}
-
-template <int DH, typename T> dipaco_status attend(const PagedArgs<T>& a, hipStream_t s) {
-  paged_rows<DH, T><<<dim3((a.T_rows + 3) / 4, a.H), 256, 0, s>>>(a);
-  DIPACO_LAUNCH_CHECK();
-  return DIPACO_OK;
-}
-
 // The splits' sums of the blocks that were split, added in their order.  A workgroup per row, DH / 4 threads a head.
 template <int DH, typename T>
 __global__ void __launch_bounds__(256) paged_join(PagedArgs<T> a) {
@@ -103,11 +43,13 @@ __global__ void __launch_bounds__(256) paged_join(PagedArgs<T> a) {
   const RowRange r = ragged_rows(a.row_start, b, a.T_rows);
   const int rows = min(r.count, a.max_new);
   if (row < r.first || row >= r.first + rows) return;
-  const bool narrow = rows * G <= NARROW_ROWS;
+  using Cut = PagedCut<T>;
+  const bool narrow = rows * G <= Cut::NARROW_ROWS;
   const int splits = narrow ? a.narrow_splits : a.wide_splits;
   for (int i = threadIdx.x; i < a.H * PER; i += 256) {
     const int head = i / PER, c = 4 * (i - head * PER), R = (row - r.first) * G + head % G;
-    const int used = narrow ? PagedBlock<5>(a, b, 0, NARROW_ROWS, splits).used : PagedBlock<6>(a, b, R / WIDE_ROWS, WIDE_ROWS, splits).used;
+    const int used = narrow ? PagedBlock<Cut::NARROW_SHIFT>(a, b, 0, Cut::NARROW_ROWS, splits).used
+                            : PagedBlock<Cut::WIDE_SHIFT>(a, b, R / Cut::WIDE_ROWS, Cut::WIDE_ROWS, splits).used;
     if (used <= 1) continue;   // its workgroup has written it
     float m = -INFINITY, l = 0.f;
     for (int s = 0; s < used; ++s) m = fmaxf(m, a.template part_state<DH>(splits, s, row, head)->x);
@@ -136,6 +78,7 @@ inline int most_splits(int page_size, int pages_per_doc) {
   return (int)std::min<int64_t>(PAGED_MOST_SPLITS, ((int64_t)page_size * pages_per_doc + SPLIT_KEYS - 1) / SPLIT_KEYS);
 }
 template <typename T> PagedPlan plan(const PagedArgs<T>& a) {
+  constexpr int NARROW_ROWS = PagedCut<T>::NARROW_ROWS, WIDE_ROWS = PagedCut<T>::WIDE_ROWS;
   const int G = a.H / a.H_kv, page_size = 1 << a.page_shift;
   const int64_t seen = std::min<int64_t>((int64_t)page_size * a.pages_per_doc, (int64_t)a.w.window + a.w.sinks + WIDE_ROWS);   // keys of a block, about
   const int most = std::max(1, (int)std::min<int64_t>(most_splits(page_size, a.pages_per_doc), (seen + SPLIT_KEYS - 1) / SPLIT_KEYS));
@@ -159,30 +102,27 @@ template <typename T> dipaco_status launch_cache_append(const PagedArgs<T>& a, i
 // GROUPS / n + 1 workgroups a split with up to 128 (32) packed rows each.  Non-decreasing in every size but the heads'.
 size_t paged_workspace_bytes(int T_rows, int H, int dh, int page_size, int pages_per_doc) {
   const size_t most = most_splits(page_size, pages_per_doc);
-  constexpr size_t GROUP_ROWS = std::max(PAGED_WIDE_GROUPS * WIDE_ROWS, PAGED_NARROW_GROUPS * NARROW_ROWS);
+  constexpr size_t GROUP_ROWS = std::max(PAGED_WIDE_GROUPS * PagedCut<bf16>::WIDE_ROWS, PAGED_NARROW_GROUPS * PagedCut<bf16>::NARROW_ROWS);
   const size_t rows = std::min(most * T_rows, (size_t)T_rows + (GROUP_ROWS + H - 1) / H);
   return 256 + rows * H * (dh + 2) * sizeof(float);
 }
 template <typename T> dipaco_status launch_attention_paged(PagedArgs<T> a, int dh, void* workspace, hipStream_t s) {
-  if constexpr (std::is_same<T, bf16>::value) {
-    const PagedPlan p = plan(a);
-    a.narrow_splits = p.narrow_splits;
-    a.wide_splits = p.wide_splits;
-    a.part = static_cast<float*>(workspace);
-    auto run = [&](auto DHc) -> dipaco_status {
-      constexpr int DH = decltype(DHc)::value;
-      if (p.wide_blocks)
-        if (dipaco_status st = launch_paged_wide_mfma<DH>(a, p.wide_blocks, s)) return st;
-      if (dipaco_status st = launch_paged_narrow_mfma<DH>(a, s)) return st;
-      if (p.narrow_splits > 1 || (p.wide_blocks && p.wide_splits > 1)) {
-        paged_join<DH, T><<<a.T_rows, 256, 0, s>>>(a);
-        DIPACO_LAUNCH_CHECK();
-      }
-      return DIPACO_OK;
-    };
-    return dh == 32 ? run(std::integral_constant<int, 32>{}) : dh == 64 ? run(std::integral_constant<int, 64>{}) : run(std::integral_constant<int, 128>{});
-  }
-  return dh == 32 ? attend<32>(a, s) : dh == 64 ? attend<64>(a, s) : attend<128>(a, s);
+  const PagedPlan p = plan(a);
+  a.narrow_splits = p.narrow_splits;
+  a.wide_splits = p.wide_splits;
+  a.part = static_cast<float*>(workspace);
+  auto run = [&](auto DHc) -> dipaco_status {
+    constexpr int DH = decltype(DHc)::value;
+    if (p.wide_blocks)
+      if (dipaco_status st = launch_paged_wide<DH>(a, p.wide_blocks, s)) return st;
+    if (dipaco_status st = launch_paged_narrow<DH>(a, s)) return st;
+    if (p.narrow_splits > 1 || (p.wide_blocks && p.wide_splits > 1)) {
+      paged_join<DH, T><<<a.T_rows, 256, 0, s>>>(a);
+      DIPACO_LAUNCH_CHECK();
+    }
+    return DIPACO_OK;
+  };
+  return dh == 32 ? run(std::integral_constant<int, 32>{}) : dh == 64 ? run(std::integral_constant<int, 64>{}) : run(std::integral_constant<int, 128>{});
 }
 template dipaco_status launch_cache_append<float>(const PagedArgs<float>&, int, hipStream_t);
 template dipaco_status launch_cache_append<bf16>(const PagedArgs<bf16>&, int, hipStream_t);

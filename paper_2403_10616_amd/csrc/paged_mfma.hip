@@ -19,6 +19,8 @@ __device__ __forceinline__ const char* uniform(const char* v) {
 }
 __device__ __forceinline__ uint32_t uniform(uint32_t v) { return __builtin_amdgcn_readfirstlane(v); }
 
+using Cut = PagedCut<bf16>;
+
 // where a document's keys of one head lie
 template <int DH> struct PagePlace {
   const char* base;          // keys of this head in page 0
@@ -69,32 +71,6 @@ __device__ __forceinline__ void add_seen(SoftmaxRow<DH>& x, const PagedArgs<bf16
   }
 }
 
-// the document and block of the i-th wide block of the call (-1: there are fewer); the whole wave
-__device__ __forceinline__ int find_wide_block(const PagedArgs<bf16>& a, int& i, int lane) {
-  for (int b0 = 0; b0 < a.B; b0 += 64) {
-    int n = 0;
-    if (b0 + lane < a.B) {
-      const int packed = min(ragged_rows(a.row_start, b0 + lane, a.T_rows).count, a.max_new) * a.group();
-      n = packed > NARROW_ROWS ? (packed + WIDE_ROWS - 1) / WIDE_ROWS : 0;
-    }
-    int upto = n;   // blocks of documents b0 .. b0 + lane
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const int before = __shfl_up(upto, d, WAVE);
-      if (lane >= d) upto += before;
-    }
-    const int all = __builtin_amdgcn_readlane(upto, 63);
-    if (i < all) {
-      const unsigned long long before = __builtin_amdgcn_ballot_w64(upto <= i);
-      const int at = __builtin_popcountll(before);
-      i -= at ? __builtin_amdgcn_readlane(upto, at - 1) : 0;
-      return b0 + at;
-    }
-    i -= all;
-  }
-  return -1;
-}
-
 // ---- wide ----------------------------------------------------------------------------------------------------------
 template <int DH>
 __global__ void __launch_bounds__(AT_THREADS, 2) paged_wide_mfma(PagedArgs<bf16> a, int blocks) {
@@ -105,7 +81,7 @@ __global__ void __launch_bounds__(AT_THREADS, 2) paged_wide_mfma(PagedArgs<bf16>
   int block = blockIdx.x - item * blocks;
   const int b = __builtin_amdgcn_readfirstlane(find_wide_block(a, block, lane));
   if (b < 0) return;
-  const PagedBlock<6> blk(a, b, __builtin_amdgcn_readfirstlane(block), WIDE_ROWS, a.wide_splits);
+  const PagedBlock<Cut::WIDE_SHIFT> blk(a, b, __builtin_amdgcn_readfirstlane(block), Cut::WIDE_ROWS, a.wide_splits);
   const int t0 = split * blk.per, n_tiles = min(blk.tiles.count - t0, blk.per);
   if (split >= max(blk.used, 1)) return;
   const int G = a.group(), r0 = blk.packed0 + 32 * wave;
@@ -202,8 +178,8 @@ __global__ void __launch_bounds__(AT_THREADS, 1) paged_narrow_mfma(PagedArgs<bf1
   extern __shared__ __attribute__((aligned(16))) char pn_smem[];   // [wave][stage]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, h = lane >> 5;
   const int item = blockIdx.x / a.narrow_splits, split = blockIdx.x - item * a.narrow_splits, b = item / a.H_kv, hk = item - b * a.H_kv;
-  const PagedBlock<5> blk(a, b, 0, NARROW_ROWS, a.narrow_splits);
-  if (blk.packed == 0 || blk.packed > NARROW_ROWS || split >= max(blk.used, 1)) return;
+  const PagedBlock<Cut::NARROW_SHIFT> blk(a, b, 0, Cut::NARROW_ROWS, a.narrow_splits);
+  if (blk.packed == 0 || blk.packed > Cut::NARROW_ROWS || split >= max(blk.used, 1)) return;
   const int t0 = split * blk.per, end = min(t0 + blk.per, blk.tiles.count), n = (end - t0 - wave + 3) >> 2;   // this wave's halves: t0 + wave, + 4, ..
   const PagedRow<DH> row(a, r, blk.packed, blk.row0, blk.pos0, hk);
   const RowSpan span{blk.lo, blk.hi};
@@ -330,14 +306,14 @@ __global__ void __launch_bounds__(AT_THREADS, 1) paged_narrow_mfma(PagedArgs<bf1
 
 }  // namespace
 
-template <int DH> dipaco_status launch_paged_narrow_mfma(const PagedArgs<bf16>& a, hipStream_t s) {
+template <int DH> dipaco_status launch_paged_narrow(const PagedArgs<bf16>& a, hipStream_t s) {
   static std::atomic<unsigned long long> lds_set{0};
   if (dipaco_status st = ensure_dynamic_lds(reinterpret_cast<const void*>(paged_narrow_mfma<DH>), narrow_lds<DH>(), lds_set)) return st;
   paged_narrow_mfma<DH><<<a.B * a.H_kv * a.narrow_splits, AT_THREADS, narrow_lds<DH>(), s>>>(a);
   DIPACO_LAUNCH_CHECK();
   return DIPACO_OK;
 }
-template <int DH> dipaco_status launch_paged_wide_mfma(const PagedArgs<bf16>& a, int blocks, hipStream_t s) {
+template <int DH> dipaco_status launch_paged_wide(const PagedArgs<bf16>& a, int blocks, hipStream_t s) {
   constexpr int LDS = 4 * tile_bytes<DH>();
   static std::atomic<unsigned long long> lds_set{0};
   if (dipaco_status st = ensure_dynamic_lds(reinterpret_cast<const void*>(paged_wide_mfma<DH>), LDS, lds_set)) return st;
@@ -345,11 +321,11 @@ template <int DH> dipaco_status launch_paged_wide_mfma(const PagedArgs<bf16>& a,
   DIPACO_LAUNCH_CHECK();
   return DIPACO_OK;
 }
-template dipaco_status launch_paged_narrow_mfma<32>(const PagedArgs<bf16>&, hipStream_t);
-template dipaco_status launch_paged_narrow_mfma<64>(const PagedArgs<bf16>&, hipStream_t);
-template dipaco_status launch_paged_narrow_mfma<128>(const PagedArgs<bf16>&, hipStream_t);
-template dipaco_status launch_paged_wide_mfma<32>(const PagedArgs<bf16>&, int, hipStream_t);
-template dipaco_status launch_paged_wide_mfma<64>(const PagedArgs<bf16>&, int, hipStream_t);
-template dipaco_status launch_paged_wide_mfma<128>(const PagedArgs<bf16>&, int, hipStream_t);
+template dipaco_status launch_paged_narrow<32>(const PagedArgs<bf16>&, hipStream_t);
+template dipaco_status launch_paged_narrow<64>(const PagedArgs<bf16>&, hipStream_t);
+template dipaco_status launch_paged_narrow<128>(const PagedArgs<bf16>&, hipStream_t);
+template dipaco_status launch_paged_wide<32>(const PagedArgs<bf16>&, int, hipStream_t);
+template dipaco_status launch_paged_wide<64>(const PagedArgs<bf16>&, int, hipStream_t);
+template dipaco_status launch_paged_wide<128>(const PagedArgs<bf16>&, int, hipStream_t);
 
 }  // namespace dipaco
