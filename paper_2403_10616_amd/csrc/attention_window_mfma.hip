@@ -50,7 +50,7 @@ __global__ void __launch_bounds__(AT_THREADS, DH == 128 ? 2 : 3) window_fwd_mfma
       __syncthreads();   // tile t is in LDS, and nobody still reads the other stage
       if (t + 1 < tiles.count) src.issue(tiles.at(t + 1), wave, lane, smem_addr + (1 - cur) * 2 * TILE_BYTES);
       const char* k_ = wf_smem + cur * 2 * TILE_BYTES;
-      attend_tile<DH>(x, qf, k_, k_ + TILE_BYTES, fo, to, tiles.at(t) * 64, 0, a.w, span, false, q, near, lane);
+      attend_tile<DH>(x, qf, k_, k_ + TILE_BYTES, fo, to, tiles.at(t) * 64, 0, a.w, span, 0, q, near, lane);
     };
     for (int t = 0; t < tiles.count; t += 2) {
       tile(std::integral_constant<int, 0>{}, t);
@@ -157,7 +157,7 @@ template <int DH> __device__ __forceinline__ void window_dq(const WindowArgs& a,
       const int k0 = tiles.at(t) * 64;
       const char* k_ = smem + cur * 2 * TILE_BYTES;
       const char* v_ = k_ + TILE_BYTES;
-      auto halves = [&](auto NTc, int half, bool masked) {
+      auto halves = [&](auto NTc, int half, int seen) {
         constexpr int NT = decltype(NTc)::value;
         f32x16 st[NT], dp[NT];
 #pragma unroll
@@ -173,21 +173,14 @@ template <int DH> __device__ __forceinline__ void window_dq(const WindowArgs& a,
         for (int i = 0; i < NT; ++i)   // dS^T without the factor 1 / sqrt(d_head), which dQ gets when it is stored
 #pragma unroll
           for (int e = 0; e < 16; ++e) st[i][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[i][e], sc, nlse2)) * (dp[i][e] - D);
-        if (masked) {
 #pragma unroll
-          for (int i = 0; i < NT; ++i)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const int key = k0 + 32 * (half + i) + acc_row(e, lane);
-              if (key > q || (key < near && key >= a.w.sinks)) st[i][e] = 0.f;
-            }
-        }
+        for (int i = 0; i < NT; ++i) hide(st[i], seen >> (8 * i), 0.f, k0 + 32 * (half + i), q, near, a.w.sinks, lane);
 #pragma unroll
         for (int i = 0; i < NT; ++i) mma_transposed_half(dq, k_ + 4096 * (half + i), to, st[i]);
       };
       const int s0 = seen_half(a.w, span, k0), s1 = seen_half(a.w, span, k0 + 32);
-      if (s0 != NONE && s1 != NONE) halves(std::integral_constant<int, 2>{}, 0, s0 + s1 != 2 * ALL_PAIRS);
-      else if (s0 != NONE || s1 != NONE) halves(std::integral_constant<int, 1>{}, s0 != NONE ? 0 : 1, s0 + s1 != ALL_PAIRS);
+      if (s0 && s1) halves(std::integral_constant<int, 2>{}, 0, s0 | s1 << 8);
+      else if (s0 | s1) halves(std::integral_constant<int, 1>{}, s0 ? 0 : 1, s0 | s1);
     }
     if (__any(q < rows && plain::not_finite(dq)) && q < rows) {
       plain::clear(dq);
@@ -300,10 +293,13 @@ __device__ __forceinline__ void window_dkv(const WindowArgs& a, const bf16* __re
           }
         }
         if (qh < kw0 + 31 || (!SINKS && qh + 31 > kw0 + a.w.window - 1)) {   // wave-uniform: some pair is hidden
+          asm volatile("");   // a branch, not selections (window_mfma.h: hide)
+          const int from = key - qh - 4 * h, upto = key_last - qh - 4 * h;
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
-            const int q = qh + acc_row(e, lane);
-            if (q < key || q > key_last) { st[e] = 0.f; dp[e] = 0.f; }
+            const bool hidden = 8 * (e >> 2) + (e & 3) < from || 8 * (e >> 2) + (e & 3) > upto;
+            st[e] = hidden ? 0.f : st[e];
+            dp[e] = hidden ? 0.f : dp[e];
           }
         }
         if (want_v) mma_transposed_half(dv, g_ + 4096 * t, to, st);

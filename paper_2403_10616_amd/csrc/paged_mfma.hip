@@ -140,7 +140,7 @@ __global__ void __launch_bounds__(AT_THREADS, 2) paged_wide_mfma(PagedArgs<bf16>
       if (t + 1 < n_tiles) holes = issue(t + 1, (t + 1) & 1);
       const char* k_ = pw_smem + (t & 1) * 2 * TILE_BYTES;
       // a position behind the table's end holds no key: rows there see up to the last one that does
-      attend_tile<DH>(x, qf, k_, k_ + TILE_BYTES, fo, to, blk.tiles.at(t0 + t) * 64, mine, a.w, span, blk.hi > at.last, min(pos, at.last), near, lane);
+      attend_tile<DH>(x, qf, k_, k_ + TILE_BYTES, fo, to, blk.tiles.at(t0 + t) * 64, mine, a.w, span, blk.hi > at.last ? UPPER | LOWER : 0, min(pos, at.last), near, lane);
     }
     x.l += __shfl_xor(x.l, 32, WAVE);
     asm volatile("" : "+v"(R));   // what follows is formed anew, not kept through the loop
@@ -248,10 +248,10 @@ __global__ void __launch_bounds__(AT_THREADS, 1) paged_narrow_mfma(PagedArgs<bf1
       asm volatile("" ::: "memory");
       if (t + NS - 1 < n) issue(t + NS - 1);   // into the stage of half t - 1, whose reads its products have waited for
       const int k0 = half_at(t), holes = holes_of((t >> 5) == ((min(t + NS - 1, n - 1)) >> 5) ? none : none_before, t);
-      const int s = holes == 3 ? NONE : seen_half(a.w, span, k0);
+      const int s = holes == 3 ? 0 : seen_half(a.w, span, k0);
       const char* k_ = ring + (t % NS) * STAGE;
-      if (s != NONE)
-        attend_half<DH, 1>(x, qf, k_, k_ + 4096, fo, to, k0, s != ALL_PAIRS || holes || blk.hi > at.last, holes, min(row.pos, at.last), row.near, a.w.sinks, lane);
+      if (s)
+        attend_half<DH, 1>(x, qf, k_, k_ + 4096, fo, to, k0, s | (blk.hi > at.last ? UPPER | LOWER : 0), holes, min(row.pos, at.last), row.near, a.w.sinks, lane);
       asm volatile("" ::: "memory");
     }
     x.l += __shfl_xor(x.l, 32, WAVE);

@@ -37,13 +37,30 @@ template <int N> __device__ __forceinline__ float max_of(const f32x16 (&st)[N]) 
   return mx;
 }
 
-// a wave's rows: their first and last position (none: hi < lo)
+// a wave's rows: their first and last position (none: hi = -1)
 struct RowSpan { int lo, hi; };
-enum Seen { NONE = 0, SOME = 1, ALL_PAIRS = 2 };
-// what rows of the span see of the 32 keys from k0 on (wave-uniform)
+// What rows of the span see of the 32 keys from k0 on (wave-uniform): nothing, or SEEN and which bounds hide some pair: keys behind a row (UPPER), keys
+// in front of a row's window (LOWER)
+enum { SEEN = 1, UPPER = 2, LOWER = 4 };
 __device__ __forceinline__ int seen_half(const Window& w, const RowSpan& r, int k0) {
-  if (k0 > r.hi || (k0 + 31 < w.near_from(r.lo) && k0 >= w.sinks)) return NONE;
-  return k0 + 31 <= r.lo && (k0 >= w.near_from(r.hi) || k0 + 31 < w.sinks) ? ALL_PAIRS : SOME;
+  if (k0 > r.hi || (k0 + 31 < w.near_from(r.lo) && k0 >= w.sinks)) return 0;
+  return SEEN | (k0 + 31 > r.lo ? UPPER : 0) | (k0 < w.near_from(r.hi) && k0 + 31 >= w.sinks ? LOWER : 0);
+}
+// v[e] = hidden where row pos does not see key k0 + acc_row(e).  A branch per bound, kept one by the empty statements: as selections the compiler would
+// make of them they cost every tile 130 vector instructions (64 keys), more than its exponentials.
+__device__ __forceinline__ void hide(f32x16& v, int seen, float hidden, int k0, int pos, int near, int sinks, int lane) {
+  if (seen & UPPER) {
+    asm volatile("");
+    const int a = pos - k0 - 4 * (lane >> 5);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) v[e] = 8 * (e >> 2) + (e & 3) > a ? hidden : v[e];
+  }
+  if (seen & LOWER) {
+    asm volatile("");
+    const int b = near - k0 - 4 * (lane >> 5), s = sinks - k0 - 4 * (lane >> 5);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) v[e] = 8 * (e >> 2) + (e & 3) < b && 8 * (e >> 2) + (e & 3) >= s ? hidden : v[e];
+  }
 }
 
 // One query row a lane pair: reference exponent, half row sum, O^T
@@ -59,10 +76,10 @@ template <int DH> struct SoftmaxRow {
   }
 };
 
-// NT halves of 32 keys from k0 on.  k_, v_: the halves' first row in LDS.  masked: some pair may be hidden.  holes: bit per 16 keys that nobody sees
+// NT halves of 32 keys from k0 on, of which the rows see `seen` (a byte each).  k_, v_: the halves' first row in LDS.  holes: bit per 16 keys that nobody sees
 template <int DH, int NT>
 __device__ __forceinline__ void attend_half(SoftmaxRow<DH>& x, const uint4 (&qf)[DH / 16], const char* k_, const char* v_, const FragOff& fo, const TrOff& to,
-                                            int k0, bool masked, int holes, int pos, int near, int sinks, int lane) {
+                                            int k0, int seen, int holes, int pos, int near, int sinks, int lane) {
   constexpr int KS = DH / 16, DT = DH / 32;
   f32x16 st[NT];
 #pragma unroll
@@ -71,15 +88,15 @@ __device__ __forceinline__ void attend_half(SoftmaxRow<DH>& x, const uint4 (&qf)
   for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
     for (int t = 0; t < NT; ++t) st[t] = mfma16(row_frag(k_, fo, ks, t), qf[ks], st[t]);
-  if (masked) {   // wave-uniform
+#pragma unroll
+  for (int t = 0; t < NT; ++t) hide(st[t], seen >> (8 * t), -INFINITY, k0 + 32 * t, pos, near, sinks, lane);
+  if (holes) {   // wave-uniform
+    asm volatile("");
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int key = k0 + 32 * t + acc_row(e, lane);
-        const bool hole = (holes >> (2 * t + (e >> 3))) & 1;
-        st[t][e] = !hole && key <= pos && (key >= near || key < sinks) ? st[t][e] : -INFINITY;
-      }
+      for (int e = 0; e < 16; ++e)
+        if ((holes >> (2 * t + (e >> 3))) & 1) st[t][e] = -INFINITY;
   }
   const float sc = score_scale<DH>() * LOG2E;
   float mx = max_of(st);
@@ -112,21 +129,14 @@ __device__ __forceinline__ void attend_half(SoftmaxRow<DH>& x, const uint4 (&qf)
     }
   }
 }
-// a tile of 64 keys: both halves in one go where both are seen, else the one that is.  masked: the mask is needed whatever the span says
+// a tile of 64 keys: both halves in one go where both are seen, else the one that is.  force: bounds to apply whatever the span says
 template <int DH>
 __device__ __forceinline__ void attend_tile(SoftmaxRow<DH>& x, const uint4 (&qf)[DH / 16], const char* k_, const char* v_, const FragOff& fo, const TrOff& to,
-                                            int k0, int holes, const Window& w, const RowSpan& span, bool masked, int pos, int near, int lane) {
-  const int a = (holes & 3) == 3 ? NONE : seen_half(w, span, k0), b = holes >> 2 == 3 ? NONE : seen_half(w, span, k0 + 32);
-  if (a != NONE && b != NONE)
-    attend_half<DH, 2>(x, qf, k_, v_, fo, to, k0, masked || a + b != 2 * ALL_PAIRS || holes, holes, pos, near, w.sinks, lane);
-  else if (a != NONE || b != NONE) {
-    const int half = a != NONE ? 0 : 1;
-    attend_half<DH, 1>(x, qf, k_ + 4096 * half, v_ + 4096 * half, fo, to, k0 + 32 * half, masked || a + b != ALL_PAIRS || holes, holes >> (2 * half), pos, near,
-                       w.sinks, lane);
-  }
+                                            int k0, int holes, const Window& w, const RowSpan& span, int force, int pos, int near, int lane) {
+  const int a = (holes & 3) == 3 ? 0 : seen_half(w, span, k0), b = holes >> 2 == 3 ? 0 : seen_half(w, span, k0 + 32);
+  if (a) attend_half<DH, 1>(x, qf, k_, v_, fo, to, k0, a | force, holes & 3, pos, near, w.sinks, lane);
+  if (b) attend_half<DH, 1>(x, qf, k_ + 4096, v_ + 4096, fo, to, k0 + 32, b | force, holes >> 2, pos, near, w.sinks, lane);
 }
-
-__device__ __forceinline__ bool bits_not_finite(float v) { return (__builtin_bit_cast(uint32_t, v) & 0x7f800000u) == 0x7f800000u; }
 
 // Two operands' rows of one document and head (keys and values; queries and output gradients), ld0 and ld1 elements apart
 template <int DH, bool TWO_STRIDES = false> struct RowTiles {
