@@ -19,7 +19,7 @@ struct WindowArgs {
 // ---- forward -----------------------------------------------------------------------------------------------------
 // A workgroup per 128 queries of a head, the last ones first: under a window that covers the document these are the longest
 template <int DH>
-__global__ void __launch_bounds__(AT_THREADS, DH == 128 ? 2 : 3) window_fwd_mfma(WindowArgs a, bf16* __restrict__ o, float* __restrict__ lse) {
+__global__ void __launch_bounds__(AT_THREADS, DH == 128 ? 2 : 4) window_fwd_mfma(WindowArgs a, bf16* __restrict__ o, float* __restrict__ lse) {
   constexpr int KS = DH / 16, TILE_BYTES = tile_bytes<DH>();
   extern __shared__ __attribute__((aligned(16))) char wf_smem[];   // [stage][K | V]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, h = lane >> 5;
@@ -157,30 +157,23 @@ template <int DH> __device__ __forceinline__ void window_dq(const WindowArgs& a,
       const int k0 = tiles.at(t) * 64;
       const char* k_ = smem + cur * 2 * TILE_BYTES;
       const char* v_ = k_ + TILE_BYTES;
-      auto halves = [&](auto NTc, int half, int seen) {
-        constexpr int NT = decltype(NTc)::value;
-        f32x16 st[NT], dp[NT];
 #pragma unroll
-        for (int i = 0; i < NT; ++i) { zero(st[i]); zero(dp[i]); }
+      for (int half = 0; half < 2; ++half) {
+        const int seen = seen_half(a.w, span, k0 + 32 * half);
+        if (!seen) continue;   // wave-uniform
+        f32x16 st, dp;
+        zero(st); zero(dp);
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks)
+        for (int ks = 0; ks < KS; ++ks) {
+          st = mfma16(row_frag(k_, fo, ks, half), qf[ks], st);
+          dp = mfma16(row_frag(v_, fo, ks, half), gf[ks], dp);
+        }
 #pragma unroll
-          for (int i = 0; i < NT; ++i) {
-            st[i] = mfma16(row_frag(k_ + 4096 * half, fo, ks, i), qf[ks], st[i]);
-            dp[i] = mfma16(row_frag(v_ + 4096 * half, fo, ks, i), gf[ks], dp[i]);
-          }
-#pragma unroll
-        for (int i = 0; i < NT; ++i)   // dS^T without the factor 1 / sqrt(d_head), which dQ gets when it is stored
-#pragma unroll
-          for (int e = 0; e < 16; ++e) st[i][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[i][e], sc, nlse2)) * (dp[i][e] - D);
-#pragma unroll
-        for (int i = 0; i < NT; ++i) hide(st[i], seen >> (8 * i), 0.f, k0 + 32 * (half + i), q, near, a.w.sinks, lane);
-#pragma unroll
-        for (int i = 0; i < NT; ++i) mma_transposed_half(dq, k_ + 4096 * (half + i), to, st[i]);
-      };
-      const int s0 = seen_half(a.w, span, k0), s1 = seen_half(a.w, span, k0 + 32);
-      if (s0 && s1) halves(std::integral_constant<int, 2>{}, 0, s0 | s1 << 8);
-      else if (s0 | s1) halves(std::integral_constant<int, 1>{}, s0 ? 0 : 1, s0 | s1);
+        for (int e = 0; e < 16; ++e)   // dS^T without the factor 1 / sqrt(d_head), which dQ gets when it is stored
+          st[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[e], sc, nlse2)) * (dp[e] - D);
+        hide(st, seen, 0.f, k0 + 32 * half, q, near, a.w.sinks, lane);
+        mma_transposed_half(dq, k_ + 4096 * half, to, st);
+      }
     }
     if (__any(q < rows && plain::not_finite(dq)) && q < rows) {
       plain::clear(dq);
@@ -273,10 +266,15 @@ __device__ __forceinline__ void window_dkv(const WindowArgs& a, const bf16* __re
         f32x16 st, dp;
         zero(st); zero(dp);
         const bool want_v = !SINKS || wave < 2, want_k = !SINKS || wave >= 2;
+        if (want_k) {
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          st = mfma16(row_frag(q_ + 4096 * t, fo, ks, 0), kf[ks], st);
-          if (want_k) dp = mfma16(row_frag(g_ + 4096 * t, fo, ks, 0), vf[ks], dp);
+          for (int ks = 0; ks < KS; ++ks) {
+            st = mfma16(row_frag(q_ + 4096 * t, fo, ks, 0), kf[ks], st);
+            dp = mfma16(row_frag(g_ + 4096 * t, fo, ks, 0), vf[ks], dp);
+          }
+        } else {
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks) st = mfma16(row_frag(q_ + 4096 * t, fo, ks, 0), kf[ks], st);
         }
         // accumulator elements 4g .. 4g + 3 are queries 8g + 4h + (0..3) of the half: their statistics are 16 contiguous bytes
 #pragma unroll

@@ -13,17 +13,18 @@
 
 namespace dipaco {
 
-// Tiles of 2^SHIFT keys that rows at positions lo .. hi see: the first `front` of the document, then `first` to that of position hi
+// Tiles of 2^SHIFT keys that rows at positions lo .. hi see: those from `first` to that of position hi, then the sinks' in front of them.  The sinks last:
+// every workgroup of a head asks for the same rows there, and a window's tile is in flight meanwhile.
 template <int SHIFT> struct TileList {
-  int front, first, count;
-  __device__ __forceinline__ TileList() : front(0), first(0), count(0) {}
+  int near, first, count;   // `near` tiles from `first` on, `count` in all
+  __device__ __forceinline__ TileList() : near(0), first(0), count(0) {}
   __device__ __forceinline__ TileList(const Window& w, int lo, int hi) {
-    const int near = w.near_from(lo);
-    first = min(near >> SHIFT, (hi >> SHIFT) + 1);   // hi lies in front of the window only where a document outgrows its table
-    front = min((min(w.sinks, near) + (1 << SHIFT) - 1) >> SHIFT, first);
-    count = front + (hi >> SHIFT) + 1 - first;
+    const int from = w.near_from(lo);
+    first = min(from >> SHIFT, (hi >> SHIFT) + 1);   // hi lies in front of the window only where a document outgrows its table
+    near = (hi >> SHIFT) + 1 - first;
+    count = near + min((min(w.sinks, from) + (1 << SHIFT) - 1) >> SHIFT, first);
   }
-  __device__ __forceinline__ int at(int t) const { return t < front ? t : first + t - front; }
+  __device__ __forceinline__ int at(int t) const { return t < near ? first + t : t - near; }
 };
 
 // packed rows of a block, and log2 of the keys of a tile
