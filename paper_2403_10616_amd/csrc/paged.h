@@ -31,7 +31,20 @@ template <int SHIFT> struct TileList {
 template <typename T> struct PagedCut { static constexpr int NARROW_ROWS = 32, NARROW_SHIFT = 5, WIDE_ROWS = 128, WIDE_SHIFT = 6; };
 template <> struct PagedCut<float> { static constexpr int NARROW_ROWS = 16, NARROW_SHIFT = 6, WIDE_ROWS = 64, WIDE_SHIFT = 5; };
 constexpr int SPLIT_KEYS = 512;   // a split has at least so many keys
-constexpr int PAGED_MOST_SPLITS = 64, PAGED_NARROW_GROUPS = 512, PAGED_WIDE_GROUPS = 512;   // splits, and the workgroups that they are to make
+constexpr int PAGED_MOST_SPLITS = 64, PAGED_NARROW_GROUPS = 1024, PAGED_WIDE_GROUPS = 512;   // splits, and the workgroups that they are to make
+
+// n / d for n < 2^31: a multiplication by ceil(2^32 / d), whose result is at most one too high, and its correction.  As the compiler divides (40
+// instructions, each waiting for the one before), the ten divisions in front of a one-token call's first load took a microsecond.
+struct Divisor {
+  uint32_t d, magic;
+  __host__ __device__ Divisor() : d(1), magic(0) {}
+  explicit Divisor(int v) : d(v), magic((uint32_t)(((1ull << 32) + v - 1) / v)) {}   // 0 for v = 1, whose quotient is n
+  __device__ __forceinline__ int operator()(int n) const {
+    if (d == 1) return n;
+    const int q = (int)__umulhi((uint32_t)n, magic);
+    return q - (q * (int)d > n ? 1 : 0);
+  }
+};
 
 template <typename T> struct PagedArgs {
   const T* qkv;              // [T rows, (H + 2 H_kv) dh]
@@ -43,10 +56,10 @@ template <typename T> struct PagedArgs {
   float* lse;                // [T rows, H], or null
   int T_rows, B, max_new, H, H_kv, n_pages, page_shift, pages_per_doc;
   Window w;
-  int narrow_splits, wide_splits;
+  Divisor group;             // H / H_kv
+  Divisor narrow_splits, wide_splits;
   float* part;               // [splits][T rows][H] x (dh sums, then in an array of its own reference exponent and sum)
 
-  __device__ __forceinline__ int group() const { return H / H_kv; }
   __device__ __forceinline__ int capacity() const { return pages_per_doc << page_shift; }
   __device__ __forceinline__ int cached(int b) const { return min(max(cache_len[b], 0), capacity()); }
   // the page of a position, or -1 where the table holds none
@@ -71,25 +84,28 @@ template <int SHIFT> struct PagedBlock {
   int b, row0, rows, packed0, packed, pos0, last;   // rows row0 .. of the call, `rows` of them; packed rows packed0 .. of `packed`; position of row 0; last one
   int lo, hi;                                       // positions of the block's first and last row
   TileList<SHIFT> tiles;
-  int per, used;                                    // tiles a split, splits that have any
-  template <typename T> __device__ __forceinline__ PagedBlock(const PagedArgs<T>& a, int b, int block, int block_rows, int splits) : b(b) {
+  int per;                                          // tiles a split: split s has tiles s per ..
+  template <typename T> __device__ __forceinline__ PagedBlock(const PagedArgs<T>& a, int b, int block, int block_rows, const Divisor& splits) : b(b) {
     const RowRange r = ragged_rows(a.row_start, b, a.T_rows);
+    const int G = a.group.d;
+    pos0 = a.cached(b);
     row0 = r.first;
     rows = min(r.count, a.max_new);
-    packed = rows * a.group();
+    packed = rows * G;
     packed0 = block * block_rows;
-    pos0 = a.cached(b);
     last = min(pos0 + rows, a.capacity()) - 1;
-    per = used = lo = hi = 0;
+    per = lo = hi = 0;
     if (packed0 >= packed) return;
-    lo = pos0 + packed0 / a.group();
-    hi = pos0 + (min(packed, packed0 + block_rows) - 1) / a.group();
+    lo = pos0 + a.group(packed0);
+    hi = pos0 + a.group(min(packed, packed0 + block_rows) - 1);
     if (last < 0) return;
     tiles = TileList<SHIFT>(a.w, lo, min(hi, last));
     if (tiles.count <= 0) { tiles.count = 0; return; }
-    per = max((tiles.count + splits - 1) / splits, SPLIT_KEYS >> SHIFT);
-    used = (tiles.count + per - 1) / per;
+    per = max(splits(tiles.count + (int)splits.d - 1), SPLIT_KEYS >> SHIFT);
   }
+  // whether a split has tiles (the first one: whether or not it has), and whether it has them all
+  __device__ __forceinline__ bool has(int split) const { return split == 0 || split * per < tiles.count; }
+  __device__ __forceinline__ bool whole() const { return tiles.count <= per; }
 };
 
 // the document and block of the i-th wide block of the call (-1: there are fewer); the whole wave
@@ -97,7 +113,7 @@ template <typename T> __device__ __forceinline__ int find_wide_block(const Paged
   for (int b0 = 0; b0 < a.B; b0 += 64) {
     int n = 0;
     if (b0 + lane < a.B) {
-      const int packed = min(ragged_rows(a.row_start, b0 + lane, a.T_rows).count, a.max_new) * a.group();
+      const int packed = min(ragged_rows(a.row_start, b0 + lane, a.T_rows).count, a.max_new) * (int)a.group.d;
       n = packed > PagedCut<T>::NARROW_ROWS ? (packed + PagedCut<T>::WIDE_ROWS - 1) / PagedCut<T>::WIDE_ROWS : 0;
     }
     int upto = n;   // blocks of documents b0 .. b0 + lane

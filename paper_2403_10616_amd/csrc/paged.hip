@@ -35,41 +35,56 @@ __global__ void __launch_bounds__(256) cache_append_rows(PagedArgs<T> a, int dh)
   }
 }
 
-// The splits' sums of the blocks that were split, added in their order.  A workgroup per row, DH / 4 threads a head.
+// The splits' sums of the blocks that were split, added in their order: a wave per row and head, a lane per split for their states (there are at
+// most 64), then a lane per columns of the head.
 template <int DH, typename T>
-__global__ void __launch_bounds__(256) paged_join(PagedArgs<T> a) {
-  constexpr int PER = DH / 4;
-  const int row = blockIdx.x, lane = threadIdx.x & 63, b = find_document(a.row_start, a.B, row, lane), G = a.group();
+__global__ void __launch_bounds__(256) paged_join(PagedArgs<T> a, Divisor heads) {
+  using Cut = PagedCut<T>;
+  constexpr int COLS = DH == 128 ? 2 : 1;
+  const int lane = threadIdx.x & 63, item = blockIdx.x * 4 + (threadIdx.x >> 6), row = heads(item), head = item - row * a.H;
+  if (row >= a.T_rows) return;   // whole waves leave
+  const int b = __builtin_amdgcn_readfirstlane(find_document(a.row_start, a.B, row, lane)), G = a.group.d;
   const RowRange r = ragged_rows(a.row_start, b, a.T_rows);
   const int rows = min(r.count, a.max_new);
   if (row < r.first || row >= r.first + rows) return;
-  using Cut = PagedCut<T>;
   const bool narrow = rows * G <= Cut::NARROW_ROWS;
-  const int splits = narrow ? a.narrow_splits : a.wide_splits;
-  for (int i = threadIdx.x; i < a.H * PER; i += 256) {
-    const int head = i / PER, c = 4 * (i - head * PER), R = (row - r.first) * G + head % G;
-    const int used = narrow ? PagedBlock<Cut::NARROW_SHIFT>(a, b, 0, Cut::NARROW_ROWS, splits).used
-                            : PagedBlock<Cut::WIDE_SHIFT>(a, b, R / Cut::WIDE_ROWS, Cut::WIDE_ROWS, splits).used;
-    if (used <= 1) continue;   // its workgroup has written it
-    float m = -INFINITY, l = 0.f;
-    for (int s = 0; s < used; ++s) m = fmaxf(m, a.template part_state<DH>(splits, s, row, head)->x);
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int s = 0; s < used; ++s) {
-      const float2 st = *a.template part_state<DH>(splits, s, row, head);
-      if (st.x == -INFINITY) continue;
-      const float w = exp2f(st.x - m);
-      const float4 p = *reinterpret_cast<const float4*>(a.template part_sums<DH>(s, row, head) + c);
-      l += w * st.y;
-      v.x += w * p.x; v.y += w * p.y; v.z += w * p.z; v.w += w * p.w;
-    }
-    const float scale = m == -INFINITY ? 0.f : 1.f / l;
-    T* const out = a.o + ((long)row * a.H + head) * DH + c;
-    out[0] = from_f32<T>(v.x * scale);
-    out[1] = from_f32<T>(v.y * scale);
-    out[2] = from_f32<T>(v.z * scale);
-    out[3] = from_f32<T>(v.w * scale);
-    if (a.lse && c == 0) a.lse[(long)row * a.H + head] = (m + log2f(l)) * 0.6931471805599453f;
+  const Divisor& splits = narrow ? a.narrow_splits : a.wide_splits;
+  int tiles, per;
+  if (narrow) {
+    const PagedBlock<Cut::NARROW_SHIFT> blk(a, b, 0, Cut::NARROW_ROWS, splits);
+    tiles = blk.tiles.count;
+    per = blk.per;
+  } else {
+    const PagedBlock<Cut::WIDE_SHIFT> blk(a, b, ((row - r.first) * G + head - a.group(head) * G) / Cut::WIDE_ROWS, Cut::WIDE_ROWS, splits);
+    tiles = blk.tiles.count;
+    per = blk.per;
   }
+  if (tiles <= per) return;   // its workgroup has written it
+  const int used = __builtin_popcountll(__builtin_amdgcn_ballot_w64(lane * per < tiles));
+  const float2 st = lane < used ? *a.template part_state<DH>(splits.d, lane, row, head) : make_float2(-INFINITY, 0.f);
+  const float m = wave_max(st.x), w = st.x == -INFINITY ? 0.f : exp2f(st.x - m), l = wave_sum(w * st.y);
+  const float* const from = a.template part_sums<DH>(0, row, head) + COLS * (lane % (DH / COLS));
+  const long step = (long)a.T_rows * a.H * DH;
+  float v[COLS] = {};
+  for (int s0 = 0; s0 < used; s0 += 8) {   // eight loads at a time; a split behind the last one has no weight
+    float p[8][COLS];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int c = 0; c < COLS; ++c) p[i][c] = from[min(s0 + i, used - 1) * step + c];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float ws = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), s0 + i));
+#pragma unroll
+      for (int c = 0; c < COLS; ++c) v[c] = __builtin_fmaf(ws, p[i][c], v[c]);
+    }
+  }
+  const float scale = m == -INFINITY ? 0.f : 1.f / l;
+  if (lane < DH / COLS) {
+#pragma unroll
+    for (int c = 0; c < COLS; ++c) a.o[((long)row * a.H + head) * DH + COLS * lane + c] = from_f32<T>(v[c] * scale);
+  }
+  if (a.lse && lane == 0) a.lse[(long)row * a.H + head] = (m + log2f(l)) * 0.6931471805599453f;
 }
 
 // How often a call's keys are cut: enough workgroups for the chip, none with less than SPLIT_KEYS keys however long the documents are
@@ -108,8 +123,8 @@ size_t paged_workspace_bytes(int T_rows, int H, int dh, int page_size, int pages
 }
 template <typename T> dipaco_status launch_attention_paged(PagedArgs<T> a, int dh, void* workspace, hipStream_t s) {
   const PagedPlan p = plan(a);
-  a.narrow_splits = p.narrow_splits;
-  a.wide_splits = p.wide_splits;
+  a.narrow_splits = Divisor(p.narrow_splits);
+  a.wide_splits = Divisor(p.wide_splits);
   a.part = static_cast<float*>(workspace);
   auto run = [&](auto DHc) -> dipaco_status {
     constexpr int DH = decltype(DHc)::value;
@@ -117,7 +132,7 @@ template <typename T> dipaco_status launch_attention_paged(PagedArgs<T> a, int d
       if (dipaco_status st = launch_paged_wide<DH>(a, p.wide_blocks, s)) return st;
     if (dipaco_status st = launch_paged_narrow<DH>(a, s)) return st;
     if (p.narrow_splits > 1 || (p.wide_blocks && p.wide_splits > 1)) {
-      paged_join<DH, T><<<a.T_rows, 256, 0, s>>>(a);
+      paged_join<DH, T><<<(a.T_rows * a.H + 3) / 4, 256, 0, s>>>(a, Divisor(a.H));
       DIPACO_LAUNCH_CHECK();
     }
     return DIPACO_OK;

@@ -13,36 +13,29 @@ using Cut = PagedCut<float>;
 
 // NARROW: 16 packed rows, which every wave holds; of a tile of 64 keys a wave takes 16.  Else 64 packed rows, 16 a wave, on tiles of 32 keys.
 template <int DH, bool NARROW>
-__global__ void __launch_bounds__(WF_THREADS, NARROW && DH == 128 ? 1 : 2) paged_f32(PagedArgs<float> a, int blocks) {
+__global__ void __launch_bounds__(WF_THREADS, NARROW && DH == 128 ? 1 : 2) paged_f32(PagedArgs<float> a, int b0) {
   extern __shared__ __attribute__((aligned(16))) float pf_smem[];   // [stage][K | V]
   constexpr int SHIFT = NARROW ? Cut::NARROW_SHIFT : Cut::WIDE_SHIFT, TILE = 1 << SHIFT, RUNS = TILE / 16, AHEAD = 64 / RUNS;
   constexpr int STAGE = 2 * window_tile_floats<DH, TILE>();
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
-  const int splits = NARROW ? a.narrow_splits : a.wide_splits;
-  int b, block = 0, hk, split;
-  if constexpr (NARROW) {
-    const int item = blockIdx.x / splits;
-    split = blockIdx.x - item * splits;
-    b = item / a.H_kv;
-    hk = item - b * a.H_kv;
-  } else {
-    const int item = blockIdx.x / blocks;
-    hk = item % a.H_kv;
-    split = item / a.H_kv;
-    block = blockIdx.x - item * blocks;
+  const Divisor& splits = NARROW ? a.narrow_splits : a.wide_splits;
+  const int hk = blockIdx.y, split = NARROW ? blockIdx.x : blockIdx.z;
+  int b = blockIdx.z + b0, block = 0;
+  if constexpr (!NARROW) {
+    block = blockIdx.x;
     b = __builtin_amdgcn_readfirstlane(find_wide_block(a, block, lane));
     if (b < 0) return;
     block = __builtin_amdgcn_readfirstlane(block);
   }
   const PagedBlock<SHIFT> blk(a, b, block, NARROW ? Cut::NARROW_ROWS : Cut::WIDE_ROWS, splits);
   if (NARROW && (blk.packed == 0 || blk.packed > Cut::NARROW_ROWS)) return;
-  if (split >= max(blk.used, 1)) return;
+  if (!blk.has(split)) return;
   const int t0 = split * blk.per, n_tiles = min(blk.tiles.count - t0, blk.per);
-  const int G = a.group(), r0 = blk.packed0 + (NARROW ? 0 : 16 * wave), R = r0 + m, token = R / G, head = hk * G + R - token * G;
+  const int G = a.group.d, r0 = blk.packed0 + (NARROW ? 0 : 16 * wave), R = r0 + m, token = a.group(R), head = hk * G + R - token * G;
   const bool valid = R < blk.packed;
   const int pos = blk.pos0 + token, near = a.w.near_from(pos);
   const long row = blk.row0 + token;
-  const FRowSpan span{blk.pos0 + r0 / G, r0 < blk.packed ? blk.pos0 + min(r0 + 15, blk.packed - 1) / G : -1};
+  const FRowSpan span{blk.pos0 + a.group(r0), r0 < blk.packed ? blk.pos0 + a.group(min(r0 + 15, blk.packed - 1)) : -1};
   const float* const q = a.qkv + row * (a.H + 2 * a.H_kv) * DH + head * DH;
   const float* const keys = a.cache + a.template key_offset<DH>(0, hk, 0);
   const long page_floats = ((long)2 * a.H_kv << a.page_shift) * DH, value = a.template value_from_key<DH>();
@@ -116,8 +109,8 @@ __global__ void __launch_bounds__(WF_THREADS, NARROW && DH == 128 ? 1 : 2) paged
       c[w] = s.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s.x - mm);
       l = __builtin_fmaf(s.y, c[w], l);
     }
-    const float scale = blk.used > 1 ? 1.f : mm == -INFINITY ? 0.f : 1.0f / l;
-    float* const out = blk.used > 1 ? a.template part_sums<DH>(split, row, head) : a.o + (row * a.H + head) * DH;
+    const float scale = !blk.whole() ? 1.f : mm == -INFINITY ? 0.f : 1.0f / l;
+    float* const out = !blk.whole() ? a.template part_sums<DH>(split, row, head) : a.o + (row * a.H + head) * DH;
     for (int d = wave; d < DH / 16; d += 4) {
       f32x4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -129,14 +122,14 @@ __global__ void __launch_bounds__(WF_THREADS, NARROW && DH == 128 ? 1 : 2) paged
       *reinterpret_cast<float4*>(out + 16 * d + 4 * g) = make_float4(v[0] * scale, v[1] * scale, v[2] * scale, v[3] * scale);
     }
     if (wave == 0 && g == 0) {
-      if (blk.used > 1) *a.template part_state<DH>(splits, split, row, head) = make_float2(mm, l);
+      if (!blk.whole()) *a.template part_state<DH>(splits.d, split, row, head) = make_float2(mm, l);
       else if (a.lse) a.lse[row * a.H + head] = (mm + __builtin_amdgcn_logf(l)) * WF_LN2;
     }
   } else {
     if (!valid) return;
-    if (blk.used > 1) {
+    if (!blk.whole()) {
       store_row<DH>(a.template part_sums<DH>(split, row, head), x.o, g, 1.f);
-      if (g == 0) *a.template part_state<DH>(splits, split, row, head) = make_float2(x.m, x.l);
+      if (g == 0) *a.template part_state<DH>(splits.d, split, row, head) = make_float2(x.m, x.l);
     } else {
       store_row<DH>(a.o + (row * a.H + head) * DH, x.o, g, x.m == -INFINITY ? 0.f : 1.0f / x.l);
       if (a.lse && g == 0) a.lse[row * a.H + head] = (x.m + __builtin_amdgcn_logf(x.l)) * WF_LN2;   // -inf where nothing is seen
@@ -153,14 +146,16 @@ template <int DH, bool NARROW> constexpr int paged_f32_lds() {
 template <int DH> dipaco_status launch_paged_narrow(const PagedArgs<float>& a, hipStream_t s) {
   static std::atomic<unsigned long long> lds_set{0};
   if (dipaco_status st = ensure_dynamic_lds(reinterpret_cast<const void*>(paged_f32<DH, true>), paged_f32_lds<DH, true>(), lds_set)) return st;
-  paged_f32<DH, true><<<a.B * a.H_kv * a.narrow_splits, WF_THREADS, paged_f32_lds<DH, true>(), s>>>(a, 0);
-  DIPACO_LAUNCH_CHECK();
+  for (int b = 0; b < a.B; b += 65535) {   // documents are the grid's z
+    paged_f32<DH, true><<<dim3(a.narrow_splits.d, a.H_kv, std::min(a.B - b, 65535)), WF_THREADS, paged_f32_lds<DH, true>(), s>>>(a, b);
+    DIPACO_LAUNCH_CHECK();
+  }
   return DIPACO_OK;
 }
 template <int DH> dipaco_status launch_paged_wide(const PagedArgs<float>& a, int blocks, hipStream_t s) {
   static std::atomic<unsigned long long> lds_set{0};
   if (dipaco_status st = ensure_dynamic_lds(reinterpret_cast<const void*>(paged_f32<DH, false>), paged_f32_lds<DH, false>(), lds_set)) return st;
-  paged_f32<DH, false><<<blocks * a.H_kv * a.wide_splits, WF_THREADS, paged_f32_lds<DH, false>(), s>>>(a, blocks);
+  paged_f32<DH, false><<<dim3(blocks, a.H_kv, a.wide_splits.d), WF_THREADS, paged_f32_lds<DH, false>(), s>>>(a, 0);
   DIPACO_LAUNCH_CHECK();
   return DIPACO_OK;
 }

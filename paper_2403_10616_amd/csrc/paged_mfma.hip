@@ -44,7 +44,7 @@ template <int DH> struct PagedRow {
   int head, pos, near;
   const bf16* q;
   __device__ __forceinline__ PagedRow(const PagedArgs<bf16>& a, int R, int packed, int row0, int pos0, int hk) {
-    const int G = a.group(), token = R / G;
+    const int G = a.group.d, token = a.group(R);
     valid = R < packed;
     row = row0 + token;
     head = hk * G + R - token * G;
@@ -73,21 +73,21 @@ __device__ __forceinline__ void add_seen(SoftmaxRow<DH>& x, const PagedArgs<bf16
 
 // ---- wide ----------------------------------------------------------------------------------------------------------
 template <int DH>
-__global__ void __launch_bounds__(AT_THREADS, 2) paged_wide_mfma(PagedArgs<bf16> a, int blocks) {
+__global__ void __launch_bounds__(AT_THREADS, 2) paged_wide_mfma(PagedArgs<bf16> a) {
   constexpr int KS = DH / 16, NP = panels<DH>(), TILE_BYTES = tile_bytes<DH>();
   extern __shared__ __attribute__((aligned(16))) char pw_smem[];   // [stage][K | V]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, h = lane >> 5;
-  const int item = blockIdx.x / blocks, hk = item % a.H_kv, split = item / a.H_kv;
-  int block = blockIdx.x - item * blocks;
+  const int hk = blockIdx.y, split = blockIdx.z;
+  int block = blockIdx.x;
   const int b = __builtin_amdgcn_readfirstlane(find_wide_block(a, block, lane));
   if (b < 0) return;
   const PagedBlock<Cut::WIDE_SHIFT> blk(a, b, __builtin_amdgcn_readfirstlane(block), Cut::WIDE_ROWS, a.wide_splits);
   const int t0 = split * blk.per, n_tiles = min(blk.tiles.count - t0, blk.per);
-  if (split >= max(blk.used, 1)) return;
-  const int G = a.group(), r0 = blk.packed0 + 32 * wave;
+  if (!blk.has(split)) return;
+  const int r0 = blk.packed0 + 32 * wave;
   int R = r0 + r;
-  const int pos = blk.pos0 + R / G, near = a.w.near_from(pos);
-  const RowSpan span{blk.pos0 + r0 / G, r0 < blk.packed ? blk.pos0 + (min(r0 + 31, blk.packed - 1)) / G : -1};
+  const int pos = blk.pos0 + a.group(R), near = a.w.near_from(pos);
+  const RowSpan span{blk.pos0 + a.group(r0), r0 < blk.packed ? blk.pos0 + a.group(min(r0 + 31, blk.packed - 1)) : -1};
   SoftmaxRow<DH> x;
   x.clear();
   if (n_tiles > 0) {
@@ -153,7 +153,7 @@ __global__ void __launch_bounds__(AT_THREADS, 2) paged_wide_mfma(PagedArgs<bf16>
   asm volatile("" : "+v"(R));
   const PagedRow<DH> row(a, R, blk.packed, blk.row0, blk.pos0, hk);
   if (!row.valid) return;
-  if (blk.used <= 1) {
+  if (blk.whole()) {
     store_transposed_out(a.o + (row.row * a.H + row.head) * DH, x.o, h, x.m == -INFINITY ? 0.f : 1.0f / x.l);
     if (a.lse && h == 0) a.lse[row.row * a.H + row.head] = (x.m + __builtin_amdgcn_logf(x.l)) * LN2;   // v_log_f32 is log2; -inf where nothing is seen
   } else {
@@ -163,24 +163,25 @@ __global__ void __launch_bounds__(AT_THREADS, 2) paged_wide_mfma(PagedArgs<bf16>
 #pragma unroll
       for (int g = 0; g < 4; ++g)
         *reinterpret_cast<float4*>(sums + 32 * dt + 8 * g + 4 * h) = make_float4(x.o[dt][4 * g], x.o[dt][4 * g + 1], x.o[dt][4 * g + 2], x.o[dt][4 * g + 3]);
-    if (h == 0) *a.template part_state<DH>(a.wide_splits, split, row.row, row.head) = make_float2(x.m, x.l);
+    if (h == 0) *a.template part_state<DH>(a.wide_splits.d, split, row.row, row.head) = make_float2(x.m, x.l);
   }
 }
 
 // ---- narrow --------------------------------------------------------------------------------------------------------
-template <int DH> constexpr int narrow_stages() { return DH == 128 ? 2 : 4; }
+constexpr int NARROW_STAGES = 2;
+template <int DH> constexpr int narrow_waves(bool many) { return (DH == 128 ? 2 : 4) * (many ? 2 : 1); }
 template <int DH> constexpr int narrow_stage() { return panels<DH>() * PANEL_BYTES; }   // 32 rows of K and V: a panel holds K's, then V's
-template <int DH> constexpr int narrow_lds() { return 4 * narrow_stages<DH>() * narrow_stage<DH>(); }
+template <int DH, int NW> constexpr int narrow_lds() { return NW * NARROW_STAGES * narrow_stage<DH>(); }
 
-template <int DH>
-__global__ void __launch_bounds__(AT_THREADS, 1) paged_narrow_mfma(PagedArgs<bf16> a) {
-  constexpr int KS = DH / 16, DT = DH / 32, NP = panels<DH>(), NS = narrow_stages<DH>(), STAGE = narrow_stage<DH>(), LPW = 8 * NP;
+template <int DH, int NW>
+__global__ void __launch_bounds__(WAVE * NW, 1) paged_narrow_mfma(PagedArgs<bf16> a, int b0) {
+  constexpr int KS = DH / 16, DT = DH / 32, NP = panels<DH>(), NS = NARROW_STAGES, STAGE = narrow_stage<DH>(), LPW = 8 * NP;
   extern __shared__ __attribute__((aligned(16))) char pn_smem[];   // [wave][stage]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, h = lane >> 5;
-  const int item = blockIdx.x / a.narrow_splits, split = blockIdx.x - item * a.narrow_splits, b = item / a.H_kv, hk = item - b * a.H_kv;
+  const int split = blockIdx.x, hk = blockIdx.y, b = blockIdx.z + b0;
   const PagedBlock<Cut::NARROW_SHIFT> blk(a, b, 0, Cut::NARROW_ROWS, a.narrow_splits);
-  if (blk.packed == 0 || blk.packed > Cut::NARROW_ROWS || split >= max(blk.used, 1)) return;
-  const int t0 = split * blk.per, end = min(t0 + blk.per, blk.tiles.count), n = (end - t0 - wave + 3) >> 2;   // this wave's halves: t0 + wave, + 4, ..
+  if (blk.packed == 0 || blk.packed > Cut::NARROW_ROWS || !blk.has(split)) return;
+  const int t0 = split * blk.per, end = min(t0 + blk.per, blk.tiles.count), n = (end - t0 - wave + NW - 1) / NW;   // this wave's halves: t0 + wave, + NW, ..
   const PagedRow<DH> row(a, r, blk.packed, blk.row0, blk.pos0, hk);
   const RowSpan span{blk.lo, blk.hi};
   SoftmaxRow<DH> x;
@@ -200,7 +201,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) paged_narrow_mfma(PagedArgs<bf1
       off[i] = (uint32_t)((lane >> 3) * DH * 2) + col[i];
     }
     int ids = 0;   // lane 2 (t % 32) + g: the page of rows 16 g .. of this wave's half t
-    auto half_at = [&](int t) { return blk.tiles.at(t0 + wave + 4 * t) * 32; };
+    auto half_at = [&](int t) { return blk.tiles.at(t0 + wave + NW * t) * 32; };
     auto holes_of = [&](unsigned long long none, int t) { return (int)((none >> (2 * (t & 31))) & 3); };
     unsigned long long none = 0;   // which of the lanes' pages are none; of the 32 halves before as well
     unsigned long long none_before = 0;
@@ -260,46 +261,53 @@ __global__ void __launch_bounds__(AT_THREADS, 1) paged_narrow_mfma(PagedArgs<bf1
       for (int t = 0; t < n; ++t) add_seen<DH>(x, a, at, row, half_at(t), 32, h);
     }
   }
-  // the four waves' sums meet in LDS: wave w adds accumulator elements 4w .. 4w + 3 of every 32 columns
+  // the waves' sums meet in LDS: wave w adds accumulator elements 4 g .. 4 g + 3 of every 32 columns for g = w, w + NW, ..
   constexpr int PER = 16 * DT * WAVE;
-  static_assert((4 * PER + 2 * 4 * WAVE) * 4 <= narrow_lds<DH>(), "the sums fit in the rings");
+  static_assert((NW * PER + 2 * NW * WAVE) * 4 <= narrow_lds<DH, NW>(), "the sums fit in the rings");
   float* const sums = reinterpret_cast<float*>(pn_smem);
-  float2* const state = reinterpret_cast<float2*>(sums + 4 * PER);
+  float2* const state = reinterpret_cast<float2*>(sums + NW * PER);
   __syncthreads();   // the rings have been read
   hand_over(x.o, sums + wave * PER, lane);
   state[wave * WAVE + lane] = make_float2(x.m, x.l);
   __syncthreads();
   if (!row.valid) return;
-  float2 st[4];
+  float2 st[NW];
+  float m = -INFINITY;
 #pragma unroll
-  for (int w = 0; w < 4; ++w) st[w] = state[w * WAVE + lane];
-  const float m = fmaxf(fmaxf(st[0].x, st[1].x), fmaxf(st[2].x, st[3].x));
-  float c[4], l = 0.f;
+  for (int w = 0; w < NW; ++w) {
+    st[w] = state[w * WAVE + lane];
+    m = fmaxf(m, st[w].x);
+  }
+  float c[NW], l = 0.f;
 #pragma unroll
-  for (int w = 0; w < 4; ++w) {
+  for (int w = 0; w < NW; ++w) {
     c[w] = st[w].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st[w].x - m);
     l = __builtin_fmaf(st[w].y, c[w], l);
   }
-  const bool whole = blk.used <= 1;
+  const bool whole = blk.whole();
   const float scale = !whole ? 1.f : m == -INFINITY ? 0.f : 1.0f / l;
 #pragma unroll
-  for (int dt = 0; dt < DT; ++dt) {
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      const float4 p = *reinterpret_cast<const float4*>(sums + w * PER + ((dt * 4 + wave) * WAVE + lane) * 4);
-      v.x = __builtin_fmaf(p.x, c[w], v.x); v.y = __builtin_fmaf(p.y, c[w], v.y); v.z = __builtin_fmaf(p.z, c[w], v.z); v.w = __builtin_fmaf(p.w, c[w], v.w);
+    for (int g0 = 0; g0 < 4; g0 += NW) {
+      const int g = g0 + wave;
+      if (NW > 4 && g > 3) break;
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int w = 0; w < NW; ++w) {
+        const float4 p = *reinterpret_cast<const float4*>(sums + w * PER + ((dt * 4 + g) * WAVE + lane) * 4);
+        v.x = __builtin_fmaf(p.x, c[w], v.x); v.y = __builtin_fmaf(p.y, c[w], v.y); v.z = __builtin_fmaf(p.z, c[w], v.z); v.w = __builtin_fmaf(p.w, c[w], v.w);
+      }
+      const int at = 32 * dt + 8 * g + 4 * h;
+      if (whole) {
+        const bf16x4 out = {(bf16)(v.x * scale), (bf16)(v.y * scale), (bf16)(v.z * scale), (bf16)(v.w * scale)};
+        *reinterpret_cast<bf16x4*>(a.o + (row.row * a.H + row.head) * DH + at) = out;
+      } else {
+        *reinterpret_cast<float4*>(a.template part_sums<DH>(split, row.row, row.head) + at) = v;
+      }
     }
-    const int at = 32 * dt + 8 * wave + 4 * h;
-    if (whole) {
-      const bf16x4 out = {(bf16)(v.x * scale), (bf16)(v.y * scale), (bf16)(v.z * scale), (bf16)(v.w * scale)};
-      *reinterpret_cast<bf16x4*>(a.o + (row.row * a.H + row.head) * DH + at) = out;
-    } else {
-      *reinterpret_cast<float4*>(a.template part_sums<DH>(split, row.row, row.head) + at) = v;
-    }
-  }
   if (wave == 0 && h == 0) {
-    if (!whole) *a.template part_state<DH>(a.narrow_splits, split, row.row, row.head) = make_float2(m, l);
+    if (!whole) *a.template part_state<DH>(a.narrow_splits.d, split, row.row, row.head) = make_float2(m, l);
     else if (a.lse) a.lse[row.row * a.H + row.head] = (m + __builtin_amdgcn_logf(l)) * LN2;
   }
 }
@@ -307,17 +315,25 @@ __global__ void __launch_bounds__(AT_THREADS, 1) paged_narrow_mfma(PagedArgs<bf1
 }  // namespace
 
 template <int DH> dipaco_status launch_paged_narrow(const PagedArgs<bf16>& a, hipStream_t s) {
-  static std::atomic<unsigned long long> lds_set{0};
-  if (dipaco_status st = ensure_dynamic_lds(reinterpret_cast<const void*>(paged_narrow_mfma<DH>), narrow_lds<DH>(), lds_set)) return st;
-  paged_narrow_mfma<DH><<<a.B * a.H_kv * a.narrow_splits, AT_THREADS, narrow_lds<DH>(), s>>>(a);
-  DIPACO_LAUNCH_CHECK();
-  return DIPACO_OK;
+  auto run = [&](auto NWc) -> dipaco_status {
+    constexpr int NW = decltype(NWc)::value, LDS = narrow_lds<DH, NW>();
+    static std::atomic<unsigned long long> lds_set{0};
+    if (dipaco_status st = ensure_dynamic_lds(reinterpret_cast<const void*>(paged_narrow_mfma<DH, NW>), LDS, lds_set)) return st;
+    for (int b = 0; b < a.B; b += 65535) {   // documents are the grid's z
+      paged_narrow_mfma<DH, NW><<<dim3(a.narrow_splits.d, a.H_kv, std::min(a.B - b, 65535)), WAVE * NW, LDS, s>>>(a, b);
+      DIPACO_LAUNCH_CHECK();
+    }
+    return DIPACO_OK;
+  };
+  // A launch of a workgroup a compute unit or less: twice the waves on each
+  return (int64_t)a.B * a.H_kv * a.narrow_splits.d <= 256 ? run(std::integral_constant<int, narrow_waves<DH>(true)>{})
+                                                          : run(std::integral_constant<int, narrow_waves<DH>(false)>{});
 }
 template <int DH> dipaco_status launch_paged_wide(const PagedArgs<bf16>& a, int blocks, hipStream_t s) {
   constexpr int LDS = 4 * tile_bytes<DH>();
   static std::atomic<unsigned long long> lds_set{0};
   if (dipaco_status st = ensure_dynamic_lds(reinterpret_cast<const void*>(paged_wide_mfma<DH>), LDS, lds_set)) return st;
-  paged_wide_mfma<DH><<<blocks * a.H_kv * a.wide_splits, AT_THREADS, LDS, s>>>(a, blocks);
+  paged_wide_mfma<DH><<<dim3(blocks, a.H_kv, a.wide_splits.d), AT_THREADS, LDS, s>>>(a);
   DIPACO_LAUNCH_CHECK();
   return DIPACO_OK;
 }
