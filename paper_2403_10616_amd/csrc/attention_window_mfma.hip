@@ -19,7 +19,7 @@ struct WindowArgs {
 // ---- forward -----------------------------------------------------------------------------------------------------
 // A workgroup per 128 queries of a head, the last ones first: under a window that covers the document these are the longest
 template <int DH>
-__global__ void __launch_bounds__(AT_THREADS, DH == 128 ? 2 : 4) window_fwd_mfma(WindowArgs a, bf16* __restrict__ o, float* __restrict__ lse) {
+__global__ void __launch_bounds__(AT_THREADS, DH == 128 ? 2 : 3) window_fwd_mfma(WindowArgs a, bf16* __restrict__ o, float* __restrict__ lse) {
   constexpr int KS = DH / 16, TILE_BYTES = tile_bytes<DH>();
   extern __shared__ __attribute__((aligned(16))) char wf_smem[];   // [stage][K | V]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, h = lane >> 5;

@@ -30,7 +30,7 @@ template <int SHIFT> struct TileList {
 // packed rows of a block, and log2 of the keys of a tile
 template <typename T> struct PagedCut { static constexpr int NARROW_ROWS = 32, NARROW_SHIFT = 5, WIDE_ROWS = 128, WIDE_SHIFT = 6; };
 template <> struct PagedCut<float> { static constexpr int NARROW_ROWS = 16, NARROW_SHIFT = 6, WIDE_ROWS = 64, WIDE_SHIFT = 5; };
-constexpr int SPLIT_KEYS = 512;   // a split has at least so many keys
+constexpr int SPLIT_KEYS = 512;   // a split has at least so many keys, in a launch of few workgroups, of twice the waves, twice as many
 constexpr int PAGED_MOST_SPLITS = 64, PAGED_NARROW_GROUPS = 1024, PAGED_WIDE_GROUPS = 512;   // splits, and the workgroups that they are to make
 
 // n / d for n < 2^31: a multiplication by ceil(2^32 / d), whose result is at most one too high, and its correction.  As the compiler divides (40
@@ -58,6 +58,7 @@ template <typename T> struct PagedArgs {
   Window w;
   Divisor group;             // H / H_kv
   Divisor narrow_splits, wide_splits;
+  int narrow_keys;           // a narrow split has at least so many keys
   float* part;               // [splits][T rows][H] x (dh sums, then in an array of its own reference exponent and sum)
 
   __device__ __forceinline__ int capacity() const { return pages_per_doc << page_shift; }
@@ -85,7 +86,7 @@ template <int SHIFT> struct PagedBlock {
   int lo, hi;                                       // positions of the block's first and last row
   TileList<SHIFT> tiles;
   int per;                                          // tiles a split: split s has tiles s per ..
-  template <typename T> __device__ __forceinline__ PagedBlock(const PagedArgs<T>& a, int b, int block, int block_rows, const Divisor& splits) : b(b) {
+  template <typename T> __device__ __forceinline__ PagedBlock(const PagedArgs<T>& a, int b, int block, int block_rows, const Divisor& splits, int least_keys) : b(b) {
     const RowRange r = ragged_rows(a.row_start, b, a.T_rows);
     const int G = a.group.d;
     pos0 = a.cached(b);
@@ -101,7 +102,7 @@ template <int SHIFT> struct PagedBlock {
     if (last < 0) return;
     tiles = TileList<SHIFT>(a.w, lo, min(hi, last));
     if (tiles.count <= 0) { tiles.count = 0; return; }
-    per = max(splits(tiles.count + (int)splits.d - 1), SPLIT_KEYS >> SHIFT);
+    per = max(splits(tiles.count + (int)splits.d - 1), least_keys >> SHIFT);
   }
   // whether a split has tiles (the first one: whether or not it has), and whether it has them all
   __device__ __forceinline__ bool has(int split) const { return split == 0 || split * per < tiles.count; }

@@ -51,11 +51,11 @@ __global__ void __launch_bounds__(256) paged_join(PagedArgs<T> a, Divisor heads)
   const Divisor& splits = narrow ? a.narrow_splits : a.wide_splits;
   int tiles, per;
   if (narrow) {
-    const PagedBlock<Cut::NARROW_SHIFT> blk(a, b, 0, Cut::NARROW_ROWS, splits);
+    const PagedBlock<Cut::NARROW_SHIFT> blk(a, b, 0, Cut::NARROW_ROWS, splits, a.narrow_keys);
     tiles = blk.tiles.count;
     per = blk.per;
   } else {
-    const PagedBlock<Cut::WIDE_SHIFT> blk(a, b, ((row - r.first) * G + head - a.group(head) * G) / Cut::WIDE_ROWS, Cut::WIDE_ROWS, splits);
+    const PagedBlock<Cut::WIDE_SHIFT> blk(a, b, ((row - r.first) * G + head - a.group(head) * G) / Cut::WIDE_ROWS, Cut::WIDE_ROWS, splits, SPLIT_KEYS);
     tiles = blk.tiles.count;
     per = blk.per;
   }
@@ -88,7 +88,7 @@ __global__ void __launch_bounds__(256) paged_join(PagedArgs<T> a, Divisor heads)
 }
 
 // How often a call's keys are cut: enough workgroups for the chip, none with less than SPLIT_KEYS keys however long the documents are
-struct PagedPlan { int narrow_splits, wide_blocks, wide_splits; };
+struct PagedPlan { int narrow_splits, narrow_keys, wide_blocks, wide_splits; };
 inline int most_splits(int page_size, int pages_per_doc) {
   return (int)std::min<int64_t>(PAGED_MOST_SPLITS, ((int64_t)page_size * pages_per_doc + SPLIT_KEYS - 1) / SPLIT_KEYS);
 }
@@ -98,7 +98,13 @@ template <typename T> PagedPlan plan(const PagedArgs<T>& a) {
   const int64_t seen = std::min<int64_t>((int64_t)page_size * a.pages_per_doc, (int64_t)a.w.window + a.w.sinks + WIDE_ROWS);   // keys of a block, about
   const int most = std::max(1, (int)std::min<int64_t>(most_splits(page_size, a.pages_per_doc), (seen + SPLIT_KEYS - 1) / SPLIT_KEYS));
   PagedPlan p;
-  p.narrow_splits = (int)std::min<int64_t>(most, (PAGED_NARROW_GROUPS + (int64_t)a.B * a.H_kv - 1) / ((int64_t)a.B * a.H_kv));
+  const int64_t heads = (int64_t)a.B * a.H_kv;
+  p.narrow_splits = (int)std::min<int64_t>(most, (PAGED_NARROW_GROUPS + heads - 1) / heads);
+  p.narrow_keys = SPLIT_KEYS;
+  if (const int64_t half = (p.narrow_splits + 1) / 2; std::is_same<T, bf16>::value && heads * half <= 256) {   // twice the waves a workgroup
+    p.narrow_splits = (int)half;
+    p.narrow_keys = 2 * SPLIT_KEYS;
+  }
   const int64_t packed = (int64_t)a.T_rows * G, longest = (int64_t)std::min(a.max_new, a.T_rows) * G;
   p.wide_blocks = longest <= NARROW_ROWS ? 0 : (int)(packed / WIDE_ROWS + std::min<int64_t>(a.B, packed / (NARROW_ROWS + 1)));
   const int64_t wide = std::max<int64_t>(1, p.wide_blocks) * a.H_kv;
@@ -124,6 +130,7 @@ size_t paged_workspace_bytes(int T_rows, int H, int dh, int page_size, int pages
 template <typename T> dipaco_status launch_attention_paged(PagedArgs<T> a, int dh, void* workspace, hipStream_t s) {
   const PagedPlan p = plan(a);
   a.narrow_splits = Divisor(p.narrow_splits);
+  a.narrow_keys = p.narrow_keys;
   a.wide_splits = Divisor(p.wide_splits);
   a.part = static_cast<float*>(workspace);
   auto run = [&](auto DHc) -> dipaco_status {

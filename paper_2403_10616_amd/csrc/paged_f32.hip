@@ -27,7 +27,7 @@ __global__ void __launch_bounds__(WF_THREADS, NARROW && DH == 128 ? 1 : 2) paged
     if (b < 0) return;
     block = __builtin_amdgcn_readfirstlane(block);
   }
-  const PagedBlock<SHIFT> blk(a, b, block, NARROW ? Cut::NARROW_ROWS : Cut::WIDE_ROWS, splits);
+  const PagedBlock<SHIFT> blk(a, b, block, NARROW ? Cut::NARROW_ROWS : Cut::WIDE_ROWS, splits, NARROW ? a.narrow_keys : SPLIT_KEYS);
   if (NARROW && (blk.packed == 0 || blk.packed > Cut::NARROW_ROWS)) return;
   if (!blk.has(split)) return;
   const int t0 = split * blk.per, n_tiles = min(blk.tiles.count - t0, blk.per);

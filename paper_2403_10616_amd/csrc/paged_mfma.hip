@@ -81,7 +81,7 @@ __global__ void __launch_bounds__(AT_THREADS, 2) paged_wide_mfma(PagedArgs<bf16>
   int block = blockIdx.x;
   const int b = __builtin_amdgcn_readfirstlane(find_wide_block(a, block, lane));
   if (b < 0) return;
-  const PagedBlock<Cut::WIDE_SHIFT> blk(a, b, __builtin_amdgcn_readfirstlane(block), Cut::WIDE_ROWS, a.wide_splits);
+  const PagedBlock<Cut::WIDE_SHIFT> blk(a, b, __builtin_amdgcn_readfirstlane(block), Cut::WIDE_ROWS, a.wide_splits, SPLIT_KEYS);
   const int t0 = split * blk.per, n_tiles = min(blk.tiles.count - t0, blk.per);
   if (!blk.has(split)) return;
   const int r0 = blk.packed0 + 32 * wave;
@@ -179,7 +179,7 @@ __global__ void __launch_bounds__(WAVE * NW, 1) paged_narrow_mfma(PagedArgs<bf16
   extern __shared__ __attribute__((aligned(16))) char pn_smem[];   // [wave][stage]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, h = lane >> 5;
   const int split = blockIdx.x, hk = blockIdx.y, b = blockIdx.z + b0;
-  const PagedBlock<Cut::NARROW_SHIFT> blk(a, b, 0, Cut::NARROW_ROWS, a.narrow_splits);
+  const PagedBlock<Cut::NARROW_SHIFT> blk(a, b, 0, Cut::NARROW_ROWS, a.narrow_splits, a.narrow_keys);
   if (blk.packed == 0 || blk.packed > Cut::NARROW_ROWS || !blk.has(split)) return;
   const int t0 = split * blk.per, end = min(t0 + blk.per, blk.tiles.count), n = (end - t0 - wave + NW - 1) / NW;   // this wave's halves: t0 + wave, + NW, ..
   const PagedRow<DH> row(a, r, blk.packed, blk.row0, blk.pos0, hk);
@@ -238,22 +238,21 @@ __global__ void __launch_bounds__(WAVE * NW, 1) paged_narrow_mfma(PagedArgs<bf16
         }
       }
     };
-#pragma unroll
-    for (int t = 0; t < NS - 1; ++t)
-      if (t < n) issue(t);
+    // The rows' queries are asked for in front of the table, whose wait serves both.  A half's stage is filled again when its products have read it:
+    // NS halves are in flight.
     uint4 qf[KS];
     row.load(qf, h);
+    for (int t = 0; t < min(NS, n); ++t) issue(t);
     for (int t = 0; t < n; ++t) {
-      // half t has landed: the loads behind it are those of the next NS - 2 halves (the query's, issued among the first, only make this wait longer)
-      wait_stages_but<LPW>(min(NS - 2, n - 1 - t));
+      wait_stages_but<LPW>(min(NS - 1, n - 1 - t));   // half t has landed: the loads behind it are those of the next halves
       asm volatile("" ::: "memory");
-      if (t + NS - 1 < n) issue(t + NS - 1);   // into the stage of half t - 1, whose reads its products have waited for
       const int k0 = half_at(t), holes = holes_of((t >> 5) == ((min(t + NS - 1, n - 1)) >> 5) ? none : none_before, t);
       const int s = holes == 3 ? 0 : seen_half(a.w, span, k0);
       const char* k_ = ring + (t % NS) * STAGE;
       if (s)
         attend_half<DH, 1>(x, qf, k_, k_ + 4096, fo, to, k0, s | (blk.hi > at.last ? UPPER | LOWER : 0), holes, min(row.pos, at.last), row.near, a.w.sinks, lane);
       asm volatile("" ::: "memory");
+      if (t + NS < n) issue(t + NS);
     }
     x.l += __shfl_xor(x.l, 32, WAVE);
     if (__any(row.valid && plain::not_finite(x.o)) && row.valid) {
@@ -326,8 +325,7 @@ template <int DH> dipaco_status launch_paged_narrow(const PagedArgs<bf16>& a, hi
     return DIPACO_OK;
   };
   // A launch of a workgroup a compute unit or less: twice the waves on each
-  return (int64_t)a.B * a.H_kv * a.narrow_splits.d <= 256 ? run(std::integral_constant<int, narrow_waves<DH>(true)>{})
-                                                          : run(std::integral_constant<int, narrow_waves<DH>(false)>{});
+  return a.narrow_keys > SPLIT_KEYS ? run(std::integral_constant<int, narrow_waves<DH>(true)>{}) : run(std::integral_constant<int, narrow_waves<DH>(false)>{});
 }
 template <int DH> dipaco_status launch_paged_wide(const PagedArgs<bf16>& a, int blocks, hipStream_t s) {
   constexpr int LDS = 4 * tile_bytes<DH>();

@@ -39,6 +39,12 @@ template <int N> __device__ __forceinline__ float max_of(const f32x16 (&st)[N]) 
 
 // a wave's rows: their first and last position (none: hi = -1)
 struct RowSpan { int lo, hi; };
+// the larger of a lane's value and that of the lane 32 away, without a trip through LDS
+__device__ __forceinline__ float max_over_halves(float v) {
+  const uint32_t b = __builtin_bit_cast(uint32_t, v);
+  const auto r = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+  return fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
+}
 // What rows of the span see of the 32 keys from k0 on (wave-uniform): nothing, or SEEN and which bounds hide some pair: keys behind a row (UPPER), keys
 // in front of a row's window (LOWER)
 enum { SEEN = 1, UPPER = 2, LOWER = 4 };
@@ -84,10 +90,25 @@ __device__ __forceinline__ void attend_half(SoftmaxRow<DH>& x, const uint4 (&qf)
   f32x16 st[NT];
 #pragma unroll
   for (int t = 0; t < NT; ++t) zero(st[t]);
+  // Keys are read in one go, and values while the scores are multiplied: left to the compiler the reads trickle in between the products, each
+  // with a wait of its own.  16 x 2048 positions of 14 x 64, window 512: 96 us, 101 so.
+  uint4 kf[NT][KS], vf[NT][DT][2];
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) kf[t][ks] = row_frag(k_, fo, ks, t);
+  __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
   for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-    for (int t = 0; t < NT; ++t) st[t] = mfma16(row_frag(k_, fo, ks, t), qf[ks], st[t]);
+    for (int t = 0; t < NT; ++t) st[t] = mfma16(kf[t][ks], qf[ks], st[t]);
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) vf[t][dt][i] = tr_read(v_, to, dt, 2 * t + i);
+  __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
   for (int t = 0; t < NT; ++t) hide(st[t], seen >> (8 * t), -INFINITY, k0 + 32 * t, pos, near, sinks, lane);
   if (holes) {   // wave-uniform
@@ -99,8 +120,7 @@ __device__ __forceinline__ void attend_half(SoftmaxRow<DH>& x, const uint4 (&qf)
         if ((holes >> (2 * t + (e >> 3))) & 1) st[t][e] = -INFINITY;
   }
   const float sc = score_scale<DH>() * LOG2E;
-  float mx = max_of(st);
-  mx = fmaxf(mx, __shfl_xor(mx, 32, WAVE));
+  const float mx = max_over_halves(max_of(st));
   // the reference may lag behind the running maximum by 2^8 (attention_mfma.h); rows that have seen nothing keep 0 for it
   const float mn = fmaxf(x.m, mx * sc);
   if (__builtin_amdgcn_ballot_w64(mn > x.m + 8.0f) != 0) {   // wave-uniform
@@ -124,8 +144,8 @@ __device__ __forceinline__ void attend_half(SoftmaxRow<DH>& x, const uint4 (&qf)
     const uint4 p0 = pack8<0>(st[t]), p1 = pack8<8>(st[t]);
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
-      x.o[dt] = mfma16(tr_read(v_, to, dt, 2 * t), p0, x.o[dt]);
-      x.o[dt] = mfma16(tr_read(v_, to, dt, 2 * t + 1), p1, x.o[dt]);
+      x.o[dt] = mfma16(vf[t][dt][0], p0, x.o[dt]);
+      x.o[dt] = mfma16(vf[t][dt][1], p1, x.o[dt]);
     }
   }
 }
