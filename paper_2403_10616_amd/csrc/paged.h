@@ -7,6 +7,9 @@
 // R % G of the group.  A workgroup takes a block of packed rows of a document and a key head, and a part ("split") of the keys that these see:
 //   narrow: a document of up to 32 packed rows (fp32: 16) is one block; its workgroup's waves take the keys in turn.
 //   wide:   128 packed rows, 32 a wave (fp32: 64, 16 a wave); the waves share the keys' tiles.
+// Every eighth workgroup of a launch goes to the same eighth of the chip.  So workgroups that find nothing to do must not come at a fixed pace: wide
+// blocks that a call does not have are its last workgroups (128 tokens over 16000 positions: 25 us, 32 with every other workgroup idle), and the narrow
+// splits of a document, of which a short one leaves some idle, begin at another one of the eight each time.
 // A split's sums go to the workspace, and paged_join adds them; a block whose keys are one split's writes its rows itself.
 #pragma once
 #include "visible.h"
@@ -31,7 +34,7 @@ template <int SHIFT> struct TileList {
 template <typename T> struct PagedCut { static constexpr int NARROW_ROWS = 32, NARROW_SHIFT = 5, WIDE_ROWS = 128, WIDE_SHIFT = 6; };
 template <> struct PagedCut<float> { static constexpr int NARROW_ROWS = 16, NARROW_SHIFT = 6, WIDE_ROWS = 64, WIDE_SHIFT = 5; };
 constexpr int SPLIT_KEYS = 512;   // a split has at least so many keys, in a launch of few workgroups, of twice the waves, twice as many
-constexpr int PAGED_MOST_SPLITS = 64, PAGED_NARROW_GROUPS = 1024, PAGED_WIDE_GROUPS = 512;   // splits, and the workgroups that they are to make
+constexpr int PAGED_MOST_SPLITS = 64, PAGED_NARROW_GROUPS = 1024, PAGED_WIDE_GROUPS = 1024;   // splits, and the workgroups that they are to make
 
 // n / d for n < 2^31: a multiplication by ceil(2^32 / d), whose result is at most one too high, and its correction.  As the compiler divides (40
 // instructions, each waiting for the one before), the ten divisions in front of a one-token call's first load took a microsecond.
@@ -61,6 +64,12 @@ template <typename T> struct PagedArgs {
   int narrow_keys;           // a narrow split has at least so many keys
   float* part;               // [splits][T rows][H] x (dh sums, then in an array of its own reference exponent and sum)
 
+  int narrow_turn;           // log2 of the (document, head)s behind which the order of their splits moves on by one
+  // the split of the p-th workgroup of a document and head
+  __device__ __forceinline__ int narrow_split(int p, int item) const {
+    const int s = p + (item >> narrow_turn);
+    return s - narrow_splits(s) * (int)narrow_splits.d;
+  }
   __device__ __forceinline__ int capacity() const { return pages_per_doc << page_shift; }
   __device__ __forceinline__ int cached(int b) const { return min(max(cache_len[b], 0), capacity()); }
   // the page of a position, or -1 where the table holds none

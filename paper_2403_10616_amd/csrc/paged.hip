@@ -131,6 +131,7 @@ template <typename T> dipaco_status launch_attention_paged(PagedArgs<T> a, int d
   const PagedPlan p = plan(a);
   a.narrow_splits = Divisor(p.narrow_splits);
   a.narrow_keys = p.narrow_keys;
+  a.narrow_turn = 3 - std::min(3, __builtin_ctz(p.narrow_splits));   // n splits begin at 8 / gcd(8, n) places by themselves
   a.wide_splits = Divisor(p.wide_splits);
   a.part = static_cast<float*>(workspace);
   auto run = [&](auto DHc) -> dipaco_status {

@@ -13,16 +13,17 @@ using Cut = PagedCut<float>;
 
 // NARROW: 16 packed rows, which every wave holds; of a tile of 64 keys a wave takes 16.  Else 64 packed rows, 16 a wave, on tiles of 32 keys.
 template <int DH, bool NARROW>
-__global__ void __launch_bounds__(WF_THREADS, NARROW && DH == 128 ? 1 : 2) paged_f32(PagedArgs<float> a, int b0) {
+__global__ void __launch_bounds__(WF_THREADS, NARROW && DH == 128 ? 1 : 2) paged_f32(PagedArgs<float> a, int first) {
   extern __shared__ __attribute__((aligned(16))) float pf_smem[];   // [stage][K | V]
   constexpr int SHIFT = NARROW ? Cut::NARROW_SHIFT : Cut::WIDE_SHIFT, TILE = 1 << SHIFT, RUNS = TILE / 16, AHEAD = 64 / RUNS;
   constexpr int STAGE = 2 * window_tile_floats<DH, TILE>();
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
   const Divisor& splits = NARROW ? a.narrow_splits : a.wide_splits;
-  const int hk = blockIdx.y, split = NARROW ? blockIdx.x : blockIdx.z;
-  int b = blockIdx.z + b0, block = 0;
+  const int hk = NARROW ? blockIdx.y : blockIdx.x;
+  int b = blockIdx.z + first, block = 0;
+  const int split = NARROW ? a.narrow_split(blockIdx.x, b * a.H_kv + hk) : blockIdx.y;
   if constexpr (!NARROW) {
-    block = blockIdx.x;
+    block = blockIdx.z + first;
     b = __builtin_amdgcn_readfirstlane(find_wide_block(a, block, lane));
     if (b < 0) return;
     block = __builtin_amdgcn_readfirstlane(block);
@@ -155,8 +156,10 @@ template <int DH> dipaco_status launch_paged_narrow(const PagedArgs<float>& a, h
 template <int DH> dipaco_status launch_paged_wide(const PagedArgs<float>& a, int blocks, hipStream_t s) {
   static std::atomic<unsigned long long> lds_set{0};
   if (dipaco_status st = ensure_dynamic_lds(reinterpret_cast<const void*>(paged_f32<DH, false>), paged_f32_lds<DH, false>(), lds_set)) return st;
-  paged_f32<DH, false><<<dim3(blocks, a.H_kv, a.wide_splits.d), WF_THREADS, paged_f32_lds<DH, false>(), s>>>(a, 0);
-  DIPACO_LAUNCH_CHECK();
+  for (int b = 0; b < blocks; b += 65535) {
+    paged_f32<DH, false><<<dim3(a.H_kv, a.wide_splits.d, std::min(blocks - b, 65535)), WF_THREADS, paged_f32_lds<DH, false>(), s>>>(a, b);
+    DIPACO_LAUNCH_CHECK();
+  }
   return DIPACO_OK;
 }
 template dipaco_status launch_paged_narrow<32>(const PagedArgs<float>&, hipStream_t);

@@ -73,12 +73,12 @@ __device__ __forceinline__ void add_seen(SoftmaxRow<DH>& x, const PagedArgs<bf16
 
 // ---- wide ----------------------------------------------------------------------------------------------------------
 template <int DH>
-__global__ void __launch_bounds__(AT_THREADS, 2) paged_wide_mfma(PagedArgs<bf16> a) {
+__global__ void __launch_bounds__(AT_THREADS, 2) paged_wide_mfma(PagedArgs<bf16> a, int block0) {
   constexpr int KS = DH / 16, NP = panels<DH>(), TILE_BYTES = tile_bytes<DH>();
   extern __shared__ __attribute__((aligned(16))) char pw_smem[];   // [stage][K | V]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, h = lane >> 5;
-  const int hk = blockIdx.y, split = blockIdx.z;
-  int block = blockIdx.x;
+  const int hk = blockIdx.x, split = blockIdx.y;
+  int block = blockIdx.z + block0;
   const int b = __builtin_amdgcn_readfirstlane(find_wide_block(a, block, lane));
   if (b < 0) return;
   const PagedBlock<Cut::WIDE_SHIFT> blk(a, b, __builtin_amdgcn_readfirstlane(block), Cut::WIDE_ROWS, a.wide_splits, SPLIT_KEYS);
@@ -171,14 +171,18 @@ __global__ void __launch_bounds__(AT_THREADS, 2) paged_wide_mfma(PagedArgs<bf16>
 constexpr int NARROW_STAGES = 2;
 template <int DH> constexpr int narrow_waves(bool many) { return (DH == 128 ? 2 : 4) * (many ? 2 : 1); }
 template <int DH> constexpr int narrow_stage() { return panels<DH>() * PANEL_BYTES; }   // 32 rows of K and V: a panel holds K's, then V's
-template <int DH, int NW> constexpr int narrow_lds() { return NW * NARROW_STAGES * narrow_stage<DH>(); }
+// the rings, and in their place at the end what the waves add up: 16 accumulator elements a lane and 32 columns, reference exponent and sum
+template <int DH, int NW> constexpr int narrow_lds() {
+  constexpr int RINGS = NW * NARROW_STAGES * narrow_stage<DH>(), SUMS = NW * WAVE * (16 * (DH / 32) + 2) * (int)sizeof(float);
+  return RINGS > SUMS ? RINGS : SUMS;
+}
 
 template <int DH, int NW>
 __global__ void __launch_bounds__(WAVE * NW, 1) paged_narrow_mfma(PagedArgs<bf16> a, int b0) {
   constexpr int KS = DH / 16, DT = DH / 32, NP = panels<DH>(), NS = NARROW_STAGES, STAGE = narrow_stage<DH>(), LPW = 8 * NP;
   extern __shared__ __attribute__((aligned(16))) char pn_smem[];   // [wave][stage]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, h = lane >> 5;
-  const int split = blockIdx.x, hk = blockIdx.y, b = blockIdx.z + b0;
+  const int hk = blockIdx.y, b = blockIdx.z + b0, split = a.narrow_split(blockIdx.x, b * a.H_kv + hk);
   const PagedBlock<Cut::NARROW_SHIFT> blk(a, b, 0, Cut::NARROW_ROWS, a.narrow_splits, a.narrow_keys);
   if (blk.packed == 0 || blk.packed > Cut::NARROW_ROWS || !blk.has(split)) return;
   const int t0 = split * blk.per, end = min(t0 + blk.per, blk.tiles.count), n = (end - t0 - wave + NW - 1) / NW;   // this wave's halves: t0 + wave, + NW, ..
@@ -262,7 +266,6 @@ __global__ void __launch_bounds__(WAVE * NW, 1) paged_narrow_mfma(PagedArgs<bf16
   }
   // the waves' sums meet in LDS: wave w adds accumulator elements 4 g .. 4 g + 3 of every 32 columns for g = w, w + NW, ..
   constexpr int PER = 16 * DT * WAVE;
-  static_assert((NW * PER + 2 * NW * WAVE) * 4 <= narrow_lds<DH, NW>(), "the sums fit in the rings");
   float* const sums = reinterpret_cast<float*>(pn_smem);
   float2* const state = reinterpret_cast<float2*>(sums + NW * PER);
   __syncthreads();   // the rings have been read
@@ -331,8 +334,10 @@ template <int DH> dipaco_status launch_paged_wide(const PagedArgs<bf16>& a, int 
   constexpr int LDS = 4 * tile_bytes<DH>();
   static std::atomic<unsigned long long> lds_set{0};
   if (dipaco_status st = ensure_dynamic_lds(reinterpret_cast<const void*>(paged_wide_mfma<DH>), LDS, lds_set)) return st;
-  paged_wide_mfma<DH><<<dim3(blocks, a.H_kv, a.wide_splits.d), AT_THREADS, LDS, s>>>(a);
-  DIPACO_LAUNCH_CHECK();
+  for (int b = 0; b < blocks; b += 65535) {
+    paged_wide_mfma<DH><<<dim3(a.H_kv, a.wide_splits.d, std::min(blocks - b, 65535)), AT_THREADS, LDS, s>>>(a, b);
+    DIPACO_LAUNCH_CHECK();
+  }
   return DIPACO_OK;
 }
 template dipaco_status launch_paged_narrow<32>(const PagedArgs<bf16>&, hipStream_t);
