@@ -329,8 +329,8 @@ size_t paged_workspace_bytes(int T_rows, int H, int dh, int page_size, int pages
 template <typename T> dipaco_status launch_attention_paged(PagedArgs<T> a, int dh, void* workspace, hipStream_t s);
 // paged_mfma.hip (bf16), paged_f32.hip
 template <int DH> dipaco_status launch_paged_narrow(const PagedArgs<bf16>& a, hipStream_t s);
-template <int DH> dipaco_status launch_paged_wide(const PagedArgs<bf16>& a, int blocks, hipStream_t s);
+template <int DH> dipaco_status launch_paged_both(const PagedArgs<bf16>& a, int blocks, hipStream_t s);
 template <int DH> dipaco_status launch_paged_narrow(const PagedArgs<float>& a, hipStream_t s);
-template <int DH> dipaco_status launch_paged_wide(const PagedArgs<float>& a, int blocks, hipStream_t s);
+template <int DH> dipaco_status launch_paged_both(const PagedArgs<float>& a, int blocks, hipStream_t s);
 
 }  // namespace dipaco

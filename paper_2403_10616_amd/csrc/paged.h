@@ -30,10 +30,9 @@ template <int SHIFT> struct TileList {
   __device__ __forceinline__ int at(int t) const { return t < near ? first + t : t - near; }
 };
 
-// packed rows of a block, and log2 of the keys of a tile
-template <typename T> struct PagedCut { static constexpr int NARROW_ROWS = 32, NARROW_SHIFT = 5, WIDE_ROWS = 128, WIDE_SHIFT = 6; };
-template <> struct PagedCut<float> { static constexpr int NARROW_ROWS = 16, NARROW_SHIFT = 6, WIDE_ROWS = 64, WIDE_SHIFT = 5; };
-constexpr int SPLIT_KEYS = 512;   // a split has at least so many keys, in a launch of few workgroups, of twice the waves, twice as many
+// packed rows of a block, log2 of the keys of a tile, and the fewest keys of a split (in a narrow launch of few workgroups, of twice the waves, twice as many)
+template <typename T> struct PagedCut { static constexpr int NARROW_ROWS = 32, NARROW_SHIFT = 5, WIDE_ROWS = 128, WIDE_SHIFT = 6, LEAST_KEYS = 512; };
+template <> struct PagedCut<float> { static constexpr int NARROW_ROWS = 16, NARROW_SHIFT = 6, WIDE_ROWS = 64, WIDE_SHIFT = 5, LEAST_KEYS = 128; };
 constexpr int PAGED_MOST_SPLITS = 64, PAGED_NARROW_GROUPS = 1024, PAGED_WIDE_GROUPS = 1024;   // splits, and the workgroups that they are to make
 
 // n / d for n < 2^31: a multiplication by ceil(2^32 / d), whose result is at most one too high, and its correction.  As the compiler divides (40

@@ -55,7 +55,7 @@ __global__ void __launch_bounds__(256) paged_join(PagedArgs<T> a, Divisor heads)
     tiles = blk.tiles.count;
     per = blk.per;
   } else {
-    const PagedBlock<Cut::WIDE_SHIFT> blk(a, b, ((row - r.first) * G + head - a.group(head) * G) / Cut::WIDE_ROWS, Cut::WIDE_ROWS, splits, SPLIT_KEYS);
+    const PagedBlock<Cut::WIDE_SHIFT> blk(a, b, ((row - r.first) * G + head - a.group(head) * G) / Cut::WIDE_ROWS, Cut::WIDE_ROWS, splits, Cut::LEAST_KEYS);
     tiles = blk.tiles.count;
     per = blk.per;
   }
@@ -87,25 +87,23 @@ __global__ void __launch_bounds__(256) paged_join(PagedArgs<T> a, Divisor heads)
   if (a.lse && lane == 0) a.lse[(long)row * a.H + head] = (m + log2f(l)) * 0.6931471805599453f;
 }
 
-// How often a call's keys are cut: enough workgroups for the chip, none with less than SPLIT_KEYS keys however long the documents are
+// How often a call's keys are cut: enough workgroups for the chip, none with less than LEAST_KEYS keys however long the documents are
 struct PagedPlan { int narrow_splits, narrow_keys, wide_blocks, wide_splits; };
-inline int most_splits(int page_size, int pages_per_doc) {
-  return (int)std::min<int64_t>(PAGED_MOST_SPLITS, ((int64_t)page_size * pages_per_doc + SPLIT_KEYS - 1) / SPLIT_KEYS);
-}
+inline int most_splits(int64_t keys, int least) { return (int)std::min<int64_t>(PAGED_MOST_SPLITS, (keys + least - 1) / least); }
 template <typename T> PagedPlan plan(const PagedArgs<T>& a) {
   constexpr int NARROW_ROWS = PagedCut<T>::NARROW_ROWS, WIDE_ROWS = PagedCut<T>::WIDE_ROWS;
   const int G = a.H / a.H_kv, page_size = 1 << a.page_shift;
   const int64_t seen = std::min<int64_t>((int64_t)page_size * a.pages_per_doc, (int64_t)a.w.window + a.w.sinks + WIDE_ROWS);   // keys of a block, about
-  const int most = std::max(1, (int)std::min<int64_t>(most_splits(page_size, a.pages_per_doc), (seen + SPLIT_KEYS - 1) / SPLIT_KEYS));
+  const int most = most_splits(seen, PagedCut<T>::LEAST_KEYS);
   PagedPlan p;
+  const int64_t packed = (int64_t)a.T_rows * G, longest = (int64_t)std::min(a.max_new, a.T_rows) * G;
   const int64_t heads = (int64_t)a.B * a.H_kv;
   p.narrow_splits = (int)std::min<int64_t>(most, (PAGED_NARROW_GROUPS + heads - 1) / heads);
-  p.narrow_keys = SPLIT_KEYS;
-  if (const int64_t half = (p.narrow_splits + 1) / 2; std::is_same<T, bf16>::value && heads * half <= 256) {   // twice the waves a workgroup
+  p.narrow_keys = PagedCut<T>::LEAST_KEYS;
+  if (const int64_t half = (p.narrow_splits + 1) / 2; std::is_same<T, bf16>::value && heads * half <= 256 && longest <= NARROW_ROWS) {   // twice the waves a workgroup
     p.narrow_splits = (int)half;
-    p.narrow_keys = 2 * SPLIT_KEYS;
+    p.narrow_keys = 2 * PagedCut<T>::LEAST_KEYS;
   }
-  const int64_t packed = (int64_t)a.T_rows * G, longest = (int64_t)std::min(a.max_new, a.T_rows) * G;
   p.wide_blocks = longest <= NARROW_ROWS ? 0 : (int)(packed / WIDE_ROWS + std::min<int64_t>(a.B, packed / (NARROW_ROWS + 1)));
   const int64_t wide = std::max<int64_t>(1, p.wide_blocks) * a.H_kv;
   p.wide_splits = (int)std::min<int64_t>(most, (PAGED_WIDE_GROUPS + wide - 1) / wide);
@@ -122,7 +120,7 @@ template <typename T> dipaco_status launch_cache_append(const PagedArgs<T>& a, i
 // Sums of at most `most` splits of T rows, and of no more packed rows than the plan's workgroups hold: a plan of n splits has at most
 // GROUPS / n + 1 workgroups a split with up to 128 (32) packed rows each.  Non-decreasing in every size but the heads'.
 size_t paged_workspace_bytes(int T_rows, int H, int dh, int page_size, int pages_per_doc) {
-  const size_t most = most_splits(page_size, pages_per_doc);
+  const size_t most = most_splits((int64_t)page_size * pages_per_doc, PagedCut<float>::LEAST_KEYS);
   constexpr size_t GROUP_ROWS = std::max(PAGED_WIDE_GROUPS * PagedCut<bf16>::WIDE_ROWS, PAGED_NARROW_GROUPS * PagedCut<bf16>::NARROW_ROWS);
   const size_t rows = std::min(most * T_rows, (size_t)T_rows + (GROUP_ROWS + H - 1) / H);
   return 256 + rows * H * (dh + 2) * sizeof(float);
@@ -136,9 +134,7 @@ template <typename T> dipaco_status launch_attention_paged(PagedArgs<T> a, int d
   a.part = static_cast<float*>(workspace);
   auto run = [&](auto DHc) -> dipaco_status {
     constexpr int DH = decltype(DHc)::value;
-    if (p.wide_blocks)
-      if (dipaco_status st = launch_paged_wide<DH>(a, p.wide_blocks, s)) return st;
-    if (dipaco_status st = launch_paged_narrow<DH>(a, s)) return st;
+    if (dipaco_status st = p.wide_blocks ? launch_paged_both<DH>(a, p.wide_blocks, s) : launch_paged_narrow<DH>(a, s)) return st;
     if (p.narrow_splits > 1 || (p.wide_blocks && p.wide_splits > 1)) {
       paged_join<DH, T><<<(a.T_rows * a.H + 3) / 4, 256, 0, s>>>(a, Divisor(a.H));
       DIPACO_LAUNCH_CHECK();

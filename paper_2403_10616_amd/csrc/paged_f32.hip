@@ -28,7 +28,7 @@ __global__ void __launch_bounds__(WF_THREADS, NARROW && DH == 128 ? 1 : 2) paged
     if (b < 0) return;
     block = __builtin_amdgcn_readfirstlane(block);
   }
-  const PagedBlock<SHIFT> blk(a, b, block, NARROW ? Cut::NARROW_ROWS : Cut::WIDE_ROWS, splits, NARROW ? a.narrow_keys : SPLIT_KEYS);
+  const PagedBlock<SHIFT> blk(a, b, block, NARROW ? Cut::NARROW_ROWS : Cut::WIDE_ROWS, splits, NARROW ? a.narrow_keys : Cut::LEAST_KEYS);
   if (NARROW && (blk.packed == 0 || blk.packed > Cut::NARROW_ROWS)) return;
   if (!blk.has(split)) return;
   const int t0 = split * blk.per, n_tiles = min(blk.tiles.count - t0, blk.per);
@@ -153,20 +153,20 @@ template <int DH> dipaco_status launch_paged_narrow(const PagedArgs<float>& a, h
   }
   return DIPACO_OK;
 }
-template <int DH> dipaco_status launch_paged_wide(const PagedArgs<float>& a, int blocks, hipStream_t s) {
+template <int DH> dipaco_status launch_paged_both(const PagedArgs<float>& a, int blocks, hipStream_t s) {
   static std::atomic<unsigned long long> lds_set{0};
   if (dipaco_status st = ensure_dynamic_lds(reinterpret_cast<const void*>(paged_f32<DH, false>), paged_f32_lds<DH, false>(), lds_set)) return st;
   for (int b = 0; b < blocks; b += 65535) {
     paged_f32<DH, false><<<dim3(a.H_kv, a.wide_splits.d, std::min(blocks - b, 65535)), WF_THREADS, paged_f32_lds<DH, false>(), s>>>(a, b);
     DIPACO_LAUNCH_CHECK();
   }
-  return DIPACO_OK;
+  return launch_paged_narrow<DH>(a, s);
 }
 template dipaco_status launch_paged_narrow<32>(const PagedArgs<float>&, hipStream_t);
 template dipaco_status launch_paged_narrow<64>(const PagedArgs<float>&, hipStream_t);
 template dipaco_status launch_paged_narrow<128>(const PagedArgs<float>&, hipStream_t);
-template dipaco_status launch_paged_wide<32>(const PagedArgs<float>&, int, hipStream_t);
-template dipaco_status launch_paged_wide<64>(const PagedArgs<float>&, int, hipStream_t);
-template dipaco_status launch_paged_wide<128>(const PagedArgs<float>&, int, hipStream_t);
+template dipaco_status launch_paged_both<32>(const PagedArgs<float>&, int, hipStream_t);
+template dipaco_status launch_paged_both<64>(const PagedArgs<float>&, int, hipStream_t);
+template dipaco_status launch_paged_both<128>(const PagedArgs<float>&, int, hipStream_t);
 
 }  // namespace dipaco

@@ -72,16 +72,13 @@ __device__ __forceinline__ void add_seen(SoftmaxRow<DH>& x, const PagedArgs<bf16
 }
 
 // ---- wide ----------------------------------------------------------------------------------------------------------
-template <int DH>
-__global__ void __launch_bounds__(AT_THREADS, 2) paged_wide_mfma(PagedArgs<bf16> a, int block0) {
+// pw_smem: [stage][K | V]
+template <int DH> __device__ __forceinline__ void wide_block(const PagedArgs<bf16>& a, int hk, int split, int block, char* pw_smem) {
   constexpr int KS = DH / 16, NP = panels<DH>(), TILE_BYTES = tile_bytes<DH>();
-  extern __shared__ __attribute__((aligned(16))) char pw_smem[];   // [stage][K | V]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, h = lane >> 5;
-  const int hk = blockIdx.x, split = blockIdx.y;
-  int block = blockIdx.z + block0;
   const int b = __builtin_amdgcn_readfirstlane(find_wide_block(a, block, lane));
   if (b < 0) return;
-  const PagedBlock<Cut::WIDE_SHIFT> blk(a, b, __builtin_amdgcn_readfirstlane(block), Cut::WIDE_ROWS, a.wide_splits, SPLIT_KEYS);
+  const PagedBlock<Cut::WIDE_SHIFT> blk(a, b, __builtin_amdgcn_readfirstlane(block), Cut::WIDE_ROWS, a.wide_splits, Cut::LEAST_KEYS);
   const int t0 = split * blk.per, n_tiles = min(blk.tiles.count - t0, blk.per);
   if (!blk.has(split)) return;
   const int r0 = blk.packed0 + 32 * wave;
@@ -168,21 +165,18 @@ __global__ void __launch_bounds__(AT_THREADS, 2) paged_wide_mfma(PagedArgs<bf16>
 }
 
 // ---- narrow --------------------------------------------------------------------------------------------------------
-constexpr int NARROW_STAGES = 2;
-template <int DH> constexpr int narrow_waves(bool many) { return (DH == 128 ? 2 : 4) * (many ? 2 : 1); }
+// Waves of a workgroup and stages of a wave's ring.  Ordinary calls: four waves that wait for each half they read, and as many workgroups a unit as
+// registers allow; launches of few workgroups: as many bytes in flight as a unit's LDS holds.
 template <int DH> constexpr int narrow_stage() { return panels<DH>() * PANEL_BYTES; }   // 32 rows of K and V: a panel holds K's, then V's
 // the rings, and in their place at the end what the waves add up: 16 accumulator elements a lane and 32 columns, reference exponent and sum
-template <int DH, int NW> constexpr int narrow_lds() {
-  constexpr int RINGS = NW * NARROW_STAGES * narrow_stage<DH>(), SUMS = NW * WAVE * (16 * (DH / 32) + 2) * (int)sizeof(float);
+template <int DH, int NW, int NS> constexpr int narrow_lds() {
+  constexpr int RINGS = NW * NS * narrow_stage<DH>(), SUMS = NW * WAVE * (16 * (DH / 32) + 2) * (int)sizeof(float);
   return RINGS > SUMS ? RINGS : SUMS;
 }
-
-template <int DH, int NW>
-__global__ void __launch_bounds__(WAVE * NW, 1) paged_narrow_mfma(PagedArgs<bf16> a, int b0) {
-  constexpr int KS = DH / 16, DT = DH / 32, NP = panels<DH>(), NS = NARROW_STAGES, STAGE = narrow_stage<DH>(), LPW = 8 * NP;
-  extern __shared__ __attribute__((aligned(16))) char pn_smem[];   // [wave][stage]
+// pn_smem: [wave][stage]
+template <int DH, int NW, int NS> __device__ __forceinline__ void narrow_document(const PagedArgs<bf16>& a, int hk, int b, int split, char* pn_smem) {
+  constexpr int KS = DH / 16, DT = DH / 32, NP = panels<DH>(), STAGE = narrow_stage<DH>(), LPW = 8 * NP;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, h = lane >> 5;
-  const int hk = blockIdx.y, b = blockIdx.z + b0, split = a.narrow_split(blockIdx.x, b * a.H_kv + hk);
   const PagedBlock<Cut::NARROW_SHIFT> blk(a, b, 0, Cut::NARROW_ROWS, a.narrow_splits, a.narrow_keys);
   if (blk.packed == 0 || blk.packed > Cut::NARROW_ROWS || !blk.has(split)) return;
   const int t0 = split * blk.per, end = min(t0 + blk.per, blk.tiles.count), n = (end - t0 - wave + NW - 1) / NW;   // this wave's halves: t0 + wave, + NW, ..
@@ -314,37 +308,61 @@ __global__ void __launch_bounds__(WAVE * NW, 1) paged_narrow_mfma(PagedArgs<bf16
   }
 }
 
+// Documents of a call that has only narrow ones
+template <int DH, int NW, int NS> __global__ void __launch_bounds__(WAVE * NW, 1) paged_narrow_mfma(PagedArgs<bf16> a, int b0) {
+  extern __shared__ __attribute__((aligned(16))) char pn_smem[];
+  const int hk = blockIdx.y, b = blockIdx.z + b0;
+  narrow_document<DH, NW, NS>(a, hk, b, a.narrow_split(blockIdx.x, b * a.H_kv + hk), pn_smem);
+}
+// A call with wide blocks, and in the same launch behind them the narrow documents that it may have: n_wide workgroups of heads x splits x blocks, then
+// those of splits x heads x documents
+struct PagedOrder { Divisor heads, head_splits; int n_wide; };
+template <int DH> __global__ void __launch_bounds__(AT_THREADS, 2) paged_both_mfma(PagedArgs<bf16> a, PagedOrder order) {
+  extern __shared__ __attribute__((aligned(16))) char pb_smem[];
+  int i = blockIdx.x;
+  if (i < order.n_wide) {
+    const int block = order.head_splits(i), j = i - block * (int)order.head_splits.d, split = order.heads(j);
+    wide_block<DH>(a, j - split * a.H_kv, split, block, pb_smem);
+    return;
+  }
+  i -= order.n_wide;
+  const int item = a.narrow_splits(i), b = order.heads(item);
+  narrow_document<DH, 4, 1>(a, item - b * a.H_kv, b, a.narrow_split(i - item * (int)a.narrow_splits.d, item), pb_smem);
+}
+
 }  // namespace
 
 template <int DH> dipaco_status launch_paged_narrow(const PagedArgs<bf16>& a, hipStream_t s) {
-  auto run = [&](auto NWc) -> dipaco_status {
-    constexpr int NW = decltype(NWc)::value, LDS = narrow_lds<DH, NW>();
+  auto run = [&](auto NWc, auto NSc) -> dipaco_status {
+    constexpr int NW = decltype(NWc)::value, NS = decltype(NSc)::value, LDS = narrow_lds<DH, NW, NS>();
     static std::atomic<unsigned long long> lds_set{0};
-    if (dipaco_status st = ensure_dynamic_lds(reinterpret_cast<const void*>(paged_narrow_mfma<DH, NW>), LDS, lds_set)) return st;
+    if (dipaco_status st = ensure_dynamic_lds(reinterpret_cast<const void*>(paged_narrow_mfma<DH, NW, NS>), LDS, lds_set)) return st;
     for (int b = 0; b < a.B; b += 65535) {   // documents are the grid's z
-      paged_narrow_mfma<DH, NW><<<dim3(a.narrow_splits.d, a.H_kv, std::min(a.B - b, 65535)), WAVE * NW, LDS, s>>>(a, b);
+      paged_narrow_mfma<DH, NW, NS><<<dim3(a.narrow_splits.d, a.H_kv, std::min(a.B - b, 65535)), WAVE * NW, LDS, s>>>(a, b);
       DIPACO_LAUNCH_CHECK();
     }
     return DIPACO_OK;
   };
-  // A launch of a workgroup a compute unit or less: twice the waves on each
-  return a.narrow_keys > SPLIT_KEYS ? run(std::integral_constant<int, narrow_waves<DH>(true)>{}) : run(std::integral_constant<int, narrow_waves<DH>(false)>{});
+  using std::integral_constant;
+  // A launch of a workgroup a compute unit or less has a unit's LDS for each
+  if (a.narrow_keys > PagedCut<bf16>::LEAST_KEYS) return run(integral_constant<int, DH == 128 ? 4 : 8>{}, integral_constant<int, 2>{});
+  return run(integral_constant<int, DH == 128 ? 2 : 4>{}, integral_constant<int, DH == 128 ? 2 : 1>{});
 }
-template <int DH> dipaco_status launch_paged_wide(const PagedArgs<bf16>& a, int blocks, hipStream_t s) {
-  constexpr int LDS = 4 * tile_bytes<DH>();
+template <int DH> dipaco_status launch_paged_both(const PagedArgs<bf16>& a, int blocks, hipStream_t s) {
+  constexpr int WIDE_LDS = 4 * tile_bytes<DH>(), NARROW_LDS = narrow_lds<DH, 4, 1>(), LDS = WIDE_LDS > NARROW_LDS ? WIDE_LDS : NARROW_LDS;
   static std::atomic<unsigned long long> lds_set{0};
-  if (dipaco_status st = ensure_dynamic_lds(reinterpret_cast<const void*>(paged_wide_mfma<DH>), LDS, lds_set)) return st;
-  for (int b = 0; b < blocks; b += 65535) {
-    paged_wide_mfma<DH><<<dim3(a.H_kv, a.wide_splits.d, std::min(blocks - b, 65535)), AT_THREADS, LDS, s>>>(a, b);
-    DIPACO_LAUNCH_CHECK();
-  }
+  if (dipaco_status st = ensure_dynamic_lds(reinterpret_cast<const void*>(paged_both_mfma<DH>), LDS, lds_set)) return st;
+  const int wide = a.H_kv * (int)a.wide_splits.d;
+  const PagedOrder order{Divisor(a.H_kv), Divisor(wide), blocks * wide};
+  paged_both_mfma<DH><<<order.n_wide + a.B * a.H_kv * (int)a.narrow_splits.d, AT_THREADS, LDS, s>>>(a, order);
+  DIPACO_LAUNCH_CHECK();
   return DIPACO_OK;
 }
 template dipaco_status launch_paged_narrow<32>(const PagedArgs<bf16>&, hipStream_t);
 template dipaco_status launch_paged_narrow<64>(const PagedArgs<bf16>&, hipStream_t);
 template dipaco_status launch_paged_narrow<128>(const PagedArgs<bf16>&, hipStream_t);
-template dipaco_status launch_paged_wide<32>(const PagedArgs<bf16>&, int, hipStream_t);
-template dipaco_status launch_paged_wide<64>(const PagedArgs<bf16>&, int, hipStream_t);
-template dipaco_status launch_paged_wide<128>(const PagedArgs<bf16>&, int, hipStream_t);
+template dipaco_status launch_paged_both<32>(const PagedArgs<bf16>&, int, hipStream_t);
+template dipaco_status launch_paged_both<64>(const PagedArgs<bf16>&, int, hipStream_t);
+template dipaco_status launch_paged_both<128>(const PagedArgs<bf16>&, int, hipStream_t);
 
 }  // namespace dipaco
