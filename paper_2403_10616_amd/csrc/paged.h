@@ -94,10 +94,13 @@ template <int SHIFT> struct PagedBlock {
   int lo, hi;                                       // positions of the block's first and last row
   TileList<SHIFT> tiles;
   int per;                                          // tiles a split: split s has tiles s per ..
-  template <typename T> __device__ __forceinline__ PagedBlock(const PagedArgs<T>& a, int b, int block, int block_rows, const Divisor& splits, int least_keys) : b(b) {
-    const RowRange r = ragged_rows(a.row_start, b, a.T_rows);
+  template <typename T> __device__ __forceinline__ PagedBlock(const PagedArgs<T>& a, int b, int block, int block_rows, const Divisor& splits, int least_keys)
+      : PagedBlock(a, b, ragged_rows(a.row_start, b, a.T_rows), a.cached(b), block, block_rows, splits, least_keys) {}
+  template <typename T>
+  __device__ __forceinline__ PagedBlock(const PagedArgs<T>& a, int b, const RowRange& r, int cached, int block, int block_rows, const Divisor& splits, int least_keys)
+      : b(b) {
     const int G = a.group.d;
-    pos0 = a.cached(b);
+    pos0 = cached;
     row0 = r.first;
     rows = min(r.count, a.max_new);
     packed = rows * G;
@@ -117,30 +120,40 @@ template <int SHIFT> struct PagedBlock {
   __device__ __forceinline__ bool whole() const { return tiles.count <= per; }
 };
 
-// the document and block of the i-th wide block of the call (-1: there are fewer); the whole wave
-template <typename T> __device__ __forceinline__ int find_wide_block(const PagedArgs<T>& a, int& i, int lane) {
-  for (int b0 = 0; b0 < a.B; b0 += 64) {
-    int n = 0;
-    if (b0 + lane < a.B) {
-      const int packed = min(ragged_rows(a.row_start, b0 + lane, a.T_rows).count, a.max_new) * (int)a.group.d;
-      n = packed > PagedCut<T>::NARROW_ROWS ? (packed + PagedCut<T>::WIDE_ROWS - 1) / PagedCut<T>::WIDE_ROWS : 0;
+// The i-th wide block of the call: its document (-1: there are fewer), which of the document's blocks, the document's rows and cached positions,
+// which the whole wave has read anyway to find it.  Everything is wave-uniform.
+struct WideBlock {
+  int b, block, cached;
+  RowRange rows;
+  template <typename T> __device__ __forceinline__ WideBlock(const PagedArgs<T>& a, int i, int lane) : b(-1), block(0), cached(0), rows{0, 0} {
+    for (int b0 = 0; b0 < a.B; b0 += 64) {
+      int n = 0, mine = 0;
+      RowRange r{0, 0};
+      if (b0 + lane < a.B) {
+        r = ragged_rows(a.row_start, b0 + lane, a.T_rows);
+        mine = a.cached(b0 + lane);
+        const int packed = min(r.count, a.max_new) * (int)a.group.d;
+        n = packed > PagedCut<T>::NARROW_ROWS ? (packed + PagedCut<T>::WIDE_ROWS - 1) / PagedCut<T>::WIDE_ROWS : 0;
+      }
+      int upto = n;   // blocks of documents b0 .. b0 + lane: a scan on the DPP lanes, of rows of 16, then across them
+      upto += __builtin_amdgcn_update_dpp(0, upto, 0x111, 0xf, 0xf, false);   // row_shr 1, 2, 4, 8
+      upto += __builtin_amdgcn_update_dpp(0, upto, 0x112, 0xf, 0xf, false);
+      upto += __builtin_amdgcn_update_dpp(0, upto, 0x114, 0xf, 0xf, false);
+      upto += __builtin_amdgcn_update_dpp(0, upto, 0x118, 0xf, 0xf, false);
+      upto += __builtin_amdgcn_update_dpp(0, upto, 0x142, 0xa, 0xf, false);   // row_bcast15 into rows 1 and 3
+      upto += __builtin_amdgcn_update_dpp(0, upto, 0x143, 0xc, 0xf, false);   // row_bcast31 into rows 2 and 3
+      const int all = __builtin_amdgcn_readlane(upto, 63);
+      if (i < all) {
+        const int at = __builtin_popcountll(__builtin_amdgcn_ballot_w64(upto <= i));
+        b = b0 + at;
+        block = i - (at ? __builtin_amdgcn_readlane(upto, at - 1) : 0);
+        cached = __builtin_amdgcn_readlane(mine, at);
+        rows = {__builtin_amdgcn_readlane(r.first, at), __builtin_amdgcn_readlane(r.count, at)};
+        return;
+      }
+      i -= all;
     }
-    int upto = n;   // blocks of documents b0 .. b0 + lane
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const int before = __shfl_up(upto, d, WAVE);
-      if (lane >= d) upto += before;
-    }
-    const int all = __builtin_amdgcn_readlane(upto, 63);
-    if (i < all) {
-      const unsigned long long before = __builtin_amdgcn_ballot_w64(upto <= i);
-      const int at = __builtin_popcountll(before);
-      i -= at ? __builtin_amdgcn_readlane(upto, at - 1) : 0;
-      return b0 + at;
-    }
-    i -= all;
   }
-  return -1;
-}
+};
 
 }  // namespace dipaco

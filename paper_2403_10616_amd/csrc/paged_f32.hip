@@ -20,15 +20,21 @@ __global__ void __launch_bounds__(WF_THREADS, NARROW && DH == 128 ? 1 : 2) paged
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
   const Divisor& splits = NARROW ? a.narrow_splits : a.wide_splits;
   const int hk = NARROW ? blockIdx.y : blockIdx.x;
-  int b = blockIdx.z + first, block = 0;
+  int b = blockIdx.z + first, block = 0, cached;
+  RowRange rows;
   const int split = NARROW ? a.narrow_split(blockIdx.x, b * a.H_kv + hk) : blockIdx.y;
-  if constexpr (!NARROW) {
-    block = blockIdx.z + first;
-    b = __builtin_amdgcn_readfirstlane(find_wide_block(a, block, lane));
+  if constexpr (NARROW) {
+    rows = ragged_rows(a.row_start, b, a.T_rows);
+    cached = a.cached(b);
+  } else {
+    const WideBlock at(a, b, lane);
+    b = at.b;
     if (b < 0) return;
-    block = __builtin_amdgcn_readfirstlane(block);
+    block = at.block;
+    rows = at.rows;
+    cached = at.cached;
   }
-  const PagedBlock<SHIFT> blk(a, b, block, NARROW ? Cut::NARROW_ROWS : Cut::WIDE_ROWS, splits, NARROW ? a.narrow_keys : Cut::LEAST_KEYS);
+  const PagedBlock<SHIFT> blk(a, b, rows, cached, block, NARROW ? Cut::NARROW_ROWS : Cut::WIDE_ROWS, splits, NARROW ? a.narrow_keys : Cut::LEAST_KEYS);
   if (NARROW && (blk.packed == 0 || blk.packed > Cut::NARROW_ROWS)) return;
   if (!blk.has(split)) return;
   const int t0 = split * blk.per, n_tiles = min(blk.tiles.count - t0, blk.per);

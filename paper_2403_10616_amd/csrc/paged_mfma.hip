@@ -17,6 +17,9 @@ __device__ __forceinline__ const char* uniform(const char* v) {
   const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)a), hi = __builtin_amdgcn_readfirstlane((uint32_t)(a >> 32));
   return reinterpret_cast<const char*>(((uint64_t)hi << 32) | lo);
 }
+__device__ __forceinline__ uint64_t lane_offset(uint64_t v, int lane) {
+  return (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), lane) << 32;
+}
 __device__ __forceinline__ uint32_t uniform(uint32_t v) { return __builtin_amdgcn_readfirstlane(v); }
 
 using Cut = PagedCut<bf16>;
@@ -76,9 +79,10 @@ __device__ __forceinline__ void add_seen(SoftmaxRow<DH>& x, const PagedArgs<bf16
 template <int DH> __device__ __forceinline__ void wide_block(const PagedArgs<bf16>& a, int hk, int split, int block, char* pw_smem) {
   constexpr int KS = DH / 16, NP = panels<DH>(), TILE_BYTES = tile_bytes<DH>();
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, h = lane >> 5;
-  const int b = __builtin_amdgcn_readfirstlane(find_wide_block(a, block, lane));
+  const WideBlock at_block(a, block, lane);
+  const int b = at_block.b;
   if (b < 0) return;
-  const PagedBlock<Cut::WIDE_SHIFT> blk(a, b, __builtin_amdgcn_readfirstlane(block), Cut::WIDE_ROWS, a.wide_splits, Cut::LEAST_KEYS);
+  const PagedBlock<Cut::WIDE_SHIFT> blk(a, b, at_block.rows, at_block.cached, at_block.block, Cut::WIDE_ROWS, a.wide_splits, Cut::LEAST_KEYS);
   const int t0 = split * blk.per, n_tiles = min(blk.tiles.count - t0, blk.per);
   if (!blk.has(split)) return;
   const int r0 = blk.packed0 + 32 * wave;
@@ -95,18 +99,22 @@ template <int DH> __device__ __forceinline__ void wide_block(const PagedArgs<bf1
     const uint32_t smem_addr = (uint32_t)(uintptr_t)pw_smem;
     const PagePlace<DH> at(a, b, hk, blk.last);
     const uint32_t col = loader_column_bytes<DH>(0, wave, lane), off = (uint32_t)((lane >> 3) * DH * 2) + col;   // the same for both row groups of a wave
-    int ids = 0;   // lane 4 (t % 16) + g: the page of rows 16 g .. of tile t
+    int ids = 0;       // lane 4 (t % 16) + g: the page of rows 16 g .. of tile t
+    uint64_t rows16 = 0;   // and where these rows' keys start, from at.base
     auto issue = [&](int t, int stage) -> int {
       const int tile = blk.tiles.at(t0 + t), row0 = tile * 64;
-      if ((t & 15) == 0) ids = a.page_of(b, min(blk.tiles.at(t0 + min(t + (lane >> 2), n_tiles - 1)) * 64 + 16 * (lane & 3), at.last));
+      if ((t & 15) == 0) {
+        const int pos = blk.tiles.at(t0 + min(t + (lane >> 2), n_tiles - 1)) * 64 + 16 * (lane & 3);
+        ids = a.page_of(b, min(pos, at.last));
+        rows16 = (uint64_t)at.at(ids, pos);
+      }
       const int l0 = 4 * (t & 15);
       const int holes = (int)((__builtin_amdgcn_ballot_w64(ids < 0) >> l0) & 15);
       const uint32_t dst = uniform(smem_addr + stage * 2 * TILE_BYTES + wave * 1024);
       if (holes == 0 && row0 + 63 <= at.last) {   // wave-uniform
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const int rows8 = row0 + 8 * (wave + 4 * i);
-          const char* const k = uniform(at.base + at.at(__builtin_amdgcn_readlane(ids, l0 + ((wave + 4 * i) >> 1)), rows8));
+          const char* const k = uniform(at.base + lane_offset(rows16, l0 + ((wave + 4 * i) >> 1)) + (wave & 1) * 8 * DH * 2);
           const char* const v = uniform(k + at.value_bytes);
 #pragma unroll
           for (int p = 0; p < NP; ++p) {
@@ -198,7 +206,8 @@ template <int DH, int NW, int NS> __device__ __forceinline__ void narrow_documen
       col[i] = (uint32_t)(c * 16);
       off[i] = (uint32_t)((lane >> 3) * DH * 2) + col[i];
     }
-    int ids = 0;   // lane 2 (t % 32) + g: the page of rows 16 g .. of this wave's half t
+    int ids = 0;           // lane 2 (t % 32) + g: the page of rows 16 g .. of this wave's half t
+    uint64_t rows16 = 0;   // and where these rows' keys start, from at.base
     auto half_at = [&](int t) { return blk.tiles.at(t0 + wave + NW * t) * 32; };
     auto holes_of = [&](unsigned long long none, int t) { return (int)((none >> (2 * (t & 31))) & 3); };
     unsigned long long none = 0;   // which of the lanes' pages are none; of the 32 halves before as well
@@ -206,7 +215,9 @@ template <int DH, int NW, int NS> __device__ __forceinline__ void narrow_documen
     auto issue = [&](int t) {
       const int row0 = half_at(t);
       if ((t & 31) == 0) {
-        ids = a.page_of(b, min(half_at(min(t + (lane >> 1), n - 1)) + 16 * (lane & 1), at.last));
+        const int pos = half_at(min(t + (lane >> 1), n - 1)) + 16 * (lane & 1);
+        ids = a.page_of(b, min(pos, at.last));
+        rows16 = (uint64_t)at.at(ids, pos);
         none_before = none;
         none = __builtin_amdgcn_ballot_w64(ids < 0);
       }
@@ -215,7 +226,7 @@ template <int DH, int NW, int NS> __device__ __forceinline__ void narrow_documen
       if (holes_of(none, t) == 0 && row0 + 31 <= at.last) {   // wave-uniform
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const char* const k = uniform(at.base + at.at(__builtin_amdgcn_readlane(ids, l0 + (i >> 1)), row0 + 8 * i));
+          const char* const k = uniform(at.base + lane_offset(rows16, l0 + (i >> 1)) + (i & 1) * 8 * DH * 2);
           const char* const v = uniform(k + at.value_bytes);
 #pragma unroll
           for (int p = 0; p < NP; ++p) {
