@@ -153,11 +153,57 @@ template <int DH> __device__ __forceinline__ void window_dq_f32(const FWindowArg
   store_row<DH>(dqkv + ((long)b * a.S + q) * ld + hd * DH, dq, g, head_scale<DH>());
 }
 
-// dK and dV: 64 keys of a key head over the queries that see them under the window alone; SINKS: 16 sinks over all queries behind them, the
-// waves two and two on the halves of a stage, for dV and for dK (attention_window_mfma.hip)
-template <int DH, bool SINKS>
+// A part's sums of 16 sinks, 32 DH floats (dK, then dV), in rows of their own of the q part of dqkv, H DH floats each
+struct FSinkParts {
+  int groups, parts, rows;   // of 16 sinks, parts a group, rows a part: ceil(32 / H)
+  template <int DH> __device__ __forceinline__ float* at(float* dqkv, int b, int S, int H, long ld, int hk, int group, int part, int f) const {
+    const int per_row = H * DH, row = ((hk * groups + group) * parts + part) * rows + f / per_row;
+    return dqkv + ((long)b * S + row) * ld + f % per_row;
+  }
+};
+enum { F_KEYS = 0, F_SINKS_WHOLE = 1, F_SINKS_PART = 2 };
+
+// where a wave's sums of its keys (four lanes each) are not finite: the pairs that see each other alone
+template <int DH>
+__device__ __forceinline__ void keys_if_not_finite(f32x4 (&dk)[DH / 16], f32x4 (&dv)[DH / 16], const FWindowArgs& a, const float* __restrict__ d_o,
+                                                   const float* __restrict__ dsum, int b, int hk, int key, int key_last, int rows, int g) {
+  if (!(__any(key < rows && (plain::not_finite(dk) || plain::not_finite(dv))) && key < rows)) return;
+  const int G = a.H / a.H_kv;
+  const long ld = (long)(a.H + 2 * a.H_kv) * DH, Sp = (a.S + 127) / 128 * 128L;
+  const float* const base = a.qkv + (long)b * a.S * ld;
+  const float* const krow = base + key * ld + (a.H + hk) * DH;
+  plain::clear(dk);
+  plain::clear(dv);
+#pragma unroll 1
+  for (int h = 0; h < G; ++h) {
+    const float* const D = dsum + (long)(b * a.H + hk * G + h) * Sp;
+    const float* const L = D + (long)a.B * a.H * Sp;
+#pragma unroll 1
+    for (int i = key; i <= key_last; ++i) {
+      const float* qr = base + i * ld + (hk * G + h) * DH;
+      const float* gr = d_o + (((long)b * a.S + i) * a.H + hk * G + h) * DH;
+      const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(plain::dot<DH>(qr, krow), head_scale<DH>() * WF_LOG2E, L[i]));
+      plain::add_row(dv, p, gr, g);
+      plain::add_row(dk, p * (plain::dot<DH>(gr, krow + a.H_kv * DH) - D[i]), qr, g);
+    }
+  }
+}
+// a key's dK and dV; 0 behind the document
+template <int DH>
+__device__ __forceinline__ void store_keys(f32x4 (&dk)[DH / 16], f32x4 (&dv)[DH / 16], const FWindowArgs& a, float* __restrict__ dqkv, int b, int hk, int key, bool inside,
+                                           int g) {
+  if (!inside) { zero_acc<DH>(dk); zero_acc<DH>(dv); }
+  float* const out = dqkv + ((long)b * a.S + key) * (a.H + 2 * a.H_kv) * DH + (a.H + hk) * DH;
+  store_row<DH>(out, dk, g, head_scale<DH>());
+  store_row<DH>(out + a.H_kv * DH, dv, g, 1.0f);
+}
+
+// dK and dV: 64 keys of a key head over the queries that see them under the window alone; or 16 sinks over all queries behind them, the
+// waves two and two on the halves of a stage, for dV and for dK, whole or in parts (attention_window_mfma.hip)
+template <int DH, int KIND>
 __device__ __forceinline__ void window_dkv_f32(const FWindowArgs& a, const float* __restrict__ d_o, const float* __restrict__ dsum, float* __restrict__ dqkv, int b,
-                                               int hk, int k0, float* smem) {
+                                               int hk, int k0, float* smem, const FSinkParts& sp, int part) {
+  constexpr bool SINKS = KIND != F_KEYS;
   constexpr int STAGE = wf_stage<DH>();
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
   const int rows = document_rows(a.lengths, b, a.S), G = a.H / a.H_kv;
@@ -177,10 +223,16 @@ __device__ __forceinline__ void window_dkv_f32(const FWindowArgs& a, const float
   if (k0 < rows && (SINKS || k0 + WF_ROWS - 1 >= sinks)) {
     const RowFrag<DH> kf = load_row<DH>(krow, g, key < rows), vf = load_row<DH>(krow + a.H_kv * DH, g, key < rows);
     const int block_last = SINKS ? rows - 1 : min(rows - 1, k0 + WF_ROWS - 1 + a.w.window - 1);
-    const int first = k0 >> 5, n_tiles = (block_last >> 5) + 1 - first, steps = G * n_tiles;
+    const int first = k0 >> 5, n_tiles = (block_last >> 5) + 1 - first;
+    int steps = G * n_tiles, done = 0;   // steps of the parts in front of this one
+    if constexpr (KIND == F_SINKS_PART) {
+      const int per = (steps + sp.parts - 1) / sp.parts;
+      done = min(part * per, steps);
+      steps = min(per, steps - done);
+    }
     TileMover<DH, WF_TILE> next;
     float next_stat = 0.f;
-    int load_tile = first, load_head = 0;
+    int load_head = done / n_tiles, load_tile = first + done - load_head * n_tiles, qt = load_tile;
     auto load = [&]() {   // the heads of the group one after the other; threads 0 .. 31 move -lse log2(e), 32 .. 63 D
       const float* const q = base + (hk * G + load_head) * DH;
       const float* const go = d_o + ((long)b * a.S * a.H + hk * G + load_head) * DH;
@@ -197,9 +249,11 @@ __device__ __forceinline__ void window_dkv_f32(const FWindowArgs& a, const float
       next.store(stage);
       if (threadIdx.x < 2 * WF_TILE) stage[2 * window_tile_floats<DH, WF_TILE>() + threadIdx.x] = next_stat;
     };
-    load();
-    store(smem);
-    for (int n = 0, qt = first; n < steps; ++n) {
+    if (steps > 0) {
+      load();
+      store(smem);
+    }
+    for (int n = 0; n < steps; ++n) {
       const float* q_ = smem + (n & 1) * STAGE;
       const float* g_ = q_ + window_tile_floats<DH, WF_TILE>();
       const float* Ls = g_ + window_tile_floats<DH, WF_TILE>();
@@ -255,29 +309,73 @@ __device__ __forceinline__ void window_dkv_f32(const FWindowArgs& a, const float
       if (wave != 0) return;
       add(dk, smem + 2 * PER);
     }
-    if (__any(key < rows && (plain::not_finite(dk) || plain::not_finite(dv))) && key < rows) {
-      plain::clear(dk);
-      plain::clear(dv);
-#pragma unroll 1
-      for (int h = 0; h < G; ++h) {
-        const float* const D = dsum + (long)(head0 + h) * Sp;
-        const float* const L = D + (long)a.B * a.H * Sp;
-#pragma unroll 1
-        for (int i = key; i <= key_last; ++i) {
-          const float* qr = base + i * ld + (hk * G + h) * DH;
-          const float* gr = d_o + (((long)b * a.S + i) * a.H + hk * G + h) * DH;
-          const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(plain::dot<DH>(qr, krow), sc, L[i]));
-          plain::add_row(dv, p, gr, g);
-          plain::add_row(dk, p * (plain::dot<DH>(gr, krow + a.H_kv * DH) - D[i]), qr, g);
-        }
+    if constexpr (KIND == F_SINKS_PART) {
+#pragma unroll
+      for (int d = 0; d < DH / 16; ++d) {
+        *reinterpret_cast<f32x4*>(sp.at<DH>(dqkv, b, a.S, a.H, ld, hk, k0 >> 4, part, (d * WAVE + lane) * 4)) = dk[d];
+        *reinterpret_cast<f32x4*>(sp.at<DH>(dqkv, b, a.S, a.H, ld, hk, k0 >> 4, part, ((DH / 16 + d) * WAVE + lane) * 4)) = dv[d];
       }
+      return;
     }
+    keys_if_not_finite<DH>(dk, dv, a, d_o, dsum, b, hk, key, key_last, rows, g);
   }
   if (key >= a.S || (SINKS ? key >= sinks : key < sinks)) return;
-  if (key >= rows) { zero_acc<DH>(dk); zero_acc<DH>(dv); }
-  float* const out = dqkv + ((long)b * a.S + key) * ld + (a.H + hk) * DH;
-  store_row<DH>(out, dk, g, head_scale<DH>());
-  store_row<DH>(out + a.H_kv * DH, dv, g, 1.0f);
+  store_keys<DH>(dk, dv, a, dqkv, b, hk, key, key < rows, g);
+}
+// The parts' sums of 16 sinks added in their order, a quarter of them a wave, and stored: a workgroup per document, key head, 16 sinks and 16 columns
+template <int DH>
+__global__ void __launch_bounds__(WF_THREADS) window_sinks_join_f32(FWindowArgs a, const float* __restrict__ d_o, const float* __restrict__ dsum,
+                                                                    float* __restrict__ dqkv, FSinkParts sp) {
+  constexpr int ND = DH / 16;
+  __shared__ __attribute__((aligned(16))) f32x4 sums[3][WAVE];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4;
+  const int n_kv = a.B * a.H_kv, unit = blockIdx.x / (2 * ND), n = blockIdx.x - unit * 2 * ND, group = unit / n_kv, bk = unit - group * n_kv, b = bk / a.H_kv,
+            hk = bk - b * a.H_kv;
+  const int rows = document_rows(a.lengths, b, a.S), sinks = rows <= a.w.window ? 0 : min(a.w.sinks, rows);
+  const long ld = (long)(a.H + 2 * a.H_kv) * DH;
+  if (16 * group >= sinks) return;
+  const int per = (sp.parts + 3) / 4, first = wave * per, end = min(first + per, sp.parts);
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
+  for (int p0 = first; p0 < end; p0 += 8) {   // eight parts at a time; those behind the last one count as zero
+    f32x4 w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = *reinterpret_cast<const f32x4*>(sp.at<DH>(dqkv, b, a.S, a.H, ld, hk, group, min(p0 + i, end - 1), (n * WAVE + lane) * 4));
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (p0 + i < end) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] += w[i][e];
+      }
+  }
+  if (wave > 0) sums[wave - 1][lane] = v;
+  __syncthreads();
+  if (wave > 0) return;
+#pragma unroll
+  for (int w = 0; w < 3; ++w)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] += sums[w][lane][e];
+  const int key = 16 * group + (lane & 15);
+  const f32x4 mine[1] = {v};
+  if (__any(key < sinks && plain::not_finite(mine))) {
+    f32x4 dk[ND], dv[ND];
+#pragma unroll
+    for (int d = 0; d < ND; ++d) dk[d] = dv[d] = f32x4{INFINITY, 0.f, 0.f, 0.f};   // whatever it held: formed anew
+    keys_if_not_finite<DH>(dk, dv, a, d_o, dsum, b, hk, key, rows - 1, rows, g);
+#pragma unroll
+    for (int d = 0; d < 2 * ND; ++d)
+      if (d == n) v = d < ND ? dk[d < ND ? d : 0] : dv[d < ND ? 0 : d - ND];
+  }
+  if (key >= sinks) return;
+  const float scale = n < ND ? head_scale<DH>() : 1.0f;
+  *reinterpret_cast<float4*>(dqkv + ((long)b * a.S + key) * ld + (a.H + hk + (n < ND ? 0 : a.H_kv)) * DH + 16 * (n < ND ? n : n - ND) + 4 * g) =
+      make_float4(v[0] * scale, v[1] * scale, v[2] * scale, v[3] * scale);
+}
+template <int DH>
+__global__ void __launch_bounds__(WF_THREADS, 2) window_sink_parts_f32(FWindowArgs a, const float* __restrict__ d_o, const float* __restrict__ dsum,
+                                                                       float* __restrict__ dqkv, FSinkParts sp) {
+  extern __shared__ __attribute__((aligned(16))) float wpf_smem[];
+  const int n_kv = a.B * a.H_kv, s = blockIdx.x / n_kv, bk = blockIdx.x - s * n_kv, b = bk / a.H_kv, group = s / sp.parts;
+  window_dkv_f32<DH, F_SINKS_PART>(a, d_o, dsum, dqkv, b, bk - b * a.H_kv, 16 * group, wpf_smem, sp, s - group * sp.parts);
 }
 
 // One launch: the sinks' workgroups, which take longest, then those of dK / dV, then dQ's
@@ -289,13 +387,13 @@ __global__ void __launch_bounds__(WF_THREADS, 2) window_bwd_f32(FWindowArgs a, c
   int i = blockIdx.x;
   if (i < sink_blocks * n_kv) {
     const int s = i / n_kv, bk = i - s * n_kv, b = bk / a.H_kv;
-    window_dkv_f32<DH, true>(a, d_o, dsum, dqkv, b, bk - b * a.H_kv, 16 * s, wbf_smem);
+    window_dkv_f32<DH, F_SINKS_WHOLE>(a, d_o, dsum, dqkv, b, bk - b * a.H_kv, 16 * s, wbf_smem, FSinkParts{}, 0);
     return;
   }
   i -= sink_blocks * n_kv;
   if (i < n_kv * nb) {
     const int kb = i / n_kv, bk = i - kb * n_kv, b = bk / a.H_kv;
-    window_dkv_f32<DH, false>(a, d_o, dsum, dqkv, b, bk - b * a.H_kv, WF_ROWS * kb, wbf_smem);
+    window_dkv_f32<DH, F_KEYS>(a, d_o, dsum, dqkv, b, bk - b * a.H_kv, WF_ROWS * kb, wbf_smem, FSinkParts{}, 0);
     return;
   }
   i -= n_kv * nb;
@@ -321,9 +419,22 @@ dipaco_status launch_window_bwd_f32(const float* qkv, const int* lengths, const 
   static std::atomic<unsigned long long> lds_set{0};
   if (dipaco_status st = ensure_dynamic_lds(reinterpret_cast<const void*>(window_bwd_f32<DH>), LDS, lds_set)) return st;
   const FWindowArgs a{qkv, lengths, B, S, H, H_kv, w};
-  const int nb = (S + WF_ROWS - 1) / WF_ROWS, sink_blocks = w.window >= S ? 0 : (std::min(w.sinks, S) + 15) / 16;
+  const int nb = (S + WF_ROWS - 1) / WF_ROWS, G = H / H_kv;
+  int sink_blocks = w.window >= S ? 0 : (std::min(w.sinks, S) + 15) / 16;
+  FSinkParts sp{sink_blocks, 1, (32 + H - 1) / H};   // as in attention_window_mfma.hip; stages of 32 queries
+  const int64_t stages = (int64_t)G * ((S + 31) / 32), rest = (int64_t)2 * B * H * nb * ((w.window + 64) / 32 + 1) / 768;
+  if (sink_blocks && stages > rest + 24 && 10 * stages > 18 * rest) sp.parts = (int)std::min<int64_t>(stages / 8, S / ((int64_t)H_kv * sink_blocks * sp.rows));
   window_stats_f32<DH><<<B * H * ((S + 127) / 128 * 2), WF_THREADS, 0, s>>>(a, o, d_o, lse, dsum);
   DIPACO_LAUNCH_CHECK();
+  if (sink_blocks && sp.parts > 1) {
+    static std::atomic<unsigned long long> parts_lds{0};
+    if (dipaco_status st = ensure_dynamic_lds(reinterpret_cast<const void*>(window_sink_parts_f32<DH>), LDS, parts_lds)) return st;
+    window_sink_parts_f32<DH><<<B * H_kv * sink_blocks * sp.parts, WF_THREADS, LDS, s>>>(a, d_o, dsum, dqkv, sp);
+    DIPACO_LAUNCH_CHECK();
+    window_sinks_join_f32<DH><<<B * H_kv * sink_blocks * (DH / 8), WF_THREADS, 0, s>>>(a, d_o, dsum, dqkv, sp);
+    DIPACO_LAUNCH_CHECK();
+    sink_blocks = 0;
+  }
   window_bwd_f32<DH><<<B * H_kv * (sink_blocks + nb) + B * H * nb, WF_THREADS, LDS, s>>>(a, d_o, dsum, dqkv, sink_blocks);
   DIPACO_LAUNCH_CHECK();
   return DIPACO_OK;

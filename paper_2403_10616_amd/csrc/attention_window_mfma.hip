@@ -197,11 +197,60 @@ template <int DH> __device__ __forceinline__ void window_dq(const WindowArgs& a,
 // Keys: 128 of a key head, 32 a wave, over the queries of every head of the group that see them under the window alone; the stages hold 64
 // queries.  Sinks are seen by all queries behind them, a multiple of what the other keys take, so a workgroup takes only 32 of them (SINKS):
 // its waves share the stage, two of them on each half of it, one for dV and one for dK, and the halves' sums meet at the end.
+// Where that would still be the longest by far, the queries are cut among `parts` workgroups, whose sums lie in the rows of dqkv that dQ is
+// written to afterwards (SinkParts), and window_sinks_join adds them.  1 x 32768 positions, 16 heads of 128 on 4, window 1024, 16 sinks: 2995 us
+// uncut (without sinks 1098), 1150 cut; 8 heads of 64 on 1, 8192 positions, window 512, 4 sinks 819 | 180.
 template <int DH> constexpr int window_dkv_stage() { return 2 * tile_bytes<DH>() + 2 * 64 * (int)sizeof(float); }   // Q | dO | -lse log2(e) | D
 
-template <int DH, bool SINKS>
+// where a wave's sums of its keys (a lane pair each) are not finite: the pairs that see each other alone
+template <int DH>
+__device__ __forceinline__ void keys_if_not_finite(f32x16 (&dk)[DH / 32], f32x16 (&dv)[DH / 32], const WindowArgs& a, const bf16* __restrict__ d_o,
+                                                   const float* __restrict__ dsum, int b, int hk, int key, int key_last, int rows, int h) {
+  if (!(__any(key < rows && (plain::not_finite(dk) || plain::not_finite(dv))) && key < rows)) return;
+  const int G = a.H / a.H_kv, ld = (a.H + 2 * a.H_kv) * DH;
+  const long Sp = (a.S + 127) / 128 * 128L;
+  const bf16* const base = a.qkv + (long)b * a.S * ld;
+  const bf16* const krow = base + (long)key * ld + (a.H + hk) * DH;
+  const float sc = score_scale<DH>() * LOG2E;
+  plain::clear(dk);
+  plain::clear(dv);
+#pragma unroll 1
+  for (int g = 0; g < G; ++g) {
+    const float* const D = dsum + (long)(b * a.H + hk * G + g) * Sp;
+    const float* const L = D + (long)a.B * a.H * Sp;
+#pragma unroll 1
+    for (int i = key; i <= key_last; ++i) {
+      const bf16* qr = base + (long)i * ld + (hk * G + g) * DH;
+      const bf16* gr = d_o + (((long)b * a.S + i) * a.H + hk * G + g) * DH;
+      const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(plain::dot<DH>(qr, krow), sc, L[i]));
+      plain::add_row(dv, p, gr, h);
+      plain::add_row(dk, p * (plain::dot<DH>(gr, krow + a.H_kv * DH) - D[i]), qr, h);
+    }
+  }
+}
+// a key's dK and dV; 0 behind the document
+template <int DH>
+__device__ __forceinline__ void store_keys(f32x16 (&dk)[DH / 32], f32x16 (&dv)[DH / 32], const WindowArgs& a, bf16* __restrict__ dqkv, int b, int hk, int key, bool inside,
+                                           int h) {
+  if (!inside) { plain::clear(dk); plain::clear(dv); }
+  bf16* const out = dqkv + ((long)b * a.S + key) * (a.H + 2 * a.H_kv) * DH + (a.H + hk) * DH;
+  store_transposed_out(out, dk, h, score_scale<DH>());
+  store_transposed_out(out + a.H_kv * DH, dv, h, 1.0f);
+}
+// A part's sums of 32 sinks, 64 DH floats (dK, then dV, as hand_over leaves them), in rows of their own of the q part of dqkv, H DH / 2 floats each
+struct SinkParts {
+  int groups, parts, rows;   // of 32 sinks, parts a group, rows a part: ceil(128 / H)
+  template <int DH> __device__ __forceinline__ float* at(bf16* dqkv, int b, int S, int H, int ld, int hk, int group, int part, int f) const {
+    const int per_row = H * DH / 2, row = ((hk * groups + group) * parts + part) * rows + f / per_row;
+    return reinterpret_cast<float*>(dqkv + ((long)b * S + row) * ld) + f % per_row;
+  }
+};
+enum { KEYS = 0, SINKS_WHOLE = 1, SINKS_PART = 2 };
+
+template <int DH, int KIND>
 __device__ __forceinline__ void window_dkv(const WindowArgs& a, const bf16* __restrict__ d_o, const float* __restrict__ dsum, bf16* __restrict__ dqkv, int b, int hk,
-                                           int k0, char* smem) {
+                                           int k0, char* smem, const SinkParts& sp, int part) {
+  constexpr bool SINKS = KIND != KEYS;
   constexpr int KS = DH / 16, DT = DH / 32, TILE_BYTES = tile_bytes<DH>(), STAGE = window_dkv_stage<DH>();
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, h = lane >> 5;
   const int rows = document_rows(a.lengths, b, a.S), ld = (a.H + 2 * a.H_kv) * DH, G = a.H / a.H_kv;
@@ -230,13 +279,23 @@ __device__ __forceinline__ void window_dkv(const WindowArgs& a, const bf16* __re
     TrOff to = tr_offsets(lane);
     const uint32_t smem_addr = (uint32_t)(uintptr_t)smem;
     const int block_last = SINKS ? rows - 1 : min(rows - 1, k0 + 127 + a.w.window - 1);
-    const int first = k0 >> 6, n_tiles = (block_last >> 6) + 1 - first, steps = G * n_tiles;
+    const int first = k0 >> 6, n_tiles = (block_last >> 6) + 1 - first;
+    int steps = G * n_tiles, done = 0;   // steps of the parts in front of this one
+    if constexpr (KIND == SINKS_PART) {
+      const int per = (steps + sp.parts - 1) / sp.parts;
+      done = min(part * per, steps);
+      steps = min(per, steps - done);
+    }
+    const int head1 = done / n_tiles;    // the first step's head and tile
     const int head0 = b * a.H + hk * G;
     RowTiles<DH, true> src(base + hk * G * DH, d_o + ((long)b * a.S * a.H + hk * G) * DH, ld, a.H * DH, rows, wave, lane);
     // statistics of a tile's 64 queries: waves 0 and 2 fetch -lse log2(e), waves 1 and 3 fetch D
     const float* stat = dsum + ((wave & 1 ? 0 : (long)a.B * a.H) + head0) * Sp + lane;
     const uint32_t stat_dst = 2 * TILE_BYTES + (wave & 1 ? 256 : 0);
-    int next_tile = first;
+    int next_tile = first + done - head1 * n_tiles;
+    src.t0 += head1 * DH;
+    src.t1 += head1 * DH;
+    stat += head1 * Sp;
     auto issue = [&](int stage) {   // the next step's tile: the heads of the group one after the other
       src.issue(next_tile, wave, lane, smem_addr + stage * STAGE);
       load4_to_lds(stat + next_tile * 64, smem_addr + stage * STAGE + stat_dst);
@@ -247,8 +306,9 @@ __device__ __forceinline__ void window_dkv(const WindowArgs& a, const bf16* __re
         stat += Sp;
       }
     };
-    issue(0);
-    for (int n = 0, qt = first, cur = 0; n < steps; ++n, cur ^= 1) {
+    int qt = next_tile;
+    if (steps > 0) issue(0);
+    for (int n = 0, cur = 0; n < steps; ++n, cur ^= 1) {
       wait_vmcnt<0>();
       __syncthreads();
       if (n + 1 < steps) issue(1 - cur);
@@ -321,32 +381,72 @@ __device__ __forceinline__ void window_dkv(const WindowArgs& a, const bf16* __re
       if (wave != 0) return;
       take_over(dk, at + 2 * PER, 0.f, 1.f, lane);
     }
-    if (__any(key < rows && (plain::not_finite(dk) || plain::not_finite(dv))) && key < rows) {
-      plain::clear(dk);
-      plain::clear(dv);
-#pragma unroll 1
-      for (int g = 0; g < G; ++g) {
-        const float* const D = dsum + (long)(head0 + g) * Sp;
-        const float* const L = D + (long)a.B * a.H * Sp;
-#pragma unroll 1
-        for (int i = key; i <= key_last; ++i) {
-          const bf16* qr = base + (long)i * ld + (hk * G + g) * DH;
-          const bf16* gr = d_o + (((long)b * a.S + i) * a.H + hk * G + g) * DH;
-          const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(plain::dot<DH>(qr, krow), sc, L[i]));
-          plain::add_row(dv, p, gr, h);
-          plain::add_row(dk, p * (plain::dot<DH>(gr, krow + a.H_kv * DH) - D[i]), qr, h);
+    if constexpr (KIND == SINKS_PART) {
+#pragma unroll
+      for (int n = 0; n < 2 * DT; ++n)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const f32x16& v = n < DT ? dk[n < DT ? n : 0] : dv[n < DT ? 0 : n - DT];
+          *reinterpret_cast<float4*>(sp.at<DH>(dqkv, b, a.S, a.H, ld, hk, k0 >> 5, part, ((n * 4 + g) * WAVE + lane) * 4)) =
+              make_float4(v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]);
         }
-      }
+      return;
     }
+    keys_if_not_finite<DH>(dk, dv, a, d_o, dsum, b, hk, key, key_last, rows, h);
   }
   int key_out = key;
   asm volatile("" : "+v"(key_out));
-  if (key_out < a.S && (SINKS ? key_out < sinks : key_out >= sinks)) {
-    if (key_out >= rows) { plain::clear(dk); plain::clear(dv); }
-    bf16* const out = dqkv + ((long)b * a.S + key_out) * ld + (a.H + hk) * DH;
-    store_transposed_out(out, dk, h, score_scale<DH>());
-    store_transposed_out(out + a.H_kv * DH, dv, h, 1.0f);
+  if (key_out < a.S && (SINKS ? key_out < sinks : key_out >= sinks)) store_keys<DH>(dk, dv, a, dqkv, b, hk, key_out, key_out < rows, h);
+}
+// The parts' sums of 32 sinks added in their order, a quarter of them a wave, and stored: a workgroup per document, key head, 32 sinks and 32 columns
+template <int DH>
+__global__ void __launch_bounds__(AT_THREADS) window_sinks_join(WindowArgs a, const bf16* __restrict__ d_o, const float* __restrict__ dsum, bf16* __restrict__ dqkv,
+                                                                SinkParts sp) {
+  constexpr int DT = DH / 32;
+  __shared__ __attribute__((aligned(16))) float sums[3][16 * WAVE];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
+  const int n_kv = a.B * a.H_kv, unit = blockIdx.x / (2 * DT), n = blockIdx.x - unit * 2 * DT, group = unit / n_kv, bk = unit - group * n_kv, b = bk / a.H_kv,
+            hk = bk - b * a.H_kv;
+  const int rows = document_rows(a.lengths, b, a.S), ld = (a.H + 2 * a.H_kv) * DH, sinks = rows <= a.w.window ? 0 : min(a.w.sinks, rows);
+  if (32 * group >= sinks) return;
+  const int per = (sp.parts + 3) / 4, first = wave * per, end = min(first + per, sp.parts);
+  f32x16 v[1];
+  plain::clear(v);
+  for (int p0 = first; p0 < end; p0 += 4) {   // four parts at a time; those behind the last one count as zero
+    float4 w[4][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        w[i][g] = *reinterpret_cast<const float4*>(sp.at<DH>(dqkv, b, a.S, a.H, ld, hk, group, min(p0 + i, end - 1), ((n * 4 + g) * WAVE + lane) * 4));
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (p0 + i < end) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) { v[0][4 * g] += w[i][g].x; v[0][4 * g + 1] += w[i][g].y; v[0][4 * g + 2] += w[i][g].z; v[0][4 * g + 3] += w[i][g].w; }
+      }
   }
+  if (wave > 0) hand_over(v, sums[wave - 1], lane);
+  __syncthreads();
+  if (wave > 0) return;
+#pragma unroll
+  for (int w = 0; w < 3; ++w) take_over(v, sums[w], 1.f, 1.f, lane);
+  const int key = 32 * group + (lane & 31);
+  if (__any(key < sinks && plain::not_finite(v))) {
+    f32x16 dk[DT], dv[DT];
+    plain::clear(dk);
+    plain::clear(dv);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) { dk[dt][0] = INFINITY; dv[dt][0] = INFINITY; }   // whatever it held: formed anew
+    keys_if_not_finite<DH>(dk, dv, a, d_o, dsum, b, hk, key, rows - 1, rows, h);
+#pragma unroll
+    for (int dt = 0; dt < 2 * DT; ++dt)
+      if (dt == n) v[0] = dt < DT ? dk[dt < DT ? dt : 0] : dv[dt < DT ? 0 : dt - DT];
+  }
+  if (key >= sinks) return;
+  bf16* const out = dqkv + ((long)b * a.S + key) * ld + (a.H + hk + (n < DT ? 0 : a.H_kv)) * DH + 32 * (n < DT ? n : n - DT);
+#pragma unroll
+  for (int g = 0; g < 4; ++g) store4(out + 8 * g + 4 * h, v[0], g, n < DT ? score_scale<DH>() : 1.0f);
 }
 
 // One launch: the sinks' workgroups, which take longest, then those of dK / dV, then dQ's
@@ -358,18 +458,26 @@ __global__ void __launch_bounds__(AT_THREADS, 2) window_bwd_mfma(WindowArgs a, c
   int i = blockIdx.x;
   if (i < sink_blocks * n_kv) {
     const int s = i / n_kv, bk = i - s * n_kv, b = bk / a.H_kv;
-    window_dkv<DH, true>(a, d_o, dsum, dqkv, b, bk - b * a.H_kv, 32 * s, wb_smem);
+    window_dkv<DH, SINKS_WHOLE>(a, d_o, dsum, dqkv, b, bk - b * a.H_kv, 32 * s, wb_smem, SinkParts{}, 0);
     return;
   }
   i -= sink_blocks * n_kv;
   if (i < n_kv * nb) {
     const int kb = i / n_kv, bk = i - kb * n_kv, b = bk / a.H_kv;
-    window_dkv<DH, false>(a, d_o, dsum, dqkv, b, bk - b * a.H_kv, 128 * kb, wb_smem);
+    window_dkv<DH, KEYS>(a, d_o, dsum, dqkv, b, bk - b * a.H_kv, 128 * kb, wb_smem, SinkParts{}, 0);
     return;
   }
   i -= n_kv * nb;
   const int n_bh = a.B * a.H, qb = i / n_bh;
   window_dq<DH>(a, d_o, dsum, dqkv, i - qb * n_bh, nb - 1 - qb, wb_smem);
+}
+
+template <int DH>
+__global__ void __launch_bounds__(AT_THREADS, 2) window_sink_parts(WindowArgs a, const bf16* __restrict__ d_o, const float* __restrict__ dsum, bf16* __restrict__ dqkv,
+                                                                   SinkParts sp) {
+  extern __shared__ __attribute__((aligned(16))) char wp_smem[];
+  const int n_kv = a.B * a.H_kv, s = blockIdx.x / n_kv, bk = blockIdx.x - s * n_kv, b = bk / a.H_kv, group = s / sp.parts;
+  window_dkv<DH, SINKS_PART>(a, d_o, dsum, dqkv, b, bk - b * a.H_kv, 32 * group, wp_smem, sp, s - group * sp.parts);
 }
 
 }  // namespace
@@ -396,9 +504,26 @@ dipaco_status launch_window_bwd_mfma(const bf16* qkv, const int* lengths, const 
   static std::atomic<unsigned long long> lds_set{0};
   if (dipaco_status st = ensure_dynamic_lds(reinterpret_cast<const void*>(window_bwd_mfma<DH>), LDS, lds_set)) return st;
   const WindowArgs a{qkv, lengths, B, S, H, H_kv, w};
-  const int nb = (S + 127) / 128, sink_blocks = w.window >= S ? 0 : (std::min(w.sinks, S) + 31) / 32;
+  const int nb = (S + 127) / 128, G = H / H_kv;
+  int sink_blocks = w.window >= S ? 0 : (std::min(w.sinks, S) + 31) / 32;
+  // Parts of the sinks' queries, of 16 stages each or as many as the rows hold, where a workgroup that took them all would outlast the rest of the launch,
+  // 512 workgroups at a time, by more than the two launches cost.  us whole | cut: the two of window_dkv; 4 x 8000 positions, 16 heads of 128 on 4, window
+  // 1000, 16 sinks (1.7 times the rest) 1069 | 1098; 16384, 14 of 64, window 1024 (1.9 times) 299 | 281; 2048, 14 of 64, window 256 (26 stages more) 41.5 | 49.
+  SinkParts sp{sink_blocks, 1, (128 + H - 1) / H};
+  const int64_t stages = (int64_t)G * ((S + 63) / 64), rest = (int64_t)2 * B * H * nb * ((w.window + 128) / 64 + 1) / 512;
+  if (sink_blocks && stages > rest + 40 && 10 * stages > 18 * rest)
+    sp.parts = (int)std::min<int64_t>(stages / 16, S / ((int64_t)H_kv * sink_blocks * sp.rows));
   window_stats_mfma<DH><<<B * H * nb, AT_THREADS, 0, s>>>(a, o, d_o, lse, dsum);
   DIPACO_LAUNCH_CHECK();
+  if (sink_blocks && sp.parts > 1) {
+    static std::atomic<unsigned long long> parts_lds{0};
+    if (dipaco_status st = ensure_dynamic_lds(reinterpret_cast<const void*>(window_sink_parts<DH>), LDS, parts_lds)) return st;
+    window_sink_parts<DH><<<B * H_kv * sink_blocks * sp.parts, AT_THREADS, LDS, s>>>(a, d_o, dsum, dqkv, sp);
+    DIPACO_LAUNCH_CHECK();
+    window_sinks_join<DH><<<B * H_kv * sink_blocks * (DH / 16), AT_THREADS, 0, s>>>(a, d_o, dsum, dqkv, sp);
+    DIPACO_LAUNCH_CHECK();
+    sink_blocks = 0;
+  }
   window_bwd_mfma<DH><<<B * H_kv * (sink_blocks + nb) + B * H * nb, AT_THREADS, LDS, s>>>(a, d_o, dsum, dqkv, sink_blocks);
   DIPACO_LAUNCH_CHECK();
   return DIPACO_OK;

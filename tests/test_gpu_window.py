@@ -111,6 +111,14 @@ def test_padded_batches(dtype, dh, S, lengths, window, sinks):
 
 
 @pytest.mark.parametrize("dtype", [dp.F32, dp.BF16])
+@pytest.mark.parametrize("B,S,H,Hkv,dh,window,sinks,lengths", [(1, 1700, 1, 1, 64, 100, 5, None), (2, 1000, 8, 2, 32, 64, 40, [1000, 130]), (1, 1300, 4, 1, 128, 200, 3, None),
+                                                               (3, 900, 6, 2, 64, 33, 33, [900, 20, 500]), (1, 800, 16, 1, 32, 10, 1, None), (1, 600, 8, 1, 64, 1, 600, None)])
+def test_sinks_of_documents_that_are_much_longer_than_the_window(dtype, B, S, H, Hkv, dh, window, sinks, lengths):
+    """the sinks' gradients are sums over all rows behind them, cut into parts where there are many"""
+    check(dtype, B, S, H, Hkv, dh, window, sinks, lengths, seed=13)
+
+
+@pytest.mark.parametrize("dtype", [dp.F32, dp.BF16])
 def test_peaked_rows(dtype):
     """scores of +-60: the running maximum moves by more than an fp32 exponential's range holds in probabilities"""
     check(dtype, 1, 400, 2, 2, 64, 150, 4, seed=9, scale=4.0)
@@ -228,3 +236,23 @@ def test_on_a_stream_of_its_own():
         got = fwd(dtype, x, None, B, S, H, Hkv, dh, 100, 0)
     torch.cuda.synchronize()
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("dtype", [dp.F32, dp.BF16])
+@pytest.mark.parametrize("dh", [32, 128])
+def test_a_value_that_is_not_finite_behind_the_sinks(dtype, dh):
+    """sinks whose gradients are cut into parts: a NaN in a row's gradient reaches the sinks, which the row sees, and its window, nothing else"""
+    S, H, Hkv, window, sinks, at = 900, 8, 1, 40, 3, 500
+    print(f"not finite behind the sinks dtype={dtype} dh={dh}", flush=True)
+    x, g = draw((S, (H + 2 * Hkv) * dh), 23, dtype).to(DEV), draw((S, H * dh), 24, dtype).to(DEV)
+    o, lse = fwd(dtype, x, None, 1, S, H, Hkv, dh, window, sinks)
+    clean = bwd(dtype, x, None, o, g, lse, 1, S, H, Hkv, dh, window, sinks)[:, H * dh:]
+    g[at, 0] = float("nan")
+    d = bwd(dtype, x, None, o, g, lse, 1, S, H, Hkv, dh, window, sinks)
+    reached = ref.sees(0, S, S, window, sinks)[at].to(DEV)
+    keys = d[:, H * dh:]
+    assert bool(torch.isnan(keys[reached][:, :Hkv * dh]).all()) and bool(torch.isnan(keys[reached][:, Hkv * dh]).all())
+    assert bool(torch.isnan(d[at, :dh]).all()) and int(torch.isnan(d[:, :H * dh]).sum()) == dh
+    tol = 16 * ref.half_step(TDT[dtype])
+    rest = (keys[~reached].double() - clean[~reached].double()).abs()
+    assert bool((rest <= tol * clean[~reached].double().abs().amax(1, keepdim=True) + 1e-4).all())
