@@ -79,8 +79,8 @@ __global__ void __launch_bounds__(AT_THREADS, DH == 128 ? 2 : 3) window_fwd_mfma
   }
 }
 
-// ---- backward: D = rowsum(dO * O) and -lse log2(e) of every row, in rows padded to whole blocks of 128 -----------------------------
-// Behind a document D is 0 and -lse log2(e) is -inf (probability 0), so that the blocks below need no bounds check.
+// ---- backward: -D = -rowsum(dO * O) and -lse log2(e) of every row, in rows padded to whole blocks of 128 -----------------------------
+// -D is what the products dO.V^T start from: the subtraction costs nothing.  Behind a document D is 0 and -lse log2(e) is -inf (probability 0), so that the blocks below need no bounds check.
 template <int DH>
 __global__ void __launch_bounds__(AT_THREADS) window_stats_mfma(WindowArgs a, const bf16* __restrict__ o, const bf16* __restrict__ d_o,
                                                                const float* __restrict__ lse, float* __restrict__ dsum) {
@@ -103,7 +103,7 @@ __global__ void __launch_bounds__(AT_THREADS) window_stats_mfma(WindowArgs a, co
 #pragma unroll
     for (int m = 1; m < LANES; m <<= 1) D += __shfl_xor(D, m, WAVE);
     if (threadIdx.x % LANES == 0) {
-      dsum[bh * Sp + q] = D;
+      dsum[bh * Sp + q] = -D;
       dsum[(n_bh + bh) * Sp + q] = q < rows ? -lse[(long)bh * a.S + q] * LOG2E : -INFINITY;
     }
   }
@@ -142,7 +142,7 @@ template <int DH> __device__ __forceinline__ void window_dq(const WindowArgs& a,
       qf[ks] = q < rows ? *reinterpret_cast<const uint4*>(qrow + 8 * (2 * ks + h)) : make_uint4(0, 0, 0, 0);
       gf[ks] = q < rows ? *reinterpret_cast<const uint4*>(grow + 8 * (2 * ks + h)) : make_uint4(0, 0, 0, 0);
     }
-    const float D = dsum[bh * Sp + q], nlse2 = dsum[((long)a.B * a.H + bh) * Sp + q];
+    const float neg_d = dsum[bh * Sp + q], nlse2 = dsum[((long)a.B * a.H + bh) * Sp + q];
     const FragOff fo = frag_offsets(lane);
     const TrOff to = tr_offsets(lane);
     const uint32_t smem_addr = (uint32_t)(uintptr_t)smem;
@@ -150,6 +150,9 @@ template <int DH> __device__ __forceinline__ void window_dq(const WindowArgs& a,
     const RowTiles<DH> src(k, k + a.H_kv * DH, ld, ld, rows, wave, lane);
     const TileList<6> tiles(a.w, q0, min(q0 + 127, rows - 1));
     src.issue(tiles.at(0), wave, lane, smem_addr);
+    f32x16 start;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) start[e] = neg_d;
     for (int t = 0, cur = 0; t < tiles.count; ++t, cur ^= 1) {
       wait_vmcnt<0>();
       __syncthreads();   // tile t is in LDS, and nobody still reads the other stage
@@ -161,8 +164,8 @@ template <int DH> __device__ __forceinline__ void window_dq(const WindowArgs& a,
       for (int half = 0; half < 2; ++half) {
         const int seen = seen_half(a.w, span, k0 + 32 * half);
         if (!seen) continue;   // wave-uniform
-        f32x16 st, dp;
-        zero(st); zero(dp);
+        f32x16 st, dp = start;
+        zero(st);
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
           st = mfma16(row_frag(k_, fo, ks, half), qf[ks], st);
@@ -170,7 +173,7 @@ template <int DH> __device__ __forceinline__ void window_dq(const WindowArgs& a,
         }
 #pragma unroll
         for (int e = 0; e < 16; ++e)   // dS^T without the factor 1 / sqrt(d_head), which dQ gets when it is stored
-          st[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[e], sc, nlse2)) * (dp[e] - D);
+          st[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[e], sc, nlse2)) * dp[e];
         hide(st, seen, 0.f, k0 + 32 * half, q, near, a.w.sinks, lane);
         mma_transposed_half(dq, k_ + 4096 * half, to, st);
       }
@@ -181,7 +184,7 @@ template <int DH> __device__ __forceinline__ void window_dq(const WindowArgs& a,
 #pragma unroll 1
       for (int t = 0; t < vis.count; ++t) {
         const bf16* kr = k + (long)vis.at(t) * ld;
-        plain::add_row(dq, __builtin_amdgcn_exp2f(__builtin_fmaf(plain::dot<DH>(qrow, kr), sc, nlse2)) * (plain::dot<DH>(grow, kr + a.H_kv * DH) - D), kr, h);
+        plain::add_row(dq, __builtin_amdgcn_exp2f(__builtin_fmaf(plain::dot<DH>(qrow, kr), sc, nlse2)) * (plain::dot<DH>(grow, kr + a.H_kv * DH) + neg_d), kr, h);
       }
     }
   }
@@ -200,7 +203,7 @@ template <int DH> __device__ __forceinline__ void window_dq(const WindowArgs& a,
 // Where that would still be the longest by far, the queries are cut among `parts` workgroups, whose sums lie in the rows of dqkv that dQ is
 // written to afterwards (SinkParts), and window_sinks_join adds them.  1 x 32768 positions, 16 heads of 128 on 4, window 1024, 16 sinks: 2995 us
 // uncut (without sinks 1098), 1150 cut; 8 heads of 64 on 1, 8192 positions, window 512, 4 sinks 819 | 180.
-template <int DH> constexpr int window_dkv_stage() { return 2 * tile_bytes<DH>() + 2 * 64 * (int)sizeof(float); }   // Q | dO | -lse log2(e) | D
+template <int DH> constexpr int window_dkv_stage() { return 2 * tile_bytes<DH>() + 2 * 64 * (int)sizeof(float); }   // Q | dO | -lse log2(e) | -D
 
 // where a wave's sums of its keys (a lane pair each) are not finite: the pairs that see each other alone
 template <int DH>
@@ -216,15 +219,15 @@ __device__ __forceinline__ void keys_if_not_finite(f32x16 (&dk)[DH / 32], f32x16
   plain::clear(dv);
 #pragma unroll 1
   for (int g = 0; g < G; ++g) {
-    const float* const D = dsum + (long)(b * a.H + hk * G + g) * Sp;
-    const float* const L = D + (long)a.B * a.H * Sp;
+    const float* const neg_d = dsum + (long)(b * a.H + hk * G + g) * Sp;
+    const float* const L = neg_d + (long)a.B * a.H * Sp;
 #pragma unroll 1
     for (int i = key; i <= key_last; ++i) {
       const bf16* qr = base + (long)i * ld + (hk * G + g) * DH;
       const bf16* gr = d_o + (((long)b * a.S + i) * a.H + hk * G + g) * DH;
       const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(plain::dot<DH>(qr, krow), sc, L[i]));
       plain::add_row(dv, p, gr, h);
-      plain::add_row(dk, p * (plain::dot<DH>(gr, krow + a.H_kv * DH) - D[i]), qr, h);
+      plain::add_row(dk, p * (plain::dot<DH>(gr, krow + a.H_kv * DH) + neg_d[i]), qr, h);
     }
   }
 }
@@ -289,7 +292,7 @@ __device__ __forceinline__ void window_dkv(const WindowArgs& a, const bf16* __re
     const int head1 = done / n_tiles;    // the first step's head and tile
     const int head0 = b * a.H + hk * G;
     RowTiles<DH, true> src(base + hk * G * DH, d_o + ((long)b * a.S * a.H + hk * G) * DH, ld, a.H * DH, rows, wave, lane);
-    // statistics of a tile's 64 queries: waves 0 and 2 fetch -lse log2(e), waves 1 and 3 fetch D
+    // statistics of a tile's 64 queries: waves 0 and 2 fetch -lse log2(e), waves 1 and 3 fetch -D
     const float* stat = dsum + ((wave & 1 ? 0 : (long)a.B * a.H) + head0) * Sp + lane;
     const uint32_t stat_dst = 2 * TILE_BYTES + (wave & 1 ? 256 : 0);
     int next_tile = first + done - head1 * n_tiles;
@@ -317,37 +320,42 @@ __device__ __forceinline__ void window_dkv(const WindowArgs& a, const bf16* __re
       const char* q_ = smem + cur * STAGE;
       const char* g_ = q_ + TILE_BYTES;
       const float* nlse2s = reinterpret_cast<const float*>(q_ + 2 * TILE_BYTES);
-      const float* Ds = nlse2s + 64;
+      const float* neg_ds = nlse2s + 64;
 #pragma unroll
       for (int i = 0; i < (SINKS ? 1 : 2); ++i) {
         const int t = SINKS ? wave & 1 : i, qh = q0 + 32 * t;   // 32 queries
         if (idle || qh + 31 < kw0 || qh > last) continue;       // wave-uniform
         if constexpr (DH == 128) rederive_offsets(fo, to);
-        f32x16 st, dp;
-        zero(st); zero(dp);
         const bool want_v = !SINKS || wave < 2, want_k = !SINKS || wave >= 2;
+        // accumulator elements 4g .. 4g + 3 are queries 8g + 4h + (0..3) of the half: their statistics are 16 contiguous bytes
+        f32x16 st, dp;
+        zero(st);
         if (want_k) {
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const float4 d = *reinterpret_cast<const float4*>(neg_ds + 32 * t + 8 * g + 4 * h);
+            dp[4 * g] = d.x; dp[4 * g + 1] = d.y; dp[4 * g + 2] = d.z; dp[4 * g + 3] = d.w;
+          }
 #pragma unroll
           for (int ks = 0; ks < KS; ++ks) {
             st = mfma16(row_frag(q_ + 4096 * t, fo, ks, 0), kf[ks], st);
             dp = mfma16(row_frag(g_ + 4096 * t, fo, ks, 0), vf[ks], dp);
           }
         } else {
+          zero(dp);
 #pragma unroll
           for (int ks = 0; ks < KS; ++ks) st = mfma16(row_frag(q_ + 4096 * t, fo, ks, 0), kf[ks], st);
         }
-        // accumulator elements 4g .. 4g + 3 are queries 8g + 4h + (0..3) of the half: their statistics are 16 contiguous bytes
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
           const float4 Lq = *reinterpret_cast<const float4*>(nlse2s + 32 * t + 8 * g + 4 * h);
-          const float4 Dv = *reinterpret_cast<const float4*>(Ds + 32 * t + 8 * g + 4 * h);
-          const float Ls[4] = {Lq.x, Lq.y, Lq.z, Lq.w}, Dd[4] = {Dv.x, Dv.y, Dv.z, Dv.w};
+          const float Ls[4] = {Lq.x, Lq.y, Lq.z, Lq.w};
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             const int e = 4 * g + j;
             const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(st[e], sc, Ls[j]));
             st[e] = p;
-            dp[e] = p * (dp[e] - Dd[j]);   // dS without 1 / sqrt(d_head), which dK gets when it is stored
+            dp[e] *= p;   // dS without 1 / sqrt(d_head), which dK gets when it is stored
           }
         }
         if (qh < kw0 + 31 || (!SINKS && qh + 31 > kw0 + a.w.window - 1)) {   // wave-uniform: some pair is hidden
