@@ -23,8 +23,7 @@ __global__ void __launch_bounds__(256) cache_append_rows(PagedArgs<T> a, int dh)
   const int b = find_document(a.row_start, a.B, row, lane);
   const RowRange r = ragged_rows(a.row_start, b, a.T_rows);
   if (row < r.first || row >= r.first + r.count) return;   // behind the last document
-  const int pos = max(a.cache_len[b], 0) + row - r.first;
-  const int page = pos < 0 ? -1 : a.page_of(b, pos);
+  const int pos = a.cached(b) + row - r.first, page = a.page_of(b, pos);
   if (page < 0) return;
   const int slot = pos & ((1 << a.page_shift) - 1), vecs = 2 * a.H_kv * dh / VEC, head = dh / VEC;
   const uint4* const from = reinterpret_cast<const uint4*>(a.qkv + (long)row * (a.H + 2 * a.H_kv) * dh + (long)a.H * dh);

@@ -76,7 +76,7 @@ __global__ void __launch_bounds__(WF_THREADS, NARROW && DH == 128 ? 1 : 2) paged
       __syncthreads();
       if constexpr (NARROW) {
         const int s = (mine >> wave) & 1 ? F_NONE : seen_16(a.w, span, k0 + 16 * wave);
-        if (s != F_NONE) attend_16<DH, 1>(x, qf, k_, v_, wave, k0 + 16 * wave, beyond || s != F_ALL, 0, min(pos, blk.last), near, a.w.sinks, m, g);
+        if (s != F_NONE) attend_16<DH>(x, qf, k_, v_, wave, k0 + 16 * wave, beyond || s != F_ALL, min(pos, blk.last), near, a.w.sinks, m, g);
       } else {
         attend_32<DH>(x, qf, k_, v_, k0, mine, a.w, span, beyond, min(pos, blk.last), near, m, g);
       }

@@ -259,7 +259,7 @@ template <int DH, int NW, int NS> __device__ __forceinline__ void narrow_documen
       const int s = holes == 3 ? 0 : seen_half(a.w, span, k0);
       const char* k_ = ring + (t % NS) * STAGE;
       if (s)
-        attend_half<DH, 1>(x, qf, k_, k_ + 4096, fo, to, k0, s | (blk.hi > at.last ? UPPER | LOWER : 0), holes, min(row.pos, at.last), row.near, a.w.sinks, lane);
+        attend_half<DH>(x, qf, k_, k_ + 4096, fo, to, k0, s | (blk.hi > at.last ? UPPER | LOWER : 0), holes, min(row.pos, at.last), row.near, a.w.sinks, lane);
       asm volatile("" ::: "memory");
       if (t + NS < n) issue(t + NS);
     }

@@ -10,9 +10,6 @@ namespace dipaco {
 struct Window {
   int window, sinks;   // window >= 1, sinks >= 0
   __host__ __device__ __forceinline__ int near_from(int i) const { return i >= window ? i - window + 1 : 0; }   // first position of i's window
-  __device__ __forceinline__ bool sees(int i, int j) const { return j <= i && (i - j < window || j < sinks); }
-  // last of n positions that sees position j
-  __device__ __forceinline__ int last_seer(int j, int n) const { return j < sinks || n - j <= window ? n - 1 : j + window - 1; }
 };
 // the positions that i sees, in order
 struct VisibleList {

@@ -62,25 +62,20 @@ template <int DH> struct FSoftmaxRow {
     l = 0.f;
   }
 };
-// N runs of 16 keys, from run t of the tile k_ (v_) on; k0: the position of run t
-template <int DH, int N>
-__device__ __forceinline__ void attend_16(FSoftmaxRow<DH>& x, const RowFrag<DH>& qf, const float* k_, const float* v_, int t, int k0, bool masked, int holes,
-                                          int pos, int near, int sinks, int m, int g) {
+// 16 keys, run t of the tile k_ (v_), from position k0 on
+template <int DH>
+__device__ __forceinline__ void attend_16(FSoftmaxRow<DH>& x, const RowFrag<DH>& qf, const float* k_, const float* v_, int t, int k0, bool masked, int pos,
+                                          int near, int sinks, int m, int g) {
   const float sc = head_scale<DH>() * WF_LOG2E;
-  f32x4 st[N];
-#pragma unroll
-  for (int i = 0; i < N; ++i) st[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-  for (int i = 0; i < N; ++i) rows_product<DH>(st[i], k_, t + i, qf, m, g);
+  f32x4 st = {0.f, 0.f, 0.f, 0.f};
+  rows_product<DH>(st, k_, t, qf, m, g);
   float mx = -INFINITY;
 #pragma unroll
-  for (int i = 0; i < N; ++i)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int key = k0 + 16 * i + 4 * g + e;
-      if (masked && !(key <= pos && (key >= near || key < sinks) && !((holes >> i) & 1))) st[i][e] = -INFINITY;
-      mx = fmaxf(mx, st[i][e]);
-    }
+  for (int e = 0; e < 4; ++e) {
+    const int key = k0 + 4 * g + e;
+    if (masked && !(key <= pos && (key >= near || key < sinks))) st[e] = -INFINITY;
+    mx = fmaxf(mx, st[e]);
+  }
   const float mn = fmaxf(x.m, max_groups(mx) * sc);
   if (__builtin_amdgcn_ballot_w64(mn > x.m + 8.0f) != 0) {   // wave-uniform; the reference may lag by 2^8
     const float corr = mn == x.m ? 1.f : __builtin_amdgcn_exp2f(x.m - mn);
@@ -93,25 +88,19 @@ __device__ __forceinline__ void attend_16(FSoftmaxRow<DH>& x, const RowFrag<DH>&
     x.m_neg = mn == -INFINITY ? 0.f : -mn;
   }
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      st[i][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[i][e], sc, x.m_neg));
-      x.l += st[i][e];
-    }
-    cols_product<DH>(x.o, v_, t + i, st[i], m, g);
+  for (int e = 0; e < 4; ++e) {
+    st[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[e], sc, x.m_neg));
+    x.l += st[e];
   }
+  cols_product<DH>(x.o, v_, t, st, m, g);
 }
-// a tile of 32 keys: both runs in one go where both are seen
+// a tile of 32 keys: the runs that are seen
 template <int DH>
 __device__ __forceinline__ void attend_32(FSoftmaxRow<DH>& x, const RowFrag<DH>& qf, const float* k_, const float* v_, int k0, int holes, const Window& w,
                                           const FRowSpan& span, bool masked, int pos, int near, int m, int g) {
   const int a = holes & 1 ? F_NONE : seen_16(w, span, k0), b = holes & 2 ? F_NONE : seen_16(w, span, k0 + 16);
-  if (a != F_NONE && b != F_NONE) attend_16<DH, 2>(x, qf, k_, v_, 0, k0, masked || a + b != 2 * F_ALL, 0, pos, near, w.sinks, m, g);
-  else if (a != F_NONE || b != F_NONE) {
-    const int t = a != F_NONE ? 0 : 1;
-    attend_16<DH, 1>(x, qf, k_, v_, t, k0 + 16 * t, masked || a + b != F_ALL, 0, pos, near, w.sinks, m, g);
-  }
+  if (a != F_NONE) attend_16<DH>(x, qf, k_, v_, 0, k0, masked || a != F_ALL, pos, near, w.sinks, m, g);
+  if (b != F_NONE) attend_16<DH>(x, qf, k_, v_, 1, k0 + 16, masked || b != F_ALL, pos, near, w.sinks, m, g);
 }
 
 }  // namespace

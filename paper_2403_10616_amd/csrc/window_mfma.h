@@ -23,17 +23,12 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
   return r;
 }
-// The maximum of N score tiles.  The first maximum is the compiler's (median with +inf), which waits for the matrix instructions that wrote
-// the tiles; the others depend on it.
-template <int N> __device__ __forceinline__ float max_of(const f32x16 (&st)[N]) {
-  float mx = __builtin_amdgcn_fmed3f(st[0][0], st[N - 1][15], INFINITY);
-  if constexpr (N == 2) {
+// The maximum of a score tile.  The first maximum is the compiler's (median with +inf), which waits for the matrix instructions that wrote the
+// tile; the others depend on it.
+__device__ __forceinline__ float max_of(const f32x16& st) {
+  float mx = __builtin_amdgcn_fmed3f(st[0], st[15], INFINITY);
 #pragma unroll
-    for (int e = 0; e < 15; ++e) mx = max3(mx, st[0][e + 1], st[1][e]);
-  } else {
-#pragma unroll
-    for (int e = 1; e < 15; e += 2) mx = max3(mx, st[0][e], st[0][e + 1]);
-  }
+  for (int e = 1; e < 15; e += 2) mx = max3(mx, st[e], st[e + 1]);
   return mx;
 }
 
@@ -82,42 +77,33 @@ template <int DH> struct SoftmaxRow {
   }
 };
 
-// NT halves of 32 keys from k0 on, of which the rows see `seen` (a byte each).  k_, v_: the halves' first row in LDS.  holes: bit per 16 keys that nobody sees
-template <int DH, int NT>
+// 32 keys from k0 on, of which the rows see `seen`.  k_, v_: their first row in LDS.  holes: bit per 16 keys that nobody sees.
+// One path for all halves: with another one for two halves at a time the compiler kept two sets of accumulators and copied between them.
+template <int DH>
 __device__ __forceinline__ void attend_half(SoftmaxRow<DH>& x, const uint4 (&qf)[DH / 16], const char* k_, const char* v_, const FragOff& fo, const TrOff& to,
                                             int k0, int seen, int holes, int pos, int near, int sinks, int lane) {
   constexpr int KS = DH / 16, DT = DH / 32;
-  f32x16 st[NT];
-#pragma unroll
-  for (int t = 0; t < NT; ++t) zero(st[t]);
+  f32x16 st;
+  zero(st);
   // Keys are read in one go, and values while the scores are multiplied: left to the compiler the reads trickle in between the products, each
   // with a wait of its own.  16 x 2048 positions of 14 x 64, window 512: 96 us, 101 so.
-  uint4 kf[NT][KS], vf[NT][DT][2];
+  uint4 kf[KS], vf[DT][2];
 #pragma unroll
-  for (int t = 0; t < NT; ++t)
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) kf[t][ks] = row_frag(k_, fo, ks, t);
+  for (int ks = 0; ks < KS; ++ks) kf[ks] = row_frag(k_, fo, ks, 0);
   __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-  for (int ks = 0; ks < KS; ++ks)
+  for (int ks = 0; ks < KS; ++ks) st = mfma16(kf[ks], qf[ks], st);
 #pragma unroll
-    for (int t = 0; t < NT; ++t) st[t] = mfma16(kf[t][ks], qf[ks], st[t]);
+  for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-  for (int t = 0; t < NT; ++t)
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-      for (int i = 0; i < 2; ++i) vf[t][dt][i] = tr_read(v_, to, dt, 2 * t + i);
+    for (int i = 0; i < 2; ++i) vf[dt][i] = tr_read(v_, to, dt, i);
   __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-  for (int t = 0; t < NT; ++t) hide(st[t], seen >> (8 * t), -INFINITY, k0 + 32 * t, pos, near, sinks, lane);
+  hide(st, seen, -INFINITY, k0, pos, near, sinks, lane);
   if (holes) {   // wave-uniform
     asm volatile("");
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-      for (int e = 0; e < 16; ++e)
-        if ((holes >> (2 * t + (e >> 3))) & 1) st[t][e] = -INFINITY;
+    for (int e = 0; e < 16; ++e)
+      if ((holes >> (e >> 3)) & 1) st[e] = -INFINITY;
   }
   const float sc = score_scale<DH>() * LOG2E;
   const float mx = max_over_halves(max_of(st));
@@ -133,29 +119,26 @@ __device__ __forceinline__ void attend_half(SoftmaxRow<DH>& x, const uint4 (&qf)
     x.m = mn;
     x.m_neg = mn == -INFINITY ? 0.f : -mn;
   }
+  float s0 = 0.f, s1 = 0.f;
 #pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    float s0 = 0.f, s1 = 0.f;
+  for (int e = 0; e < 16; ++e) st[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[e], sc, x.m_neg));
 #pragma unroll
-    for (int e = 0; e < 16; ++e) st[t][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[t][e], sc, x.m_neg));
+  for (int e = 0; e < 16; e += 2) { s0 += st[e]; s1 += st[e + 1]; }
+  x.l += s0 + s1;
+  const uint4 p0 = pack8<0>(st), p1 = pack8<8>(st);
 #pragma unroll
-    for (int e = 0; e < 16; e += 2) { s0 += st[t][e]; s1 += st[t][e + 1]; }
-    x.l += s0 + s1;
-    const uint4 p0 = pack8<0>(st[t]), p1 = pack8<8>(st[t]);
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt) {
-      x.o[dt] = mfma16(vf[t][dt][0], p0, x.o[dt]);
-      x.o[dt] = mfma16(vf[t][dt][1], p1, x.o[dt]);
-    }
+  for (int dt = 0; dt < DT; ++dt) {
+    x.o[dt] = mfma16(vf[dt][0], p0, x.o[dt]);
+    x.o[dt] = mfma16(vf[dt][1], p1, x.o[dt]);
   }
 }
-// a tile of 64 keys: both halves in one go where both are seen, else the one that is.  force: bounds to apply whatever the span says
+// a tile of 64 keys: the halves that are seen.  force: bounds to apply whatever the span says
 template <int DH>
 __device__ __forceinline__ void attend_tile(SoftmaxRow<DH>& x, const uint4 (&qf)[DH / 16], const char* k_, const char* v_, const FragOff& fo, const TrOff& to,
                                             int k0, int holes, const Window& w, const RowSpan& span, int force, int pos, int near, int lane) {
   const int a = (holes & 3) == 3 ? 0 : seen_half(w, span, k0), b = holes >> 2 == 3 ? 0 : seen_half(w, span, k0 + 32);
-  if (a) attend_half<DH, 1>(x, qf, k_, v_, fo, to, k0, a | force, holes & 3, pos, near, w.sinks, lane);
-  if (b) attend_half<DH, 1>(x, qf, k_ + 4096, v_ + 4096, fo, to, k0 + 32, b | force, holes >> 2, pos, near, w.sinks, lane);
+  if (a) attend_half<DH>(x, qf, k_, v_, fo, to, k0, a | force, holes & 3, pos, near, w.sinks, lane);
+  if (b) attend_half<DH>(x, qf, k_ + 4096, v_ + 4096, fo, to, k0 + 32, b | force, holes >> 2, pos, near, w.sinks, lane);
 }
 
 // Two operands' rows of one document and head (keys and values; queries and output gradients), ld0 and ld1 elements apart
