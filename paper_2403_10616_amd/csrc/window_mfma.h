@@ -3,8 +3,13 @@
 //
 // Tiles, fragments and the order of contraction are those of attention_mfma.h: S^T = K.Q^T, so that a query's softmax state is a lane's and
 // the probabilities are the next product's operand without leaving registers.  New here is which tiles are read: a workgroup walks
-// the tiles of the sinks, then those of its rows' windows (TileList); a wave takes of each tile the halves of 32 keys that any of
+// the tiles of its rows' windows, then those of the sinks (TileList); a wave takes of each tile the halves of 32 keys that any of
 // its 32 rows sees, and applies the mask only where some pair of the half is hidden.
+//
+// Bound: a half costs a wave 2 DH matrix-core cycles x 4 (DH = 64: 256) and about 80 vector instructions (16 of them exponentials), which a SIMD
+// does not overlap, under a clock that the power limit sets (1.5 - 1.8 GHz).  Forward, us: 16 x 2048 positions, 14 heads of 64, window 512, 4 sinks 100
+// (530 TFLOP/s of visible pairs), window 2048 160; 2 x up to 32768, 16 heads of 128 on 4, window 4096 1750 (950); 8 x 2048, 8 heads of 128, causal 90
+// (attention_mfma.h: 112).
 //
 // Probabilities are rounded to bf16 where the second product multiplies them (2^-8 of each, the size of the output's own rounding);
 // their sum is taken in fp32 before that, so that lse keeps fp32's digits.
