@@ -163,7 +163,7 @@ struct FSinkParts {
     return dqkv + ((long)b * S + row) * ld + f % per_row;
   }
 };
-enum { F_KEYS = 0, F_SINKS_WHOLE = 1, F_SINKS_PART = 2 };
+enum { F_KEYS = 0, F_SINKS_WHOLE = 1, F_SINKS_PART = 2, F_KEYS_SHARED = 3 };
 
 // where a wave's sums of its keys (four lanes each) are not finite: the pairs that see each other alone
 template <int DH>
@@ -201,30 +201,33 @@ __device__ __forceinline__ void store_keys(f32x4 (&dk)[DH / 16], f32x4 (&dv)[DH 
 }
 
 // dK and dV: 64 keys of a key head over the queries that see them under the window alone; or 16 sinks over all queries behind them, the
-// waves two and two on the halves of a stage, for dV and for dK, whole or in parts (attention_window_mfma.hip)
+// waves two and two on the halves of a stage, for dV and for dK, whole or in parts (attention_window_mfma.hip).  Fewer blocks of keys than compute units
+// are taken 16 keys a workgroup too, us: 1 x 2000, 8 heads of 64 on 2, causal (64 blocks) 737 -> 383; 1 x 4096, 8 on 2, window 512 (128) 273 -> 205; 2 x 1000, 8
+// heads, causal (256) 133 | 133; 1 x 2048, 14 heads, window 256 (448) 106 -> 127.
 template <int DH, int KIND>
 __device__ __forceinline__ void window_dkv_f32(const FWindowArgs& a, const float* __restrict__ d_o, const float* __restrict__ dsum, float* __restrict__ dqkv, int b,
                                                int hk, int k0, float* smem, const FSinkParts& sp, int part) {
-  constexpr bool SINKS = KIND != F_KEYS;
+  constexpr bool SINKS = KIND == F_SINKS_WHOLE || KIND == F_SINKS_PART, SHARED = KIND != F_KEYS;   // SHARED: the waves share 16 keys
+  constexpr int BLOCK = SHARED ? 16 : WF_ROWS;
   constexpr int STAGE = wf_stage<DH>();
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
   const int rows = document_rows(a.lengths, b, a.S), G = a.H / a.H_kv;
   const int sinks = rows <= a.w.window ? 0 : min(a.w.sinks, rows);   // a window that covers the document leaves the sinks nothing of their own
   if (SINKS && k0 >= sinks) return;
   const long ld = (long)(a.H + 2 * a.H_kv) * DH, Sp = (a.S + 127) / 128 * 128L;
-  const int kw0 = k0 + (SINKS ? 0 : 16 * wave), key = kw0 + m, head0 = b * a.H + hk * G;
+  const int kw0 = k0 + (SHARED ? 0 : 16 * wave), key = kw0 + m, head0 = b * a.H + hk * G;
   const float* const base = a.qkv + (long)b * a.S * ld;
   const float* const krow = base + key * ld + (a.H + hk) * DH;
   const int last = SINKS ? rows - 1 : min(rows - 1, kw0 + 15 + a.w.window - 1), key_last = SINKS ? rows - 1 : min(rows - 1, key + a.w.window - 1);
   const bool idle = kw0 >= rows || (!SINKS && kw0 + 15 < sinks);
-  const bool want_v = !SINKS || wave < 2, want_k = !SINKS || wave >= 2;
+  const bool want_v = !SHARED || wave < 2, want_k = !SHARED || wave >= 2;
   const float sc = head_scale<DH>() * WF_LOG2E;
   f32x4 dk[DH / 16], dv[DH / 16];
   zero_acc<DH>(dk);
   zero_acc<DH>(dv);
-  if (k0 < rows && (SINKS || k0 + WF_ROWS - 1 >= sinks)) {
+  if (k0 < rows && (SINKS || k0 + BLOCK - 1 >= sinks)) {
     const RowFrag<DH> kf = load_row<DH>(krow, g, key < rows), vf = load_row<DH>(krow + a.H_kv * DH, g, key < rows);
-    const int block_last = SINKS ? rows - 1 : min(rows - 1, k0 + WF_ROWS - 1 + a.w.window - 1);
+    const int block_last = SINKS ? rows - 1 : min(rows - 1, k0 + BLOCK - 1 + a.w.window - 1);
     const int first = k0 >> 5, n_tiles = (block_last >> 5) + 1 - first;
     int steps = G * n_tiles, done = 0;   // steps of the parts in front of this one
     if constexpr (KIND == F_SINKS_PART) {
@@ -265,8 +268,8 @@ __device__ __forceinline__ void window_dkv_f32(const FWindowArgs& a, const float
       const int q0 = qt * 32;
       if (++qt == first + n_tiles) qt = first;
 #pragma unroll
-      for (int i = 0; i < (SINKS ? 1 : 2); ++i) {
-        const int t = SINKS ? wave & 1 : i, qh = q0 + 16 * t;
+      for (int i = 0; i < (SHARED ? 1 : 2); ++i) {
+        const int t = SHARED ? wave & 1 : i, qh = q0 + 16 * t;
         if (idle || qh + 15 < kw0 || qh > last) continue;   // wave-uniform
         f32x4 st = {0.f, 0.f, 0.f, 0.f}, dp = {0.f, 0.f, 0.f, 0.f};
         rows_product<DH>(st, q_, t, kf, m, g);
@@ -285,7 +288,7 @@ __device__ __forceinline__ void window_dkv_f32(const FWindowArgs& a, const float
       }
       if (more) store(smem + ((n + 1) & 1) * STAGE);
     }
-    if constexpr (SINKS) {   // waves 1 and 3 hand their half of the queries over; then wave 2 its dK to wave 0
+    if constexpr (SHARED) {   // waves 1 and 3 hand their half of the queries over; then wave 2 its dK to wave 0
       constexpr int PER = DH / 16 * 4 * WAVE;
       static_assert(3 * PER <= 2 * STAGE, "the sums fit in the stages");
       auto put = [&](const f32x4 (&v)[DH / 16], float* at) {
@@ -321,6 +324,7 @@ __device__ __forceinline__ void window_dkv_f32(const FWindowArgs& a, const float
     }
     keys_if_not_finite<DH>(dk, dv, a, d_o, dsum, b, hk, key, key_last, rows, g);
   }
+  if (SHARED && wave != 0) return;   // blocks behind the document
   if (key >= a.S || (SINKS ? key >= sinks : key < sinks)) return;
   store_keys<DH>(dk, dv, a, dqkv, b, hk, key, key < rows, g);
 }
@@ -383,7 +387,7 @@ __global__ void __launch_bounds__(WF_THREADS, 2) window_sink_parts_f32(FWindowAr
 // One launch: the sinks' workgroups, which take longest, then those of dK / dV, then dQ's
 template <int DH>
 __global__ void __launch_bounds__(WF_THREADS, 2) window_bwd_f32(FWindowArgs a, const float* __restrict__ d_o, const float* __restrict__ dsum,
-                                                                float* __restrict__ dqkv, int sink_blocks) {
+                                                                float* __restrict__ dqkv, int sink_blocks, bool shared) {
   extern __shared__ __attribute__((aligned(16))) float wbf_smem[];
   const int n_kv = a.B * a.H_kv, nb = (a.S + WF_ROWS - 1) / WF_ROWS;
   int i = blockIdx.x;
@@ -393,12 +397,14 @@ __global__ void __launch_bounds__(WF_THREADS, 2) window_bwd_f32(FWindowArgs a, c
     return;
   }
   i -= sink_blocks * n_kv;
-  if (i < n_kv * nb) {
+  const int key_blocks = shared ? 4 * nb : nb;
+  if (i < n_kv * key_blocks) {
     const int kb = i / n_kv, bk = i - kb * n_kv, b = bk / a.H_kv;
-    window_dkv_f32<DH, F_KEYS>(a, d_o, dsum, dqkv, b, bk - b * a.H_kv, WF_ROWS * kb, wbf_smem, FSinkParts{}, 0);
+    if (shared) window_dkv_f32<DH, F_KEYS_SHARED>(a, d_o, dsum, dqkv, b, bk - b * a.H_kv, 16 * kb, wbf_smem, FSinkParts{}, 0);
+    else window_dkv_f32<DH, F_KEYS>(a, d_o, dsum, dqkv, b, bk - b * a.H_kv, WF_ROWS * kb, wbf_smem, FSinkParts{}, 0);
     return;
   }
-  i -= n_kv * nb;
+  i -= n_kv * key_blocks;
   const int n_bh = a.B * a.H, qb = i / n_bh;
   window_dq_f32<DH>(a, d_o, dsum, dqkv, i - qb * n_bh, nb - 1 - qb, wbf_smem);
 }
@@ -437,7 +443,8 @@ dipaco_status launch_window_bwd_f32(const float* qkv, const int* lengths, const 
     DIPACO_LAUNCH_CHECK();
     sink_blocks = 0;
   }
-  window_bwd_f32<DH><<<B * H_kv * (sink_blocks + nb) + B * H * nb, WF_THREADS, LDS, s>>>(a, d_o, dsum, dqkv, sink_blocks);
+  const bool shared = (int64_t)B * H_kv * nb < 256;   // F_KEYS_SHARED: fewer workgroups than compute units
+  window_bwd_f32<DH><<<B * H_kv * (sink_blocks + (shared ? 4 : 1) * nb) + B * H * nb, WF_THREADS, LDS, s>>>(a, d_o, dsum, dqkv, sink_blocks, shared);
   DIPACO_LAUNCH_CHECK();
   return DIPACO_OK;
 }

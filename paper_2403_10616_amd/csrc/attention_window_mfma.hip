@@ -22,11 +22,14 @@ struct WindowArgs {
 
 // ---- forward -----------------------------------------------------------------------------------------------------
 // A workgroup per 128 queries of a head, the last ones first: under a window that covers the document these are the longest
-template <int DH>
-__global__ void __launch_bounds__(AT_THREADS, DH == 128 ? 2 : 3) window_fwd_mfma(WindowArgs a, bf16* __restrict__ o, float* __restrict__ lse) {
-  constexpr int KS = DH / 16, TILE_BYTES = tile_bytes<DH>();
-  extern __shared__ __attribute__((aligned(16))) char wf_smem[];   // [stage][K | V]
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, h = lane >> 5;
+// NG = 2: two groups of four waves take the block's tiles in turn, each in stages of its own, and their sums meet in LDS.
+template <int DH, int NG>
+__global__ void __launch_bounds__(AT_THREADS * NG, NG == 2 || DH == 128 ? 2 : 3) window_fwd_mfma(WindowArgs a, bf16* __restrict__ o, float* __restrict__ lse) {
+  constexpr int KS = DH / 16, DT = DH / 32, TILE_BYTES = tile_bytes<DH>();
+  extern __shared__ __attribute__((aligned(16))) char wf_rings[];   // [group][stage][K | V]
+  const int lane = threadIdx.x & 63, wave_all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, h = lane >> 5;
+  const int grp = NG == 1 ? 0 : wave_all >> 2, wave = wave_all & 3;
+  char* const wf_smem = wf_rings + grp * 4 * TILE_BYTES;
   const int n_bh = a.B * a.H, qb = (int)blockIdx.x / n_bh, bh = (int)blockIdx.x - qb * n_bh, b = bh / a.H, hd = bh - b * a.H, hk = hd / (a.H / a.H_kv);
   const int q0 = ((a.S + 127) / 128 - 1 - qb) * 128, q = q0 + 32 * wave + r;
   const int rows = document_rows(a.lengths, b, a.S), ld = (a.H + 2 * a.H_kv) * DH;
@@ -47,18 +50,38 @@ __global__ void __launch_bounds__(AT_THREADS, DH == 128 ? 2 : 3) window_fwd_mfma
     const bf16* const k = base + (a.H + hk) * DH;
     const RowTiles<DH> src(k, k + a.H_kv * DH, ld, ld, rows, wave, lane);
     const TileList<6> tiles(a.w, q0, min(q0 + 127, rows - 1));
-    src.issue(tiles.at(0), wave, lane, smem_addr);
+    if (grp < tiles.count) src.issue(tiles.at(grp), wave, lane, smem_addr);
     auto tile = [&](auto CUR, int t) {
       constexpr int cur = decltype(CUR)::value;
       wait_vmcnt<0>();
       __syncthreads();   // tile t is in LDS, and nobody still reads the other stage
-      if (t + 1 < tiles.count) src.issue(tiles.at(t + 1), wave, lane, smem_addr + (1 - cur) * 2 * TILE_BYTES);
+      if (t + NG < tiles.count) src.issue(tiles.at(t + NG), wave, lane, smem_addr + (1 - cur) * 2 * TILE_BYTES);
+      if (NG == 2 && t >= tiles.count) return;
       const char* k_ = wf_smem + cur * 2 * TILE_BYTES;
       attend_tile<DH>(x, qf, k_, k_ + TILE_BYTES, fo, to, tiles.at(t) * 64, 0, a.w, span, 0, q, near, lane);
     };
-    for (int t = 0; t < tiles.count; t += 2) {
-      tile(std::integral_constant<int, 0>{}, t);
-      if (t + 1 < tiles.count) tile(std::integral_constant<int, 1>{}, t + 1);
+    for (int t = 0; t < tiles.count; t += 2 * NG) {   // both groups walk as often as the first: the barriers are the workgroup's
+      tile(std::integral_constant<int, 0>{}, t + grp);
+      if (t + NG < tiles.count) tile(std::integral_constant<int, 1>{}, t + NG + grp);
+    }
+    if constexpr (NG == 2) {
+      constexpr int PER = (16 * DT + 2) * WAVE;   // floats a wave hands over: O^T, the reference exponent, the half row sum
+      static_assert(4 * PER * 4 <= NG * 4 * TILE_BYTES, "the sums fit in the rings");
+      float* const at = reinterpret_cast<float*>(wf_rings) + wave * PER;
+      __syncthreads();   // the rings have been read
+      if (grp == 1) {
+        hand_over(x.o, at, lane);
+        at[16 * DT * WAVE + lane] = x.m;
+        at[(16 * DT + 1) * WAVE + lane] = x.l;
+      }
+      __syncthreads();
+      if (grp == 1) return;
+      const float m1 = at[16 * DT * WAVE + lane], mn = fmaxf(x.m, m1);   // -inf: a group that has seen nothing
+      const float c0 = x.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x.m - mn), c1 = m1 == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m1 - mn);
+      x.l = x.l * c0 + at[(16 * DT + 1) * WAVE + lane] * c1;
+      take_over(x.o, at, c0, c1, lane);
+      x.m = mn;
+      x.m_neg = -mn;
     }
     x.l += __shfl_xor(x.l, 32, WAVE);
     if (__any(q < rows && plain::not_finite(x.o)) && q < rows) {
@@ -73,7 +96,8 @@ __global__ void __launch_bounds__(AT_THREADS, DH == 128 ? 2 : 3) window_fwd_mfma
       }
     }
   }
-  int q_out = q;   // addresses of the outputs are formed behind the loop
+  if (grp == 1) return;   // blocks behind the document
+  int q_out = q;          // addresses of the outputs are formed behind the loop
   asm volatile("" : "+v"(q_out));
   if (q_out < a.S) {
     bf16* const out = o + ((long)b * a.S + q_out) * a.H * DH + hd * DH;
@@ -204,7 +228,9 @@ template <int DH> __device__ __forceinline__ void window_dq(const WindowArgs& a,
 // Keys: 128 of a key head, 32 a wave, over the queries of every head of the group that see them under the window alone; the stages hold 64
 // queries.  Sinks are seen by all queries behind them, a multiple of what the other keys take, so a workgroup takes only 32 of them (SINKS):
 // its waves share the stage, two of them on each half of it, one for dV and one for dK, and the halves' sums meet at the end.
-// Where that would still be the longest by far, the queries are cut among `parts` workgroups, whose sums lie in the rows of dqkv that dQ is
+// A launch of fewer blocks of keys than compute units is made of such workgroups altogether (KEYS_SHARED), us: 1 x 8192, 8 heads of 64 on 1, window 512 (64
+// blocks) 150 -> 79; 2 x 1000, 8 heads, causal (128) 39 -> 35; 1 x 2048, 14 heads, window 256 (224) 40 -> 38.5; 8 x 512, 8 heads (256) 31 -> 37.
+// Where a workgroup for 32 sinks would still be the longest by far, the queries are cut among `parts` workgroups, whose sums lie in the rows of dqkv that dQ is
 // written to afterwards (SinkParts), and window_sinks_join adds them.  1 x 32768 positions, 16 heads of 128 on 4, window 1024, 16 sinks: 2995 us
 // uncut (without sinks 1082), 1155 cut; 8 heads of 64 on 1, 8192 positions, window 512, 4 sinks 819 | 170.
 template <int DH> constexpr int window_dkv_stage() { return 2 * tile_bytes<DH>() + 2 * 64 * (int)sizeof(float); }   // Q | dO | -lse log2(e) | -D
@@ -252,18 +278,19 @@ struct SinkParts {
     return reinterpret_cast<float*>(dqkv + ((long)b * S + row) * ld) + f % per_row;
   }
 };
-enum { KEYS = 0, SINKS_WHOLE = 1, SINKS_PART = 2 };
+enum { KEYS = 0, SINKS_WHOLE = 1, SINKS_PART = 2, KEYS_SHARED = 3 };
 
 template <int DH, int KIND>
 __device__ __forceinline__ void window_dkv(const WindowArgs& a, const bf16* __restrict__ d_o, const float* __restrict__ dsum, bf16* __restrict__ dqkv, int b, int hk,
                                            int k0, char* smem, const SinkParts& sp, int part) {
-  constexpr bool SINKS = KIND != KEYS;
+  constexpr bool SINKS = KIND == SINKS_WHOLE || KIND == SINKS_PART, SHARED = KIND != KEYS;   // SHARED: the waves share 32 keys
+  constexpr int BLOCK = SHARED ? 32 : 128;
   constexpr int KS = DH / 16, DT = DH / 32, TILE_BYTES = tile_bytes<DH>(), STAGE = window_dkv_stage<DH>();
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, h = lane >> 5;
   const int rows = document_rows(a.lengths, b, a.S), ld = (a.H + 2 * a.H_kv) * DH, G = a.H / a.H_kv;
   const int sinks = rows <= a.w.window ? 0 : min(a.w.sinks, rows);   // a window that covers the document leaves the sinks nothing of their own
   if (SINKS && k0 >= sinks) return;
-  const int kw0 = k0 + (SINKS ? 0 : 32 * wave), key = kw0 + r;
+  const int kw0 = k0 + (SHARED ? 0 : 32 * wave), key = kw0 + r;
   const long Sp = (a.S + 127) / 128 * 128L;
   const bf16* const base = a.qkv + (long)b * a.S * ld;
   const bf16* const krow = base + (long)key * ld + (a.H + hk) * DH;
@@ -275,7 +302,7 @@ __device__ __forceinline__ void window_dkv(const WindowArgs& a, const bf16* __re
   f32x16 dk[DT], dv[DT];
   plain::clear(dk);
   plain::clear(dv);
-  if (k0 < rows && (SINKS || k0 + 127 >= sinks)) {
+  if (k0 < rows && (SINKS || k0 + BLOCK - 1 >= sinks)) {
     uint4 kf[KS], vf[KS];
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
@@ -285,7 +312,7 @@ __device__ __forceinline__ void window_dkv(const WindowArgs& a, const bf16* __re
     FragOff fo = frag_offsets(lane);
     TrOff to = tr_offsets(lane);
     const uint32_t smem_addr = (uint32_t)(uintptr_t)smem;
-    const int block_last = SINKS ? rows - 1 : min(rows - 1, k0 + 127 + a.w.window - 1);
+    const int block_last = SINKS ? rows - 1 : min(rows - 1, k0 + BLOCK - 1 + a.w.window - 1);
     const int first = k0 >> 6, n_tiles = (block_last >> 6) + 1 - first;
     int steps = G * n_tiles, done = 0;   // steps of the parts in front of this one
     if constexpr (KIND == SINKS_PART) {
@@ -326,11 +353,11 @@ __device__ __forceinline__ void window_dkv(const WindowArgs& a, const bf16* __re
       const float* nlse2s = reinterpret_cast<const float*>(q_ + 2 * TILE_BYTES);
       const float* neg_ds = nlse2s + 64;
 #pragma unroll
-      for (int i = 0; i < (SINKS ? 1 : 2); ++i) {
-        const int t = SINKS ? wave & 1 : i, qh = q0 + 32 * t;   // 32 queries
+      for (int i = 0; i < (SHARED ? 1 : 2); ++i) {
+        const int t = SHARED ? wave & 1 : i, qh = q0 + 32 * t;   // 32 queries
         if (idle || qh + 31 < kw0 || qh > last) continue;       // wave-uniform
         if constexpr (DH == 128) rederive_offsets(fo, to);
-        const bool want_v = !SINKS || wave < 2, want_k = !SINKS || wave >= 2;
+        const bool want_v = !SHARED || wave < 2, want_k = !SHARED || wave >= 2;
         // accumulator elements 4g .. 4g + 3 are queries 8g + 4h + (0..3) of the half: their statistics are 16 contiguous bytes
         f32x16 st, dp;
         zero(st);
@@ -376,7 +403,7 @@ __device__ __forceinline__ void window_dkv(const WindowArgs& a, const bf16* __re
         if (want_k) mma_transposed_half(dk, q_ + 4096 * t, to, dp);
       }
     }
-    if constexpr (SINKS) {   // the odd waves hand their half of the queries over; then wave 2 its dK to wave 0
+    if constexpr (SHARED) {   // the odd waves hand their half of the queries over; then wave 2 its dK to wave 0
       constexpr int PER = 16 * DT * WAVE;
       static_assert(3 * PER * 4 <= 2 * STAGE, "the sums fit in the stages");
       float* const at = reinterpret_cast<float*>(smem);
@@ -406,6 +433,7 @@ __device__ __forceinline__ void window_dkv(const WindowArgs& a, const bf16* __re
     }
     keys_if_not_finite<DH>(dk, dv, a, d_o, dsum, b, hk, key, key_last, rows, h);
   }
+  if (SHARED && wave != 0) return;   // blocks behind the document
   int key_out = key;
   asm volatile("" : "+v"(key_out));
   if (key_out < a.S && (SINKS ? key_out < sinks : key_out >= sinks)) store_keys<DH>(dk, dv, a, dqkv, b, hk, key_out, key_out < rows, h);
@@ -464,7 +492,7 @@ __global__ void __launch_bounds__(AT_THREADS) window_sinks_join(WindowArgs a, co
 // One launch: the sinks' workgroups, which take longest, then those of dK / dV, then dQ's
 template <int DH>
 __global__ void __launch_bounds__(AT_THREADS, 2) window_bwd_mfma(WindowArgs a, const bf16* __restrict__ d_o, const float* __restrict__ dsum, bf16* __restrict__ dqkv,
-                                                                 int sink_blocks) {
+                                                                 int sink_blocks, bool shared) {
   extern __shared__ __attribute__((aligned(16))) char wb_smem[];
   const int n_kv = a.B * a.H_kv, nb = (a.S + 127) / 128;
   int i = blockIdx.x;
@@ -474,12 +502,14 @@ __global__ void __launch_bounds__(AT_THREADS, 2) window_bwd_mfma(WindowArgs a, c
     return;
   }
   i -= sink_blocks * n_kv;
-  if (i < n_kv * nb) {
+  const int key_blocks = shared ? 4 * nb : nb;
+  if (i < n_kv * key_blocks) {
     const int kb = i / n_kv, bk = i - kb * n_kv, b = bk / a.H_kv;
-    window_dkv<DH, KEYS>(a, d_o, dsum, dqkv, b, bk - b * a.H_kv, 128 * kb, wb_smem, SinkParts{}, 0);
+    if (shared) window_dkv<DH, KEYS_SHARED>(a, d_o, dsum, dqkv, b, bk - b * a.H_kv, 32 * kb, wb_smem, SinkParts{}, 0);
+    else window_dkv<DH, KEYS>(a, d_o, dsum, dqkv, b, bk - b * a.H_kv, 128 * kb, wb_smem, SinkParts{}, 0);
     return;
   }
-  i -= n_kv * nb;
+  i -= n_kv * key_blocks;
   const int n_bh = a.B * a.H, qb = i / n_bh;
   window_dq<DH>(a, d_o, dsum, dqkv, i - qb * n_bh, nb - 1 - qb, wb_smem);
 }
@@ -496,12 +526,21 @@ __global__ void __launch_bounds__(AT_THREADS, 2) window_sink_parts(WindowArgs a,
 
 template <int DH>
 dipaco_status launch_window_fwd_mfma(const bf16* qkv, const int* lengths, bf16* o, float* lse, int B, int S, int H, int H_kv, Window w, hipStream_t s) {
-  constexpr int LDS = 2 * 2 * tile_bytes<DH>();
-  static std::atomic<unsigned long long> lds_set{0};
-  if (dipaco_status st = ensure_dynamic_lds(reinterpret_cast<const void*>(window_fwd_mfma<DH>), LDS, lds_set)) return st;
-  window_fwd_mfma<DH><<<B * H * ((S + 127) / 128), AT_THREADS, LDS, s>>>(WindowArgs{qkv, lengths, B, S, H, H_kv, w}, o, lse);
-  DIPACO_LAUNCH_CHECK();
-  return DIPACO_OK;
+  const int nqb = (S + 127) / 128, blocks = B * H * nqb;
+  auto run = [&](auto NGc) -> dipaco_status {
+    constexpr int NG = decltype(NGc)::value, LDS = NG * 4 * tile_bytes<DH>();
+    static std::atomic<unsigned long long> lds_set{0};
+    if (dipaco_status st = ensure_dynamic_lds(reinterpret_cast<const void*>(window_fwd_mfma<DH, NG>), LDS, lds_set)) return st;
+    window_fwd_mfma<DH, NG><<<blocks, AT_THREADS * NG, LDS, s>>>(WindowArgs{qkv, lengths, B, S, H, H_kv, w}, o, lse);
+    DIPACO_LAUNCH_CHECK();
+    return DIPACO_OK;
+  };
+  // Two groups where the longest block's tiles, at least seven of them, are the launch's length: the blocks' tiles together are no more than 256 compute units
+  // take in that time.  us one -> two (blocks, tiles): 1 x 2048, 14 heads of 64, window 512 (224, 11) 16.6 -> 14.6; 1 x 2000, 8 heads, causal (128, 32) 32.7 ->
+  // 24.7; 2 x 2048, 14 heads, causal (448, 32) 38.3 -> 31.4; 8 x 512, 8 heads, causal (256, 8) 12.0 -> 11.7; beyond: 1 x 4096, 14 heads, window 512 (448, 11)
+  // 23.6 -> 25.6; 4 x 300, 8 heads, window 64 (96, 4) 8.2 -> 9.0; 1 x 300, 4 heads of 128, causal (12, 6) 10.2 -> 11.7.
+  const int tiles = std::min((w.window + w.sinks + 127) / 64 + 1, 2 * nqb), mean = std::min(tiles, nqb + 1);
+  return tiles >= 7 && (int64_t)blocks * mean <= 256LL * tiles ? run(std::integral_constant<int, 2>{}) : run(std::integral_constant<int, 1>{});
 }
 template dipaco_status launch_window_fwd_mfma<32>(const bf16*, const int*, bf16*, float*, int, int, int, int, Window, hipStream_t);
 template dipaco_status launch_window_fwd_mfma<64>(const bf16*, const int*, bf16*, float*, int, int, int, int, Window, hipStream_t);
@@ -536,7 +575,8 @@ dipaco_status launch_window_bwd_mfma(const bf16* qkv, const int* lengths, const 
     DIPACO_LAUNCH_CHECK();
     sink_blocks = 0;
   }
-  window_bwd_mfma<DH><<<B * H_kv * (sink_blocks + nb) + B * H * nb, AT_THREADS, LDS, s>>>(a, d_o, dsum, dqkv, sink_blocks);
+  const bool shared = (int64_t)B * H_kv * nb < 256;   // KEYS_SHARED: fewer workgroups than compute units
+  window_bwd_mfma<DH><<<B * H_kv * (sink_blocks + (shared ? 4 : 1) * nb) + B * H * nb, AT_THREADS, LDS, s>>>(a, d_o, dsum, dqkv, sink_blocks, shared);
   DIPACO_LAUNCH_CHECK();
   return DIPACO_OK;
 }

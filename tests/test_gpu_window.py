@@ -256,3 +256,10 @@ def test_a_value_that_is_not_finite_behind_the_sinks(dtype, dh):
     tol = 16 * ref.half_step(TDT[dtype])
     rest = (keys[~reached].double() - clean[~reached].double()).abs()
     assert bool((rest <= tol * clean[~reached].double().abs().amax(1, keepdim=True) + 1e-4).all())
+
+
+@pytest.mark.parametrize("B,S,H,Hkv,dh,window,sinks,lengths", [(1, 700, 2, 2, 64, ALL, 0, None), (2, 450, 3, 1, 32, ALL, 0, [450, 100]), (1, 900, 2, 1, 128, 400, 9, None),
+                                                               (40, 449, 2, 2, 64, ALL, 0, None), (20, 400, 14, 7, 64, 300, 2, None)])
+def test_blocks_of_one_and_of_two_groups_of_waves(B, S, H, Hkv, dh, window, sinks, lengths):
+    """few long blocks (two groups of waves a block, 32 keys a workgroup in the gradient) and enough of them"""
+    check(dp.BF16, B, S, H, Hkv, dh, window, sinks, lengths, seed=15)
