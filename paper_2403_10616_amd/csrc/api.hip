@@ -411,7 +411,7 @@ static PagedArgs<T> paged_args(const void* qkv, const int32_t* row_start, const 
   int shift = 4;
   while ((1 << shift) < page_size) ++shift;
   return {static_cast<const T*>(qkv), row_start, cache_len, pages, const_cast<T*>(static_cast<const T*>(cache)), static_cast<T*>(o), lse, rows, B,
-          max_new, H, H_kv, n_pages, shift, pages_per_doc, w, Divisor(H / H_kv), Divisor(1), Divisor(1), 1, nullptr, 0};
+          max_new, H, H_kv, n_pages, shift, pages_per_doc, w, Divisor(H / H_kv), Divisor(1), Divisor(1), 1, nullptr, nullptr, 0};
 }
 
 }  // namespace dipaco

@@ -61,8 +61,8 @@ template <typename T> struct PagedArgs {
   Divisor group;             // H / H_kv
   Divisor narrow_splits, wide_splits;
   int narrow_keys;           // a narrow split has at least so many keys
-  float* part;               // [splits][T rows][H] x (dh sums, then in an array of its own reference exponent and sum)
-
+  float* part;               // [splits][T rows][H][dh] sums
+  float2* state;             // [splits][T rows][H] reference exponents and sums of exponentials; narrow and wide splits use the rows of their documents
   int narrow_turn;           // log2 of the (document, head)s behind which the order of their splits moves on by one
   // the split of the p-th workgroup of a document and head
   __device__ __forceinline__ int narrow_split(int p, int item) const {
@@ -83,9 +83,7 @@ template <typename T> struct PagedArgs {
   }
   template <int DH> __device__ __forceinline__ long value_from_key() const { return ((long)H_kv << page_shift) * DH; }
   template <int DH> __device__ __forceinline__ float* part_sums(int split, long row, int head) const { return part + (((long)split * T_rows + row) * H + head) * DH; }
-  template <int DH> __device__ __forceinline__ float2* part_state(int splits, int split, long row, int head) const {
-    return reinterpret_cast<float2*>(part + (long)splits * T_rows * H * DH) + ((long)split * T_rows + row) * H + head;
-  }
+  __device__ __forceinline__ float2* part_state(int split, long row, int head) const { return state + ((long)split * T_rows + row) * H + head; }
 };
 
 // A block of packed rows of one document: which rows, the tiles that they see, and how many of these a split takes

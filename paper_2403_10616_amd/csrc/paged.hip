@@ -61,7 +61,7 @@ __global__ void __launch_bounds__(256) paged_join(PagedArgs<T> a, Divisor heads)
   }
   if (tiles <= per) return;   // its workgroup has written it
   const int used = __builtin_popcountll(__builtin_amdgcn_ballot_w64(lane * per < tiles));
-  const float2 st = lane < used ? *a.template part_state<DH>(splits.d, lane, row, head) : make_float2(-INFINITY, 0.f);
+  const float2 st = lane < used ? *a.part_state(lane, row, head) : make_float2(-INFINITY, 0.f);
   const float m = wave_max(st.x), w = st.x == -INFINITY ? 0.f : exp2f(st.x - m), l = wave_sum(w * st.y);
   const float* const from = a.template part_sums<DH>(0, row, head) + COLS * (lane % (DH / COLS));
   const long step = (long)a.T_rows * a.H * DH;
@@ -91,6 +91,11 @@ __global__ void __launch_bounds__(256) paged_join(PagedArgs<T> a, Divisor heads)
 // How often a call's keys are cut: enough workgroups for the chip, none with less than LEAST_KEYS keys however long the documents are
 struct PagedPlan { int narrow_splits, narrow_keys, wide_blocks, wide_splits; };
 inline int most_splits(int64_t keys, int least) { return (int)std::min<int64_t>(PAGED_MOST_SPLITS, (keys + least - 1) / least); }
+// Rows of partial sums that a workspace holds: `most` splits of every row, or as many as the workgroups that splits are made for have rows
+constexpr size_t PAGED_GROUP_ROWS = std::max(PAGED_WIDE_GROUPS * PagedCut<bf16>::WIDE_ROWS, PAGED_NARROW_GROUPS * PagedCut<bf16>::NARROW_ROWS);
+inline size_t partial_rows(int T_rows, int H, int64_t capacity) {
+  return std::min((size_t)most_splits(capacity, PagedCut<float>::LEAST_KEYS) * T_rows, (size_t)T_rows + (PAGED_GROUP_ROWS + H - 1) / H);
+}
 template <typename T> PagedPlan plan(const PagedArgs<T>& a) {
   constexpr int NARROW_ROWS = PagedCut<T>::NARROW_ROWS, WIDE_ROWS = PagedCut<T>::WIDE_ROWS;
   const int G = a.H / a.H_kv, page_size = 1 << a.page_shift;
@@ -108,6 +113,10 @@ template <typename T> PagedPlan plan(const PagedArgs<T>& a) {
   p.wide_blocks = longest <= NARROW_ROWS ? 0 : (int)(packed / WIDE_ROWS + std::min<int64_t>(a.B, packed / (NARROW_ROWS + 1)));
   const int64_t wide = std::max<int64_t>(1, p.wide_blocks) * a.H_kv;
   p.wide_splits = (int)std::min<int64_t>(most, (PAGED_WIDE_GROUPS + wide - 1) / wide);
+  // a call of narrow documents beside long chunks: the splits of the one have room for all rows of the other
+  const int room = (int)std::min<size_t>(PAGED_MOST_SPLITS, partial_rows(a.T_rows, a.H, (int64_t)page_size * a.pages_per_doc) / a.T_rows);
+  p.narrow_splits = std::min(p.narrow_splits, room);
+  p.wide_splits = std::min(p.wide_splits, room);
   return p;
 }
 
@@ -118,13 +127,9 @@ template <typename T> dipaco_status launch_cache_append(const PagedArgs<T>& a, i
   DIPACO_LAUNCH_CHECK();
   return DIPACO_OK;
 }
-// Sums of at most `most` splits of T rows, and of no more packed rows than the plan's workgroups hold: a plan of n splits has at most
-// GROUPS / n + 1 workgroups a split with up to 128 (32) packed rows each.  Non-decreasing in every size but the heads'.
+// Non-decreasing in every size but the heads'
 size_t paged_workspace_bytes(int T_rows, int H, int dh, int page_size, int pages_per_doc) {
-  const size_t most = most_splits((int64_t)page_size * pages_per_doc, PagedCut<float>::LEAST_KEYS);
-  constexpr size_t GROUP_ROWS = std::max(PAGED_WIDE_GROUPS * PagedCut<bf16>::WIDE_ROWS, PAGED_NARROW_GROUPS * PagedCut<bf16>::NARROW_ROWS);
-  const size_t rows = std::min(most * T_rows, (size_t)T_rows + (GROUP_ROWS + H - 1) / H);
-  return 256 + rows * H * (dh + 2) * sizeof(float);
+  return 256 + partial_rows(T_rows, H, (int64_t)page_size * pages_per_doc) * H * (dh + 2) * sizeof(float);
 }
 template <typename T> dipaco_status launch_attention_paged(PagedArgs<T> a, int dh, void* workspace, hipStream_t s) {
   const PagedPlan p = plan(a);
@@ -132,7 +137,9 @@ template <typename T> dipaco_status launch_attention_paged(PagedArgs<T> a, int d
   a.narrow_keys = p.narrow_keys;
   a.narrow_turn = 3 - std::min(3, __builtin_ctz(p.narrow_splits));   // n splits begin at 8 / gcd(8, n) places by themselves
   a.wide_splits = Divisor(p.wide_splits);
-  a.part = static_cast<float*>(workspace);
+  a.state = static_cast<float2*>(workspace);
+  const size_t states = (size_t)std::max(p.narrow_splits, p.wide_splits) * a.T_rows * a.H;
+  a.part = static_cast<float*>(workspace) + (2 * states + 3) / 4 * 4;
   auto run = [&](auto DHc) -> dipaco_status {
     constexpr int DH = decltype(DHc)::value;
     if (dipaco_status st = p.wide_blocks ? launch_paged_both<DH>(a, p.wide_blocks, s) : launch_paged_narrow<DH>(a, s)) return st;

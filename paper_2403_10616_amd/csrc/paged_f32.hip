@@ -131,14 +131,14 @@ __global__ void __launch_bounds__(WF_THREADS, NARROW && DH == 128 ? 1 : 2) paged
       *reinterpret_cast<float4*>(out + 16 * d + 4 * g) = make_float4(v[0] * scale, v[1] * scale, v[2] * scale, v[3] * scale);
     }
     if (wave == 0 && g == 0) {
-      if (!blk.whole()) *a.template part_state<DH>(splits.d, split, row, head) = make_float2(mm, l);
+      if (!blk.whole()) *a.part_state(split, row, head) = make_float2(mm, l);
       else if (a.lse) a.lse[row * a.H + head] = (mm + __builtin_amdgcn_logf(l)) * WF_LN2;
     }
   } else {
     if (!valid) return;
     if (!blk.whole()) {
       store_row<DH>(a.template part_sums<DH>(split, row, head), x.o, g, 1.f);
-      if (g == 0) *a.template part_state<DH>(splits.d, split, row, head) = make_float2(x.m, x.l);
+      if (g == 0) *a.part_state(split, row, head) = make_float2(x.m, x.l);
     } else {
       store_row<DH>(a.o + (row * a.H + head) * DH, x.o, g, x.m == -INFINITY ? 0.f : 1.0f / x.l);
       if (a.lse && g == 0) a.lse[row * a.H + head] = (x.m + __builtin_amdgcn_logf(x.l)) * WF_LN2;   // -inf where nothing is seen

@@ -173,7 +173,7 @@ template <int DH> __device__ __forceinline__ void wide_block(const PagedArgs<bf1
 #pragma unroll
       for (int g = 0; g < 4; ++g)
         *reinterpret_cast<float4*>(sums + 32 * dt + 8 * g + 4 * h) = make_float4(x.o[dt][4 * g], x.o[dt][4 * g + 1], x.o[dt][4 * g + 2], x.o[dt][4 * g + 3]);
-    if (h == 0) *a.template part_state<DH>(a.wide_splits.d, split, row.row, row.head) = make_float2(x.m, x.l);
+    if (h == 0) *a.part_state(split, row.row, row.head) = make_float2(x.m, x.l);
   }
 }
 
@@ -266,7 +266,10 @@ template <int DH, int NW, int NS> __device__ __forceinline__ void narrow_documen
       if (s)
         attend_half<DH>(x, qf, k_, k_ + 4096, fo, to, k0, s | (blk.hi > at.last ? UPPER | LOWER : 0), holes, min(row.pos, at.last), row.near, a.w.sinks, lane);
       asm volatile("" ::: "memory");
-      if (t + NS < n) issue(t + NS);
+      if (t + NS < n) {
+        __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (3 << 14));   // lgkmcnt(0): every read of the stage that is filled again has returned
+        issue(t + NS);
+      }
     }
     x.l += __shfl_xor(x.l, 32, WAVE);
     if (__any(row.valid && plain::not_finite(x.o)) && row.valid) {
@@ -319,7 +322,7 @@ template <int DH, int NW, int NS> __device__ __forceinline__ void narrow_documen
       }
     }
   if (wave == 0 && h == 0) {
-    if (!whole) *a.template part_state<DH>(a.narrow_splits.d, split, row.row, row.head) = make_float2(m, l);
+    if (!whole) *a.part_state(split, row.row, row.head) = make_float2(m, l);
     else if (a.lse) a.lse[row.row * a.H + row.head] = (m + __builtin_amdgcn_logf(l)) * LN2;
   }
 }

@@ -133,6 +133,40 @@ def test_long_caches(dtype, cached, new, H, Hkv, dh, page, window, sinks):
 
 
 @pytest.mark.parametrize("dtype", [dp.F32, dp.BF16])
+@pytest.mark.parametrize("cached,new,H,Hkv,dh,page,window,sinks", [
+    ([6000, 2000, 50], [1, 300, 400], 8, 1, 64, 64, ALL, 0), ([10, 4000, 4000, 300], [500, 1, 2, 0], 8, 4, 32, 16, ALL, 0),
+    ([3000, 3000], [3, 257], 4, 4, 128, 32, 2500, 8), ([5000, 0, 900], [1, 64, 64], 2, 1, 64, 16, 4000, 0)])
+def test_tokens_beside_chunks(dtype, cached, new, H, Hkv, dh, page, window, sinks):
+    """documents of few packed rows and long caches in one call with long chunks: each cut into splits of its own number"""
+    check(dtype, cached, new, H, Hkv, dh, page, window, sinks, seed=16)
+
+
+def guarded_workspace(n):
+    """n bytes of 255 between two runs of 4096 bytes of 170"""
+    whole = torch.full((n + 8192,), 170, dtype=torch.uint8, device=DEV)
+    whole[4096:4096 + n] = 255
+    return whole, whole[4096:4096 + n]
+
+
+@pytest.mark.parametrize("dtype", [dp.F32, dp.BF16])
+@pytest.mark.parametrize("cached,new,H,Hkv,dh", [([6000, 2000, 50], [1, 300, 400], 8, 1, 64), ([4000], [1], 8, 8, 128), ([9000, 9000], [1, 2], 4, 1, 32), ([700], [200], 2, 2, 64)])
+def test_the_workspace_is_as_large_as_it_is_said_to_be(dtype, cached, new, H, Hkv, dh):
+    print(f"workspace dtype={dtype} cached={cached} new={new} H={H} Hkv={Hkv} dh={dh}", flush=True)
+    page = 32
+    c = Cache(dtype, [a + b for a, b in zip(cached, new)], Hkv, dh, page, 3)
+    c.data.normal_()
+    st = starts_of(new)
+    x = draw((st[-1], (H + 2 * Hkv) * dh), 4, dtype).to(DEV)
+    want, want_lse = c.attend(x, st, cached, H, max(new), ALL, 0)
+    n = dp.dipaco_k_attention_paged_workspace_bytes(st[-1], len(new), max(new), H, Hkv, dh, page, c.per_doc)
+    whole, ws = guarded_workspace(n)
+    o, lse = torch.empty_like(want), torch.empty_like(want_lse)
+    dp.dipaco_k_attention_paged(dtype, x, i32(st), i32(cached), c.pages, c.data, o, lse, st[-1], len(new), max(new), H, Hkv, dh, c.n_pages, page, c.per_doc, ALL, 0, ws)
+    assert torch.equal(o, want) and torch.equal(lse, want_lse)
+    assert bool((whole[:4096] == 170).all()) and bool((whole[4096 + n:] == 170).all())
+
+
+@pytest.mark.parametrize("dtype", [dp.F32, dp.BF16])
 @pytest.mark.parametrize("new", [[1, 1], [50, 3]])
 def test_peaked_rows(dtype, new):
     check(dtype, [400, 30], new, 4, 2, 64, 16, ALL, 0, seed=8, scale=8.0)
