@@ -263,3 +263,22 @@ def test_a_value_that_is_not_finite_behind_the_sinks(dtype, dh):
 def test_blocks_of_one_and_of_two_groups_of_waves(B, S, H, Hkv, dh, window, sinks, lengths):
     """few long blocks (two groups of waves a block, 32 keys a workgroup in the gradient) and enough of them"""
     check(dp.BF16, B, S, H, Hkv, dh, window, sinks, lengths, seed=15)
+
+
+def test_offsets_beyond_32_bits():
+    """a batch whose rows lie beyond 2^32 bytes and 2^31 elements of qkv: the last document, bit for bit as it is alone"""
+    dtype, B, S, H, Hkv, dh, window = dp.BF16, 6, 65536, 16, 16, 128, 100
+    g = torch.Generator(device=DEV)
+    g.manual_seed(3)
+    x = torch.empty((B * S, (H + 2 * Hkv) * dh), dtype=torch.bfloat16, device=DEV).normal_(generator=g)
+    d_o = torch.empty((B * S, H * dh), dtype=torch.bfloat16, device=DEV).normal_(generator=g)
+    assert x.numel() > 1 << 31
+    o, lse = fwd(dtype, x, None, B, S, H, Hkv, dh, window, 0)
+    d = bwd(dtype, x, None, o, d_o, lse, B, S, H, Hkv, dh, window, 0)
+    for b in (0, B - 1):
+        at = slice(b * S, (b + 1) * S)
+        o1, lse1 = fwd(dtype, x[at].contiguous(), None, 1, S, H, Hkv, dh, window, 0)
+        assert torch.equal(o[at], o1) and torch.equal(lse[b], lse1[0])
+        d1 = bwd(dtype, x[at].contiguous(), None, o1, d_o[at].contiguous(), lse1, 1, S, H, Hkv, dh, window, 0)
+        assert torch.equal(d[at], d1)
+        assert bool(torch.isfinite(d1).all()) and float(d1.float().abs().amax()) > 0
