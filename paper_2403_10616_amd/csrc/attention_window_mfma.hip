@@ -489,10 +489,11 @@ __global__ void __launch_bounds__(AT_THREADS) window_sinks_join(WindowArgs a, co
   for (int g = 0; g < 4; ++g) store4(out + 8 * g + 4 * h, v[0], g, n < DT ? score_scale<DH>() : 1.0f);
 }
 
-// One launch: the sinks' workgroups, which take longest, then those of dK / dV, then dQ's
-template <int DH>
-__global__ void __launch_bounds__(AT_THREADS, 2) window_bwd_mfma(WindowArgs a, const bf16* __restrict__ d_o, const float* __restrict__ dsum, bf16* __restrict__ dqkv,
-                                                                 int sink_blocks, bool shared) {
+// One launch: the sinks' workgroups, which take longest, then those of dK / dV, then dQ's.  A kernel for either kind of dK / dV: with both in one, head size 64
+// has 169 registers, two waves a SIMD.
+template <int DH, bool SHARED>
+__global__ void __launch_bounds__(AT_THREADS, DH == 128 ? 2 : 3) window_bwd_mfma(WindowArgs a, const bf16* __restrict__ d_o, const float* __restrict__ dsum,
+                                                                                 bf16* __restrict__ dqkv, int sink_blocks) {
   extern __shared__ __attribute__((aligned(16))) char wb_smem[];
   const int n_kv = a.B * a.H_kv, nb = (a.S + 127) / 128;
   int i = blockIdx.x;
@@ -502,11 +503,10 @@ __global__ void __launch_bounds__(AT_THREADS, 2) window_bwd_mfma(WindowArgs a, c
     return;
   }
   i -= sink_blocks * n_kv;
-  const int key_blocks = shared ? 4 * nb : nb;
+  const int key_blocks = SHARED ? 4 * nb : nb;
   if (i < n_kv * key_blocks) {
     const int kb = i / n_kv, bk = i - kb * n_kv, b = bk / a.H_kv;
-    if (shared) window_dkv<DH, KEYS_SHARED>(a, d_o, dsum, dqkv, b, bk - b * a.H_kv, 32 * kb, wb_smem, SinkParts{}, 0);
-    else window_dkv<DH, KEYS>(a, d_o, dsum, dqkv, b, bk - b * a.H_kv, 128 * kb, wb_smem, SinkParts{}, 0);
+    window_dkv<DH, SHARED ? KEYS_SHARED : KEYS>(a, d_o, dsum, dqkv, b, bk - b * a.H_kv, (SHARED ? 32 : 128) * kb, wb_smem, SinkParts{}, 0);
     return;
   }
   i -= n_kv * key_blocks;
@@ -552,8 +552,6 @@ dipaco_status launch_window_bwd_mfma(const bf16* qkv, const int* lengths, const 
                                      int H, int H_kv, Window w, hipStream_t s) {
   constexpr int LDS = 2 * window_dkv_stage<DH>();
   static_assert(LDS >= 4 * tile_bytes<DH>(), "dQ's stages fit");
-  static std::atomic<unsigned long long> lds_set{0};
-  if (dipaco_status st = ensure_dynamic_lds(reinterpret_cast<const void*>(window_bwd_mfma<DH>), LDS, lds_set)) return st;
   const WindowArgs a{qkv, lengths, B, S, H, H_kv, w};
   const int nb = (S + 127) / 128, G = H / H_kv;
   int sink_blocks = w.window >= S ? 0 : (std::min(w.sinks, S) + 31) / 32;
@@ -576,9 +574,15 @@ dipaco_status launch_window_bwd_mfma(const bf16* qkv, const int* lengths, const 
     sink_blocks = 0;
   }
   const bool shared = (int64_t)B * H_kv * nb < 256;   // KEYS_SHARED: fewer workgroups than compute units
-  window_bwd_mfma<DH><<<B * H_kv * (sink_blocks + (shared ? 4 : 1) * nb) + B * H * nb, AT_THREADS, LDS, s>>>(a, d_o, dsum, dqkv, sink_blocks, shared);
-  DIPACO_LAUNCH_CHECK();
-  return DIPACO_OK;
+  auto run = [&](auto SHAREDc) -> dipaco_status {
+    constexpr bool SHARED = decltype(SHAREDc)::value;
+    static std::atomic<unsigned long long> lds_set{0};
+    if (dipaco_status st = ensure_dynamic_lds(reinterpret_cast<const void*>(window_bwd_mfma<DH, SHARED>), LDS, lds_set)) return st;
+    window_bwd_mfma<DH, SHARED><<<B * H_kv * (sink_blocks + (SHARED ? 4 : 1) * nb) + B * H * nb, AT_THREADS, LDS, s>>>(a, d_o, dsum, dqkv, sink_blocks);
+    DIPACO_LAUNCH_CHECK();
+    return DIPACO_OK;
+  };
+  return shared ? run(std::true_type{}) : run(std::false_type{});
 }
 template dipaco_status launch_window_bwd_mfma<32>(const bf16*, const int*, const bf16*, const bf16*, const float*, bf16*, float*, int, int, int, int, Window, hipStream_t);
 template dipaco_status launch_window_bwd_mfma<64>(const bf16*, const int*, const bf16*, const bf16*, const float*, bf16*, float*, int, int, int, int, Window, hipStream_t);
