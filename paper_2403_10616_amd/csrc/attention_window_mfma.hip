@@ -2,7 +2,7 @@
 //
 // Backward: dQ per block of 128 queries and dK / dV per block of 128 keys, each forming S and dO.V^T anew (seven products where one pass would need five), so
 // that every output has one writer and a fixed order of sums.  Us: 16 x 2048, 14 heads of 64, window 512, 4 sinks 305 (the statistics 22 of them); 4 x 8000, 16
-// heads of 128 on 4, window 1000 990; 8 x 2048, 8 heads of 128, causal 273 (attention_mfma.h: 354).
+// heads of 128 on 4, window 1000 1020; 8 x 2048, 8 heads of 128, causal 273 (attention_mfma.h: 354).
 //
 // Rows that a wave ends with results that are not finite are taken again over the pairs that see each other alone (attention_plain.h says
 // why), so that such values reach exactly the rows that see them.
