@@ -35,56 +35,118 @@ __global__ void __launch_bounds__(256) cache_append_rows(PagedArgs<T> a, int dh)
   }
 }
 
-// The splits' sums of the blocks that were split, added in their order: a wave per row and head, a lane per split for their states (there are at
-// most 64), then a lane per columns of the head.
-template <int DH, typename T>
-__global__ void __launch_bounds__(256) paged_join(PagedArgs<T> a, Divisor heads) {
+// over the 16 lanes of a row, in every one of them: rotations of the row by 8, 4, 2, 1
+template <int N> __device__ __forceinline__ float rotated16(float v) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x120 + N, 0xf, 0xf, false));
+}
+__device__ __forceinline__ float group16_max(float v) {
+  v = fmaxf(v, rotated16<8>(v));
+  v = fmaxf(v, rotated16<4>(v));
+  v = fmaxf(v, rotated16<2>(v));
+  return fmaxf(v, rotated16<1>(v));
+}
+__device__ __forceinline__ float group16_sum(float v) {
+  v += rotated16<8>(v);
+  v += rotated16<4>(v);
+  v += rotated16<2>(v);
+  return v + rotated16<1>(v);
+}
+
+// The splits' sums of the blocks that were split, added in their order: HEADS heads of a row a wave, 64 / HEADS lanes each, which hold the splits' states
+// (there are at most 64) and then columns of the head.
+template <int DH, typename T, int HEADS>
+__global__ void __launch_bounds__(256) paged_join(PagedArgs<T> a, Divisor waves) {   // of a row
   using Cut = PagedCut<T>;
-  constexpr int COLS = DH == 128 ? 2 : 1;
-  const int lane = threadIdx.x & 63, item = blockIdx.x * 4 + (threadIdx.x >> 6), row = heads(item), head = item - row * a.H;
+  constexpr int LANES = 64 / HEADS, COLS = DH > LANES ? DH / LANES : 1, HELD = PAGED_MOST_SPLITS / LANES;
+  const int lane = threadIdx.x & 63, sub = lane & (LANES - 1), item = blockIdx.x * 4 + (threadIdx.x >> 6), row = waves(item);
   if (row >= a.T_rows) return;   // whole waves leave
+  const int head_of = HEADS * (item - row * (int)waves.d) + lane / LANES, head = min(head_of, a.H - 1);
   const int b = __builtin_amdgcn_readfirstlane(find_document(a.row_start, a.B, row, lane)), G = a.group.d;
   const RowRange r = ragged_rows(a.row_start, b, a.T_rows);
   const int rows = min(r.count, a.max_new);
   if (row < r.first || row >= r.first + rows) return;
-  const bool narrow = rows * G <= Cut::NARROW_ROWS;
-  const Divisor& splits = narrow ? a.narrow_splits : a.wide_splits;
   int tiles, per;
-  if (narrow) {
-    const PagedBlock<Cut::NARROW_SHIFT> blk(a, b, 0, Cut::NARROW_ROWS, splits, a.narrow_keys);
+  if (rows * G <= Cut::NARROW_ROWS) {
+    const PagedBlock<Cut::NARROW_SHIFT> blk(a, b, 0, Cut::NARROW_ROWS, a.narrow_splits, a.narrow_keys);
     tiles = blk.tiles.count;
     per = blk.per;
   } else {
-    const PagedBlock<Cut::WIDE_SHIFT> blk(a, b, ((row - r.first) * G + head - a.group(head) * G) / Cut::WIDE_ROWS, Cut::WIDE_ROWS, splits, Cut::LEAST_KEYS);
+    const PagedBlock<Cut::WIDE_SHIFT> blk(a, b, ((row - r.first) * G + head - a.group(head) * G) / Cut::WIDE_ROWS, Cut::WIDE_ROWS, a.wide_splits, Cut::LEAST_KEYS);
     tiles = blk.tiles.count;
     per = blk.per;
   }
-  if (tiles <= per) return;   // its workgroup has written it
-  const int used = __builtin_popcountll(__builtin_amdgcn_ballot_w64(lane * per < tiles));
-  const float2 st = lane < used ? *a.part_state(lane, row, head) : make_float2(-INFINITY, 0.f);
-  const float m = wave_max(st.x), w = st.x == -INFINITY ? 0.f : exp2f(st.x - m), l = wave_sum(w * st.y);
-  const float* const from = a.template part_sums<DH>(0, row, head) + COLS * (lane % (DH / COLS));
+  if (head_of >= a.H || tiles <= per) tiles = 0;   // a block of one split has been written by its workgroup
+  if (!__any(tiles > 0)) return;
+  float2 st[HELD];
+  float m = -INFINITY, w[HELD], l = 0.f;
+#pragma unroll
+  for (int j = 0; j < HELD; ++j) {
+    st[j] = make_float2(-INFINITY, 0.f);
+    if ((LANES * j + sub) * per < tiles) st[j] = *a.part_state(LANES * j + sub, row, head);
+    m = fmaxf(m, st[j].x);
+  }
+  m = HEADS == 1 ? wave_max(m) : group16_max(m);
+#pragma unroll
+  for (int j = 0; j < HELD; ++j) {
+    w[j] = st[j].x == -INFINITY ? 0.f : exp2f(st[j].x - m);
+    l = __builtin_fmaf(w[j], st[j].y, l);
+  }
+  l = HEADS == 1 ? wave_sum(l) : group16_sum(l);
+  const float* const from = a.template part_sums<DH>(0, row, head) + COLS * (sub % (DH / COLS));
   const long step = (long)a.T_rows * a.H * DH;
   float v[COLS] = {};
-  for (int s0 = 0; s0 < used; s0 += 8) {   // eight loads at a time; a split behind the last one has no weight
-    float p[8][COLS];
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+  for (int j = 0; j < HELD; ++j) {
 #pragma unroll
-      for (int c = 0; c < COLS; ++c) p[i][c] = from[min(s0 + i, used - 1) * step + c];
+    for (int s0 = 0; s0 < LANES; s0 += 8) {   // eight splits at a time; one behind the last has no weight
+      if (!__any((LANES * j + s0) * per < tiles)) break;
+      float p[8][COLS];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float ws = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), s0 + i));
+      for (int i = 0; i < 8; ++i) {
+        const int s = LANES * j + s0 + i;
+        const float* const at = from + (s * per < tiles ? s : 0) * step;
+        if constexpr (COLS == 1) {
+          p[i][0] = *at;
+        } else if constexpr (COLS == 2) {
+          const float2 x = *reinterpret_cast<const float2*>(at);
+          p[i][0] = x.x; p[i][1] = x.y;
+        } else {
 #pragma unroll
-      for (int c = 0; c < COLS; ++c) v[c] = __builtin_fmaf(ws, p[i][c], v[c]);
+          for (int c = 0; c < COLS; c += 4) {
+            const float4 x = *reinterpret_cast<const float4*>(at + c);
+            p[i][c] = x.x; p[i][c + 1] = x.y; p[i][c + 2] = x.z; p[i][c + 3] = x.w;
+          }
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const bool has = (LANES * j + s0 + i) * per < tiles;
+        const float ws = __shfl(w[j], (lane - sub) + s0 + i, WAVE);
+#pragma unroll
+        for (int c = 0; c < COLS; ++c) v[c] = has ? __builtin_fmaf(ws, p[i][c], v[c]) : v[c];
+      }
     }
   }
+  if (tiles == 0 || COLS * sub >= DH) return;
   const float scale = m == -INFINITY ? 0.f : 1.f / l;
-  if (lane < DH / COLS) {
+  T out[COLS];
 #pragma unroll
-    for (int c = 0; c < COLS; ++c) a.o[((long)row * a.H + head) * DH + COLS * lane + c] = from_f32<T>(v[c] * scale);
+  for (int c = 0; c < COLS; ++c) out[c] = from_f32<T>(v[c] * scale);
+  T* const to = a.o + ((long)row * a.H + head) * DH + COLS * sub;
+  constexpr int BYTES = COLS * (int)sizeof(T);
+  if constexpr (COLS == 1) *to = out[0];
+  else if constexpr (BYTES == 4) *reinterpret_cast<uint32_t*>(to) = __builtin_bit_cast(uint32_t, out);
+  else if constexpr (BYTES == 8) *reinterpret_cast<uint2*>(to) = __builtin_bit_cast(uint2, out);
+  else {
+#pragma unroll
+    for (int c = 0; c < COLS; c += 16 / (int)sizeof(T)) {
+      T part[16 / sizeof(T)];
+#pragma unroll
+      for (int e = 0; e < 16 / (int)sizeof(T); ++e) part[e] = out[c + e];
+      *reinterpret_cast<uint4*>(to + c) = __builtin_bit_cast(uint4, part);
+    }
   }
-  if (a.lse && lane == 0) a.lse[(long)row * a.H + head] = (m + log2f(l)) * 0.6931471805599453f;
+  if (a.lse && sub == 0) a.lse[(long)row * a.H + head] = (m + log2f(l)) * 0.6931471805599453f;
 }
 
 // The join of 64 rows of 16 x 128, up to 4 splits: 4.5 us; of 1500 rows of 14 x 64, up to 4 splits: 9.5.
@@ -144,7 +206,12 @@ template <typename T> dipaco_status launch_attention_paged(PagedArgs<T> a, int d
     constexpr int DH = decltype(DHc)::value;
     if (dipaco_status st = p.wide_blocks ? launch_paged_both<DH>(a, p.wide_blocks, s) : launch_paged_narrow<DH>(a, s)) return st;
     if (p.narrow_splits > 1 || (p.wide_blocks && p.wide_splits > 1)) {
-      paged_join<DH, T><<<(a.T_rows * a.H + 3) / 4, 256, 0, s>>>(a, Divisor(a.H));
+      // Four heads a wave where rows and heads are more than the chip holds waves.  A call's us at one a wave | four: 1 x 2000 tokens, 14 heads of 64, 36 |
+      // 31; 1 x 512 over 8000, 16 of 128, 67.5 | 66; 1 x 128 over 16000, 14 of 64, 26 | 27; one over 30000, 32 of 128, 29 | 32.
+      const bool four = (int64_t)a.T_rows * a.H >= 256 * 32;
+      const int waves = four ? (a.H + 3) / 4 : a.H;   // of a row
+      if (four) paged_join<DH, T, 4><<<(a.T_rows * waves + 3) / 4, 256, 0, s>>>(a, Divisor(waves));
+      else paged_join<DH, T, 1><<<(a.T_rows * waves + 3) / 4, 256, 0, s>>>(a, Divisor(waves));
       DIPACO_LAUNCH_CHECK();
     }
     return DIPACO_OK;

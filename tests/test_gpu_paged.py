@@ -141,6 +141,14 @@ def test_tokens_beside_chunks(dtype, cached, new, H, Hkv, dh, page, window, sink
     check(dtype, cached, new, H, Hkv, dh, page, window, sinks, seed=16)
 
 
+@pytest.mark.parametrize("dtype", [dp.F32, dp.BF16])
+@pytest.mark.parametrize("cached,new,H,Hkv,dh,page,window,sinks", [
+    ([3000, 40], [1, 1800], 6, 3, 64, 32, ALL, 0), ([2000, 500, 0], [3, 850, 1], 10, 2, 32, 16, 1200, 5), ([700, 1500], [950, 2], 9, 9, 128, 64, ALL, 0)])
+def test_rows_of_many_waves(dtype, cached, new, H, Hkv, dh, page, window, sinks):
+    """more rows and heads than the chip holds waves, numbers of heads that four does not divide, documents of one split beside those of several"""
+    check(dtype, cached, new, H, Hkv, dh, page, window, sinks, seed=21)
+
+
 def guarded_workspace(n):
     """n bytes of 255 between two runs of 4096 bytes of 170"""
     whole = torch.full((n + 8192,), 170, dtype=torch.uint8, device=DEV)
