@@ -86,6 +86,9 @@ template <typename T> struct PagedArgs {
   __device__ __forceinline__ float2* part_state(int split, long row, int head) const { return state + ((long)split * T_rows + row) * H + head; }
 };
 
+// Workgroups of a launch of both kinds: n_wide of heads x splits x blocks, then those of splits x heads x documents
+struct PagedOrder { Divisor heads, head_splits; int n_wide; };
+
 // A block of packed rows of one document: which rows, the tiles that they see, and how many of these a split takes
 template <int SHIFT> struct PagedBlock {
   int b, row0, rows, packed0, packed, pos0, last;   // rows row0 .. of the call, `rows` of them; packed rows packed0 .. of `packed`; position of row 0; last one

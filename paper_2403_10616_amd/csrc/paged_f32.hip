@@ -2,7 +2,7 @@
 //
 // The table's entries are fetched 64 at a time, a lane each (16 positions an entry); a thread takes the page of the row that it moves from the
 // lane that holds it.  Rows that must not be read are replaced by the last position's, as in paged_mfma.hip.
-// Us: 5 documents of up to 40 tokens over up to 700, 8 heads of 32 on 2 13.4 (of which the join 3.5); 1 x 500 over 1000, 8 heads of 64, 31; one token over
+// Us: 5 documents of up to 40 tokens over up to 700, 8 heads of 32 on 2 12.5 (of which the join 3.5); 1 x 500 over 1000, 8 heads of 64, 31; one token over
 // 2000, 8 heads of 64, 9.7; 32 over up to 4000, 8 heads of 64 on 2, 17 (2.3 TB/s).
 #include "kernels.h"
 #include "window_f32.h"
@@ -14,17 +14,14 @@ namespace {
 using Cut = PagedCut<float>;
 
 // NARROW: 16 packed rows, which every wave holds; of a tile of 64 keys a wave takes 16.  Else 64 packed rows, 16 a wave, on tiles of 32 keys.
-template <int DH, bool NARROW>
-__global__ void __launch_bounds__(WF_THREADS, NARROW && DH == 128 ? 1 : 2) paged_f32(PagedArgs<float> a, int first) {
-  extern __shared__ __attribute__((aligned(16))) float pf_smem[];   // [stage][K | V]
+// b: the document, or the call's wide block; pf_smem: [stage][K | V]
+template <int DH, bool NARROW> __device__ __forceinline__ void paged_part(const PagedArgs<float>& a, int hk, int split, int b, float* pf_smem) {
   constexpr int SHIFT = NARROW ? Cut::NARROW_SHIFT : Cut::WIDE_SHIFT, TILE = 1 << SHIFT, RUNS = TILE / 16, AHEAD = 64 / RUNS;
   constexpr int STAGE = 2 * window_tile_floats<DH, TILE>();
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
   const Divisor& splits = NARROW ? a.narrow_splits : a.wide_splits;
-  const int hk = NARROW ? blockIdx.y : blockIdx.x;
-  int b = blockIdx.z + first, block = 0, cached;
+  int block = 0, cached;
   RowRange rows;
-  const int split = NARROW ? a.narrow_split(blockIdx.x, b * a.H_kv + hk) : blockIdx.y;
   if constexpr (NARROW) {
     rows = ragged_rows(a.row_start, b, a.T_rows);
     cached = a.cached(b);
@@ -146,6 +143,25 @@ __global__ void __launch_bounds__(WF_THREADS, NARROW && DH == 128 ? 1 : 2) paged
   }
 }
 
+template <int DH, bool NARROW> __global__ void __launch_bounds__(WF_THREADS, NARROW && DH == 128 ? 1 : 2) paged_f32(PagedArgs<float> a, int first) {
+  extern __shared__ __attribute__((aligned(16))) float pf_smem[];
+  const int hk = NARROW ? blockIdx.y : blockIdx.x, b = blockIdx.z + first;
+  paged_part<DH, NARROW>(a, hk, NARROW ? a.narrow_split(blockIdx.x, b * a.H_kv + hk) : blockIdx.y, b, pf_smem);
+}
+// Both kinds in a launch
+template <int DH> __global__ void __launch_bounds__(WF_THREADS, DH == 128 ? 1 : 2) paged_f32_both(PagedArgs<float> a, PagedOrder order) {
+  extern __shared__ __attribute__((aligned(16))) float pfb_smem[];
+  int i = blockIdx.x;
+  if (i < order.n_wide) {
+    const int block = order.head_splits(i), j = i - block * (int)order.head_splits.d, split = order.heads(j);
+    paged_part<DH, false>(a, j - split * a.H_kv, split, block, pfb_smem);
+    return;
+  }
+  i -= order.n_wide;
+  const int item = a.narrow_splits(i), b = order.heads(item);
+  paged_part<DH, true>(a, item - b * a.H_kv, a.narrow_split(i - item * (int)a.narrow_splits.d, item), b, pfb_smem);
+}
+
 template <int DH, bool NARROW> constexpr int paged_f32_lds() {
   return 2 * 2 * window_tile_floats<DH, 1 << (NARROW ? Cut::NARROW_SHIFT : Cut::WIDE_SHIFT)>() * (int)sizeof(float);
 }
@@ -163,6 +179,19 @@ template <int DH> dipaco_status launch_paged_narrow(const PagedArgs<float>& a, h
 }
 template <int DH> dipaco_status launch_paged_both(const PagedArgs<float>& a, int blocks, hipStream_t s) {
   static std::atomic<unsigned long long> lds_set{0};
+  // One launch where the compute units hold all its workgroups at once: the narrow ones' LDS, twice the wide ones', then keeps nobody waiting.  Us, two launches
+  // | one: 5 x up to 40 tokens over up to 700, 8 heads of 32 on 2, 13.6 | 12.5; 1 x 64 over 1000, 8 of 64, 16.7 | 15.7; 4 x up to 100 over up to 500, 8 of 128
+  // on 2, level; and a launch less of the host's time, 15.7 | 12.4 a call of the first through the Python binding.
+  constexpr int LDS = std::max(paged_f32_lds<DH, true>(), paged_f32_lds<DH, false>());
+  const int64_t wide = (int64_t)a.H_kv * a.wide_splits.d, groups = wide * blocks + (int64_t)a.B * a.H_kv * a.narrow_splits.d;
+  if (groups <= 256 * (163840 / LDS)) {
+    static std::atomic<unsigned long long> both_set{0};
+    if (dipaco_status st = ensure_dynamic_lds(reinterpret_cast<const void*>(paged_f32_both<DH>), LDS, both_set)) return st;
+    const PagedOrder order{Divisor(a.H_kv), Divisor((int)wide), (int)wide * blocks};
+    paged_f32_both<DH><<<(int)groups, WF_THREADS, LDS, s>>>(a, order);
+    DIPACO_LAUNCH_CHECK();
+    return DIPACO_OK;
+  }
   if (dipaco_status st = ensure_dynamic_lds(reinterpret_cast<const void*>(paged_f32<DH, false>), paged_f32_lds<DH, false>(), lds_set)) return st;
   for (int b = 0; b < blocks; b += 65535) {
     paged_f32<DH, false><<<dim3(a.H_kv, a.wide_splits.d, std::min(blocks - b, 65535)), WF_THREADS, paged_f32_lds<DH, false>(), s>>>(a, b);

@@ -333,9 +333,7 @@ template <int DH, int NW, int NS> __global__ void __launch_bounds__(WAVE * NW, 1
   const int hk = blockIdx.y, b = blockIdx.z + b0;
   narrow_document<DH, NW, NS>(a, hk, b, a.narrow_split(blockIdx.x, b * a.H_kv + hk), pn_smem);
 }
-// A call with wide blocks, and in the same launch behind them the narrow documents that it may have: n_wide workgroups of heads x splits x blocks, then
-// those of splits x heads x documents
-struct PagedOrder { Divisor heads, head_splits; int n_wide; };
+// A call with wide blocks, and in the same launch behind them the narrow documents that it may have
 template <int DH> __global__ void __launch_bounds__(AT_THREADS, 2) paged_both_mfma(PagedArgs<bf16> a, PagedOrder order) {
   extern __shared__ __attribute__((aligned(16))) char pb_smem[];
   int i = blockIdx.x;
