@@ -123,8 +123,8 @@ dipaco_status dipaco_k_cache_append(int32_t dtype, const void* qkv, const int32_
 
 /* Attention of the new tokens over the cache that they have been appended to (same row_start and cache_len), with the window
  * and sinks of dipaco_k_attention_window_fwd over positions: chunk by chunk, or token by token, the rows of that call.
- *   o [T, H*dh];  lse fp32 [T, H] or NULL.  A row that sees nothing (its pages are gone): o = 0, lse = -inf.  Rows of nobody
- *   are left as they were.  max_new: no document has more new tokens in this call (rows beyond it are left as they were).
+ *   o [T, H*dh];  lse fp32 [T, H] or NULL.  A row that sees nothing (its pages are gone): o = 0, lse = -inf; one whose visible
+ *   scores are all -inf: o = NaN, lse = -inf, as in that call.  Rows of nobody are left as they were.  max_new: no document has more new tokens in this call (rows beyond it are left as they were).
  * workspace: device, >= dipaco_k_attention_paged_workspace_bytes(...) (0 = invalid shape), contents undefined before and
  * after; calls that may overlap in time, captured ones included, need one each.  A value that is not finite reaches exactly
  * the rows that see it.  Results are bit-reproducible; those of one row may differ in rounding with the other rows of the call. */

@@ -48,6 +48,10 @@ struct Divisor {
   }
 };
 
+// The reference exponent of a row is -inf where it has seen nothing.  One that has seen scores, all of them -inf, has this instead once its keys are
+// through: it loses against every finite reference, and if it stays the row is 0 / 0 as its definition is, not the 0 of a row that sees nothing.
+constexpr float ALL_MINUS_INFINITY = -3.402823466e38f;
+
 template <typename T> struct PagedArgs {
   const T* qkv;              // [T rows, (H + 2 H_kv) dh]
   const int* row_start;      // [B + 1]
@@ -77,6 +81,15 @@ template <typename T> struct PagedArgs {
     if (at >= pages_per_doc) return -1;
     const int p = pages[(long)b * pages_per_doc + at];
     return (unsigned)p < (unsigned)n_pages ? p : -1;
+  }
+  // whether a row at position pos, whose window begins at `near`, sees any of the n keys from k0 on, none behind `last`; k0 is a multiple of 16, and so are
+  // pages' sizes: the keys of a run of 16 share one
+  __device__ __forceinline__ bool sees_any(int b, int pos, int near, int last, int k0, int n) const {
+    const int upto = min(min(pos, last), k0 + n - 1);
+#pragma unroll 1
+    for (int p = k0; p <= upto; p += 16)
+      if ((min(p + 15, upto) >= near || p < w.sinks) && page_of(b, p) >= 0) return true;
+    return false;
   }
   template <int DH> __device__ __forceinline__ long key_offset(int page, int hk, int slot) const {
     return ((((long)page * 2 * H_kv + hk) << page_shift) + slot) * DH;

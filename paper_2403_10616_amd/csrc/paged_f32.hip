@@ -95,6 +95,8 @@ template <int DH, bool NARROW> __device__ __forceinline__ void paged_part(const 
         }
       }
     }
+    for (int t = 0; t < n_tiles && __any(valid && x.m == -INFINITY); ++t)   // scores that were all -inf are not nothing (ALL_MINUS_INFINITY)
+      if (valid && x.m == -INFINITY && a.sees_any(b, pos, near, blk.last, (blk.tiles.at(t0 + t) << SHIFT) + (NARROW ? 16 * wave : 0), NARROW ? 16 : TILE)) x.m = ALL_MINUS_INFINITY;
   }
   if constexpr (NARROW) {   // the waves' sums meet in LDS: wave w adds columns 16 d + .. of every d with d % 4 = w
     constexpr int PER = DH / 16 * 4 * WAVE;

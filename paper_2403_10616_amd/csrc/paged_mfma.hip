@@ -79,6 +79,12 @@ __device__ __forceinline__ void add_seen(SoftmaxRow<DH>& x, const PagedArgs<bf16
   }
 }
 
+// a row whose scores so far were all -inf has seen something if it sees any of the n keys from k0 on
+template <int DH>
+__device__ __forceinline__ void note_seen(SoftmaxRow<DH>& x, const PagedArgs<bf16>& a, const PagePlace<DH>& at, const PagedRow<DH>& row, int k0, int n) {
+  if (row.valid && x.m == -INFINITY && a.sees_any(at.b, row.pos, row.near, at.last, k0, n)) x.m = ALL_MINUS_INFINITY;
+}
+
 // ---- wide ----------------------------------------------------------------------------------------------------------
 // pw_smem: [stage][K | V]
 template <int DH> __device__ __forceinline__ void wide_block(const PagedArgs<bf16>& a, int hk, int split, int block, char* pw_smem) {
@@ -159,6 +165,7 @@ template <int DH> __device__ __forceinline__ void wide_block(const PagedArgs<bf1
       plain::clear(x.o);
       for (int t = 0; t < n_tiles; ++t) add_seen<DH>(x, a, at, row, blk.tiles.at(t0 + t) * 64, 64, h);
     }
+    for (int t = 0; t < n_tiles && __any(row.valid && x.m == -INFINITY); ++t) note_seen<DH>(x, a, at, row, blk.tiles.at(t0 + t) * 64, 64);
   }
   asm volatile("" : "+v"(R));
   const PagedRow<DH> row(a, R, blk.packed, blk.row0, blk.pos0, hk);
@@ -276,6 +283,7 @@ template <int DH, int NW, int NS> __device__ __forceinline__ void narrow_documen
       plain::clear(x.o);
       for (int t = 0; t < n; ++t) add_seen<DH>(x, a, at, row, half_at(t), 32, h);
     }
+    for (int t = 0; t < n && __any(row.valid && x.m == -INFINITY); ++t) note_seen<DH>(x, a, at, row, half_at(t), 32);
   }
   // the waves' sums meet in LDS: wave w adds accumulator elements 4 g .. 4 g + 3 of every 32 columns for g = w, w + NW, ..
   constexpr int PER = 16 * DT * WAVE;

@@ -68,3 +68,35 @@ def backward(q, k, v, o, g, lse, mask, dtype):
         dv[:, y] += p.T @ gg
         ev[:, y] += ((rel + extra) * p).T @ gg.abs() + terms_k * (p.T @ gg.abs())
     return dq, dk, dv, eq + h * dq.abs(), ek + h * dk.abs(), ev + h * dv.abs()
+
+
+def inside(got, want, bound, what=""):
+    """Every element of `got` is within `bound` of `want`.  Nothing passes that is not shown to: where `want` is finite `got` has to be
+    finite too (a NaN compares as neither inside nor outside), an infinity has to be that infinity and a NaN a NaN."""
+    got, want = got.double().cpu(), want.double()
+    same = (got == want) | (torch.isnan(got) & torch.isnan(want))
+    near = torch.isfinite(want) & torch.isfinite(got) & ((got - want).abs() <= bound + 1e-30)
+    out = ~(same | near)
+    at = out.nonzero()[:3].tolist()
+    assert not bool(out.any()), f"{what}: {int(out.sum())} of {out.numel()} out of bounds, among them {[(i, float(got[tuple(i)]), float(want[tuple(i)])) for i in at]}"
+
+
+def definition(q, k, v, mask):
+    """o and lse in 64 bits for inputs of any value: a sum runs over the pairs of the mask alone, so that a value that is not finite
+    reaches exactly the rows that see it.  A row that sees nothing has o = 0 and lse = -inf; one whose visible scores are all -inf has
+    o = NaN (0 / 0) and lse = -inf."""
+    n, H, dh = q.shape
+    G, c = H // k.shape[1], 1.0 / math.sqrt(dh)
+    o, lse = torch.zeros((n, H, dh), dtype=torch.float64), torch.full((n, H), -math.inf, dtype=torch.float64)
+    for i in range(n):
+        j = mask[i].nonzero()[:, 0]
+        if len(j):
+            kk, vv = k[j].repeat_interleave(G, 1), v[j].repeat_interleave(G, 1)          # [keys, H, dh]
+            s = (q[i] * kk).sum(2) * c
+            top = s.amax(0)                                                              # NaN where a score is
+            p = torch.exp(s - top)                                                       # NaN where top is infinite
+            p = torch.where(torch.isinf(top) & (top < 0), torch.zeros_like(p), p)        # all -inf: a sum of zeros
+            total = p.sum(0)
+            o[i] = (p[:, :, None] * vv).sum(0) / total[:, None]
+            lse[i] = top + torch.log(total)
+    return o, lse

@@ -39,3 +39,38 @@ def test_reference_is_what_automatic_differentiation_gives(n, H, Hkv, dh, window
             step[at] = 1e-5
             slope = ((_dense(x + step, H, Hkv, dh, mask) - _dense(x - step, H, Hkv, dh, mask)) * d_o).sum() / 2e-5
             assert abs(float(slope - got[at])) <= 1e-8
+
+
+@pytest.mark.parametrize("got,want,fine", [(1.0, 1.0, True), (1.0 + 1e-3, 1.0, True), (1.1, 1.0, False), (math.nan, 1.0, False), (math.inf, 1.0, False), (1.0, math.nan, False),
+                                           (1.0, math.inf, False), (math.inf, math.inf, True), (-math.inf, math.inf, False), (math.nan, math.nan, True), (math.nan, -math.inf, False)])
+@pytest.mark.parametrize("bound", [2e-3, math.inf])
+def test_a_value_is_inside_its_bound_only_if_it_is_shown_to_be(got, want, fine, bound):
+    fine = fine or (bound == math.inf and math.isfinite(got) and math.isfinite(want))
+    g, w = torch.zeros(2, 3), torch.zeros(2, 3, dtype=torch.float64)
+    g[1, 2], w[1, 2] = got, want
+    if fine:
+        ref.inside(g, w, torch.full_like(w, bound))
+    else:
+        with pytest.raises(AssertionError):
+            ref.inside(g, w, torch.full_like(w, bound))
+
+
+def test_the_definition_of_rows_that_see_infinities_and_nothing():
+    g = torch.Generator().manual_seed(4)
+    q, k, v = (torch.randn(6, 2, 4, generator=g, dtype=torch.float64) for _ in range(3))
+    mask = ref.sees(0, 6, 6, 3, 1)
+    o, lse = ref.definition(q, k, v, mask)
+    wo, wl, _, _ = ref.forward(q, k, v, mask, torch.float32)
+    torch.testing.assert_close(o, wo, rtol=1e-12, atol=1e-12)
+    torch.testing.assert_close(lse, wl, rtol=1e-12, atol=1e-12)
+    q[:, :, 0] = -q[:, :, 0].abs()
+    k[0, :, 0] = math.inf                       # every row sees key 0: row 0 nothing else, the others with probability 0
+    mask[4] = False
+    o, lse = ref.definition(q, k, v, mask)
+    assert bool(torch.isnan(o[0]).all()) and bool((lse[0] == -math.inf).all())
+    assert not o[4].any() and bool((lse[4] == -math.inf).all())
+    m2 = mask.clone()
+    m2[:, 0] = False
+    wo, wl = ref.definition(q[1:4], k, v, m2[1:4])
+    torch.testing.assert_close(o[1:4], wo, rtol=1e-12, atol=1e-12)
+    torch.testing.assert_close(lse[1:4], wl, rtol=1e-12, atol=1e-12)
