@@ -114,7 +114,10 @@ dipaco_status dipaco_k_attention_window_bwd(int32_t dtype, const void* qkv, cons
  *   row_start  device int32 [B + 1], not decreasing, 0 .. T: rows row_start[b] .. row_start[b+1] - 1 are the new tokens
  *              of document b, none or more.  Rows behind row_start[B] belong to nobody.
  *   cache_len  device int32 [B]: positions that document b had in front of them: its first new token is position
- *              cache_len[b].  All of these are read on the device: a captured graph follows their values.
+ *              cache_len[b], 0 .. 2^31 - 2^24 (values outside are taken as the nearest inside).  A position behind the table,
+ *              pages_per_doc * page_size or more, has no page: it is not written, nobody sees it, and its row sees what of
+ *              the table lies in its window or among the sinks.
+ *              All of these are read on the device: a captured graph follows their values.
  * T <= 2^23, T * H <= 2^25, B <= 2^20, B * H <= 2^22, pages_per_doc * page_size <= 2^28.
  * dipaco_k_cache_append writes the new tokens' keys and values into the pages. */
 dipaco_status dipaco_k_cache_append(int32_t dtype, const void* qkv, const int32_t* row_start, const int32_t* cache_len,

@@ -1178,8 +1178,7 @@ dipaco_status dipaco_k_attention_paged(int32_t dtype, const void* qkv, const int
   if (workspace_bytes < paged_workspace_bytes(T, H, dh, page_size, pages_per_doc))
     return fail(DIPACO_EWORKSPACE, "workspace smaller than dipaco_k_attention_paged_workspace_bytes");
   hipStream_t st = static_cast<hipStream_t>(stream);
-  const int most = pages_per_doc * page_size + T;   // positions
-  const Window w{std::min(window, most), std::min(sinks, most)};
+  const Window w{window, sinks};   // whole: positions may lie beyond the table
   return dtype == DIPACO_BF16
              ? launch_attention_paged(paged_args<bf16>(qkv, row_start, cache_len, pages, cache, o, lse, T, B, max_new, H, H_kv, n_pages, page_size,
                                                        pages_per_doc, w), dh, workspace, st)

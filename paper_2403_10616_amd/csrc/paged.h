@@ -23,7 +23,7 @@ template <int SHIFT> struct TileList {
   __device__ __forceinline__ TileList() : near(0), first(0), count(0) {}
   __device__ __forceinline__ TileList(const Window& w, int lo, int hi) {
     const int from = w.near_from(lo);
-    first = min(from >> SHIFT, (hi >> SHIFT) + 1);   // hi lies in front of the window only where a document outgrows its table
+    first = min(from >> SHIFT, (hi >> SHIFT) + 1);   // hi, the table's last position, lies in front of the window where a document has outgrown it
     near = (hi >> SHIFT) + 1 - first;
     count = near + min((min(w.sinks, from) + (1 << SHIFT) - 1) >> SHIFT, first);
   }
@@ -74,7 +74,9 @@ template <typename T> struct PagedArgs {
     return s - narrow_splits(s) * (int)narrow_splits.d;
   }
   __device__ __forceinline__ int capacity() const { return pages_per_doc << page_shift; }
-  __device__ __forceinline__ int cached(int b) const { return min(max(cache_len[b], 0), capacity()); }
+  // A document may have outgrown its table: its rows keep their positions, and see of the table what the window and the sinks reach.  The bound is
+  // arithmetic's: a row's position, at most 2^23 behind, stays below 2^31.
+  __device__ __forceinline__ int cached(int b) const { return min(max(cache_len[b], 0), 0x7f000000); }
   // the page of a position, or -1 where the table holds none
   __device__ __forceinline__ int page_of(int b, int pos) const {
     const int at = pos >> page_shift;

@@ -1,4 +1,4 @@
-"""Attention over a paged cache at its edges: rows whose visible scores are infinite."""
+"""Attention over a paged cache at its edges: rows whose visible scores are infinite, documents that have outgrown their table."""
 import math
 
 import pytest
@@ -7,7 +7,7 @@ import torch
 import attention_reference as ref
 import paper_2403_10616_amd as dp
 from gpu_util import DEV
-from test_gpu_paged import Cache, i32
+from test_gpu_paged import Cache, i32, starts_of
 from test_gpu_window import ALL, TDT, draw, fwd, heads_of
 
 pytestmark = pytest.mark.gpu
@@ -75,3 +75,35 @@ def test_a_row_whose_visible_scores_are_all_minus_infinity_is_not_a_row_that_see
 @pytest.mark.parametrize("cached,new,window,keys", [(0, 1, ALL, [0]), (0, 70, 1, [0, 69]), (2000, 1, ALL, [1234]), (1500, 90, 40, [1490, 1530]), (2000, 1, ALL, range(2001))])
 def test_a_score_that_is_infinite_or_no_number_reaches_the_rows_that_see_it(dtype, value, cached, new, window, keys):
     rows_over_infinite_keys(dtype, cached, new, 2, 1, 64, 16, window, 0, list(keys), value)
+
+
+@TYPES
+@pytest.mark.parametrize("dh,page", [(32, 16), (64, 32), (128, 16)])
+@pytest.mark.parametrize("H,Hkv", [(2, 2), (4, 1)])
+@pytest.mark.parametrize("cached,new,window,sinks", [
+    ([70, 64, 60], [1, 1, 1], 20, 0), ([70, 64, 60], [3, 30, 30], 20, 2), ([70, 64, 3], [1, 60, 90], 20, 0), ([90, 0, 64], [40, 5, 1], ALL, 0),
+    ([1 << 30, (1 << 28) + 7, 1000], [2, 33, 1], ALL, 0), ([(1 << 30) - 5, 1 << 29, 100], [9, 1, 40], (1 << 31) - 1, 0), ([1 << 30, 84, 83], [1, 1, 1], 20, 5)])
+def test_rows_of_a_document_that_has_outgrown_its_table(dtype, dh, page, H, Hkv, cached, new, window, sinks):
+    """64 positions a table: rows keep their positions, and see of the table what a row at such a position sees"""
+    print(f"outgrown dtype={dtype} cached={cached} new={new} H={H} Hkv={Hkv} dh={dh} page={page} W={window} sinks={sinks}", flush=True)
+    t, room, B = TDT[dtype], 64, len(cached)
+    c = Cache(dtype, [room] * B, Hkv, dh, page, 3)
+    data = draw(tuple(c.data.shape), 5, dtype)
+    c.data.copy_(data)
+    st = starts_of(new)
+    x = draw((st[-1], (H + 2 * Hkv) * dh), 6, dtype)
+    rows = x.to(DEV)
+    dp.dipaco_k_cache_append(dtype, rows, i32(st), i32(cached), c.pages, c.data, st[-1], B, H, Hkv, dh, c.n_pages, page, c.per_doc)
+    for b, (m, n) in enumerate(zip(cached, new)):
+        for p in range(m, min(m + n, room)):
+            data[c.table[b][p // page], :, :, p % page] = x[st[b] + p - m, H * dh:].reshape(2, Hkv, dh)
+    assert torch.equal(c.data.cpu(), data)
+    o, lse = c.attend(rows, st, cached, H, max(new), window, sinks)
+    for b, (m, n) in enumerate(zip(cached, new)):
+        kv = torch.cat([data[p] for p in c.table[b]], 2).double().permute(2, 0, 1, 3)           # [position, 2, Hkv, dh]
+        mask = ref.sees(m, n, room, window, sinks)
+        q = heads_of(x[st[b]:st[b + 1]], n, H, Hkv, dh)[0]
+        wo, wl = ref.definition(q, kv[:, 0], kv[:, 1], mask)
+        _, _, eo, el = ref.forward(q, kv[:, 0], kv[:, 1], mask, t)
+        ref.inside(o[st[b]:st[b + 1]].reshape(n, H, dh), wo, eo, f"o[{b}]")
+        ref.inside(lse[st[b]:st[b + 1]], wl, el.nan_to_num(), f"lse[{b}]")
