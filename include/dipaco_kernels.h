@@ -92,7 +92,9 @@ dipaco_status dipaco_k_attention_bwd(int32_t dtype, const void* qkv, const void*
  *   lengths: NULL, or device int32 [B]: document b is the first lengths[b] of its S rows (taken as 0 below 0, as S above).
  *   Rows behind it are padding: they are not read, whatever they hold, and o, lse and dqkv are written 0 there.
  * A value that is not finite reaches exactly the rows that see it.  B * S < 2^31, H * S <= 2^25,
- * (H + 2*H_kv) * dh <= 2^20.  Results are bit-reproducible. */
+ * (H + 2*H_kv) * dh <= 2^20.  Results are bit-reproducible.
+ * bf16, here, in the gradient and over a paged cache, as in dipaco_k_attention_*: probabilities (and dS) enter their products with 16 bits for dh 32
+ * and 128, whose results are as exact as their rounding to bf16, and rounded to bf16 for dh 64; sums, lse and D are fp32. */
 dipaco_status dipaco_k_attention_window_fwd(int32_t dtype, const void* qkv, const int32_t* lengths, void* o, float* lse,
                                             int32_t B, int32_t S, int32_t H, int32_t H_kv, int32_t dh, int32_t window,
                                             int32_t sinks, void* stream);

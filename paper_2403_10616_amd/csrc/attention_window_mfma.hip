@@ -139,11 +139,20 @@ __global__ void __launch_bounds__(AT_THREADS) window_stats_mfma(WindowArgs a, co
 
 // acc^T[dt] += (tile^T)[columns 32 dt .., the 32 rows from `tile` on] . src
 template <int DT> __device__ __forceinline__ void mma_transposed_half(f32x16 (&acc)[DT], const char* tile, const TrOff& to, const f32x16& src) {
-  const uint4 p0 = pack8<0>(src), p1 = pack8<8>(src);
+  if constexpr (split_p<32 * DT>()) {   // half a fragment at a time (attention_mfma.h: mma_transposed)
+    const auto p0 = p_frag<true, 0>(src);
 #pragma unroll
-  for (int dt = 0; dt < DT; ++dt) {
-    acc[dt] = mfma16(tr_read(tile, to, dt, 0), p0, acc[dt]);
-    acc[dt] = mfma16(tr_read(tile, to, dt, 1), p1, acc[dt]);
+    for (int dt = 0; dt < DT; ++dt) acc[dt] = mfma_p(tr_read(tile, to, dt, 0), p0, acc[dt]);
+    const auto p1 = p_frag<true, 8>(src);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) acc[dt] = mfma_p(tr_read(tile, to, dt, 1), p1, acc[dt]);
+  } else {
+    const uint4 p0 = pack8<0>(src), p1 = pack8<8>(src);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+      acc[dt] = mfma16(tr_read(tile, to, dt, 0), p0, acc[dt]);
+      acc[dt] = mfma16(tr_read(tile, to, dt, 1), p1, acc[dt]);
+    }
   }
 }
 

@@ -11,8 +11,10 @@
 // (530 TFLOP/s of visible pairs), window 2048 160; 2 x up to 32768, 16 heads of 128 on 4, window 4096 1750 (950); 8 x 2048, 8 heads of 128, causal 90
 // (attention_mfma.h: 112).
 //
-// Probabilities are rounded to bf16 where the second product multiplies them (2^-8 of each, the size of the output's own rounding);
-// their sum is taken in fp32 before that, so that lse keeps fp32's digits.
+// Probabilities enter the second product as in attention_mfma.h: as two bf16 numbers, 16 bits in all, for head sizes 32 and 128 (the output's own rounding hides
+// the rest), rounded to bf16 for head size 64 (half a step of 2^-8 each, the size of the output's rounding).  Their sum is taken in fp32 before that, so
+// that lse keeps fp32's digits.  Two numbers cost head size 128 a quarter to a third: 2 x up to 32768 positions, 16 heads on 4, window 4096, 1800 -> 2300 - 2450 us,
+// its gradient on 4 x up to 8000, window 1000, 945 -> 1130 - 1190.
 #pragma once
 #include "attention_mfma.h"
 #include "paged.h"
@@ -130,11 +132,11 @@ __device__ __forceinline__ void attend_half(SoftmaxRow<DH>& x, const uint4 (&qf)
 #pragma unroll
   for (int e = 0; e < 16; e += 2) { s0 += st[e]; s1 += st[e + 1]; }
   x.l += s0 + s1;
-  const uint4 p0 = pack8<0>(st), p1 = pack8<8>(st);
+  const auto p0 = p_frag<split_p<DH>(), 0>(st), p1 = p_frag<split_p<DH>(), 8>(st);
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) {
-    x.o[dt] = mfma16(vf[dt][0], p0, x.o[dt]);
-    x.o[dt] = mfma16(vf[dt][1], p1, x.o[dt]);
+    x.o[dt] = mfma_p(vf[dt][0], p0, x.o[dt]);
+    x.o[dt] = mfma_p(vf[dt][1], p1, x.o[dt]);
   }
 }
 // a tile of 64 keys: the halves that are seen.  force: bounds to apply whatever the span says
