@@ -201,9 +201,11 @@ __device__ __forceinline__ void store_keys(f32x4 (&dk)[DH / 16], f32x4 (&dv)[DH 
 }
 
 // dK and dV: 64 keys of a key head over the queries that see them under the window alone; or 16 sinks over all queries behind them, the
-// waves two and two on the halves of a stage, for dV and for dK, whole or in parts (attention_window_mfma.hip).  Fewer blocks of keys than compute units
-// are taken 16 keys a workgroup too, us: 1 x 2000, 8 heads of 64 on 2, causal (64 blocks) 737 -> 383; 1 x 4096, 8 on 2, window 512 (128) 273 -> 205; 2 x 1000, 8
-// heads, causal (256) 133 | 133; 1 x 2048, 14 heads, window 256 (448) 106 -> 127.
+// waves two and two on the halves of a stage, for dV and for dK, whole or in parts (attention_window_mfma.hip).  A launch of few blocks of keys takes 16 keys a
+// workgroup too: fewer than compute units (head size 128: than 160) where heads share keys, fewer than 64 where each has its own.  us whole | shared, head size 64,
+// then 128: 1 x 2048, 16 heads on 4, window 256 (128 blocks) 144 | 104, 237 | 212; 24 on 6 (192) 158 | 147, 260 | 304; 64: 1 x 2000, 8 on 2, causal (64) 735 | 383;
+// heads of their own: 1 x 300, 8 heads, window 64 (40) 18.2 | 16.1, 28.7 | 25.0; 1 x 512, 8, causal (64) 53.4 | 54.3, 91 | 95; 1 x 1024, 8, window 256 (128) 36 | 44,
+// 61 | 102; 14, window 64 (224) 25 | 32.5, 42 | 62, causal 130 | 121, 234 | 303.
 template <int DH, int KIND>
 __device__ __forceinline__ void window_dkv_f32(const FWindowArgs& a, const float* __restrict__ d_o, const float* __restrict__ dsum, float* __restrict__ dqkv, int b,
                                                int hk, int k0, float* smem, const FSinkParts& sp, int part) {
@@ -429,7 +431,11 @@ dipaco_status launch_window_bwd_f32(const float* qkv, const int* lengths, const 
   const FWindowArgs a{qkv, lengths, B, S, H, H_kv, w};
   const int nb = (S + WF_ROWS - 1) / WF_ROWS, G = H / H_kv;
   int sink_blocks = w.window >= S ? 0 : (std::min(w.sinks, S) + 15) / 16;
-  FSinkParts sp{sink_blocks, 1, (32 + H - 1) / H};   // as in attention_window_mfma.hip; stages of 32 queries
+  // As in attention_window_mfma.hip; stages of 32 queries, eight or more a part, 768 workgroups at a time.  us whole | cut (stages, those of the rest): 1 x 8192, 8
+  // heads of 64 on 2, window 512 (1024, 50) 1400 | 320; 1 x 2048, 14 of 64, window 256 (64, 12) 130 | 104; 1 x 1000, 8, window 100 (32, 2) 51 | 46; 1 x 700, window
+  // 64 (22, 1) 37 | 41; 1 x 16384, 14, window 1024 (512, 326) 1732 | 1721; 4 x 4000, 8 on 4, window 1000 (250, 178) 864 | 871; window 500, 8 heads (125, 94) 514 |
+  // 529.  The first four with four stages a part 321, 99, 41, 33.5, with sixteen 328, 114, 56, 38.
+  FSinkParts sp{sink_blocks, 1, (32 + H - 1) / H};
   const int64_t stages = (int64_t)G * ((S + 31) / 32), rest = (int64_t)2 * B * H * nb * ((w.window + 64) / 32 + 1) / 768;
   if (sink_blocks && stages > rest + 24 && 10 * stages > 18 * rest) sp.parts = (int)std::min<int64_t>(stages / 8, S / ((int64_t)H_kv * sink_blocks * sp.rows));
   window_stats_f32<DH><<<B * H * ((S + 127) / 128 * 2), WF_THREADS, 0, s>>>(a, o, d_o, lse, dsum);
@@ -443,7 +449,7 @@ dipaco_status launch_window_bwd_f32(const float* qkv, const int* lengths, const 
     DIPACO_LAUNCH_CHECK();
     sink_blocks = 0;
   }
-  const bool shared = (int64_t)B * H_kv * nb < 256;   // F_KEYS_SHARED: fewer workgroups than compute units
+  const bool shared = (int64_t)B * H_kv * nb < (G == 1 ? 64 : DH == 128 ? 160 : 256);   // F_KEYS_SHARED, as measured at window_dkv_f32
   window_bwd_f32<DH><<<B * H_kv * (sink_blocks + (shared ? 4 : 1) * nb) + B * H * nb, WF_THREADS, LDS, s>>>(a, d_o, dsum, dqkv, sink_blocks, shared);
   DIPACO_LAUNCH_CHECK();
   return DIPACO_OK;

@@ -237,8 +237,11 @@ template <int DH> __device__ __forceinline__ void window_dq(const WindowArgs& a,
 // Keys: 128 of a key head, 32 a wave, over the queries of every head of the group that see them under the window alone; the stages hold 64
 // queries.  Sinks are seen by all queries behind them, a multiple of what the other keys take, so a workgroup takes only 32 of them (SINKS):
 // its waves share the stage, two of them on each half of it, one for dV and one for dK, and the halves' sums meet at the end.
-// A launch of fewer blocks of keys than compute units is made of such workgroups altogether (KEYS_SHARED), us: 1 x 8192, 8 heads of 64 on 1, window 512 (64
-// blocks) 150 -> 79; 2 x 1000, 8 heads, causal (128) 39 -> 35; 1 x 2048, 14 heads, window 256 (224) 40 -> 38.5; 8 x 512, 8 heads (256) 31 -> 37.
+// A launch of few blocks of keys is made of such workgroups altogether (KEYS_SHARED): fewer than compute units where heads share keys (a block then takes the
+// queries of a whole group and outlasts dQ's), fewer than 112 where each head has its own.  us whole | shared, head size 64, then 128: 1 x 8192, 8 heads on 1, window 512 (64 blocks)
+// 146 | 80, 297 | 153; 1 x 4096, 16 on 4, window 256 (128) 57 | 42, 108 | 85; 2 x 4096, 12 on 3, window 1000 (192) 146 | 134, 305 | 299, window 256 60 | 56, 115 |
+// 123; heads of their own: 1 x 512, 8 heads, causal (32) 22 | 17, 42 | 29; 1 x 2048, 6, window 256 (96) 20.3 | 19.2, 39 | 36.5; 8 heads (128) 18.9 | 20.1, 37 | 46,
+// causal 59 | 56, 125 | 103; 10 heads, causal (160) 64 | 58.5, 131 | 127; 14 heads (224) 66.5 | 71.5, 139 | 144, window 256 25.6 | 32, 47 | 65.
 // Where a workgroup for 32 sinks would still be the longest by far, the queries are cut among `parts` workgroups, whose sums lie in the rows of dqkv that dQ is
 // written to afterwards (SinkParts), and window_sinks_join adds them.  1 x 32768 positions, 16 heads of 128 on 4, window 1024, 16 sinks: 2995 us
 // uncut (without sinks 1082), 1155 cut; 8 heads of 64 on 1, 8192 positions, window 512, 4 sinks 819 | 170.
@@ -582,7 +585,7 @@ dipaco_status launch_window_bwd_mfma(const bf16* qkv, const int* lengths, const 
     DIPACO_LAUNCH_CHECK();
     sink_blocks = 0;
   }
-  const bool shared = (int64_t)B * H_kv * nb < 256;   // KEYS_SHARED: fewer workgroups than compute units
+  const bool shared = (int64_t)B * H_kv * nb < (G == 1 ? 112 : 256);   // KEYS_SHARED, as measured at window_dkv
   auto run = [&](auto SHAREDc) -> dipaco_status {
     constexpr bool SHARED = decltype(SHAREDc)::value;
     static std::atomic<unsigned long long> lds_set{0};
