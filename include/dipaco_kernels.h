@@ -1,9 +1,10 @@
 /*
  * dipaco_kernels.h - kernel-level entry points of libdipaco.so.
  *
- * These expose single kernels of the path step (Algorithm 1 inner loop of arXiv 2403.10616: the pieces of
+ * Most expose single kernels of the path step (Algorithm 1 inner loop of arXiv 2403.10616: the pieces of
  * f(x, theta_i) and its gradient) so that each can be checked against its plain definition and timed against
- * its own roofline.  They follow the conventions of dipaco.h: caller-owned device pointers, 16-byte aligned,
+ * its own roofline.  Attention with a window and over a paged cache stands beside them for programs that score or continue
+ * text piece by piece; no step calls it.  They follow the conventions of dipaco.h: caller-owned device pointers, 16-byte aligned,
  * work enqueued on `stream`, non-zero status = nothing enqueued.  dtype is a dipaco_dtype: the element type of
  * every `void*` operand (fp32 or bf16); accumulation is always fp32.
  */

@@ -1,8 +1,8 @@
 // fp32 attention with a sliding window and sinks over packed rows of a padded batch, forward and backward (window_f32.h).
 //
 // A workgroup takes 64 queries (keys) of a head, 16 a wave.  Bound by the fp32 matrix cores on whole 16 x 16 tiles.  Us, forward | backward: 16 x 2048
-// positions, 14 heads of 64, window 512, 4 sinks 540 | 1685 (98 | 79 TFLOP/s of what is needed; the backward pass multiplies 7 / 5 of it); 8 x 500, 8 heads of
-// 64, window 100 24 | 51; 1 x 8192, 8 heads of 64 on 2, window 512, 4 sinks 96 | 322.  Rows that end with results that are not finite are taken again over the pairs that
+// positions, 14 heads of 64, window 512, 4 sinks 525 | 1682 (101 | 79 TFLOP/s of what is needed; the backward pass multiplies 7 / 5 of it); 8 x 500, 8 heads of
+// 64, window 100 21 | 51; 1 x 8192, 8 heads of 64 on 2, window 512, 4 sinks 96 | 322.  Rows that end with results that are not finite are taken again over the pairs that
 // see each other alone (attention_plain.h).
 #include "kernels.h"
 #include "window_f32.h"

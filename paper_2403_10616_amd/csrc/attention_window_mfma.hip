@@ -1,8 +1,8 @@
 // bf16 attention with a sliding window and sinks over packed rows of a padded batch (window_mfma.h has the forward pass's inner loops).
 //
 // Backward: dQ per block of 128 queries and dK / dV per block of 128 keys, each forming S and dO.V^T anew (seven products where one pass would need five), so
-// that every output has one writer and a fixed order of sums.  Us: 16 x 2048, 14 heads of 64, window 512, 4 sinks 305 (the statistics 22 of them); 4 x 8000, 16
-// heads of 128 on 4, window 1000 1020; 8 x 2048, 8 heads of 128, causal 273 (attention_mfma.h: 354).
+// that every output has one writer and a fixed order of sums.  Us: 16 x 2048, 14 heads of 64, window 512, 4 sinks 310 (the statistics 23 of them); 4 x 8000, 16
+// heads of 128 on 4, window 1000 1335; 8 x 2048, 8 heads, causal, of 128 338 (attention_mfma.h on the same box 352), of 64 139 (154).
 //
 // Rows that a wave ends with results that are not finite are taken again over the pairs that see each other alone (attention_plain.h says
 // why), so that such values reach exactly the rows that see them.
@@ -243,8 +243,8 @@ template <int DH> __device__ __forceinline__ void window_dq(const WindowArgs& a,
 // 123; heads of their own: 1 x 512, 8 heads, causal (32) 22 | 17, 42 | 29; 1 x 2048, 6, window 256 (96) 20.3 | 19.2, 39 | 36.5; 8 heads (128) 18.9 | 20.1, 37 | 46,
 // causal 59 | 56, 125 | 103; 10 heads, causal (160) 64 | 58.5, 131 | 127; 14 heads (224) 66.5 | 71.5, 139 | 144, window 256 25.6 | 32, 47 | 65.
 // Where a workgroup for 32 sinks would still be the longest by far, the queries are cut among `parts` workgroups, whose sums lie in the rows of dqkv that dQ is
-// written to afterwards (SinkParts), and window_sinks_join adds them.  1 x 32768 positions, 16 heads of 128 on 4, window 1024, 16 sinks: 2995 us
-// uncut (without sinks 1082), 1155 cut; 8 heads of 64 on 1, 8192 positions, window 512, 4 sinks 819 | 170.
+// written to afterwards (SinkParts), and window_sinks_join adds them.  1 x 32768 positions, 16 heads of 128 on 4, window 1024, 16 sinks: 3435 us
+// uncut (without sinks 1378), 1449 cut; 8 heads of 64 on 1, 8192 positions, window 512, 4 sinks 772 | 106.
 template <int DH> constexpr int window_dkv_stage() { return 2 * tile_bytes<DH>() + 2 * 64 * (int)sizeof(float); }   // Q | dO | -lse log2(e) | -D
 
 // where a wave's sums of its keys (a lane pair each) are not finite: the pairs that see each other alone
@@ -548,9 +548,10 @@ dipaco_status launch_window_fwd_mfma(const bf16* qkv, const int* lengths, bf16* 
     return DIPACO_OK;
   };
   // Two groups where the longest block's tiles, at least seven of them, are the launch's length: the blocks' tiles together are no more than 256 compute units
-  // take in that time.  us one -> two (blocks, tiles): 1 x 2048, 14 heads of 64, window 512 (224, 11) 16.6 -> 14.6; 1 x 2000, 8 heads, causal (128, 32) 32.7 ->
-  // 24.7; 2 x 2048, 14 heads, causal (448, 32) 38.3 -> 31.4; 8 x 512, 8 heads, causal (256, 8) 12.0 -> 11.7; beyond: 1 x 4096, 14 heads, window 512 (448, 11)
-  // 23.6 -> 25.6; 4 x 300, 8 heads, window 64 (96, 4) 8.2 -> 9.0; 1 x 300, 4 heads of 128, causal (12, 6) 10.2 -> 11.7.
+  // take in that time.  us one -> two (blocks, tiles), head size 64, then 128: 1 x 2048, 14 heads, window 512 (224, 11) 16.5 -> 14.3, 26.8 -> 25.3; 1 x 2000, 8
+  // heads, causal (128, 32) 32.8 -> 24.7, 53 -> 44; 2 x 2048, 14 heads, causal (448, 32) 35.5 -> 30.6, 64 -> 59; 8 x 512, 8 heads, causal (256, 8) 11.2 -> 10.7,
+  // 18.1 -> 18.7; beyond: 1 x 4096, 14 heads, window 512 (448, 11) 21.3 -> 24.5, 39 -> 46; 4 x 300, 8 heads, window 64 (96, 4) 7.0 -> 7.6; 1 x 300, 4 heads of
+  // 128, causal (12, 6) 11.4 -> 12.2.
   const int tiles = std::min((w.window + w.sinks + 127) / 64 + 1, 2 * nqb), mean = std::min(tiles, nqb + 1);
   return tiles >= 7 && (int64_t)blocks * mean <= 256LL * tiles ? run(std::integral_constant<int, 2>{}) : run(std::integral_constant<int, 1>{});
 }
@@ -569,7 +570,7 @@ dipaco_status launch_window_bwd_mfma(const bf16* qkv, const int* lengths, const 
   int sink_blocks = w.window >= S ? 0 : (std::min(w.sinks, S) + 31) / 32;
   // Parts of the sinks' queries, of 16 stages each or as many as the rows hold, where a workgroup that took them all would outlast the rest of the launch,
   // 512 workgroups at a time, by more than the two launches cost.  us whole | cut: the two of window_dkv; 4 x 8000 positions, 16 heads of 128 on 4, window
-  // 1000, 16 sinks (1.7 times the rest) 1069 | 1098; 16384, 14 of 64, window 1024 (1.9 times) 299 | 281; 2048, 14 of 64, window 256 (26 stages more) 41.5 | 49.
+  // 1000, 16 sinks (1.7 times the rest) 1329 | 1340; 16384, 14 of 64, window 1024 (1.9 times) 287 | 277; 2048, 14 of 64, window 256 (26 stages more) 39.5 | 54.
   SinkParts sp{sink_blocks, 1, (128 + H - 1) / H};
   const int64_t stages = (int64_t)G * ((S + 63) / 64), rest = (int64_t)2 * B * H * nb * ((w.window + 128) / 64 + 1) / 512;
   if (sink_blocks && stages > rest + 40 && 10 * stages > 18 * rest)

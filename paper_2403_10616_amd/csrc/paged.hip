@@ -1,8 +1,8 @@
 // Serving: keys and values of new tokens into a paged cache, and attention of these tokens over it (paged.h has the layout).
 //
 // append: a wave per row copies its k | v into the row's slot, 16 bytes a lane.  Bound by latency (a row's place takes three dependent
-// loads: its document, the document's length, the page) and, for whole chunks, by the bytes: 64 tokens of 14 x 64 3.0 us, 8 x up to 2000 of 8 x 128 17 us
-// (5.7 TB/s read and written).
+// loads: its document, the document's length, the page) and, for whole chunks, by the bytes: 35 tokens of 64 documents, 14 x 64, 3.0 us, 11984 tokens of 8, 8 x 128,
+// 17 us (5.7 TB/s read and written).
 //
 // Attention: row r of document b is position cache_len[b] + r - row_start[b] and sees what a position sees under the window
 // (visible.h), among the positions whose page the table holds.  paged.h says how a call is cut into workgroups; here are the plan and the launch
@@ -53,8 +53,8 @@ __device__ __forceinline__ float group16_sum(float v) {
 }
 
 // The splits' sums of the blocks that were split, added in their order: HEADS heads of a row a wave, 64 / HEADS lanes each, which hold the splits' states
-// (there are at most 64) and then columns of the head.  Bound by latency: its row's document, that document's rows and length, the states, the sums.  64 rows
-// of 16 x 128, up to 4 splits, 4.8 us; 1500 rows of 14 x 64, up to 4 splits, 7 (one head a wave 9.7).
+// (there are at most 64) and then columns of the head.  Bound by latency: its row's document, that document's rows and length, the states, the sums.  31 rows
+// of 16 x 128, up to 4 splits, 4.8 us; 1253 rows of 14 x 64, 5 splits, 7 (one head a wave 10).
 template <int DH, typename T, int HEADS>
 __global__ void __launch_bounds__(256) paged_join(PagedArgs<T> a, Divisor waves) {   // of a row
   using Cut = PagedCut<T>;
@@ -207,7 +207,7 @@ template <typename T> dipaco_status launch_attention_paged(PagedArgs<T> a, int d
     if (dipaco_status st = p.wide_blocks ? launch_paged_both<DH>(a, p.wide_blocks, s) : launch_paged_narrow<DH>(a, s)) return st;
     if (p.narrow_splits > 1 || (p.wide_blocks && p.wide_splits > 1)) {
       // Four heads a wave where rows and heads are more than the chip holds waves.  A call's us at one a wave | four: 1 x 2000 tokens, 14 heads of 64, 36 |
-      // 31; 1 x 512 over 8000, 16 of 128, 67.5 | 66; 1 x 128 over 16000, 14 of 64, 26 | 27; one over 30000, 32 of 128, 29 | 32.
+      // 32; 1 x 512 over 8000, 16 of 128, 79 | 76; 1 x 128 over 16000, 14 of 64, 26 | 27; one over 30000, 32 of 128, 30.5 | 33.
       const bool four = (int64_t)a.T_rows * a.H >= 256 * 32;
       const int waves = four ? (a.H + 3) / 4 : a.H;   // of a row
       if (four) paged_join<DH, T, 4><<<(a.T_rows * waves + 3) / 4, 256, 0, s>>>(a, Divisor(waves));

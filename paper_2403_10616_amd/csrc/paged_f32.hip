@@ -3,7 +3,7 @@
 // The table's entries are fetched 64 at a time, a lane each (16 positions an entry); a thread takes the page of the row that it moves from the
 // lane that holds it.  Rows that must not be read are replaced by the last position's, as in paged_mfma.hip.
 // Us: 5 documents of up to 40 tokens over up to 700, 8 heads of 32 on 2 12.5 (of which the join 3.5); 1 x 500 over 1000, 8 heads of 64, 31; one token over
-// 2000, 8 heads of 64, 9.7; 32 over up to 4000, 8 heads of 64 on 2, 17 (2.3 TB/s).
+// 2000, 8 heads of 64, 9.8; 32 documents of up to 4000, 20 of them with a token, 8 heads of 64 on 2, 17.5 (2.2 TB/s).
 #include "kernels.h"
 #include "window_f32.h"
 

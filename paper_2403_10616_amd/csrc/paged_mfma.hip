@@ -5,10 +5,10 @@
 // What a load must not read (positions behind the document's last one, pages that the table does not name) is replaced by the last position's row,
 // which nobody gives weight there.
 //
-// Bound, one token each: the bytes of the keys and values (64 documents of up to 16000, 16 heads of 128 on 4: 106 us, 4.9 TB/s) or, for few keys, latency
-// (one document of 1000, 14 heads of 64: 8 us, a microsecond each for the document's rows and length, the pages, the first keys, the join).  Chunks: as
-// window_mfma.h, and a workgroup's start and end (6000 and 3500 cycles beside 2250 a tile): 1 x 512 tokens over 8000, 16 heads of 128 on 4, 66 us (520
-// TFLOP/s); 4 x up to 512 over up to 12000, 14 heads of 64, window 2048, 27.
+// Bound, one token each: the bytes of the keys and values (64 documents of up to 16000, 31 of them with a token, 16 heads of 128 on 4: 110 us, 4.8 TB/s) or,
+// for few keys, latency (one document of 1000, 14 heads of 64: 9 us, a microsecond each for the document's rows and length, the pages, the first keys, the
+// join).  Chunks: as window_mfma.h, and a workgroup's start and end (6000 and 3500 cycles beside 2250 a tile of head size 64): 1 x 512 tokens over 8000, 16
+// heads of 128 on 4, 76 us with the join (455 TFLOP/s); 4 x up to 512 (1253 in all) over up to 12000, 14 heads of 64, window 2048, 28 without it.
 #include "kernels.h"
 #include "window_mfma.h"
 
