@@ -2,7 +2,7 @@
 //
 // Backward: dQ per block of 128 queries and dK / dV per block of 128 keys, each forming S and dO.V^T anew (seven products where one pass would need five), so
 // that every output has one writer and a fixed order of sums.  Us: 16 x 2048, 14 heads of 64, window 512, 4 sinks 310 (the statistics 23 of them); 4 x 8000, 16
-// heads of 128 on 4, window 1000 1335; 8 x 2048, 8 heads, causal, of 128 338 (attention_mfma.h on the same box 352), of 64 139 (154).
+// heads of 128 on 4, window 1000 1335; 8 x 2048, 8 heads, causal, of 128 338 (attention_mfma.h in the same run 352), of 64 139 (154).
 //
 // Rows that a wave ends with results that are not finite are taken again over the pairs that see each other alone (attention_plain.h says
 // why), so that such values reach exactly the rows that see them.

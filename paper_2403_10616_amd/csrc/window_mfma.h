@@ -9,11 +9,11 @@
 // Bound: a half costs a wave DH / 8 matrix instructions of 32 cycles (head size 64: 256 cycles; with two numbers a probability, below, 3 DH / 16: head size 128
 // 768) and about 80 vector instructions of four (16 of them exponentials, which take longer; 48 more to split probabilities), which a SIMD overlaps
 // little, under a clock that the power limit sets (1.4 - 1.8 GHz).  Forward, us: 16 x 2048 positions, 14 heads of 64, window 512, 4 sinks 108 (490 TFLOP/s of
-// visible pairs), window 2048 165; 2 x up to 32768, 16 heads of 128 on 4, window 4096 2340 (580); 8 x 2048, 8 heads, causal, of 128 111 (attention_mfma.h on
-// the same box 119), of 64 50 (51).
+// visible pairs), window 2048 165; 2 x up to 32768, 16 heads of 128 on 4, window 4096 2340 (580); 8 x 2048, 8 heads, causal, of 128 111 (attention_mfma.h
+// in the same run 119), of 64 50 (51).
 //
 // Probabilities enter the second product as in attention_mfma.h: as two bf16 numbers, 16 bits in all, for head sizes 32 and 128 (the output's own rounding hides
-// the rest), rounded to bf16 for head size 64 (half a step of 2^-8 each, the size of the output's rounding).  Their sum is taken in fp32 before that, so
+// the rest), rounded to bf16 for head size 64 (off by at most 2^-8 of each, as the output is).  Their sum is taken in fp32 before that, so
 // that lse keeps fp32's digits.  Two numbers cost head size 128 a quarter to a third: 2 x up to 32768 positions, 16 heads on 4, window 4096, 1800 -> 2300 - 2450 us,
 // the gradient on 4 x up to 8000, window 1000, 945 -> 1130 - 1190; what splits a pair of them by a dot product instruction saved 2 % and was left out.
 #pragma once
