@@ -142,6 +142,67 @@ dipaco_status dipaco_k_attention_paged(int32_t dtype, const void* qkv, const int
                                        int32_t page_size, int32_t pages_per_doc, int32_t window, int32_t sinks,
                                        void* workspace, size_t workspace_bytes, void* stream);
 
+/* Drafted decoding over a paged cache: a cheaper path, or anything else, proposes several tokens for each document, and the path runs all of
+ * them in one step.  A document's new rows are a tree: row 0 is the last token that is certain, every other row a drafted
+ * token.  A step is dipaco_k_draft_tree; per block of the path dipaco_k_cache_append (row i goes to slot cache_len + i) and
+ * dipaco_k_attention_tree; dipaco_k_draft_verify on the logits of all rows; dipaco_k_cache_keep; then cache_len grows by `kept`.
+ *   parent     device int32 [T]: the row's parent, counted from its document's row 0; an earlier row of the document.  Any other
+ *              value: the row is a root.
+ *   row_start, cache_len, pages, cache, T, B: as above.  max_new: no document has more rows in this call (rows beyond it are left as
+ *              they were), at most 1024.
+ * dipaco_k_draft_tree:
+ *   depth      device int32 [T]: a row's ancestors, their number.  Its token stands at position cache_len + depth.
+ *   seen       device uint64 [T, ceil(max_new / 64)]: bit a % 64 of word a / 64 where the row sees row a of its document: itself and
+ *              its ancestors.  Rows of nobody are left as they were. */
+dipaco_status dipaco_k_draft_tree(const int32_t* parent, const int32_t* row_start, int32_t* depth, uint64_t* seen, int32_t T, int32_t B,
+                                  int32_t max_new, void* stream);
+
+/* Attention of the rows over the cache that they have been appended to.  Row i of document b stands at position cache_len[b] + depth and
+ * sees cached position j < cache_len[b] where j > position - window or j < sinks, and row a of the document (slot cache_len[b] + a) where
+ * its bit of `seen` is set; window >= max_new, so that no row's ancestor lies in front of its window.
+ *   depth, seen  as dipaco_k_draft_tree writes them for the same max_new.  Others may be given: a depth is taken as the nearest in 0 .. i, bits
+ *                of rows that the document does not have are ignored, and a row may see any others, or none.
+ * Everything else, the workspace included, as in dipaco_k_attention_paged. */
+size_t dipaco_k_attention_tree_workspace_bytes(int32_t T, int32_t B, int32_t max_new, int32_t H, int32_t H_kv, int32_t dh,
+                                               int32_t page_size, int32_t pages_per_doc);
+dipaco_status dipaco_k_attention_tree(int32_t dtype, const void* qkv, const int32_t* row_start, const int32_t* cache_len, const int32_t* depth,
+                                      const uint64_t* seen, const int32_t* pages, const void* cache, void* o, float* lse, int32_t T,
+                                      int32_t B, int32_t max_new, int32_t H, int32_t H_kv, int32_t dh, int32_t n_pages,
+                                      int32_t page_size, int32_t pages_per_doc, int32_t window, int32_t sinks, void* workspace,
+                                      size_t workspace_bytes, void* stream);
+
+/* Which drafts stay, by given random numbers, so that every token has the distribution that the target alone would give it.
+ *   target, draft  dtype [T, V] logits of the path and of what drafted.  Row i's are those of the token behind it: the children of row i
+ *                  were drawn from softmax(draft_i / draft_temperature) (distinct = 0: each by itself; 1: one after the other, none
+ *                  twice).  draft = NULL: the drafts were not drawn but picked, whatever the random numbers will be.
+ *   tokens         device int32 [T];  u device fp32 [T], v device fp32 [B]: uniform in [0, 1), independent of the drafts.
+ * From node = row 0: r = softmax(target_node / temperature), at temperature 0 all of it at the largest logit (the first such);
+ * q = softmax(draft_node / draft_temperature).  The children of node, in order, of token x:
+ *     q(x) = 0, or x not in [0, V): passed over;
+ *     u q(x) < r(x): taken, and the walk goes on from there;
+ *     else r <- max(r - q, 0) over its sum, and for distinct = 1 q(x) <- 0 and q <- q over its sum.
+ *   draft = NULL: q is 1 at x and 0 elsewhere.  Where no child is taken the next token is the first y with r(0) + .. + r(y) > v; an r
+ *   whose sum is 0 is softmax(target_node / temperature) again.  Decided in 64 bits.
+ *   path   device int32 [B, max_new]: row 0 and the rows taken, in order, then -1.   kept device int32 [B]: their number, 0 for a document
+ *          without rows.   next device int32 [B]: the next token; -1 for a document without rows, and where the target's logits are no
+ *          distribution (a NaN, a +inf, or nothing above -inf), where the walk ends.  Draft logits that are none: no child is taken.
+ * temperature >= 0, draft_temperature > 0 (not read without draft), both finite.  1 <= V <= 2^18, max_new <= 1024, T <= 2^23, B <= 2^20.
+ * workspace: device, >= dipaco_k_draft_verify_workspace_bytes(T, B, V) (0 = invalid shape), contents undefined before and after; calls
+ * that may overlap in time, captured ones included, need one each.  Results are bit-reproducible. */
+size_t dipaco_k_draft_verify_workspace_bytes(int32_t T, int32_t B, int32_t V);
+dipaco_status dipaco_k_draft_verify(int32_t dtype, const void* target, const void* draft, const int32_t* tokens, const int32_t* parent,
+                                    const int32_t* row_start, const float* u, const float* v, int32_t* path, int32_t* kept, int32_t* next,
+                                    int32_t T, int32_t B, int32_t max_new, int32_t V, float temperature, float draft_temperature,
+                                    int32_t distinct, void* workspace, size_t workspace_bytes, void* stream);
+
+/* The rows that stay move to their places: in every cache slot cache_len[b] + i takes the keys and values of slot cache_len[b] + path[b, i],
+ * i < kept[b].  caches: host array of n_layers device pointers, caches of the same pages.  path [B, max_new] and kept as
+ * dipaco_k_draft_verify writes them; kept is taken as the nearest in 0 .. max_new, and a path ends at the first entry that does not rise or is
+ * not in 0 .. max_new - 1.  A row whose slot, the old one or the new, has no page stays where it is.  */
+dipaco_status dipaco_k_cache_keep(int32_t dtype, const int32_t* path, const int32_t* kept, const int32_t* cache_len, const int32_t* pages,
+                                  void* const* caches, int32_t n_layers, int32_t B, int32_t max_new, int32_t H_kv, int32_t dh,
+                                  int32_t n_pages, int32_t page_size, int32_t pages_per_doc, void* stream);
+
 /* Measurement aid, no part of the method: register-only loops that show how the matrix cores and the vector ALU of a
  * SIMD share instruction issue (the inner loops of the attention kernels are priced with it).  One workgroup of
  * 256 * waves_per_simd threads per compute unit (256 workgroups) runs `iters` iterations of

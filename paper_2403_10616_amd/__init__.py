@@ -105,6 +105,13 @@ _SIGS = {
     "dipaco_k_cache_append": (C.c_int, [C.c_int32] + [C.c_void_p] * 5 + [C.c_int32] * 8 + [C.c_void_p]),
     "dipaco_k_attention_paged_workspace_bytes": (C.c_size_t, [C.c_int32] * 8),
     "dipaco_k_attention_paged": (C.c_int, [C.c_int32] + [C.c_void_p] * 7 + [C.c_int32] * 11 + [C.c_void_p, C.c_size_t, C.c_void_p]),
+    "dipaco_k_draft_tree": (C.c_int, [C.c_void_p] * 4 + [C.c_int32] * 3 + [C.c_void_p]),
+    "dipaco_k_attention_tree_workspace_bytes": (C.c_size_t, [C.c_int32] * 8),
+    "dipaco_k_attention_tree": (C.c_int, [C.c_int32] + [C.c_void_p] * 9 + [C.c_int32] * 11 + [C.c_void_p, C.c_size_t, C.c_void_p]),
+    "dipaco_k_draft_verify_workspace_bytes": (C.c_size_t, [C.c_int32] * 3),
+    "dipaco_k_draft_verify": (C.c_int, [C.c_int32] + [C.c_void_p] * 10 + [C.c_int32] * 4 + [C.c_float, C.c_float, C.c_int32, C.c_void_p,
+                                                                                        C.c_size_t, C.c_void_p]),
+    "dipaco_k_cache_keep": (C.c_int, [C.c_int32] + [C.c_void_p] * 4 + [C.POINTER(C.c_void_p)] + [C.c_int32] * 8 + [C.c_void_p]),
 }
 
 EXPORTS = tuple(_SIGS)
@@ -476,3 +483,41 @@ def dipaco_k_attention_paged(dtype: int, qkv, row_start, cache_len, pages, cache
                                            _ptr(lse), T, B, max_new, H, H_kv, dh, n_pages, page_size, pages_per_doc, window,
                                            sinks, _ptr(workspace), workspace.numel() * workspace.element_size(),
                                            _stream(stream)))
+
+
+def dipaco_k_draft_tree(parent, row_start, depth, seen, T: int, B: int, max_new: int, stream=None):
+    _check(load().dipaco_k_draft_tree(_ptr(parent), _ptr(row_start), _ptr(depth), _ptr(seen), T, B, max_new, _stream(stream)))
+
+
+def dipaco_k_attention_tree_workspace_bytes(T: int, B: int, max_new: int, H: int, H_kv: int, dh: int, page_size: int,
+                                            pages_per_doc: int) -> int:
+    return int(load().dipaco_k_attention_tree_workspace_bytes(T, B, max_new, H, H_kv, dh, page_size, pages_per_doc))
+
+
+def dipaco_k_attention_tree(dtype: int, qkv, row_start, cache_len, depth, seen, pages, cache, o, lse, T: int, B: int, max_new: int,
+                            H: int, H_kv: int, dh: int, n_pages: int, page_size: int, pages_per_doc: int, window: int, sinks: int,
+                            workspace, stream=None):
+    _check(load().dipaco_k_attention_tree(dtype, _ptr(qkv), _ptr(row_start), _ptr(cache_len), _ptr(depth), _ptr(seen), _ptr(pages),
+                                          _ptr(cache), _ptr(o), _ptr(lse), T, B, max_new, H, H_kv, dh, n_pages, page_size,
+                                          pages_per_doc, window, sinks, _ptr(workspace),
+                                          workspace.numel() * workspace.element_size(), _stream(stream)))
+
+
+def dipaco_k_draft_verify_workspace_bytes(T: int, B: int, V: int) -> int:
+    return int(load().dipaco_k_draft_verify_workspace_bytes(T, B, V))
+
+
+def dipaco_k_draft_verify(dtype: int, target, draft, tokens, parent, row_start, u, v, path, kept, next_token, T: int, B: int,
+                          max_new: int, V: int, temperature: float, draft_temperature: float, distinct: bool, workspace, stream=None):
+    _check(load().dipaco_k_draft_verify(dtype, _ptr(target), _ptr(draft), _ptr(tokens), _ptr(parent), _ptr(row_start), _ptr(u), _ptr(v),
+                                        _ptr(path), _ptr(kept), _ptr(next_token), T, B, max_new, V, temperature, draft_temperature,
+                                        int(bool(distinct)), _ptr(workspace), workspace.numel() * workspace.element_size(),
+                                        _stream(stream)))
+
+
+def dipaco_k_cache_keep(dtype: int, path, kept, cache_len, pages, caches, B: int, max_new: int, H_kv: int, dh: int, n_pages: int,
+                        page_size: int, pages_per_doc: int, stream=None):
+    """caches: the device tensors of all layers"""
+    ptrs = (C.c_void_p * len(caches))(*[_ptr(c) for c in caches])
+    _check(load().dipaco_k_cache_keep(dtype, _ptr(path), _ptr(kept), _ptr(cache_len), _ptr(pages), ptrs, len(caches), B, max_new, H_kv,
+                                      dh, n_pages, page_size, pages_per_doc, _stream(stream)))

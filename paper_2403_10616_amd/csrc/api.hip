@@ -404,6 +404,11 @@ static dipaco_status check_cache(int32_t T, int32_t B, int32_t H, int32_t n_page
   if ((int64_t)pages_per_doc * page_size > (1 << 28)) return fail(DIPACO_ESHAPE, "a document may hold 2^28 positions");
   return DIPACO_OK;
 }
+static dipaco_status check_drafts(int32_t T, int32_t B, int32_t max_new) {
+  if (T < 0 || B < 1 || max_new < 0) return fail(DIPACO_EINVAL, "T >= 0, B >= 1 and max_new >= 0 required");
+  if (T > (1 << 23) || B > (1 << 20) || max_new > DRAFT_MOST_ROWS) return fail(DIPACO_ESHAPE, "T <= 2^23, B <= 2^20 and max_new <= 1024 required");
+  return DIPACO_OK;
+}
 template <typename T>
 static PagedArgs<T> paged_args(const void* qkv, const int32_t* row_start, const int32_t* cache_len, const int32_t* pages, const void* cache, void* o,
                                float* lse, int32_t rows, int32_t B, int32_t max_new, int32_t H, int32_t H_kv, int32_t n_pages, int32_t page_size,
@@ -1184,6 +1189,96 @@ dipaco_status dipaco_k_attention_paged(int32_t dtype, const void* qkv, const int
                                                        pages_per_doc, w), dh, workspace, st)
              : launch_attention_paged(paged_args<float>(qkv, row_start, cache_len, pages, cache, o, lse, T, B, max_new, H, H_kv, n_pages, page_size,
                                                         pages_per_doc, w), dh, workspace, st);
+}
+
+// ---- drafted decoding ------------------------------------------------------------------------------------
+dipaco_status dipaco_k_draft_tree(const int32_t* parent, const int32_t* row_start, int32_t* depth, uint64_t* seen, int32_t T, int32_t B, int32_t max_new,
+                                  void* stream) {
+  TRY(check_drafts(T, B, max_new));
+  if (T == 0 || max_new == 0) return DIPACO_OK;
+  TRY(check_ptr(parent, "parent")); TRY(check_ptr(row_start, "row_start")); TRY(check_ptr(depth, "depth")); TRY(check_ptr(seen, "seen"));
+  return launch_draft_tree(parent, row_start, depth, seen, T, B, max_new, static_cast<hipStream_t>(stream));
+}
+
+size_t dipaco_k_attention_tree_workspace_bytes(int32_t T, int32_t B, int32_t max_new, int32_t H, int32_t H_kv, int32_t dh, int32_t page_size,
+                                               int32_t pages_per_doc) {
+  if (check_heads(DIPACO_F32, H, H_kv, dh) != DIPACO_OK || check_cache(T, B, H, 1, page_size, pages_per_doc) != DIPACO_OK || check_drafts(T, B, max_new) != DIPACO_OK)
+    return 0;
+  return paged_workspace_bytes(T, H, dh, page_size, pages_per_doc);
+}
+
+dipaco_status dipaco_k_attention_tree(int32_t dtype, const void* qkv, const int32_t* row_start, const int32_t* cache_len, const int32_t* depth,
+                                      const uint64_t* seen, const int32_t* pages, const void* cache, void* o, float* lse, int32_t T, int32_t B,
+                                      int32_t max_new, int32_t H, int32_t H_kv, int32_t dh, int32_t n_pages, int32_t page_size, int32_t pages_per_doc,
+                                      int32_t window, int32_t sinks, void* workspace, size_t workspace_bytes, void* stream) {
+  TRY(check_heads(dtype, H, H_kv, dh));
+  TRY(check_cache(T, B, H, n_pages, page_size, pages_per_doc));
+  TRY(check_window(window, sinks));
+  TRY(check_drafts(T, B, max_new));
+  if (window < max_new) return fail(DIPACO_ESHAPE, "window >= max_new required: a row sees its ancestors");
+  if (T == 0 || max_new == 0) return DIPACO_OK;
+  TRY(check_ptr(qkv, "qkv")); TRY(check_ptr(row_start, "row_start")); TRY(check_ptr(cache_len, "cache_len")); TRY(check_ptr(depth, "depth"));
+  TRY(check_ptr(seen, "seen")); TRY(check_ptr(pages, "pages")); TRY(check_ptr(cache, "cache")); TRY(check_ptr(o, "o")); TRY(check_ptr(workspace, "workspace"));
+  if (lse) TRY(check_ptr(lse, "lse"));
+  if (workspace_bytes < paged_workspace_bytes(T, H, dh, page_size, pages_per_doc))
+    return fail(DIPACO_EWORKSPACE, "workspace smaller than dipaco_k_attention_tree_workspace_bytes");
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const Window w{window, sinks};
+  return dtype == DIPACO_BF16
+             ? launch_attention_tree(paged_args<bf16>(qkv, row_start, cache_len, pages, cache, o, lse, T, B, max_new, H, H_kv, n_pages, page_size,
+                                                      pages_per_doc, w), depth, seen, dh, workspace, st)
+             : launch_attention_tree(paged_args<float>(qkv, row_start, cache_len, pages, cache, o, lse, T, B, max_new, H, H_kv, n_pages, page_size,
+                                                       pages_per_doc, w), depth, seen, dh, workspace, st);
+}
+
+size_t dipaco_k_draft_verify_workspace_bytes(int32_t T, int32_t B, int32_t V) {
+  if (check_drafts(T, B, 1) != DIPACO_OK || V < 1 || V > (1 << 18)) return 0;
+  return draft_verify_workspace_bytes(B, V);
+}
+
+dipaco_status dipaco_k_draft_verify(int32_t dtype, const void* target, const void* draft, const int32_t* tokens, const int32_t* parent, const int32_t* row_start,
+                                    const float* u, const float* v, int32_t* path, int32_t* kept, int32_t* next, int32_t T, int32_t B, int32_t max_new,
+                                    int32_t V, float temperature, float draft_temperature, int32_t distinct, void* workspace, size_t workspace_bytes,
+                                    void* stream) {
+  if (dtype != DIPACO_F32 && dtype != DIPACO_BF16) return fail(DIPACO_EINVAL, "dtype must be DIPACO_F32 or DIPACO_BF16");
+  TRY(check_drafts(T, B, max_new));
+  if (V < 1) return fail(DIPACO_EINVAL, "V >= 1 required");
+  if (V > (1 << 18)) return fail(DIPACO_ESHAPE, "V <= 2^18 required");
+  if (!std::isfinite(temperature) || temperature < 0.f) return fail(DIPACO_EINVAL, "temperature must be finite and not negative");
+  if (draft && (!std::isfinite(draft_temperature) || draft_temperature <= 0.f)) return fail(DIPACO_EINVAL, "draft_temperature must be finite and positive");
+  if (distinct != 0 && distinct != 1) return fail(DIPACO_EINVAL, "distinct must be 0 or 1");
+  TRY(check_ptr(row_start, "row_start")); TRY(check_ptr(kept, "kept")); TRY(check_ptr(next, "next")); TRY(check_ptr(workspace, "workspace"));
+  if (T > 0) {
+    TRY(check_ptr(target, "target")); TRY(check_ptr(tokens, "tokens")); TRY(check_ptr(parent, "parent")); TRY(check_ptr(u, "u")); TRY(check_ptr(v, "v"));
+    if (draft) TRY(check_ptr(draft, "draft"));
+  }
+  if (max_new > 0) TRY(check_ptr(path, "path"));
+  if (workspace_bytes < draft_verify_workspace_bytes(B, V)) return fail(DIPACO_EWORKSPACE, "workspace smaller than dipaco_k_draft_verify_workspace_bytes");
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const double scale = temperature > 0.f ? 1.0 / temperature : 0.0, draft_scale = draft ? 1.0 / draft_temperature : 1.0;
+  auto run = [&](auto zero) {
+    using E = decltype(zero);
+    return launch_draft_verify(VerifyArgs<E>{static_cast<const E*>(target), static_cast<const E*>(draft), tokens, parent, row_start, u, v, path, kept, next, T, B,
+                                             max_new, V, scale, draft_scale, distinct, static_cast<double*>(workspace)}, st);
+  };
+  return dtype == DIPACO_BF16 ? run(bf16{}) : run(float{});
+}
+
+dipaco_status dipaco_k_cache_keep(int32_t dtype, const int32_t* path, const int32_t* kept, const int32_t* cache_len, const int32_t* pages, void* const* caches,
+                                  int32_t n_layers, int32_t B, int32_t max_new, int32_t H_kv, int32_t dh, int32_t n_pages, int32_t page_size,
+                                  int32_t pages_per_doc, void* stream) {
+  TRY(check_heads(dtype, H_kv, H_kv, dh));
+  TRY(check_cache(0, B, H_kv, n_pages, page_size, pages_per_doc));
+  TRY(check_drafts(0, B, max_new));
+  if (n_layers < 0) return fail(DIPACO_EINVAL, "n_layers >= 0 required");
+  if (n_layers == 0 || max_new == 0) return DIPACO_OK;
+  TRY(check_ptr(path, "path")); TRY(check_ptr(kept, "kept")); TRY(check_ptr(cache_len, "cache_len")); TRY(check_ptr(pages, "pages"));
+  if (!caches) return fail(DIPACO_EINVAL, "caches is NULL");
+  for (int l = 0; l < n_layers; ++l) TRY(check_ptr(caches[l], "a cache"));
+  int shift = 4;
+  while ((1 << shift) < page_size) ++shift;
+  const KeepArgs a{path, kept, cache_len, pages, B, max_new, H_kv, n_pages, shift, pages_per_doc, dh * (dtype == DIPACO_BF16 ? 2 : 4) / 16, {}};
+  return launch_cache_keep(a, caches, n_layers, static_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"

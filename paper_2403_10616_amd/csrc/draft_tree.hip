@@ -1,0 +1,74 @@
+// What rows of a tree of drafted tokens see: themselves and their ancestors, as bits, and how many ancestors that are.
+//
+// A thread holds a row; its bits and the row that they reach up to lie in LDS.  A round joins to a row's bits those of the row that they reach, which
+// doubles their reach: ceil(log2(depth + 1)) rounds whatever the tree's shape, where following parents one by one takes a chain's length.
+#include "draft.h"
+#include "kernels.h"
+
+namespace dipaco {
+
+namespace {
+
+template <int WORDS>
+__global__ void __launch_bounds__(DRAFT_MOST_ROWS) draft_tree_rows(const int* parent, const int* row_start, int* depth, uint64_t* seen, int T_rows, int max_new, int words,
+                                                                   int b0) {
+  extern __shared__ __attribute__((aligned(16))) uint64_t dt_smem[];   // [rows][WORDS] bits, then [rows] how far up they reach: the row, or -1
+  const int i = threadIdx.x;
+  const RowRange r = ragged_rows(row_start, b0 + blockIdx.x, T_rows);
+  const int n = min(r.count, max_new);
+  int* const reach = reinterpret_cast<int*>(dt_smem + (size_t)max_new * WORDS);
+  uint64_t mine[WORDS];
+#pragma unroll
+  for (int w = 0; w < WORDS; ++w) mine[w] = i >> 6 == w ? 1ull << (i & 63) : 0;
+  int up = -1;
+  if (i < n) {
+    up = draft_parent(parent[r.first + i], i);
+#pragma unroll
+    for (int w = 0; w < WORDS; ++w) dt_smem[i * WORDS + w] = mine[w];
+    reach[i] = up;
+  }
+  while (__syncthreads_or(up >= 0)) {
+    int next = -1;
+    if (up >= 0) {
+#pragma unroll
+      for (int w = 0; w < WORDS; ++w) mine[w] |= dt_smem[up * WORDS + w];
+      next = reach[up];
+    }
+    __syncthreads();
+    if (up >= 0) {
+#pragma unroll
+      for (int w = 0; w < WORDS; ++w) dt_smem[i * WORDS + w] = mine[w];
+      reach[i] = next;
+    }
+    up = next;
+  }
+  if (i >= n) return;
+  int count = 0;
+#pragma unroll
+  for (int w = 0; w < WORDS; ++w) count += __builtin_popcountll(mine[w]);
+  depth[r.first + i] = count - 1;
+#pragma unroll
+  for (int w = 0; w < WORDS; ++w)
+    if (w < words) seen[(long)(r.first + i) * words + w] = mine[w];
+}
+
+}  // namespace
+
+dipaco_status launch_draft_tree(const int* parent, const int* row_start, int* depth, uint64_t* seen, int T_rows, int B, int max_new, hipStream_t s) {
+  const int words = draft_words(max_new);
+  auto run = [&](auto Wc) -> dipaco_status {
+    constexpr int WORDS = decltype(Wc)::value;
+    static std::atomic<unsigned long long> lds_set{0};
+    if (dipaco_status st = ensure_dynamic_lds(reinterpret_cast<const void*>(draft_tree_rows<WORDS>), DRAFT_MOST_ROWS * (8 * WORDS + 4), lds_set)) return st;
+    launch_parts(B, [&](long long first, unsigned count) {
+      draft_tree_rows<WORDS><<<count, (max_new + 63) / 64 * 64, (size_t)max_new * (8 * WORDS + 4), s>>>(parent, row_start, depth, seen, T_rows, max_new, words, (int)first);
+    });
+    DIPACO_LAUNCH_CHECK();
+    return DIPACO_OK;
+  };
+  using std::integral_constant;
+  return words <= 1 ? run(integral_constant<int, 1>{}) : words <= 2 ? run(integral_constant<int, 2>{}) : words <= 4 ? run(integral_constant<int, 4>{})
+       : words <= 8 ? run(integral_constant<int, 8>{}) : run(integral_constant<int, 16>{});
+}
+
+}  // namespace dipaco

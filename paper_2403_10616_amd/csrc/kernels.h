@@ -3,6 +3,7 @@
 #include <algorithm>
 
 #include "common.h"
+#include "draft.h"
 #include "paged.h"
 #include "visible.h"
 
@@ -332,5 +333,11 @@ template <int DH> dipaco_status launch_paged_narrow(const PagedArgs<bf16>& a, hi
 template <int DH> dipaco_status launch_paged_both(const PagedArgs<bf16>& a, int blocks, hipStream_t s);
 template <int DH> dipaco_status launch_paged_narrow(const PagedArgs<float>& a, hipStream_t s);
 template <int DH> dipaco_status launch_paged_both(const PagedArgs<float>& a, int blocks, hipStream_t s);
+// ---- draft_tree.hip, attention_tree.hip, draft_verify.hip, cache_keep.hip: a step of drafted decoding ------------
+dipaco_status launch_draft_tree(const int* parent, const int* row_start, int* depth, uint64_t* seen, int T_rows, int B, int max_new, hipStream_t s);
+template <typename T> dipaco_status launch_attention_tree(const PagedArgs<T>& a, const int* depth, const uint64_t* seen, int dh, void* workspace, hipStream_t s);
+size_t draft_verify_workspace_bytes(int B, int V);
+template <typename T> dipaco_status launch_draft_verify(const VerifyArgs<T>& a, hipStream_t s);
+dipaco_status launch_cache_keep(KeepArgs a, void* const* caches, int n_layers, hipStream_t s);
 
 }  // namespace dipaco
