@@ -31,7 +31,7 @@ __global__ void __launch_bounds__(WF_THREADS, 2) window_fwd_f32(FWindowArgs a, f
   const long ld = (long)(a.H + 2 * a.H_kv) * DH;
   const float* const base = a.qkv + (long)b * a.S * ld;
   const FRowSpan span{qw0, qw0 < rows ? min(qw0 + 15, rows - 1) : -1};
-  const int near = a.w.near_from(q);
+  const ChainView view{q, a.w.near_from(q), a.w.sinks};
   FSoftmaxRow<DH> x;
   x.clear();
   if (q0 < rows) {
@@ -53,7 +53,7 @@ __global__ void __launch_bounds__(WF_THREADS, 2) window_fwd_f32(FWindowArgs a, f
       const bool more = t + 1 < tiles.count;
       if (more) load(t + 1);
       __syncthreads();   // tile t is in LDS, and everybody is done with the stage of tile t - 1
-      attend_32<DH>(x, qf, k_, k_ + window_tile_floats<DH, WF_TILE>(), tiles.at(t) * 32, 0, a.w, span, false, q, near, m, g);
+      attend_32<DH>(x, qf, k_, k_ + window_tile_floats<DH, WF_TILE>(), tiles.at(t) * 32, 0, a.w, span, false, view, m, g);
       if (more) next.store(wff_smem + ((t + 1) & 1) * STAGE);
     }
     x.l = sum_groups(x.l);

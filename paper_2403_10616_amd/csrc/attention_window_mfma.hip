@@ -38,7 +38,7 @@ __global__ void __launch_bounds__(AT_THREADS * NG, NG == 2 || DH == 128 ? 2 : 3)
   const RowSpan span{q0 + 32 * wave, q0 + 32 * wave < rows ? min(q0 + 32 * wave + 31, rows - 1) : -1};
   SoftmaxRow<DH> x;
   x.clear();
-  const int near = a.w.near_from(q);
+  const ChainView view{q, a.w.near_from(q), a.w.sinks};
   const float sc = score_scale<DH>() * LOG2E;
   if (q0 < rows) {
     uint4 qf[KS];
@@ -58,7 +58,7 @@ __global__ void __launch_bounds__(AT_THREADS * NG, NG == 2 || DH == 128 ? 2 : 3)
       if (t + NG < tiles.count) src.issue(tiles.at(t + NG), wave, lane, smem_addr + (1 - cur) * 2 * TILE_BYTES);
       if (NG == 2 && t >= tiles.count) return;
       const char* k_ = wf_smem + cur * 2 * TILE_BYTES;
-      attend_tile<DH>(x, qf, k_, k_ + TILE_BYTES, fo, to, tiles.at(t) * 64, 0, a.w, span, 0, q, near, lane);
+      attend_tile<DH>(x, qf, k_, k_ + TILE_BYTES, fo, to, tiles.at(t) * 64, 0, a.w, span, 0, view, lane);
     };
     for (int t = 0; t < tiles.count; t += 2 * NG) {   // both groups walk as often as the first: the barriers are the workgroup's
       tile(std::integral_constant<int, 0>{}, t + grp);

@@ -328,14 +328,15 @@ dipaco_status launch_window_bwd_f32(const float* qkv, const int* lengths, const 
 template <typename T> dipaco_status launch_cache_append(const PagedArgs<T>& a, int dh, hipStream_t s);
 size_t paged_workspace_bytes(int T_rows, int H, int dh, int page_size, int pages_per_doc);
 template <typename T> dipaco_status launch_attention_paged(PagedArgs<T> a, int dh, void* workspace, hipStream_t s);
-// paged_mfma.hip (bf16), paged_f32.hip
-template <int DH> dipaco_status launch_paged_narrow(const PagedArgs<bf16>& a, hipStream_t s);
-template <int DH> dipaco_status launch_paged_both(const PagedArgs<bf16>& a, int blocks, hipStream_t s);
-template <int DH> dipaco_status launch_paged_narrow(const PagedArgs<float>& a, hipStream_t s);
-template <int DH> dipaco_status launch_paged_both(const PagedArgs<float>& a, int blocks, hipStream_t s);
-// ---- draft_tree.hip, attention_tree.hip, draft_verify.hip, cache_keep.hip: a step of drafted decoding ------------
-dipaco_status launch_draft_tree(const int* parent, const int* row_start, int* depth, uint64_t* seen, int T_rows, int B, int max_new, hipStream_t s);
 template <typename T> dipaco_status launch_attention_tree(const PagedArgs<T>& a, const int* depth, const uint64_t* seen, int dh, void* workspace, hipStream_t s);
+// paged_mfma.hip (bf16), paged_f32.hip.  Args: PagedArgs or TreeArgs
+template <int DH, template <typename> class Args> dipaco_status launch_paged_narrow(const Args<bf16>& a, hipStream_t s);
+template <int DH, template <typename> class Args> dipaco_status launch_paged_both(const Args<bf16>& a, int blocks, hipStream_t s);
+template <int DH, template <typename> class Args> dipaco_status launch_paged_narrow(const Args<float>& a, hipStream_t s);
+template <int DH, template <typename> class Args> dipaco_status launch_paged_both(const Args<float>& a, int blocks, hipStream_t s);
+
+// ---- draft_tree.hip, draft_verify.hip, cache_keep.hip: a step of drafted decoding ------------
+dipaco_status launch_draft_tree(const int* parent, const int* row_start, int* depth, uint64_t* seen, int T_rows, int B, int max_new, hipStream_t s);
 size_t draft_verify_workspace_bytes(int B, int V);
 template <typename T> dipaco_status launch_draft_verify(const VerifyArgs<T>& a, hipStream_t s);
 dipaco_status launch_cache_keep(KeepArgs a, void* const* caches, int n_layers, hipStream_t s);

@@ -52,7 +52,37 @@ struct Divisor {
 // through: it loses against every finite reference, and if it stays the row is 0 / 0 as its definition is, not the 0 of a row that sees nothing.
 constexpr float ALL_MINUS_INFINITY = -3.402823466e38f;
 
+// What a row sees, key by key.  near: first position of its window
+struct ChainView {
+  int pos, near, sinks;   // up to position pos
+  __device__ __forceinline__ bool sees(int key) const { return key <= pos && (key >= near || key < sinks); }
+};
+// A row of a tree: positions in front of `cached` by the window and the sinks, those behind by its bits, none behind `last`
+struct TreeView {
+  const uint32_t* bits;
+  int words, cached, last, near, sinks;
+  bool any;               // whether it has seen one of its bits' keys
+  // the bits of the 32 positions from k0 on; set for positions in front of `cached`
+  __device__ __forceinline__ uint32_t word(int k0) const {
+    const int s = k0 - cached;
+    uint32_t w = ~0u;
+    if (s > -32) {
+      const int i = s >> 5;
+      const uint32_t a = i < 0 ? ~0u : i < words ? bits[i] : 0u, b = i + 1 < words ? bits[i + 1] : 0u;
+      w = __builtin_amdgcn_alignbit(b, a, s & 31);
+    }
+    const int upto = last - k0;
+    return upto >= 31 ? w : upto < 0 ? 0u : w & ((2u << upto) - 1);
+  }
+  // seen: as word, without keys that no page holds
+  __device__ __forceinline__ void note(int k0, uint32_t seen) {
+    any |= (k0 >= cached ? seen : cached - k0 >= 32 ? 0u : seen >> (cached - k0)) != 0;
+  }
+  __device__ __forceinline__ bool sees(int key) const { return (word(key) & 1) && (key >= cached || key >= near || key < sinks); }
+};
+
 template <typename T> struct PagedArgs {
+  static constexpr bool TREE = false;   // a document's new rows see each other in order
   const T* qkv;              // [T rows, (H + 2 H_kv) dh]
   const int* row_start;      // [B + 1]
   const int* cache_len;      // [B]
@@ -93,6 +123,11 @@ template <typename T> struct PagedArgs {
       if ((min(p + 15, upto) >= near || p < w.sinks) && page_of(b, p) >= 0) return true;
     return false;
   }
+  __device__ __forceinline__ bool sees_any(int b, const ChainView& x, int last, int k0, int n) const { return sees_any(b, x.pos, x.near, last, k0, n); }
+  // a tree's row: its words have been looked at already
+  __device__ __forceinline__ bool sees_any(int b, const TreeView& x, int last, int k0, int n) const { return x.any || sees_any(b, x.cached - 1, x.near, last, k0, n); }
+  // of the row that is new token `token` of a document with `rows` of them from row0 on
+  __device__ __forceinline__ ChainView view(int, int, int pos0, int last, int token) const { return {min(pos0 + token, last), w.near_from(pos0 + token), w.sinks}; }
   template <int DH> __device__ __forceinline__ long key_offset(int page, int hk, int slot) const {
     return ((((long)page * 2 * H_kv + hk) << page_shift) + slot) * DH;
   }
@@ -101,19 +136,33 @@ template <typename T> struct PagedArgs {
   __device__ __forceinline__ float2* part_state(int split, long row, int head) const { return state + ((long)split * T_rows + row) * H + head; }
 };
 
+// The new rows are trees: a row's position is its depth behind the cached ones, and of the new rows it sees those of its bits
+template <typename T> struct TreeArgs : PagedArgs<T> {
+  static constexpr bool TREE = true;
+  const int* depth;          // [T rows]
+  const uint32_t* seen;      // [T rows, words]
+  int words;
+  __device__ __forceinline__ TreeView view(int row0, int rows, int pos0, int last, int token) const {
+    token = min(token, rows - 1);
+    const long row = row0 + token;
+    const int pos = pos0 + min(max(depth[row], 0), token);
+    return {seen + row * words, words, pos0, last, min(this->w.near_from(pos), pos0), this->w.sinks, false};
+  }
+};
+
 // Workgroups of a launch of both kinds: n_wide of heads x splits x blocks, then those of splits x heads x documents
 struct PagedOrder { Divisor heads, head_splits; int n_wide; };
 
 // A block of packed rows of one document: which rows, the tiles that they see, and how many of these a split takes
 template <int SHIFT> struct PagedBlock {
   int b, row0, rows, packed0, packed, pos0, last;   // rows row0 .. of the call, `rows` of them; packed rows packed0 .. of `packed`; position of row 0; last one
-  int lo, hi;                                       // positions of the block's first and last row
+  int lo, hi;                                       // positions of the block's first and last row; TREE: of the document's new slots
   TileList<SHIFT> tiles;
   int per;                                          // tiles a split: split s has tiles s per ..
-  template <typename T> __device__ __forceinline__ PagedBlock(const PagedArgs<T>& a, int b, int block, int block_rows, const Divisor& splits, int least_keys)
+  template <typename A> __device__ __forceinline__ PagedBlock(const A& a, int b, int block, int block_rows, const Divisor& splits, int least_keys)
       : PagedBlock(a, b, ragged_rows(a.row_start, b, a.T_rows), a.cached(b), block, block_rows, splits, least_keys) {}
-  template <typename T>
-  __device__ __forceinline__ PagedBlock(const PagedArgs<T>& a, int b, const RowRange& r, int cached, int block, int block_rows, const Divisor& splits, int least_keys)
+  template <typename A>
+  __device__ __forceinline__ PagedBlock(const A& a, int b, const RowRange& r, int cached, int block, int block_rows, const Divisor& splits, int least_keys)
       : b(b) {
     const int G = a.group.d;
     pos0 = cached;
@@ -124,8 +173,13 @@ template <int SHIFT> struct PagedBlock {
     last = min(pos0 + rows, a.capacity()) - 1;
     per = lo = hi = 0;
     if (packed0 >= packed) return;
-    lo = pos0 + a.group(packed0);
-    hi = pos0 + a.group(min(packed, packed0 + block_rows) - 1);
+    if (A::TREE) {   // any row may see all of them
+      lo = pos0;
+      hi = pos0 + rows - 1;
+    } else {
+      lo = pos0 + a.group(packed0);
+      hi = pos0 + a.group(min(packed, packed0 + block_rows) - 1);
+    }
     if (last < 0) return;
     tiles = TileList<SHIFT>(a.w, lo, min(hi, last));
     if (tiles.count <= 0) { tiles.count = 0; return; }

@@ -55,8 +55,8 @@ __device__ __forceinline__ float group16_sum(float v) {
 // The splits' sums of the blocks that were split, added in their order: HEADS heads of a row a wave, 64 / HEADS lanes each, which hold the splits' states
 // (there are at most 64) and then columns of the head.  Bound by latency: its row's document, that document's rows and length, the states, the sums.  31 rows
 // of 16 x 128, up to 4 splits, 4.8 us; 1253 rows of 14 x 64, 5 splits, 7 (one head a wave 10).
-template <int DH, typename T, int HEADS>
-__global__ void __launch_bounds__(256) paged_join(PagedArgs<T> a, Divisor waves) {   // of a row
+template <int DH, typename T, int HEADS, template <typename> class Args>
+__global__ void __launch_bounds__(256) paged_join(Args<T> a, Divisor waves) {   // of a row
   using Cut = PagedCut<T>;
   constexpr int LANES = 64 / HEADS, COLS = DH > LANES ? DH / LANES : 1, HELD = PAGED_MOST_SPLITS / LANES;
   const int lane = threadIdx.x & 63, sub = lane & (LANES - 1), item = blockIdx.x * 4 + (threadIdx.x >> 6), row = waves(item);
@@ -193,8 +193,8 @@ template <typename T> dipaco_status launch_cache_append(const PagedArgs<T>& a, i
 size_t paged_workspace_bytes(int T_rows, int H, int dh, int page_size, int pages_per_doc) {
   return 256 + partial_rows(T_rows, H, (int64_t)page_size * pages_per_doc) * H * (dh + 2) * sizeof(float);
 }
-template <typename T> dipaco_status launch_attention_paged(PagedArgs<T> a, int dh, void* workspace, hipStream_t s) {
-  const PagedPlan p = plan(a);
+template <typename T, template <typename> class Args> static dipaco_status launch_paged(Args<T> a, int dh, void* workspace, hipStream_t s) {
+  const PagedPlan p = plan<T>(a);
   a.narrow_splits = Divisor(p.narrow_splits);
   a.narrow_keys = p.narrow_keys;
   a.narrow_turn = 3 - std::min(3, __builtin_ctz(p.narrow_splits));   // n splits begin at 8 / gcd(8, n) places by themselves
@@ -210,17 +210,28 @@ template <typename T> dipaco_status launch_attention_paged(PagedArgs<T> a, int d
       // 32; 1 x 512 over 8000, 16 of 128, 79 | 76; 1 x 128 over 16000, 14 of 64, 26 | 27; one over 30000, 32 of 128, 30.5 | 33.
       const bool four = (int64_t)a.T_rows * a.H >= 256 * 32;
       const int waves = four ? (a.H + 3) / 4 : a.H;   // of a row
-      if (four) paged_join<DH, T, 4><<<(a.T_rows * waves + 3) / 4, 256, 0, s>>>(a, Divisor(waves));
-      else paged_join<DH, T, 1><<<(a.T_rows * waves + 3) / 4, 256, 0, s>>>(a, Divisor(waves));
+      if (four) paged_join<DH, T, 4, Args><<<(a.T_rows * waves + 3) / 4, 256, 0, s>>>(a, Divisor(waves));
+      else paged_join<DH, T, 1, Args><<<(a.T_rows * waves + 3) / 4, 256, 0, s>>>(a, Divisor(waves));
       DIPACO_LAUNCH_CHECK();
     }
     return DIPACO_OK;
   };
   return dh == 32 ? run(std::integral_constant<int, 32>{}) : dh == 64 ? run(std::integral_constant<int, 64>{}) : run(std::integral_constant<int, 128>{});
 }
+template <typename T> dipaco_status launch_attention_paged(PagedArgs<T> a, int dh, void* workspace, hipStream_t s) { return launch_paged(a, dh, workspace, s); }
+template <typename T> dipaco_status launch_attention_tree(const PagedArgs<T>& a, const int* depth, const uint64_t* seen, int dh, void* workspace, hipStream_t s) {
+  TreeArgs<T> t;
+  static_cast<PagedArgs<T>&>(t) = a;
+  t.depth = depth;
+  t.seen = reinterpret_cast<const uint32_t*>(seen);
+  t.words = 2 * draft_words(a.max_new);
+  return launch_paged(t, dh, workspace, s);
+}
 template dipaco_status launch_cache_append<float>(const PagedArgs<float>&, int, hipStream_t);
 template dipaco_status launch_cache_append<bf16>(const PagedArgs<bf16>&, int, hipStream_t);
 template dipaco_status launch_attention_paged<float>(PagedArgs<float>, int, void*, hipStream_t);
 template dipaco_status launch_attention_paged<bf16>(PagedArgs<bf16>, int, void*, hipStream_t);
+template dipaco_status launch_attention_tree<float>(const PagedArgs<float>&, const int*, const uint64_t*, int, void*, hipStream_t);
+template dipaco_status launch_attention_tree<bf16>(const PagedArgs<bf16>&, const int*, const uint64_t*, int, void*, hipStream_t);
 
 }  // namespace dipaco

@@ -15,7 +15,7 @@ using Cut = PagedCut<float>;
 
 // NARROW: 16 packed rows, which every wave holds; of a tile of 64 keys a wave takes 16.  Else 64 packed rows, 16 a wave, on tiles of 32 keys.
 // b: the document, or the call's wide block; pf_smem: [stage][K | V]
-template <int DH, bool NARROW> __device__ __forceinline__ void paged_part(const PagedArgs<float>& a, int hk, int split, int b, float* pf_smem) {
+template <int DH, bool NARROW, typename A> __device__ __forceinline__ void paged_part(const A& a, int hk, int split, int b, float* pf_smem) {
   constexpr int SHIFT = NARROW ? Cut::NARROW_SHIFT : Cut::WIDE_SHIFT, TILE = 1 << SHIFT, RUNS = TILE / 16, AHEAD = 64 / RUNS;
   constexpr int STAGE = 2 * window_tile_floats<DH, TILE>();
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
@@ -39,9 +39,10 @@ template <int DH, bool NARROW> __device__ __forceinline__ void paged_part(const 
   const int t0 = split * blk.per, n_tiles = min(blk.tiles.count - t0, blk.per);
   const int G = a.group.d, r0 = blk.packed0 + (NARROW ? 0 : 16 * wave), R = r0 + m, token = a.group(R), head = hk * G + R - token * G;
   const bool valid = R < blk.packed;
-  const int pos = blk.pos0 + token, near = a.w.near_from(pos);
+  auto view = a.view(blk.row0, blk.rows, blk.pos0, blk.last, token);
   const long row = blk.row0 + token;
-  const FRowSpan span{blk.pos0 + a.group(r0), r0 < blk.packed ? blk.pos0 + a.group(min(r0 + 15, blk.packed - 1)) : -1};
+  // TREE: keys from pos0 on are seen by some rows and not by others
+  const FRowSpan span{A::TREE ? blk.pos0 - 1 : blk.pos0 + a.group(r0), r0 >= blk.packed ? -1 : A::TREE ? blk.hi : blk.pos0 + a.group(min(r0 + 15, blk.packed - 1))};
   const float* const q = a.qkv + row * (a.H + 2 * a.H_kv) * DH + head * DH;
   const float* const keys = a.cache + a.template key_offset<DH>(0, hk, 0);
   const long page_floats = ((long)2 * a.H_kv << a.page_shift) * DH, value = a.template value_from_key<DH>();
@@ -75,9 +76,9 @@ template <int DH, bool NARROW> __device__ __forceinline__ void paged_part(const 
       __syncthreads();
       if constexpr (NARROW) {
         const int s = (mine >> wave) & 1 ? F_NONE : seen_16(a.w, span, k0 + 16 * wave);
-        if (s != F_NONE) attend_16<DH>(x, qf, k_, v_, wave, k0 + 16 * wave, beyond || s != F_ALL, min(pos, blk.last), near, a.w.sinks, m, g);
+        if (s != F_NONE) attend_16<DH>(x, qf, k_, v_, wave, k0 + 16 * wave, beyond || s != F_ALL, view, m, g);
       } else {
-        attend_32<DH>(x, qf, k_, v_, k0, mine, a.w, span, beyond, min(pos, blk.last), near, m, g);
+        attend_32<DH>(x, qf, k_, v_, k0, mine, a.w, span, beyond, view, m, g);
       }
       if (more) next.store(pf_smem + ((t + 1) & 1) * STAGE);
     }
@@ -89,14 +90,14 @@ template <int DH, bool NARROW> __device__ __forceinline__ void paged_part(const 
 #pragma unroll 1
         for (int key = k0; key < k0 + (NARROW ? 16 : TILE); ++key) {
           const int page = key > blk.last ? -1 : a.page_of(b, key);
-          if (page < 0 || key > pos || (key < near && key >= a.w.sinks)) continue;
+          if (page < 0 || !view.sees(key)) continue;
           const float* const k = keys + page * page_floats + (long)(key & in_page) * DH;
           plain::add_row(x.o, __builtin_amdgcn_exp2f(__builtin_fmaf(plain::dot<DH>(q, k), head_scale<DH>() * WF_LOG2E, x.m_neg)), k + value, g);
         }
       }
     }
     for (int t = 0; t < n_tiles && __any(valid && x.m == -INFINITY); ++t)   // scores that were all -inf are not nothing (ALL_MINUS_INFINITY)
-      if (valid && x.m == -INFINITY && a.sees_any(b, pos, near, blk.last, (blk.tiles.at(t0 + t) << SHIFT) + (NARROW ? 16 * wave : 0), NARROW ? 16 : TILE)) x.m = ALL_MINUS_INFINITY;
+      if (valid && x.m == -INFINITY && a.sees_any(b, view, blk.last, (blk.tiles.at(t0 + t) << SHIFT) + (NARROW ? 16 * wave : 0), NARROW ? 16 : TILE)) x.m = ALL_MINUS_INFINITY;
   }
   if constexpr (NARROW) {   // the waves' sums meet in LDS: wave w adds columns 16 d + .. of every d with d % 4 = w
     constexpr int PER = DH / 16 * 4 * WAVE;
@@ -145,13 +146,13 @@ template <int DH, bool NARROW> __device__ __forceinline__ void paged_part(const 
   }
 }
 
-template <int DH, bool NARROW> __global__ void __launch_bounds__(WF_THREADS, NARROW && DH == 128 ? 1 : 2) paged_f32(PagedArgs<float> a, int first) {
+template <int DH, bool NARROW, template <typename> class Args> __global__ void __launch_bounds__(WF_THREADS, NARROW && DH == 128 ? 1 : 2) paged_f32(Args<float> a, int first) {
   extern __shared__ __attribute__((aligned(16))) float pf_smem[];
   const int hk = NARROW ? blockIdx.y : blockIdx.x, b = blockIdx.z + first;
   paged_part<DH, NARROW>(a, hk, NARROW ? a.narrow_split(blockIdx.x, b * a.H_kv + hk) : blockIdx.y, b, pf_smem);
 }
 // Both kinds in a launch
-template <int DH> __global__ void __launch_bounds__(WF_THREADS, DH == 128 ? 1 : 2) paged_f32_both(PagedArgs<float> a, PagedOrder order) {
+template <int DH, template <typename> class Args> __global__ void __launch_bounds__(WF_THREADS, DH == 128 ? 1 : 2) paged_f32_both(Args<float> a, PagedOrder order) {
   extern __shared__ __attribute__((aligned(16))) float pfb_smem[];
   int i = blockIdx.x;
   if (i < order.n_wide) {
@@ -170,16 +171,16 @@ template <int DH, bool NARROW> constexpr int paged_f32_lds() {
 
 }  // namespace
 
-template <int DH> dipaco_status launch_paged_narrow(const PagedArgs<float>& a, hipStream_t s) {
+template <int DH, template <typename> class Args> dipaco_status launch_paged_narrow(const Args<float>& a, hipStream_t s) {
   static std::atomic<unsigned long long> lds_set{0};
-  if (dipaco_status st = ensure_dynamic_lds(reinterpret_cast<const void*>(paged_f32<DH, true>), paged_f32_lds<DH, true>(), lds_set)) return st;
+  if (dipaco_status st = ensure_dynamic_lds(reinterpret_cast<const void*>(paged_f32<DH, true, Args>), paged_f32_lds<DH, true>(), lds_set)) return st;
   for (int b = 0; b < a.B; b += 65535) {   // documents are the grid's z
-    paged_f32<DH, true><<<dim3(a.narrow_splits.d, a.H_kv, std::min(a.B - b, 65535)), WF_THREADS, paged_f32_lds<DH, true>(), s>>>(a, b);
+    paged_f32<DH, true, Args><<<dim3(a.narrow_splits.d, a.H_kv, std::min(a.B - b, 65535)), WF_THREADS, paged_f32_lds<DH, true>(), s>>>(a, b);
     DIPACO_LAUNCH_CHECK();
   }
   return DIPACO_OK;
 }
-template <int DH> dipaco_status launch_paged_both(const PagedArgs<float>& a, int blocks, hipStream_t s) {
+template <int DH, template <typename> class Args> dipaco_status launch_paged_both(const Args<float>& a, int blocks, hipStream_t s) {
   static std::atomic<unsigned long long> lds_set{0};
   // One launch where the compute units hold all its workgroups at once: the narrow ones' LDS, twice the wide ones', then keeps nobody waiting.  Us, two launches
   // | one: 5 x up to 40 tokens over up to 700, 8 heads of 32 on 2, 13.6 | 12.5; 1 x 64 over 1000, 8 of 64, 16.7 | 15.7; 4 x up to 100 over up to 500, 8 of 128
@@ -188,24 +189,23 @@ template <int DH> dipaco_status launch_paged_both(const PagedArgs<float>& a, int
   const int64_t wide = (int64_t)a.H_kv * a.wide_splits.d, groups = wide * blocks + (int64_t)a.B * a.H_kv * a.narrow_splits.d;
   if (groups <= 256 * (163840 / LDS)) {
     static std::atomic<unsigned long long> both_set{0};
-    if (dipaco_status st = ensure_dynamic_lds(reinterpret_cast<const void*>(paged_f32_both<DH>), LDS, both_set)) return st;
+    if (dipaco_status st = ensure_dynamic_lds(reinterpret_cast<const void*>(paged_f32_both<DH, Args>), LDS, both_set)) return st;
     const PagedOrder order{Divisor(a.H_kv), Divisor((int)wide), (int)wide * blocks};
-    paged_f32_both<DH><<<(int)groups, WF_THREADS, LDS, s>>>(a, order);
+    paged_f32_both<DH, Args><<<(int)groups, WF_THREADS, LDS, s>>>(a, order);
     DIPACO_LAUNCH_CHECK();
     return DIPACO_OK;
   }
-  if (dipaco_status st = ensure_dynamic_lds(reinterpret_cast<const void*>(paged_f32<DH, false>), paged_f32_lds<DH, false>(), lds_set)) return st;
+  if (dipaco_status st = ensure_dynamic_lds(reinterpret_cast<const void*>(paged_f32<DH, false, Args>), paged_f32_lds<DH, false>(), lds_set)) return st;
   for (int b = 0; b < blocks; b += 65535) {
-    paged_f32<DH, false><<<dim3(a.H_kv, a.wide_splits.d, std::min(blocks - b, 65535)), WF_THREADS, paged_f32_lds<DH, false>(), s>>>(a, b);
+    paged_f32<DH, false, Args><<<dim3(a.H_kv, a.wide_splits.d, std::min(blocks - b, 65535)), WF_THREADS, paged_f32_lds<DH, false>(), s>>>(a, b);
     DIPACO_LAUNCH_CHECK();
   }
   return launch_paged_narrow<DH>(a, s);
 }
-template dipaco_status launch_paged_narrow<32>(const PagedArgs<float>&, hipStream_t);
-template dipaco_status launch_paged_narrow<64>(const PagedArgs<float>&, hipStream_t);
-template dipaco_status launch_paged_narrow<128>(const PagedArgs<float>&, hipStream_t);
-template dipaco_status launch_paged_both<32>(const PagedArgs<float>&, int, hipStream_t);
-template dipaco_status launch_paged_both<64>(const PagedArgs<float>&, int, hipStream_t);
-template dipaco_status launch_paged_both<128>(const PagedArgs<float>&, int, hipStream_t);
+#define DIPACO_PAGED_F32(DH, ARGS)                                                        \
+  template dipaco_status launch_paged_narrow<DH, ARGS>(const ARGS<float>&, hipStream_t); \
+  template dipaco_status launch_paged_both<DH, ARGS>(const ARGS<float>&, int, hipStream_t);
+DIPACO_PAGED_F32(32, PagedArgs) DIPACO_PAGED_F32(64, PagedArgs) DIPACO_PAGED_F32(128, PagedArgs)
+DIPACO_PAGED_F32(32, TreeArgs) DIPACO_PAGED_F32(64, TreeArgs) DIPACO_PAGED_F32(128, TreeArgs)
 
 }  // namespace dipaco

@@ -45,19 +45,17 @@ template <int DH> struct PagePlace {
   __device__ __forceinline__ long at(int page, int pos) const { return page * page_bytes + (long)((pos & ((1 << shift) - 1)) * DH * 2); }
 };
 
-// A row of the block: which, where its query lies and what it sees
+// A row of the block: which, and where its query lies
 template <int DH> struct PagedRow {
   bool valid;
   long row;
-  int head, pos, near;
+  int head;
   const bf16* q;
-  __device__ __forceinline__ PagedRow(const PagedArgs<bf16>& a, int R, int packed, int row0, int pos0, int hk) {
+  __device__ __forceinline__ PagedRow(const PagedArgs<bf16>& a, int R, int packed, int row0, int hk) {
     const int G = a.group.d, token = a.group(R);
     valid = R < packed;
     row = row0 + token;
     head = hk * G + R - token * G;
-    pos = pos0 + token;
-    near = a.w.near_from(pos);
     q = a.qkv + row * (a.H + 2 * a.H_kv) * DH + head * DH;
   }
   __device__ __forceinline__ void load(uint4 (&qf)[DH / 16], int h) const {
@@ -66,13 +64,13 @@ template <int DH> struct PagedRow {
   }
 };
 // o of a row over the keys k0 .. k0 + n - 1 that it sees, pair by pair: x.o += ...
-template <int DH>
-__device__ __forceinline__ void add_seen(SoftmaxRow<DH>& x, const PagedArgs<bf16>& a, const PagePlace<DH>& at, const PagedRow<DH>& row, int k0, int n, int h) {
+template <int DH, typename View>
+__device__ __forceinline__ void add_seen(SoftmaxRow<DH>& x, const PagedArgs<bf16>& a, const PagePlace<DH>& at, const PagedRow<DH>& row, const View& view, int k0, int n, int h) {
   const float sc = score_scale<DH>() * LOG2E;
 #pragma unroll 1
   for (int key = k0; key < k0 + n; ++key) {
     const int page = key > at.last ? -1 : a.page_of(at.b, key);
-    if (page < 0 || key > row.pos || (key < row.near && key >= a.w.sinks)) continue;
+    if (page < 0 || !view.sees(key)) continue;
     const char* const k = at.base + at.at(page, key);
     const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(plain::dot<DH>(row.q, reinterpret_cast<const bf16*>(k)), sc, x.m_neg));
     plain::add_row(x.o, p, reinterpret_cast<const bf16*>(k + at.value_bytes), h);
@@ -80,14 +78,14 @@ __device__ __forceinline__ void add_seen(SoftmaxRow<DH>& x, const PagedArgs<bf16
 }
 
 // a row whose scores so far were all -inf has seen something if it sees any of the n keys from k0 on
-template <int DH>
-__device__ __forceinline__ void note_seen(SoftmaxRow<DH>& x, const PagedArgs<bf16>& a, const PagePlace<DH>& at, const PagedRow<DH>& row, int k0, int n) {
-  if (row.valid && x.m == -INFINITY && a.sees_any(at.b, row.pos, row.near, at.last, k0, n)) x.m = ALL_MINUS_INFINITY;
+template <int DH, typename View>
+__device__ __forceinline__ void note_seen(SoftmaxRow<DH>& x, const PagedArgs<bf16>& a, const PagePlace<DH>& at, const PagedRow<DH>& row, const View& view, int k0, int n) {
+  if (row.valid && x.m == -INFINITY && a.sees_any(at.b, view, at.last, k0, n)) x.m = ALL_MINUS_INFINITY;
 }
 
 // ---- wide ----------------------------------------------------------------------------------------------------------
 // pw_smem: [stage][K | V]
-template <int DH> __device__ __forceinline__ void wide_block(const PagedArgs<bf16>& a, int hk, int split, int block, char* pw_smem) {
+template <int DH, typename A> __device__ __forceinline__ void wide_block(const A& a, int hk, int split, int block, char* pw_smem) {
   constexpr int KS = DH / 16, NP = panels<DH>(), TILE_BYTES = tile_bytes<DH>();
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, h = lane >> 5;
   const WideBlock at_block(a, block, lane);
@@ -98,13 +96,14 @@ template <int DH> __device__ __forceinline__ void wide_block(const PagedArgs<bf1
   if (!blk.has(split)) return;
   const int r0 = blk.packed0 + 32 * wave;
   int R = r0 + r;
-  const int pos = blk.pos0 + a.group(R), near = a.w.near_from(pos);
-  const RowSpan span{blk.pos0 + a.group(r0), r0 < blk.packed ? blk.pos0 + a.group(min(r0 + 31, blk.packed - 1)) : -1};
+  auto view = a.view(blk.row0, blk.rows, blk.pos0, blk.last, a.group(R));
+  // TREE: keys from pos0 on are seen by some rows and not by others
+  const RowSpan span{A::TREE ? blk.pos0 - 1 : blk.pos0 + a.group(r0), r0 >= blk.packed ? -1 : A::TREE ? blk.hi : blk.pos0 + a.group(min(r0 + 31, blk.packed - 1))};
   SoftmaxRow<DH> x;
   x.clear();
   if (n_tiles > 0) {
     uint4 qf[KS];
-    PagedRow<DH>(a, R, blk.packed, blk.row0, blk.pos0, hk).load(qf, h);
+    PagedRow<DH>(a, R, blk.packed, blk.row0, hk).load(qf, h);
     const FragOff fo = frag_offsets(lane);
     const TrOff to = tr_offsets(lane);
     const uint32_t smem_addr = (uint32_t)(uintptr_t)pw_smem;
@@ -156,19 +155,20 @@ template <int DH> __device__ __forceinline__ void wide_block(const PagedArgs<bf1
       if (t + 1 < n_tiles) holes = issue(t + 1, (t + 1) & 1);
       const char* k_ = pw_smem + (t & 1) * 2 * TILE_BYTES;
       // a position behind the table's end holds no key: rows there see up to the last one that does
-      attend_tile<DH>(x, qf, k_, k_ + TILE_BYTES, fo, to, blk.tiles.at(t0 + t) * 64, mine, a.w, span, blk.hi > at.last ? UPPER | LOWER : 0, min(pos, at.last), near, lane);
+      attend_tile<DH>(x, qf, k_, k_ + TILE_BYTES, fo, to, blk.tiles.at(t0 + t) * 64, mine, a.w, span, blk.hi > at.last ? UPPER | LOWER : 0, view, lane);
     }
     x.l += __shfl_xor(x.l, 32, WAVE);
     asm volatile("" : "+v"(R));   // what follows is formed anew, not kept through the loop
-    const PagedRow<DH> row(a, R, blk.packed, blk.row0, blk.pos0, hk);
+    const PagedRow<DH> row(a, R, blk.packed, blk.row0, hk);
+    if constexpr (!A::TREE) view = a.view(blk.row0, blk.rows, blk.pos0, blk.last, a.group(R));
     if (__any(row.valid && plain::not_finite(x.o)) && row.valid) {
       plain::clear(x.o);
-      for (int t = 0; t < n_tiles; ++t) add_seen<DH>(x, a, at, row, blk.tiles.at(t0 + t) * 64, 64, h);
+      for (int t = 0; t < n_tiles; ++t) add_seen<DH>(x, a, at, row, view, blk.tiles.at(t0 + t) * 64, 64, h);
     }
-    for (int t = 0; t < n_tiles && __any(row.valid && x.m == -INFINITY); ++t) note_seen<DH>(x, a, at, row, blk.tiles.at(t0 + t) * 64, 64);
+    for (int t = 0; t < n_tiles && __any(row.valid && x.m == -INFINITY); ++t) note_seen<DH>(x, a, at, row, view, blk.tiles.at(t0 + t) * 64, 64);
   }
   asm volatile("" : "+v"(R));
-  const PagedRow<DH> row(a, R, blk.packed, blk.row0, blk.pos0, hk);
+  const PagedRow<DH> row(a, R, blk.packed, blk.row0, hk);
   if (!row.valid) return;
   if (blk.whole()) {
     store_transposed_out(a.o + (row.row * a.H + row.head) * DH, x.o, h, x.m == -INFINITY ? 0.f : 1.0f / x.l);
@@ -194,14 +194,15 @@ template <int DH, int NW, int NS> constexpr int narrow_lds() {
   return RINGS > SUMS ? RINGS : SUMS;
 }
 // pn_smem: [wave][stage]
-template <int DH, int NW, int NS> __device__ __forceinline__ void narrow_document(const PagedArgs<bf16>& a, int hk, int b, int split, char* pn_smem) {
+template <int DH, int NW, int NS, typename A> __device__ __forceinline__ void narrow_document(const A& a, int hk, int b, int split, char* pn_smem) {
   constexpr int KS = DH / 16, DT = DH / 32, NP = panels<DH>(), STAGE = narrow_stage<DH>(), LPW = 8 * NP;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, h = lane >> 5;
   const PagedBlock<Cut::NARROW_SHIFT> blk(a, b, 0, Cut::NARROW_ROWS, a.narrow_splits, a.narrow_keys);
   if (blk.packed == 0 || blk.packed > Cut::NARROW_ROWS || !blk.has(split)) return;
   const int t0 = split * blk.per, end = min(t0 + blk.per, blk.tiles.count), n = (end - t0 - wave + NW - 1) / NW;   // this wave's halves: t0 + wave, + NW, ..
-  const PagedRow<DH> row(a, r, blk.packed, blk.row0, blk.pos0, hk);
-  const RowSpan span{blk.lo, blk.hi};
+  const PagedRow<DH> row(a, r, blk.packed, blk.row0, hk);
+  auto view = a.view(blk.row0, blk.rows, blk.pos0, blk.last, a.group(r));
+  const RowSpan span{A::TREE ? blk.pos0 - 1 : blk.lo, blk.hi};
   SoftmaxRow<DH> x;
   x.clear();
   if (n > 0) {
@@ -271,7 +272,7 @@ template <int DH, int NW, int NS> __device__ __forceinline__ void narrow_documen
       const int s = holes == 3 ? 0 : seen_half(a.w, span, k0);
       const char* k_ = ring + (t % NS) * STAGE;
       if (s)
-        attend_half<DH>(x, qf, k_, k_ + 4096, fo, to, k0, s | (blk.hi > at.last ? UPPER | LOWER : 0), holes, min(row.pos, at.last), row.near, a.w.sinks, lane);
+        attend_half<DH>(x, qf, k_, k_ + 4096, fo, to, k0, s | (blk.hi > at.last ? UPPER | LOWER : 0), holes, view, lane);
       asm volatile("" ::: "memory");
       if (t + NS < n) {
         __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (3 << 14));   // lgkmcnt(0): every read of the stage that is filled again has returned
@@ -281,9 +282,9 @@ template <int DH, int NW, int NS> __device__ __forceinline__ void narrow_documen
     x.l += __shfl_xor(x.l, 32, WAVE);
     if (__any(row.valid && plain::not_finite(x.o)) && row.valid) {
       plain::clear(x.o);
-      for (int t = 0; t < n; ++t) add_seen<DH>(x, a, at, row, half_at(t), 32, h);
+      for (int t = 0; t < n; ++t) add_seen<DH>(x, a, at, row, view, half_at(t), 32, h);
     }
-    for (int t = 0; t < n && __any(row.valid && x.m == -INFINITY); ++t) note_seen<DH>(x, a, at, row, half_at(t), 32);
+    for (int t = 0; t < n && __any(row.valid && x.m == -INFINITY); ++t) note_seen<DH>(x, a, at, row, view, half_at(t), 32);
   }
   // the waves' sums meet in LDS: wave w adds accumulator elements 4 g .. 4 g + 3 of every 32 columns for g = w, w + NW, ..
   constexpr int PER = 16 * DT * WAVE;
@@ -336,13 +337,13 @@ template <int DH, int NW, int NS> __device__ __forceinline__ void narrow_documen
 }
 
 // Documents of a call that has only narrow ones
-template <int DH, int NW, int NS> __global__ void __launch_bounds__(WAVE * NW, 1) paged_narrow_mfma(PagedArgs<bf16> a, int b0) {
+template <int DH, int NW, int NS, template <typename> class Args> __global__ void __launch_bounds__(WAVE * NW, 1) paged_narrow_mfma(Args<bf16> a, int b0) {
   extern __shared__ __attribute__((aligned(16))) char pn_smem[];
   const int hk = blockIdx.y, b = blockIdx.z + b0;
   narrow_document<DH, NW, NS>(a, hk, b, a.narrow_split(blockIdx.x, b * a.H_kv + hk), pn_smem);
 }
 // A call with wide blocks, and in the same launch behind them the narrow documents that it may have
-template <int DH> __global__ void __launch_bounds__(AT_THREADS, 2) paged_both_mfma(PagedArgs<bf16> a, PagedOrder order) {
+template <int DH, template <typename> class Args> __global__ void __launch_bounds__(AT_THREADS, 2) paged_both_mfma(Args<bf16> a, PagedOrder order) {
   extern __shared__ __attribute__((aligned(16))) char pb_smem[];
   int i = blockIdx.x;
   if (i < order.n_wide) {
@@ -357,13 +358,13 @@ template <int DH> __global__ void __launch_bounds__(AT_THREADS, 2) paged_both_mf
 
 }  // namespace
 
-template <int DH> dipaco_status launch_paged_narrow(const PagedArgs<bf16>& a, hipStream_t s) {
+template <int DH, template <typename> class Args> dipaco_status launch_paged_narrow(const Args<bf16>& a, hipStream_t s) {
   auto run = [&](auto NWc, auto NSc) -> dipaco_status {
     constexpr int NW = decltype(NWc)::value, NS = decltype(NSc)::value, LDS = narrow_lds<DH, NW, NS>();
     static std::atomic<unsigned long long> lds_set{0};
-    if (dipaco_status st = ensure_dynamic_lds(reinterpret_cast<const void*>(paged_narrow_mfma<DH, NW, NS>), LDS, lds_set)) return st;
+    if (dipaco_status st = ensure_dynamic_lds(reinterpret_cast<const void*>(paged_narrow_mfma<DH, NW, NS, Args>), LDS, lds_set)) return st;
     for (int b = 0; b < a.B; b += 65535) {   // documents are the grid's z
-      paged_narrow_mfma<DH, NW, NS><<<dim3(a.narrow_splits.d, a.H_kv, std::min(a.B - b, 65535)), WAVE * NW, LDS, s>>>(a, b);
+      paged_narrow_mfma<DH, NW, NS, Args><<<dim3(a.narrow_splits.d, a.H_kv, std::min(a.B - b, 65535)), WAVE * NW, LDS, s>>>(a, b);
       DIPACO_LAUNCH_CHECK();
     }
     return DIPACO_OK;
@@ -373,21 +374,20 @@ template <int DH> dipaco_status launch_paged_narrow(const PagedArgs<bf16>& a, hi
   if (a.narrow_keys > PagedCut<bf16>::LEAST_KEYS) return run(integral_constant<int, DH == 128 ? 4 : 8>{}, integral_constant<int, 2>{});
   return run(integral_constant<int, DH == 128 ? 2 : 4>{}, integral_constant<int, DH == 128 ? 2 : 1>{});
 }
-template <int DH> dipaco_status launch_paged_both(const PagedArgs<bf16>& a, int blocks, hipStream_t s) {
+template <int DH, template <typename> class Args> dipaco_status launch_paged_both(const Args<bf16>& a, int blocks, hipStream_t s) {
   constexpr int WIDE_LDS = 4 * tile_bytes<DH>(), NARROW_LDS = narrow_lds<DH, 4, 1>(), LDS = WIDE_LDS > NARROW_LDS ? WIDE_LDS : NARROW_LDS;
   static std::atomic<unsigned long long> lds_set{0};
-  if (dipaco_status st = ensure_dynamic_lds(reinterpret_cast<const void*>(paged_both_mfma<DH>), LDS, lds_set)) return st;
+  if (dipaco_status st = ensure_dynamic_lds(reinterpret_cast<const void*>(paged_both_mfma<DH, Args>), LDS, lds_set)) return st;
   const int wide = a.H_kv * (int)a.wide_splits.d;
   const PagedOrder order{Divisor(a.H_kv), Divisor(wide), blocks * wide};
-  paged_both_mfma<DH><<<order.n_wide + a.B * a.H_kv * (int)a.narrow_splits.d, AT_THREADS, LDS, s>>>(a, order);
+  paged_both_mfma<DH, Args><<<order.n_wide + a.B * a.H_kv * (int)a.narrow_splits.d, AT_THREADS, LDS, s>>>(a, order);
   DIPACO_LAUNCH_CHECK();
   return DIPACO_OK;
 }
-template dipaco_status launch_paged_narrow<32>(const PagedArgs<bf16>&, hipStream_t);
-template dipaco_status launch_paged_narrow<64>(const PagedArgs<bf16>&, hipStream_t);
-template dipaco_status launch_paged_narrow<128>(const PagedArgs<bf16>&, hipStream_t);
-template dipaco_status launch_paged_both<32>(const PagedArgs<bf16>&, int, hipStream_t);
-template dipaco_status launch_paged_both<64>(const PagedArgs<bf16>&, int, hipStream_t);
-template dipaco_status launch_paged_both<128>(const PagedArgs<bf16>&, int, hipStream_t);
+#define DIPACO_PAGED_MFMA(DH, ARGS)                                                      \
+  template dipaco_status launch_paged_narrow<DH, ARGS>(const ARGS<bf16>&, hipStream_t); \
+  template dipaco_status launch_paged_both<DH, ARGS>(const ARGS<bf16>&, int, hipStream_t);
+DIPACO_PAGED_MFMA(32, PagedArgs) DIPACO_PAGED_MFMA(64, PagedArgs) DIPACO_PAGED_MFMA(128, PagedArgs)
+DIPACO_PAGED_MFMA(32, TreeArgs) DIPACO_PAGED_MFMA(64, TreeArgs) DIPACO_PAGED_MFMA(128, TreeArgs)
 
 }  // namespace dipaco

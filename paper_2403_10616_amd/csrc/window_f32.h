@@ -62,18 +62,36 @@ template <int DH> struct FSoftmaxRow {
     l = 0.f;
   }
 };
+// bit e: the lane's row sees key 4 g + e of the 16 from k0 on
+__device__ __forceinline__ int seen_keys(const ChainView& x, int k0, int g) {
+  int bits = 0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) bits |= x.sees(k0 + 4 * g + e) ? 1 << e : 0;
+  return bits;
+}
+__device__ __forceinline__ int seen_keys(TreeView& x, int k0, int g) {
+  const uint32_t word = x.word(k0) & 0xffffu;
+  x.note(k0, word);
+  int bits = word >> (4 * g);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const int key = k0 + 4 * g + e;
+    if (key < x.near && key >= x.sinks) bits &= ~(1 << e);
+  }
+  return bits;
+}
 // 16 keys, run t of the tile k_ (v_), from position k0 on
-template <int DH>
-__device__ __forceinline__ void attend_16(FSoftmaxRow<DH>& x, const RowFrag<DH>& qf, const float* k_, const float* v_, int t, int k0, bool masked, int pos,
-                                          int near, int sinks, int m, int g) {
+template <int DH, typename View>
+__device__ __forceinline__ void attend_16(FSoftmaxRow<DH>& x, const RowFrag<DH>& qf, const float* k_, const float* v_, int t, int k0, bool masked, View& view,
+                                          int m, int g) {
   const float sc = head_scale<DH>() * WF_LOG2E;
   f32x4 st = {0.f, 0.f, 0.f, 0.f};
   rows_product<DH>(st, k_, t, qf, m, g);
   float mx = -INFINITY;
+  const int seen = masked ? seen_keys(view, k0, g) : 15;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    const int key = k0 + 4 * g + e;
-    if (masked && !(key <= pos && (key >= near || key < sinks))) st[e] = -INFINITY;
+    if (!(seen & (1 << e))) st[e] = -INFINITY;
     mx = fmaxf(mx, st[e]);
   }
   const float mn = fmaxf(x.m, max_groups(mx) * sc);
@@ -95,12 +113,12 @@ __device__ __forceinline__ void attend_16(FSoftmaxRow<DH>& x, const RowFrag<DH>&
   cols_product<DH>(x.o, v_, t, st, m, g);
 }
 // a tile of 32 keys: the runs that are seen
-template <int DH>
+template <int DH, typename View>
 __device__ __forceinline__ void attend_32(FSoftmaxRow<DH>& x, const RowFrag<DH>& qf, const float* k_, const float* v_, int k0, int holes, const Window& w,
-                                          const FRowSpan& span, bool masked, int pos, int near, int m, int g) {
+                                          const FRowSpan& span, bool masked, View& view, int m, int g) {
   const int a = holes & 1 ? F_NONE : seen_16(w, span, k0), b = holes & 2 ? F_NONE : seen_16(w, span, k0 + 16);
-  if (a != F_NONE) attend_16<DH>(x, qf, k_, v_, 0, k0, masked || a != F_ALL, pos, near, w.sinks, m, g);
-  if (b != F_NONE) attend_16<DH>(x, qf, k_, v_, 1, k0 + 16, masked || b != F_ALL, pos, near, w.sinks, m, g);
+  if (a != F_NONE) attend_16<DH>(x, qf, k_, v_, 0, k0, masked || a != F_ALL, view, m, g);
+  if (b != F_NONE) attend_16<DH>(x, qf, k_, v_, 1, k0 + 16, masked || b != F_ALL, view, m, g);
 }
 
 }  // namespace

@@ -72,6 +72,21 @@ __device__ __forceinline__ void hide(f32x16& v, int seen, float hidden, int k0, 
   }
 }
 
+__device__ __forceinline__ void hide(f32x16& v, int seen, float hidden, int k0, const ChainView& x, int, int lane) {
+  hide(v, seen, hidden, k0, x.pos, x.near, x.sinks, lane);
+}
+// Rows of a tree: UPPER where some of the keys are no cached positions.  holes: bit per 16 keys that nobody sees
+__device__ __forceinline__ void hide(f32x16& v, int seen, float hidden, int k0, TreeView& x, int holes, int lane) {
+  if (seen & UPPER) {
+    const uint32_t word = x.word(k0) & ~((holes & 1 ? 0xffffu : 0u) | (holes & 2 ? 0xffff0000u : 0u));
+    x.note(k0, word);
+    const uint32_t mine = word >> (4 * (lane >> 5));
+#pragma unroll
+    for (int e = 0; e < 16; ++e) v[e] = mine & (1u << (8 * (e >> 2) + (e & 3))) ? v[e] : hidden;
+  }
+  if (seen & LOWER) hide(v, LOWER, hidden, k0, 0, x.near, x.sinks, lane);
+}
+
 // One query row a lane pair: reference exponent, half row sum, O^T
 template <int DH> struct SoftmaxRow {
   f32x16 o[DH / 32];
@@ -87,9 +102,9 @@ template <int DH> struct SoftmaxRow {
 
 // 32 keys from k0 on, of which the rows see `seen`.  k_, v_: their first row in LDS.  holes: bit per 16 keys that nobody sees.
 // One path for all halves: with another one for two halves at a time the compiler kept two sets of accumulators and copied between them.
-template <int DH>
+template <int DH, typename View>
 __device__ __forceinline__ void attend_half(SoftmaxRow<DH>& x, const uint4 (&qf)[DH / 16], const char* k_, const char* v_, const FragOff& fo, const TrOff& to,
-                                            int k0, int seen, int holes, int pos, int near, int sinks, int lane) {
+                                            int k0, int seen, int holes, View& view, int lane) {
   constexpr int KS = DH / 16, DT = DH / 32;
   f32x16 st;
   zero(st);
@@ -106,7 +121,7 @@ __device__ __forceinline__ void attend_half(SoftmaxRow<DH>& x, const uint4 (&qf)
 #pragma unroll
     for (int i = 0; i < 2; ++i) vf[dt][i] = tr_read(v_, to, dt, i);
   __builtin_amdgcn_sched_barrier(0);
-  hide(st, seen, -INFINITY, k0, pos, near, sinks, lane);
+  hide(st, seen, -INFINITY, k0, view, holes, lane);
   if (holes) {   // wave-uniform
     asm volatile("");
 #pragma unroll
@@ -141,12 +156,12 @@ __device__ __forceinline__ void attend_half(SoftmaxRow<DH>& x, const uint4 (&qf)
   }
 }
 // a tile of 64 keys: the halves that are seen.  force: bounds to apply whatever the span says
-template <int DH>
+template <int DH, typename View>
 __device__ __forceinline__ void attend_tile(SoftmaxRow<DH>& x, const uint4 (&qf)[DH / 16], const char* k_, const char* v_, const FragOff& fo, const TrOff& to,
-                                            int k0, int holes, const Window& w, const RowSpan& span, int force, int pos, int near, int lane) {
+                                            int k0, int holes, const Window& w, const RowSpan& span, int force, View& view, int lane) {
   const int a = (holes & 3) == 3 ? 0 : seen_half(w, span, k0), b = holes >> 2 == 3 ? 0 : seen_half(w, span, k0 + 32);
-  if (a) attend_half<DH>(x, qf, k_, v_, fo, to, k0, a | force, holes & 3, pos, near, w.sinks, lane);
-  if (b) attend_half<DH>(x, qf, k_ + 4096, v_ + 4096, fo, to, k0 + 32, b | force, holes >> 2, pos, near, w.sinks, lane);
+  if (a) attend_half<DH>(x, qf, k_, v_, fo, to, k0, a | force, holes & 3, view, lane);
+  if (b) attend_half<DH>(x, qf, k_ + 4096, v_ + 4096, fo, to, k0 + 32, b | force, holes >> 2, view, lane);
 }
 
 // Two operands' rows of one document and head (keys and values; queries and output gradients), ld0 and ld1 elements apart
