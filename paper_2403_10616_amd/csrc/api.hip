@@ -1233,7 +1233,7 @@ dipaco_status dipaco_k_attention_tree(int32_t dtype, const void* qkv, const int3
 
 size_t dipaco_k_draft_verify_workspace_bytes(int32_t T, int32_t B, int32_t V) {
   if (check_drafts(T, B, 1) != DIPACO_OK || V < 1 || V > (1 << 18)) return 0;
-  return draft_verify_workspace_bytes(B, V);
+  return draft_verify_workspace_bytes(T, B, V);
 }
 
 dipaco_status dipaco_k_draft_verify(int32_t dtype, const void* target, const void* draft, const int32_t* tokens, const int32_t* parent, const int32_t* row_start,
@@ -1253,13 +1253,13 @@ dipaco_status dipaco_k_draft_verify(int32_t dtype, const void* target, const voi
     if (draft) TRY(check_ptr(draft, "draft"));
   }
   if (max_new > 0) TRY(check_ptr(path, "path"));
-  if (workspace_bytes < draft_verify_workspace_bytes(B, V)) return fail(DIPACO_EWORKSPACE, "workspace smaller than dipaco_k_draft_verify_workspace_bytes");
+  if (workspace_bytes < draft_verify_workspace_bytes(T, B, V)) return fail(DIPACO_EWORKSPACE, "workspace smaller than dipaco_k_draft_verify_workspace_bytes");
   hipStream_t st = static_cast<hipStream_t>(stream);
-  const double scale = temperature > 0.f ? 1.0 / temperature : 0.0, draft_scale = draft ? 1.0 / draft_temperature : 1.0;
+  const double log2_e = 1.4426950408889634, rate = temperature > 0.f ? log2_e / temperature : 0.0, draft_rate = draft ? log2_e / draft_temperature : 1.0;
   auto run = [&](auto zero) {
     using E = decltype(zero);
     return launch_draft_verify(VerifyArgs<E>{static_cast<const E*>(target), static_cast<const E*>(draft), tokens, parent, row_start, u, v, path, kept, next, T, B,
-                                             max_new, V, scale, draft_scale, distinct, static_cast<double*>(workspace)}, st);
+                                             max_new, V, rate, draft_rate, distinct, static_cast<double*>(workspace)}, st);
   };
   return dtype == DIPACO_BF16 ? run(bf16{}) : run(float{});
 }

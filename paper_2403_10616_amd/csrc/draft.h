@@ -16,9 +16,9 @@ template <typename T> struct VerifyArgs {
   const float *u, *v;        // [T rows], [B]
   int *path, *kept, *next;   // [B, max_new], [B], [B]
   int T_rows, B, max_new, V;
-  double scale, draft_scale; // 1 / temperature; 0: all probability at the first maximum
+  double rate, draft_rate;   // log2(e) / temperature; 0: all probability at the first maximum
   int distinct;
-  double* rest;              // [B, V]: what the target has left of a document's row
+  double* rest;              // [B, V]: what a document's walk has left of the target's row; other parts of the workspace follow
 };
 
 constexpr int KEEP_MOST_LAYERS = 64;   // of a launch

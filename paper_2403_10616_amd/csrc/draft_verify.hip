@@ -1,7 +1,13 @@
 // Which drafted tokens stay, and the token behind them (include/dipaco_kernels.h has the rule): a workgroup walks a document's tree from row 0.
 //
-// A token hangs on a border (u q < r, a running sum above v times the whole), so exponentials, sums and what is left of the target are 64-bit numbers: then the
-// order of a sum decides nothing but one draw in 10^10.
+// A token hangs on a border (u q < r, a running sum above v times the whole), so exponentials, sums and what is left of the target are 64-bit numbers: then
+// neither the order of a sum nor an exponential's last digits (2^-42 here) decide more than one draw in 10^10.
+//
+// A row of scores is cut into up to 32 parts of whole 1024 scores, a wave each: largest score, sum of exponentials against it.  From these the row's
+// sum is formed, and the part that a drawn token lies in is found without reading the others again; only parts that hold refused tokens are summed anew.
+#include <algorithm>
+#include <type_traits>
+
 #include "draft.h"
 #include "kernels.h"
 
@@ -9,15 +15,50 @@ namespace dipaco {
 
 namespace {
 
-constexpr int DV_THREADS = 1024, DV_WAVES = DV_THREADS / 64;
+constexpr int DV_THREADS = 1024, DV_WAVES = DV_THREADS / 64, DV_PARTS = 32, DV_CHUNK = 1024;
 
-__device__ __forceinline__ double wave_total(double v) {
-#pragma unroll
-  for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d, WAVE);
+// 2^t for t <= 0, to 2^-42 of it: 2^f = sum of (f ln 2)^k / k! for |f| <= 1/2, up to k = 10 (the next term is below 2^-42)
+__device__ __forceinline__ double power_of_two(double t) {
+  t = fmax(t, -1100.0);   // what is far below, -inf and NaN: 0 in 64 bits
+  const double n = rint(t), f = t - n;
+  double p = 7.054911620801121e-09;
+  p = fma(p, f, 1.0178086009239696e-07);
+  p = fma(p, f, 1.3215486790144305e-06);
+  p = fma(p, f, 1.5252733804059838e-05);
+  p = fma(p, f, 1.5403530393381606e-04);
+  p = fma(p, f, 1.3333558146428441e-03);
+  p = fma(p, f, 9.618129107628477e-03);
+  p = fma(p, f, 5.5504108664821576e-02);
+  p = fma(p, f, 2.402265069591007e-01);
+  p = fma(p, f, 6.931471805599453e-01);
+  p = fma(p, f, 1.0);
+  return ldexp(p, (int)n);
+}
+template <int CTRL, int ROW_MASK> __device__ __forceinline__ double dpp_fetch64(double v) {
+  const uint64_t b = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)b, CTRL, ROW_MASK, 0xf, false);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(b >> 32), CTRL, ROW_MASK, 0xf, false);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ double lane_value(double v, int lane) {
+  const uint64_t b = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)b, lane), hi = __builtin_amdgcn_readlane((int)(uint32_t)(b >> 32), lane);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+// lane i: the sum of lanes 0 .. i, in a fixed order
+__device__ __forceinline__ double wave_upto(double v) {
+  v += dpp_fetch64<0x111, 0xf>(v);   // row_shr 1, 2, 4, 8
+  v += dpp_fetch64<0x112, 0xf>(v);
+  v += dpp_fetch64<0x114, 0xf>(v);
+  v += dpp_fetch64<0x118, 0xf>(v);
+  v += dpp_fetch64<0x142, 0xa>(v);   // row_bcast15 into rows 1 and 3
+  v += dpp_fetch64<0x143, 0xc>(v);   // row_bcast31 into rows 2 and 3
   return v;
 }
+__device__ __forceinline__ double wave_total(double v) { return lane_value(wave_upto(v), 63); }
+
 // VEC scores from y0 on, which any address may hold; -inf behind the last
-template <typename T> __device__ __forceinline__ void load_scores(const T* row, int y0, int V, float (&x)[Vec16<T>::N]) {
+template <typename T> __device__ __forceinline__ void load_scores(const T* row, int y0, int V, float* x) {
   constexpr int VEC = Vec16<T>::N;
   if (y0 + VEC <= V) {
     T e[VEC];
@@ -30,259 +71,362 @@ template <typename T> __device__ __forceinline__ void load_scores(const T* row, 
   }
 }
 
-struct RowStat {
+// rate: log2(e) / temperature; 0: all probability at the first maximum
+__device__ __forceinline__ double weight(double rate, float top, int at, float x, int y) {
+  return rate != 0.0 ? power_of_two(fma((double)x, rate, -(double)top * rate)) : y == at ? 1.0 : 0.0;
+}
+
+struct PartStat {
   float top;      // largest score
-  int at;         // its first place
-  double total;   // sum of exp((x - top) scale)
-  bool ok;        // whether the row is a distribution: no NaN, no +inf, something above -inf
+  int at;         // its first place (formed where rate is 0)
+  double total;   // sum of 2^((x - top) rate); NaN where a score is NaN or +inf
+};
+struct Cut {
+  int len, count;   // scores of a part, parts
+  __host__ __device__ explicit Cut(int V) : len(((V + DV_PARTS - 1) / DV_PARTS + DV_CHUNK - 1) / DV_CHUNK * DV_CHUNK), count((V + len - 1) / len) {}
 };
 
-template <typename T> struct Walk {
-  static constexpr int VEC = Vec16<T>::N;
-  const VerifyArgs<T>& a;
-  double* const sums;           // [2 DV_WAVES]
-  uint32_t* const refused;      // [V bits] tokens of this row that were tried and not taken
-  const int tid, lane, wave;
-  __device__ __forceinline__ Walk(const VerifyArgs<T>& a, double* sums, uint32_t* refused)
-      : a(a), sums(sums), refused(refused), tid(threadIdx.x), lane(threadIdx.x & 63), wave(threadIdx.x >> 6) {}
-  __device__ __forceinline__ bool is_refused(int y) const { return (refused[y >> 5] >> (y & 31)) & 1; }
-  // over the workgroup, in every thread, waves added in order
-  __device__ __forceinline__ double total(double v) const {
-    v = wave_total(v);
-    __syncthreads();
-    if (lane == 0) sums[wave] = v;
-    __syncthreads();
-    double t = 0.0;
-#pragma unroll
-    for (int w = 0; w < DV_WAVES; ++w) t += sums[w];
-    return t;
-  }
-  __device__ RowStat stat(const T* row, double scale) const {
-    float top = -INFINITY;
-    bool nan = false;
-    for (int y0 = tid * VEC; y0 < a.V; y0 += DV_THREADS * VEC) {
-      float x[VEC];
-      load_scores(row, y0, a.V, x);
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) {
-        top = fmaxf(top, x[i]);
-        nan |= x[i] != x[i];
-      }
-    }
-    top = wave_max(top);
-    const bool bad = __syncthreads_or(nan);
-    float* const tops = reinterpret_cast<float*>(sums);
-    if (lane == 0) tops[wave] = top;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < DV_WAVES; ++w) top = fmaxf(top, tops[w]);
-    RowStat s{top, a.V, 0.0, !bad && top != INFINITY && top != -INFINITY};
-    if (!s.ok) return s;
-    double e = 0.0;
-    int at = a.V;
-    for (int y0 = tid * VEC; y0 < a.V; y0 += DV_THREADS * VEC) {
-      float x[VEC];
-      load_scores(row, y0, a.V, x);
-#pragma unroll
-      for (int i = VEC - 1; i >= 0; --i) {
-        if (x[i] == top) at = min(at, y0 + i);
-        if (scale != 0.0) e += exp(((double)x[i] - top) * scale);
-      }
-    }
-    s.total = scale != 0.0 ? total(e) : 1.0;
-    // the first place: the smallest index, an exact maximum of 64-bit numbers
-    double first = (double)-at;
-#pragma unroll
-    for (int d = 32; d; d >>= 1) first = fmax(first, __shfl_xor(first, d, WAVE));
-    __syncthreads();
-    if (lane == 0) sums[wave] = first;
-    __syncthreads();
-    for (int w = 0; w < DV_WAVES; ++w) first = fmax(first, sums[w]);
-    s.at = (int)-first;
-    return s;
-  }
-  // not normalised: divided by total it is the probability of y, whose score is x
-  __device__ __forceinline__ double weight(const RowStat& s, double scale, float x, int y) const {
-    return scale != 0.0 ? exp(((double)x - s.top) * scale) : y == s.at ? 1.0 : 0.0;
-  }
-  // The first y whose running sum of weights is above v of them all; per(y0, w) fills VEC weights from y0 on.  -1 where there is none.
-  template <typename F> __device__ int sample(double v, F per) const {
-    int lo = 0, n = a.V;              // the answer lies in [lo, lo + n)
-    double before = 0.0, target = 0.0;
-    for (bool first = true;; first = false) {
-      const int part = ((n + DV_WAVES - 1) / DV_WAVES + VEC - 1) / VEC * VEC;   // of a wave
-      double e = 0.0;
-      for (int y0 = lo + wave * part + lane * VEC; y0 < min(lo + (wave + 1) * part, lo + n); y0 += 64 * VEC) {
-        double w[VEC];
-        per(y0, w);
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) e += y0 + i < lo + n ? w[i] : 0.0;
-      }
-      e = wave_total(e);
-      __syncthreads();
-      if (lane == 0) sums[wave] = e;
-      __syncthreads();
-      if (first) {
-        double all = 0.0;
-        for (int w = 0; w < DV_WAVES; ++w) all += sums[w];
-        if (!(all > 0.0)) return -1;
-        target = v * all;
-      }
-      int at = -1;
-      double here = before, base = before;
-      for (int w = 0; w < DV_WAVES; ++w) {
-        if (sums[w] > 0.0) {
-          at = w;                     // rounding may leave the target above every sum: the last part that holds any
-          base = here;
-        }
-        here += sums[w];
-        if (at == w && here > target) break;
-      }
-      if (at < 0) return -1;
-      lo += at * part;
-      n = min(part, n - at * part);
-      before = base;
-      if (n <= 64) break;
-    }
-    __syncthreads();
-    // one wave, a weight a lane
-    double w[VEC], mine = 0.0;
-    if (lane < n) {
-      const int y0 = lo + lane / VEC * VEC;
-      per(y0, w);
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) mine = lane % VEC == i ? w[i] : mine;
-    }
-    double upto = mine;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const double x = __shfl_up(upto, d, WAVE);
-      if (lane >= d) upto += x;
-    }
-    const unsigned long long any = __builtin_amdgcn_ballot_w64(mine > 0.0), over = __builtin_amdgcn_ballot_w64(mine > 0.0 && before + upto > target);
-    if (any == 0) return -1;
-    return lo + (over ? __builtin_ctzll(over) : 63 - __builtin_clzll(any));
-  }
-};
-
-template <typename T> __global__ void __launch_bounds__(DV_THREADS) draft_verify_walk(VerifyArgs<T> a, int b0) {
+// A wave takes a part of a row: 16 scores a lane at a time
+template <typename T> __device__ __forceinline__ PartStat part_stat(const T* row, int lo, int hi, double rate, int lane) {
   constexpr int VEC = Vec16<T>::N;
-  __shared__ double sums[2 * DV_WAVES];
-  __shared__ int parent[DRAFT_MOST_ROWS];
-  extern __shared__ __attribute__((aligned(16))) uint32_t dv_refused[];   // V bits
-  const int tid = threadIdx.x, b = b0 + blockIdx.x;
+  float top = -INFINITY;
+  int at = 0x7fffffff;
+  bool nan = false;
+  double sum = 0.0;
+  for (int base = lo; base < hi; base += DV_CHUNK) {
+    float x[16], most = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 16; i += VEC) load_scores(row, base + 64 * i + lane * VEC, hi, x + i);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      most = fmaxf(most, x[i]);
+      nan |= x[i] != x[i];
+    }
+    if (rate == 0.0) {
+      if (most > top) {
+#pragma unroll
+        for (int i = 15; i >= 0; --i)
+          if (x[i] == most) at = base + 64 * (i / VEC * VEC) + lane * VEC + i % VEC;
+      }
+      top = fmaxf(top, most);
+      continue;
+    }
+    if (most > top) {
+      sum *= power_of_two(fma((double)top, rate, -(double)most * rate));
+      top = most;
+    }
+    const double shift = -(double)top * rate;
+    double s0 = 0.0, s1 = 0.0;
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) {
+      s0 += power_of_two(fma((double)x[i], rate, shift));
+      s1 += power_of_two(fma((double)x[i + 1], rate, shift));
+    }
+    sum += s0 + s1;
+  }
+  PartStat p;
+  p.top = wave_max(top);
+  p.at = -1;
+  if (rate == 0.0) {
+    if (top != p.top) at = 0x7fffffff;
+#pragma unroll
+    for (int d = 32; d; d >>= 1) at = min(at, __shfl_xor(at, d, WAVE));
+    p.at = at;
+    p.total = 1.0;
+  } else {
+    p.total = wave_total(sum * power_of_two(fma((double)top, rate, -(double)p.top * rate)));
+  }
+  if (__any(nan) || p.top == INFINITY) p.total = NAN;
+  return p;
+}
+
+// A row, from its parts: ok where it is a distribution
+struct RowStat {
+  float top;
+  int at;
+  double total;
+  __device__ __forceinline__ bool ok() const { return total > 0.0; }
+};
+// of a part's sum against the row's largest score
+__device__ __forceinline__ double part_total(const PartStat& p, float top, double rate) {
+  return rate != 0.0 ? p.total * power_of_two(fma((double)p.top, rate, -(double)top * rate)) : p.total;
+}
+__device__ __forceinline__ RowStat join(const PartStat* parts, int n, double rate) {
+  RowStat r{-INFINITY, -1, 0.0};
+  for (int i = 0; i < n; ++i) {
+    const PartStat p = parts[i];
+    if (p.top > r.top) r.at = p.at;
+    r.top = fmaxf(r.top, p.top);
+  }
+  for (int i = 0; i < n; ++i) r.total += part_total(parts[i], r.top, rate);   // NaN stays
+  if (r.top == -INFINITY) r.total = 0.0;
+  if (rate == 0.0 && r.total > 0.0) r.total = 1.0;
+  return r;
+}
+
+// The parts of all rows of the call: [T rows][parts] of the target, then of the draft
+template <typename T> __global__ void __launch_bounds__(256) draft_verify_parts(VerifyArgs<T> a, PartStat* parts, int n_rows, Divisor count) {
+  const Cut cut(a.V);
+  const int item = blockIdx.x * 4 + (threadIdx.x >> 6), r = count(item), part = item - r * (int)count.d;
+  if (r >= n_rows) return;
+  const bool of_draft = r >= a.T_rows;
+  const T* const row = of_draft ? a.draft + (long)(r - a.T_rows) * a.V : a.target + (long)r * a.V;
+  const PartStat p = part_stat(row, part * cut.len, min((part + 1) * cut.len, a.V), of_draft ? a.draft_rate : a.rate, threadIdx.x & 63);
+  if ((threadIdx.x & 63) == 0) parts[item] = p;
+}
+
+// LDS of a walk: per row, then the bits of refused tokens
+struct WalkRow {
+  int parent, token;
+  double target, draft;   // weights of the row's token in its parent's distributions (AHEAD)
+  RowStat p, q;           // the row's own distributions (AHEAD)
+  float u;
+};
+
+// AHEAD: the parts of all rows have been formed by another launch; else a row's are formed when the walk comes to it
+template <typename T, bool AHEAD> __global__ void __launch_bounds__(DV_THREADS) draft_verify_walk(VerifyArgs<T> a, const PartStat* parts, int b0) {
+  constexpr int VEC = Vec16<T>::N;
+  __shared__ PartStat stats[2][DV_PARTS];   // of the walk's row: target, draft
+  __shared__ double sums[DV_PARTS];
+  extern __shared__ __attribute__((aligned(16))) char dv_smem[];
+  WalkRow* const rows = reinterpret_cast<WalkRow*>(dv_smem);
+  uint32_t* const refused = reinterpret_cast<uint32_t*>(rows + a.max_new);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), b = b0 + blockIdx.x;
+  const Cut cut(a.V);
   const RowRange r = ragged_rows(a.row_start, b, a.T_rows);
   const int n = min(r.count, a.max_new);
   int* const path = a.path + (long)b * a.max_new;
-  if (tid < n) parent[tid] = draft_parent(a.parent[r.first + tid], tid);
-  for (int i = tid; i < (a.V + 31) / 32; i += DV_THREADS) dv_refused[i] = 0;
-  const Walk<T> walk(a, sums, dv_refused);
+  const double rate = a.rate, draft_rate = a.draft_rate;
+  if (tid < n) {
+    WalkRow& x = rows[tid];
+    x.parent = draft_parent(a.parent[r.first + tid], tid);
+    x.token = a.tokens[r.first + tid];
+    x.u = a.u[r.first + tid];
+    if (AHEAD) {
+      const bool known = x.parent >= 0 && x.token >= 0 && x.token < a.V;
+      const long at = (long)(r.first + x.parent) * a.V + x.token;
+      const float t = known ? to_f32(a.target[at]) : 0.f, d = known && a.draft ? to_f32(a.draft[at]) : 0.f;
+      x.p = join(parts + (long)(r.first + tid) * cut.count, cut.count, rate);
+      if (a.draft) x.q = join(parts + (long)(a.T_rows + r.first + tid) * cut.count, cut.count, draft_rate);
+      x.target = t;
+      x.draft = d;
+    }
+  }
+  for (int i = tid; i < (a.V + 31) / 32; i += DV_THREADS) refused[i] = 0;
+  __syncthreads();
+  if (AHEAD && tid < n && rows[tid].parent >= 0) {
+    WalkRow& x = rows[tid];
+    const RowStat p = rows[x.parent].p;
+    x.target = weight(rate, p.top, p.at, (float)x.target, x.token);
+    if (a.draft) {
+      const RowStat q = rows[x.parent].q;
+      x.draft = weight(draft_rate, q.top, q.at, (float)x.draft, x.token);
+    }
+  }
+  if (AHEAD) __syncthreads();
+  auto is_refused = [&](int y) { return (refused[y >> 5] >> (y & 31)) & 1; };
+  // a row's distribution, its parts left in stats[which]
+  auto stat = [&](const T* row, double row_rate, int which) {
+    __syncthreads();
+    for (int part = wave; part < cut.count; part += DV_WAVES) {
+      const PartStat p = part_stat(row, part * cut.len, min((part + 1) * cut.len, a.V), row_rate, lane);
+      if (lane == 0) stats[which][part] = p;
+    }
+    __syncthreads();
+    return join(stats[which], cut.count, row_rate);
+  };
   double* const rest = a.rest + (long)b * a.V;
   int node = 0, kept = n > 0 ? 1 : 0, next = -1;
   if (tid == 0 && n > 0) path[0] = 0;
-  __syncthreads();
   while (n > 0) {
     const T* const target = a.target + (long)(r.first + node) * a.V;
     const T* const draft = a.draft ? a.draft + (long)(r.first + node) * a.V : nullptr;
-    const RowStat P = walk.stat(target, a.scale);
-    if (!P.ok) break;   // no next token
-    RowStat Q{};
+    const RowStat P = AHEAD ? rows[node].p : stat(target, rate, 0);
+    if (!P.ok()) break;   // no next token
+    RowStat Q{-INFINITY, -1, 0.0};
+    if (AHEAD && draft) Q = rows[node].q;
+    bool have_q = AHEAD;
     int child = node, taken = -1, tried = 0;
-    double left = 1.0, q_left = 0.0, r_inv = 1.0;   // what the refused tokens have left of the target (no draft scores), of the draft, and of `rest`
-    bool dead = false;                              // the target has nothing left
+    double left = 1.0, q_left = Q.total, r_inv = 1.0;   // what the refused tokens have left of the target (no draft scores), of the draft; of `rest`
+    bool dead = false;                                  // the target has nothing left
     while (!dead) {
-      // the next child
-      int mine = DRAFT_MOST_ROWS;
-      const int i = tid;
-      const bool is_child = i < n && i > child && parent[i] == node;
-      const unsigned long long m = __builtin_amdgcn_ballot_w64(is_child);
-      if (m) mine = (tid & ~63) + __builtin_ctzll(m);
-      __syncthreads();
-      int* const firsts = reinterpret_cast<int*>(sums);
-      if ((tid & 63) == 0) firsts[tid >> 6] = mine;
-      __syncthreads();
-      child = DRAFT_MOST_ROWS;
-      for (int w = 0; w < DV_WAVES; ++w) child = min(child, firsts[w]);
-      __syncthreads();
-      if (child >= n) break;
-      if (draft && !tried && Q.total == 0.0) {
-        Q = walk.stat(draft, a.draft_scale);
-        if (!Q.ok) break;   // what was drawn from no distribution is not taken
-        q_left = Q.total;
+      int found = n;   // the next child
+      for (int i0 = (child + 1) & ~63; i0 < n && found == n; i0 += 64) {
+        const int i = i0 + lane;
+        const unsigned long long m = __builtin_amdgcn_ballot_w64(i < n && i > child && rows[i].parent == node);
+        if (m) found = i0 + __builtin_ctzll(m);
       }
-      const int x = a.tokens[r.first + child];
+      child = found;
+      if (child >= n) break;
+      if (draft && !have_q) {
+        Q = stat(draft, draft_rate, 1);
+        q_left = Q.total;
+        have_q = true;
+      }
+      if (draft && !Q.ok()) break;   // what was drawn from no distribution is not taken
+      const int x = rows[child].token;
       if (x < 0 || x >= a.V) continue;
-      const bool before = walk.is_refused(x);
-      const double q = !draft ? 1.0 : before && a.distinct ? 0.0 : walk.weight(Q, a.draft_scale, to_f32(draft[x]), x) / q_left;
-      if (!(q > 0.0)) continue;
-      double rx;
-      if (!draft) rx = before ? 0.0 : walk.weight(P, a.scale, to_f32(target[x]), x) / P.total / left;
-      else rx = tried ? rest[x] * r_inv : walk.weight(P, a.scale, to_f32(target[x]), x) / P.total;
-      if ((double)a.u[r.first + child] * q < rx) {
+      const bool before = tried && is_refused(x);
+      const double wx = AHEAD ? rows[child].target : weight(rate, P.top, P.at, to_f32(target[x]), x);
+      double q = 1.0, rx;
+      if (draft) {
+        const double w = AHEAD ? rows[child].draft : weight(draft_rate, Q.top, Q.at, to_f32(draft[x]), x);
+        q = before && a.distinct ? 0.0 : w / q_left;
+        if (!(q > 0.0)) continue;
+        rx = tried ? rest[x] * r_inv : wx / P.total;
+      } else {
+        rx = before ? 0.0 : wx / P.total / left;
+      }
+      if ((double)rows[child].u * q < rx) {
         taken = child;
         break;
       }
       __syncthreads();
-      if (tid == 0) dv_refused[x >> 5] |= 1u << (x & 31);
+      if (tid == 0) refused[x >> 5] |= 1u << (x & 31);
       __syncthreads();
       if (!draft) {
-        if (!before) left -= walk.weight(P, a.scale, to_f32(target[x]), x) / P.total;
+        if (!before) left -= wx / P.total;
         dead = !(left > 0.0);
       } else {
-        double all = 0.0, q_all = 0.0;
-        for (int y0 = tid * VEC; y0 < a.V; y0 += DV_THREADS * VEC) {
-          float xt[VEC], xd[VEC];
-          if (!tried) load_scores(target, y0, a.V, xt);
-          load_scores(draft, y0, a.V, xd);
+        const double p_inv = 1.0 / P.total, q_inv = 1.0 / q_left;
+        for (int part = wave; part < cut.count; part += DV_WAVES) {
+          const int lo = part * cut.len, hi = min(lo + cut.len, a.V);
+          double all = 0.0, q_all = 0.0;
+          for (int y0 = lo + lane * VEC; y0 < hi; y0 += 64 * VEC) {
+            float xt[VEC], xd[VEC];
+            if (!tried) load_scores(target, y0, hi, xt);
+            load_scores(draft, y0, hi, xd);
 #pragma unroll
-          for (int i = 0; i < VEC; ++i) {
-            const int y = y0 + i;
-            if (y >= a.V) break;
-            const double w = walk.weight(Q, a.draft_scale, xd[i], y);
-            // of the tokens refused before this one the draft has nothing left, and the target neither
-            const bool gone = a.distinct && walk.is_refused(y);
-            const double p = tried ? rest[y] * r_inv : walk.weight(P, a.scale, xt[i], y) / P.total;
-            const double now = fmax(p - (gone && y != x ? 0.0 : w / q_left), 0.0);
-            rest[y] = now;
-            all += now;
-            if (!gone) q_all += w;
+            for (int i = 0; i < VEC; ++i) {
+              const int y = y0 + i;
+              if (y < hi) {
+                const double w = weight(draft_rate, Q.top, Q.at, xd[i], y);
+                // of the tokens refused before this one the draft has nothing left, and the target neither
+                const bool gone = a.distinct && is_refused(y);
+                const double p = tried ? rest[y] * r_inv : weight(rate, P.top, P.at, xt[i], y) * p_inv;
+                const double now = fmax(p - (gone && y != x ? 0.0 : w * q_inv), 0.0);
+                rest[y] = now;
+                all += now;
+                if (!gone) q_all += w;
+              }
+            }
+          }
+          all = wave_total(all);
+          q_all = wave_total(q_all);
+          if (lane == 0) {
+            sums[part] = all;
+            stats[1][part].total = q_all;
           }
         }
-        all = walk.total(all);
-        if (a.distinct) q_left = walk.total(q_all);
+        __syncthreads();
+        double all = 0.0, q_all = 0.0;
+        for (int part = 0; part < cut.count; ++part) {
+          all += sums[part];
+          q_all += stats[1][part].total;
+        }
+        if (a.distinct) q_left = q_all;
         dead = !(all > 0.0);
         r_inv = 1.0 / all;
       }
       ++tried;
     }
     if (taken < 0) {
-      const double v = (double)a.v[b];
-      auto target_weights = [&](int y0, double (&w)[VEC], bool without) {
+      // The next token: from `rest`, whose parts' sums are in place, or from the target's row without the refused tokens, or from all of it
+      const bool from_rest = draft && tried && !dead;
+      bool without = !draft && tried && !dead;
+      auto weights = [&](int y0, int hi, double (&w)[VEC]) {
         float xt[VEC];
-        load_scores(target, y0, a.V, xt);
+        if (!from_rest) load_scores(target, y0, hi, xt);
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) w[i] = y0 + i < a.V && !(without && walk.is_refused(y0 + i)) ? walk.weight(P, a.scale, xt[i], y0 + i) : 0.0;
+        for (int i = 0; i < VEC; ++i) {
+          const int y = y0 + i;
+          w[i] = y >= hi ? 0.0 : from_rest ? rest[y] : without && is_refused(y) ? 0.0 : weight(rate, P.top, P.at, xt[i], y);
+        }
       };
-      if (tried && !dead) {
-        if (draft) next = walk.sample(v, [&](int y0, double (&w)[VEC]) {
+      double all = 0.0;
+      for (;;) {
+        if (!from_rest) {
+          __syncthreads();
+          for (int part = wave; part < cut.count; part += DV_WAVES) {
+            const int lo = part * cut.len, hi = min(lo + cut.len, a.V);
+            bool anew = false;
+            if (without)
+              for (int w = (lo >> 5) + lane; w < (hi + 31) >> 5; w += 64) anew |= refused[w] != 0;
+            const PartStat p = AHEAD ? parts[(long)(r.first + node) * cut.count + part] : stats[0][part];
+            double of_part = rate != 0.0 ? part_total(p, P.top, rate) : P.at >= lo && P.at < hi ? 1.0 : 0.0;
+            if (__any(anew)) {
+              of_part = 0.0;
+              for (int y0 = lo + lane * VEC; y0 < hi; y0 += 64 * VEC) {
+                double w[VEC];
+                weights(y0, hi, w);
 #pragma unroll
-          for (int i = 0; i < VEC; ++i) w[i] = y0 + i < a.V ? rest[y0 + i] : 0.0;
-        });
-        else next = walk.sample(v, [&](int y0, double (&w)[VEC]) { target_weights(y0, w, true); });
+                for (int i = 0; i < VEC; ++i) of_part += w[i];
+              }
+              of_part = wave_total(of_part);
+            }
+            if (lane == 0) sums[part] = of_part;
+          }
+          __syncthreads();
+        }
+        for (int part = 0; part < cut.count; ++part) all += sums[part];
+        if (all > 0.0 || !without) break;
+        without = false;   // random numbers outside their range may have refused every token
       }
-      if (next < 0) next = walk.sample(v, [&](int y0, double (&w)[VEC]) { target_weights(y0, w, false); });
+      const double aim = (double)a.v[b] * all;
+      // the first part whose running sum is above the aim; rounding may leave it above them all: the last that holds any
+      int lo = 0, len = a.V;
+      double before = 0.0;
+      auto choose = [&](int n_parts, int part_len) {
+        int at = 0;
+        double here = before, base = before;
+        for (int part = 0; part < n_parts; ++part) {
+          if (sums[part] > 0.0) {
+            at = part;
+            base = here;
+          }
+          here += sums[part];
+          if (at == part && here > aim) break;
+        }
+        lo += at * part_len;
+        len = min(part_len, len - at * part_len);
+        before = base;
+      };
+      choose(cut.count, cut.len);
+      while (len > 64) {   // then sixteenths of it
+        const int end = lo + len, part_len = ((len + DV_WAVES - 1) / DV_WAVES + VEC - 1) / VEC * VEC, from = lo + wave * part_len, to = min(from + part_len, end);
+        double e = 0.0;
+        for (int y0 = from + lane * VEC; y0 < to; y0 += 64 * VEC) {
+          double w[VEC];
+          weights(y0, to, w);
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) e += w[i];
+        }
+        e = wave_total(e);
+        __syncthreads();
+        if (lane == 0) sums[wave] = e;
+        __syncthreads();
+        choose(DV_WAVES, part_len);
+      }
+      double mine = 0.0;   // a score a lane
+      if (lane < len) {
+        double w[VEC];
+        weights(lo + lane / VEC * VEC, lo + len, w);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) mine = lane % VEC == i ? w[i] : mine;
+      }
+      const double upto = before + wave_upto(mine);
+      const unsigned long long any = __builtin_amdgcn_ballot_w64(mine > 0.0), over = __builtin_amdgcn_ballot_w64(mine > 0.0 && upto > aim);
+      next = any == 0 ? -1 : lo + (over ? __builtin_ctzll(over) : 63 - __builtin_clzll(any));
       break;
     }
-    __syncthreads();
-    if (tried)   // tokens refused here are children of this row
-      for (int i = node + 1 + tid; i < n; i += DV_THREADS) {
-        const int x = a.tokens[r.first + i];
-        if (parent[i] == node && x >= 0 && x < a.V) dv_refused[x >> 5] = 0;
-      }
+    if (tried) {   // tokens refused here are children of this row
+      __syncthreads();
+      if (tid < n && rows[tid].parent == node && rows[tid].token >= 0 && rows[tid].token < a.V) refused[rows[tid].token >> 5] = 0;
+      __syncthreads();
+    }
     node = taken;
     if (tid == 0) path[kept] = node;
     ++kept;
-    __syncthreads();
   }
   for (int i = kept + tid; i < a.max_new; i += DV_THREADS) path[i] = -1;
   if (tid == 0) {
@@ -291,14 +435,31 @@ template <typename T> __global__ void __launch_bounds__(DV_THREADS) draft_verify
   }
 }
 
+constexpr int64_t DV_AHEAD_PARTS = 1 << 15;   // parts that are formed ahead of the walks
+
 }  // namespace
 
-size_t draft_verify_workspace_bytes(int B, int V) { return (size_t)B * V * sizeof(double) + 256; }
+// [documents][V] of what the target has left, then the parts
+size_t draft_verify_workspace_bytes(int T_rows, int B, int V) {
+  return (size_t)B * V * sizeof(double) + 16 + (size_t)std::min<int64_t>(2 * (int64_t)T_rows * Cut(V).count, DV_AHEAD_PARTS) * sizeof(PartStat);
+}
 template <typename T> dipaco_status launch_draft_verify(const VerifyArgs<T>& a, hipStream_t s) {
-  const int lds = (a.V + 31) / 32 * 4;
-  launch_parts(a.B, [&](long long first, unsigned count) { draft_verify_walk<T><<<count, DV_THREADS, lds, s>>>(a, (int)first); });
+  const Cut cut(a.V);
+  const int64_t n = (int64_t)a.T_rows * cut.count * (a.draft ? 2 : 1);
+  const int lds = a.max_new * (int)sizeof(WalkRow) + (a.V + 31) / 32 * 4;
+  PartStat* const parts = reinterpret_cast<PartStat*>((reinterpret_cast<uintptr_t>(a.rest + (size_t)a.B * a.V) + 15) & ~(uintptr_t)15);
+  auto walk = [&](auto AHEADc) -> dipaco_status {
+    constexpr bool AHEAD = decltype(AHEADc)::value;
+    static std::atomic<unsigned long long> lds_set{0};
+    if (dipaco_status st = ensure_dynamic_lds(reinterpret_cast<const void*>(draft_verify_walk<T, AHEAD>), 128 << 10, lds_set)) return st;
+    launch_parts(a.B, [&](long long first, unsigned count) { draft_verify_walk<T, AHEAD><<<count, DV_THREADS, lds, s>>>(a, parts, (int)first); });
+    DIPACO_LAUNCH_CHECK();
+    return DIPACO_OK;
+  };
+  if (n == 0 || n > DV_AHEAD_PARTS) return walk(std::false_type{});
+  draft_verify_parts<T><<<(int)((n + 3) / 4), 256, 0, s>>>(a, parts, a.T_rows * (a.draft ? 2 : 1), Divisor(cut.count));
   DIPACO_LAUNCH_CHECK();
-  return DIPACO_OK;
+  return walk(std::true_type{});
 }
 template dipaco_status launch_draft_verify<float>(const VerifyArgs<float>&, hipStream_t);
 template dipaco_status launch_draft_verify<bf16>(const VerifyArgs<bf16>&, hipStream_t);

@@ -337,7 +337,7 @@ template <int DH, template <typename> class Args> dipaco_status launch_paged_bot
 
 // ---- draft_tree.hip, draft_verify.hip, cache_keep.hip: a step of drafted decoding ------------
 dipaco_status launch_draft_tree(const int* parent, const int* row_start, int* depth, uint64_t* seen, int T_rows, int B, int max_new, hipStream_t s);
-size_t draft_verify_workspace_bytes(int B, int V);
+size_t draft_verify_workspace_bytes(int T_rows, int B, int V);
 template <typename T> dipaco_status launch_draft_verify(const VerifyArgs<T>& a, hipStream_t s);
 dipaco_status launch_cache_keep(KeepArgs a, void* const* caches, int n_layers, hipStream_t s);
 
