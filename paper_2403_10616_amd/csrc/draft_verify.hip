@@ -151,16 +151,19 @@ struct RowStat {
 __device__ __forceinline__ double part_total(const PartStat& p, float top, double rate) {
   return rate != 0.0 ? p.total * power_of_two(fma((double)p.top, rate, -(double)top * rate)) : p.total;
 }
-__device__ __forceinline__ RowStat join(const PartStat* parts, int n, double rate) {
-  RowStat r{-INFINITY, -1, 0.0};
-  for (int i = 0; i < n; ++i) {
-    const PartStat p = parts[i];
-    if (p.top > r.top) r.at = p.at;
-    r.top = fmaxf(r.top, p.top);
-  }
-  for (int i = 0; i < n; ++i) r.total += part_total(parts[i], r.top, rate);   // NaN stays
+// a part a lane, by a whole wave
+__device__ __forceinline__ RowStat join(const PartStat* parts, int n, double rate, int lane) {
+  PartStat p{-INFINITY, -1, 0.0};
+  if (lane < n) p = parts[lane];
+  RowStat r;
+  r.top = wave_max(p.top);
+  r.total = wave_total(lane < n ? part_total(p, r.top, rate) : 0.0);   // NaN stays
   if (r.top == -INFINITY) r.total = 0.0;
-  if (rate == 0.0 && r.total > 0.0) r.total = 1.0;
+  r.at = -1;
+  if (rate == 0.0) {
+    r.at = __builtin_amdgcn_readlane(p.at, __builtin_ctzll(__builtin_amdgcn_ballot_w64(p.top == r.top) | 1ull << 63));
+    if (r.total > 0.0) r.total = 1.0;
+  }
   return r;
 }
 
@@ -184,7 +187,7 @@ struct WalkRow {
 };
 
 // AHEAD: the parts of all rows have been formed by another launch; else a row's are formed when the walk comes to it
-template <typename T, bool AHEAD> __global__ void __launch_bounds__(DV_THREADS) draft_verify_walk(VerifyArgs<T> a, const PartStat* parts, int b0) {
+template <typename T, bool AHEAD> __global__ void __launch_bounds__(DV_THREADS) __attribute__((amdgpu_waves_per_eu(4, 4))) draft_verify_walk(VerifyArgs<T> a, const PartStat* parts, int b0) {
   constexpr int VEC = Vec16<T>::N;
   __shared__ PartStat stats[2][DV_PARTS];   // of the walk's row: target, draft
   __shared__ double sums[DV_PARTS];
@@ -205,11 +208,22 @@ template <typename T, bool AHEAD> __global__ void __launch_bounds__(DV_THREADS) 
     if (AHEAD) {
       const bool known = x.parent >= 0 && x.token >= 0 && x.token < a.V;
       const long at = (long)(r.first + x.parent) * a.V + x.token;
-      const float t = known ? to_f32(a.target[at]) : 0.f, d = known && a.draft ? to_f32(a.draft[at]) : 0.f;
-      x.p = join(parts + (long)(r.first + tid) * cut.count, cut.count, rate);
-      if (a.draft) x.q = join(parts + (long)(a.T_rows + r.first + tid) * cut.count, cut.count, draft_rate);
-      x.target = t;
-      x.draft = d;
+      x.target = known ? to_f32(a.target[at]) : 0.f;
+      x.draft = known && a.draft ? to_f32(a.draft[at]) : 0.f;
+    }
+  }
+  if (AHEAD) {
+    const long of_draft = (long)a.T_rows * cut.count;
+#pragma unroll 2
+    for (int i = wave; i < n; i += DV_WAVES) {
+      const PartStat* const at = parts + (long)(r.first + i) * cut.count;
+      const RowStat p = join(at, cut.count, rate, lane);
+      RowStat q{-INFINITY, -1, 0.0};
+      if (a.draft) q = join(at + of_draft, cut.count, draft_rate, lane);
+      if (lane == 0) {
+        rows[i].p = p;
+        rows[i].q = q;
+      }
     }
   }
   for (int i = tid; i < (a.V + 31) / 32; i += DV_THREADS) refused[i] = 0;
@@ -233,8 +247,10 @@ template <typename T, bool AHEAD> __global__ void __launch_bounds__(DV_THREADS) 
       if (lane == 0) stats[which][part] = p;
     }
     __syncthreads();
-    return join(stats[which], cut.count, row_rate);
+    return join(stats[which], cut.count, row_rate, lane);
   };
+  // score i of a lane among the 1024 from base on
+  auto place = [&](int base, int i) { return base + 64 * (i / VEC * VEC) + lane * VEC + i % VEC; };
   double* const rest = a.rest + (long)b * a.V;
   int node = 0, kept = n > 0 ? 1 : 0, next = -1;
   if (tid == 0 && n > 0) path[0] = 0;
@@ -292,13 +308,16 @@ template <typename T, bool AHEAD> __global__ void __launch_bounds__(DV_THREADS) 
         for (int part = wave; part < cut.count; part += DV_WAVES) {
           const int lo = part * cut.len, hi = min(lo + cut.len, a.V);
           double all = 0.0, q_all = 0.0;
-          for (int y0 = lo + lane * VEC; y0 < hi; y0 += 64 * VEC) {
-            float xt[VEC], xd[VEC];
-            if (!tried) load_scores(target, y0, hi, xt);
-            load_scores(draft, y0, hi, xd);
+          for (int base = lo; base < hi; base += DV_CHUNK) {
+            float xt[16], xd[16];
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-              const int y = y0 + i;
+            for (int i = 0; i < 16; i += VEC) {
+              if (!tried) load_scores(target, place(base, i), hi, xt + i);
+              load_scores(draft, place(base, i), hi, xd + i);
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const int y = place(base, i);
               if (y < hi) {
                 const double w = weight(draft_rate, Q.top, Q.at, xd[i], y);
                 // of the tokens refused before this one the draft has nothing left, and the target neither
@@ -319,12 +338,8 @@ template <typename T, bool AHEAD> __global__ void __launch_bounds__(DV_THREADS) 
           }
         }
         __syncthreads();
-        double all = 0.0, q_all = 0.0;
-        for (int part = 0; part < cut.count; ++part) {
-          all += sums[part];
-          q_all += stats[1][part].total;
-        }
-        if (a.distinct) q_left = q_all;
+        const double all = wave_total(lane < cut.count ? sums[lane] : 0.0);
+        if (a.distinct) q_left = wave_total(lane < cut.count ? stats[1][lane].total : 0.0);
         dead = !(all > 0.0);
         r_inv = 1.0 / all;
       }
@@ -334,14 +349,19 @@ template <typename T, bool AHEAD> __global__ void __launch_bounds__(DV_THREADS) 
       // The next token: from `rest`, whose parts' sums are in place, or from the target's row without the refused tokens, or from all of it
       const bool from_rest = draft && tried && !dead;
       bool without = !draft && tried && !dead;
-      auto weights = [&](int y0, int hi, double (&w)[VEC]) {
-        float xt[VEC];
-        if (!from_rest) load_scores(target, y0, hi, xt);
+      auto weight_at = [&](int y, float x) { return from_rest ? rest[y] : without && is_refused(y) ? 0.0 : weight(rate, P.top, P.at, x, y); };
+      // sum over lo .. hi - 1, by a wave
+      auto weights = [&](int lo, int hi) {
+        double e = 0.0;
+        for (int base = lo; base < hi; base += DV_CHUNK) {
+          float x[16];
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-          const int y = y0 + i;
-          w[i] = y >= hi ? 0.0 : from_rest ? rest[y] : without && is_refused(y) ? 0.0 : weight(rate, P.top, P.at, xt[i], y);
+          for (int i = 0; i < 16; i += VEC)
+            if (!from_rest) load_scores(target, place(base, i), hi, x + i);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) e += place(base, i) < hi ? weight_at(place(base, i), x[i]) : 0.0;
         }
+        return wave_total(e);
       };
       double all = 0.0;
       for (;;) {
@@ -354,21 +374,12 @@ template <typename T, bool AHEAD> __global__ void __launch_bounds__(DV_THREADS) 
               for (int w = (lo >> 5) + lane; w < (hi + 31) >> 5; w += 64) anew |= refused[w] != 0;
             const PartStat p = AHEAD ? parts[(long)(r.first + node) * cut.count + part] : stats[0][part];
             double of_part = rate != 0.0 ? part_total(p, P.top, rate) : P.at >= lo && P.at < hi ? 1.0 : 0.0;
-            if (__any(anew)) {
-              of_part = 0.0;
-              for (int y0 = lo + lane * VEC; y0 < hi; y0 += 64 * VEC) {
-                double w[VEC];
-                weights(y0, hi, w);
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) of_part += w[i];
-              }
-              of_part = wave_total(of_part);
-            }
+            if (__any(anew)) of_part = weights(lo, hi);
             if (lane == 0) sums[part] = of_part;
           }
           __syncthreads();
         }
-        for (int part = 0; part < cut.count; ++part) all += sums[part];
+        all = wave_total(lane < cut.count ? sums[lane] : 0.0);
         if (all > 0.0 || !without) break;
         without = false;   // random numbers outside their range may have refused every token
       }
@@ -376,47 +387,32 @@ template <typename T, bool AHEAD> __global__ void __launch_bounds__(DV_THREADS) 
       // the first part whose running sum is above the aim; rounding may leave it above them all: the last that holds any
       int lo = 0, len = a.V;
       double before = 0.0;
+      auto first_above = [&](double mine, double& base) {   // a lane each; -1: none holds any
+        const double upto = before + wave_upto(mine);
+        const unsigned long long any = __builtin_amdgcn_ballot_w64(mine > 0.0), over = __builtin_amdgcn_ballot_w64(mine > 0.0 && upto > aim);
+        const int at = any == 0 ? -1 : over ? __builtin_ctzll(over) : 63 - __builtin_clzll(any);
+        base = at > 0 ? lane_value(upto, at - 1) : before;
+        return at;
+      };
       auto choose = [&](int n_parts, int part_len) {
-        int at = 0;
-        double here = before, base = before;
-        for (int part = 0; part < n_parts; ++part) {
-          if (sums[part] > 0.0) {
-            at = part;
-            base = here;
-          }
-          here += sums[part];
-          if (at == part && here > aim) break;
-        }
+        double base;
+        const int at = max(first_above(lane < n_parts ? sums[lane] : 0.0, base), 0);
         lo += at * part_len;
         len = min(part_len, len - at * part_len);
         before = base;
       };
       choose(cut.count, cut.len);
       while (len > 64) {   // then sixteenths of it
-        const int end = lo + len, part_len = ((len + DV_WAVES - 1) / DV_WAVES + VEC - 1) / VEC * VEC, from = lo + wave * part_len, to = min(from + part_len, end);
-        double e = 0.0;
-        for (int y0 = from + lane * VEC; y0 < to; y0 += 64 * VEC) {
-          double w[VEC];
-          weights(y0, to, w);
-#pragma unroll
-          for (int i = 0; i < VEC; ++i) e += w[i];
-        }
-        e = wave_total(e);
+        const int part_len = (len + DV_WAVES - 1) / DV_WAVES, from = lo + wave * part_len;
+        const double e = weights(from, min(from + part_len, lo + len));
         __syncthreads();
         if (lane == 0) sums[wave] = e;
         __syncthreads();
         choose(DV_WAVES, part_len);
       }
-      double mine = 0.0;   // a score a lane
-      if (lane < len) {
-        double w[VEC];
-        weights(lo + lane / VEC * VEC, lo + len, w);
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) mine = lane % VEC == i ? w[i] : mine;
-      }
-      const double upto = before + wave_upto(mine);
-      const unsigned long long any = __builtin_amdgcn_ballot_w64(mine > 0.0), over = __builtin_amdgcn_ballot_w64(mine > 0.0 && upto > aim);
-      next = any == 0 ? -1 : lo + (over ? __builtin_ctzll(over) : 63 - __builtin_clzll(any));
+      double base;   // a score a lane
+      const int at = first_above(lane < len ? weight_at(lo + lane, from_rest ? 0.f : to_f32(target[lo + lane])) : 0.0, base);
+      next = at < 0 ? -1 : lo + at;
       break;
     }
     if (tried) {   // tokens refused here are children of this row
