@@ -186,8 +186,9 @@ struct WalkRow {
   float u;
 };
 
-// AHEAD: the parts of all rows have been formed by another launch; else a row's are formed when the walk comes to it
-template <typename T, bool AHEAD> __global__ void __launch_bounds__(DV_THREADS) __attribute__((amdgpu_waves_per_eu(4, 4))) draft_verify_walk(VerifyArgs<T> a, const PartStat* parts, int b0) {
+// AHEAD: the parts of all rows have been formed by another launch; else a row's are formed when the walk comes to it.  GREEDY: temperature 0.  Both are the
+// kernel's because a branch at every score keeps the compiler from holding the series' coefficients: two copies a score where there is one now.
+template <typename T, bool AHEAD, bool GREEDY> __global__ void __launch_bounds__(DV_THREADS) __attribute__((amdgpu_waves_per_eu(4, 4))) draft_verify_walk(VerifyArgs<T> a, const PartStat* parts, int b0) {
   constexpr int VEC = Vec16<T>::N;
   __shared__ PartStat stats[2][DV_PARTS];   // of the walk's row: target, draft
   __shared__ double sums[DV_PARTS];
@@ -199,7 +200,7 @@ template <typename T, bool AHEAD> __global__ void __launch_bounds__(DV_THREADS) 
   const RowRange r = ragged_rows(a.row_start, b, a.T_rows);
   const int n = min(r.count, a.max_new);
   int* const path = a.path + (long)b * a.max_new;
-  const double rate = a.rate, draft_rate = a.draft_rate;
+  const double rate = GREEDY ? 0.0 : a.rate, draft_rate = a.draft_rate;
   if (tid < n) {
     WalkRow& x = rows[tid];
     x.parent = draft_parent(a.parent[r.first + tid], tid);
@@ -249,8 +250,8 @@ template <typename T, bool AHEAD> __global__ void __launch_bounds__(DV_THREADS) 
     __syncthreads();
     return join(stats[which], cut.count, row_rate, lane);
   };
-  // score i of a lane among the 1024 from base on
-  auto place = [&](int base, int i) { return base + 64 * (i / VEC * VEC) + lane * VEC + i % VEC; };
+  // bit i: token y0 + i has been refused; y0 is a multiple of VEC
+  auto refused_from = [&](int y0) { return refused[y0 >> 5] >> (y0 & 31); };
   double* const rest = a.rest + (long)b * a.V;
   int node = 0, kept = n > 0 ? 1 : 0, next = -1;
   if (tid == 0 && n > 0) path[0] = 0;
@@ -304,39 +305,66 @@ template <typename T, bool AHEAD> __global__ void __launch_bounds__(DV_THREADS) 
         if (!before) left -= wx / P.total;
         dead = !(left > 0.0);
       } else {
-        const double p_inv = 1.0 / P.total, q_inv = 1.0 / q_left;
-        for (int part = wave; part < cut.count; part += DV_WAVES) {
-          const int lo = part * cut.len, hi = min(lo + cut.len, a.V);
-          double all = 0.0, q_all = 0.0;
-          for (int base = lo; base < hi; base += DV_CHUNK) {
-            float xt[16], xd[16];
+        // rest <- max(what is left of the target - the draft, 0), and the sums of both
+        const double p_inv = 1.0 / P.total, q_inv = 1.0 / q_left, p_shift = -(double)P.top * rate, q_shift = -(double)Q.top * draft_rate;
+        auto refuse = [&](auto FIRSTc, auto DISTINCTc) {
+          constexpr bool FIRST = decltype(FIRSTc)::value, DISTINCT = decltype(DISTINCTc)::value;
+          for (int part = wave; part < cut.count; part += DV_WAVES) {
+            const int lo = part * cut.len, hi = min(lo + cut.len, a.V);
+            double all = 0.0, q_all = 0.0;
+            for (int base = lo + lane * VEC; base < hi; base += DV_CHUNK) {
+              float xt[16], xd[16];
+              double before[16];
 #pragma unroll
-            for (int i = 0; i < 16; i += VEC) {
-              if (!tried) load_scores(target, place(base, i), hi, xt + i);
-              load_scores(draft, place(base, i), hi, xd + i);
-            }
+              for (int j = 0; j < 16; j += VEC) {
+                load_scores(draft, base + 64 * j, hi, xd + j);
+                if (FIRST) load_scores(target, base + 64 * j, hi, xt + j);
+                else
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const int y = place(base, i);
-              if (y < hi) {
-                const double w = weight(draft_rate, Q.top, Q.at, xd[i], y);
-                // of the tokens refused before this one the draft has nothing left, and the target neither
-                const bool gone = a.distinct && is_refused(y);
-                const double p = tried ? rest[y] * r_inv : weight(rate, P.top, P.at, xt[i], y) * p_inv;
-                const double now = fmax(p - (gone && y != x ? 0.0 : w * q_inv), 0.0);
-                rest[y] = now;
-                all += now;
-                if (!gone) q_all += w;
+                  for (int i = 0; i < VEC; ++i) before[j + i] = rest[min(base + 64 * j + i, hi - 1)];
+              }
+#pragma unroll
+              for (int j = 0; j < 16; j += VEC) {
+                const int y0 = base + 64 * j;
+                const uint32_t gone = DISTINCT && y0 < hi ? refused_from(y0) : 0;
+                double now[VEC];
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) {   // a score of -inf behind the part's end: 0
+                  double w = power_of_two(fma((double)xd[j + i], draft_rate, q_shift)), p;
+                  if (!FIRST) p = before[j + i] * r_inv;
+                  else if (GREEDY) p = y0 + i == P.at ? 1.0 : 0.0;
+                  else p = power_of_two(fma((double)xt[j + i], rate, p_shift)) * p_inv;
+                  if (DISTINCT) {   // of the tokens refused before this one the draft has nothing left, and the target neither
+                    const bool is_gone = gone & (1u << i);
+                    q_all += is_gone ? 0.0 : w;
+                    w = is_gone && y0 + i != x ? 0.0 : w;
+                  }
+                  now[i] = fmax(fma(w, -q_inv, p), 0.0);
+                }
+                if (y0 + VEC <= hi) {
+                  __builtin_memcpy(rest + y0, now, sizeof(now));
+#pragma unroll
+                  for (int i = 0; i < VEC; ++i) all += now[i];
+                } else {
+#pragma unroll
+                  for (int i = 0; i < VEC; ++i)
+                    if (y0 + i < hi) {
+                      rest[y0 + i] = now[i];
+                      all += now[i];
+                    }
+                }
               }
             }
+            all = wave_total(all);
+            if (DISTINCT) q_all = wave_total(q_all);
+            if (lane == 0) {
+              sums[part] = all;
+              stats[1][part].total = q_all;
+            }
           }
-          all = wave_total(all);
-          q_all = wave_total(q_all);
-          if (lane == 0) {
-            sums[part] = all;
-            stats[1][part].total = q_all;
-          }
-        }
+        };
+        if (tried) a.distinct ? refuse(std::false_type{}, std::true_type{}) : refuse(std::false_type{}, std::false_type{});
+        else a.distinct ? refuse(std::true_type{}, std::true_type{}) : refuse(std::true_type{}, std::false_type{});
         __syncthreads();
         const double all = wave_total(lane < cut.count ? sums[lane] : 0.0);
         if (a.distinct) q_left = wave_total(lane < cut.count ? stats[1][lane].total : 0.0);
@@ -349,17 +377,28 @@ template <typename T, bool AHEAD> __global__ void __launch_bounds__(DV_THREADS) 
       // The next token: from `rest`, whose parts' sums are in place, or from the target's row without the refused tokens, or from all of it
       const bool from_rest = draft && tried && !dead;
       bool without = !draft && tried && !dead;
-      auto weight_at = [&](int y, float x) { return from_rest ? rest[y] : without && is_refused(y) ? 0.0 : weight(rate, P.top, P.at, x, y); };
-      // sum over lo .. hi - 1, by a wave
+      const double shift = -(double)P.top * rate;
+      auto of_target = [&](float x, int y, uint32_t gone) { return gone & 1 ? 0.0 : GREEDY ? (y == P.at && x > -INFINITY ? 1.0 : 0.0) : power_of_two(fma((double)x, rate, shift)); };   // x = -inf: behind what is summed
+      // sum over lo .. hi - 1, by a wave; lo is a multiple of VEC
       auto weights = [&](int lo, int hi) {
         double e = 0.0;
-        for (int base = lo; base < hi; base += DV_CHUNK) {
-          float x[16];
+        for (int base = lo + lane * VEC; base < hi; base += DV_CHUNK) {
+          if (from_rest) {
 #pragma unroll
-          for (int i = 0; i < 16; i += VEC)
-            if (!from_rest) load_scores(target, place(base, i), hi, x + i);
+            for (int j = 0; j < 16; j += VEC)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) e += place(base, i) < hi ? weight_at(place(base, i), x[i]) : 0.0;
+              for (int i = 0; i < VEC; ++i) e += base + 64 * j + i < hi ? rest[base + 64 * j + i] : 0.0;
+          } else {
+            float x[16];
+#pragma unroll
+            for (int j = 0; j < 16; j += VEC) load_scores(target, base + 64 * j, hi, x + j);
+#pragma unroll
+            for (int j = 0; j < 16; j += VEC) {
+              const uint32_t gone = without && base + 64 * j < hi ? refused_from(base + 64 * j) : 0;
+#pragma unroll
+              for (int i = 0; i < VEC; ++i) e += of_target(x[j + i], base + 64 * j + i, gone >> i);
+            }
+          }
         }
         return wave_total(e);
       };
@@ -403,7 +442,7 @@ template <typename T, bool AHEAD> __global__ void __launch_bounds__(DV_THREADS) 
       };
       choose(cut.count, cut.len);
       while (len > 64) {   // then sixteenths of it
-        const int part_len = (len + DV_WAVES - 1) / DV_WAVES, from = lo + wave * part_len;
+        const int part_len = ((len + DV_WAVES - 1) / DV_WAVES + VEC - 1) / VEC * VEC, from = lo + wave * part_len;
         const double e = weights(from, min(from + part_len, lo + len));
         __syncthreads();
         if (lane == 0) sums[wave] = e;
@@ -411,7 +450,9 @@ template <typename T, bool AHEAD> __global__ void __launch_bounds__(DV_THREADS) 
         choose(DV_WAVES, part_len);
       }
       double base;   // a score a lane
-      const int at = first_above(lane < len ? weight_at(lo + lane, from_rest ? 0.f : to_f32(target[lo + lane])) : 0.0, base);
+      const int y = min(lo + lane, lo + len - 1);
+      const double mine = from_rest ? rest[y] : of_target(to_f32(target[y]), y, without ? is_refused(y) : 0);
+      const int at = first_above(lane < len ? mine : 0.0, base);
       next = at < 0 ? -1 : lo + at;
       break;
     }
@@ -444,18 +485,21 @@ template <typename T> dipaco_status launch_draft_verify(const VerifyArgs<T>& a, 
   const int64_t n = (int64_t)a.T_rows * cut.count * (a.draft ? 2 : 1);
   const int lds = a.max_new * (int)sizeof(WalkRow) + (a.V + 31) / 32 * 4;
   PartStat* const parts = reinterpret_cast<PartStat*>((reinterpret_cast<uintptr_t>(a.rest + (size_t)a.B * a.V) + 15) & ~(uintptr_t)15);
-  auto walk = [&](auto AHEADc) -> dipaco_status {
-    constexpr bool AHEAD = decltype(AHEADc)::value;
+  auto walk = [&](auto AHEADc, auto GREEDYc) -> dipaco_status {
+    constexpr bool AHEAD = decltype(AHEADc)::value, GREEDY = decltype(GREEDYc)::value;
     static std::atomic<unsigned long long> lds_set{0};
-    if (dipaco_status st = ensure_dynamic_lds(reinterpret_cast<const void*>(draft_verify_walk<T, AHEAD>), 128 << 10, lds_set)) return st;
-    launch_parts(a.B, [&](long long first, unsigned count) { draft_verify_walk<T, AHEAD><<<count, DV_THREADS, lds, s>>>(a, parts, (int)first); });
+    if (dipaco_status st = ensure_dynamic_lds(reinterpret_cast<const void*>(draft_verify_walk<T, AHEAD, GREEDY>), 128 << 10, lds_set)) return st;
+    launch_parts(a.B, [&](long long first, unsigned count) { draft_verify_walk<T, AHEAD, GREEDY><<<count, DV_THREADS, lds, s>>>(a, parts, (int)first); });
     DIPACO_LAUNCH_CHECK();
     return DIPACO_OK;
   };
-  if (n == 0 || n > DV_AHEAD_PARTS) return walk(std::false_type{});
+  using std::false_type;
+  using std::true_type;
+  const bool greedy = a.rate == 0.0;
+  if (n == 0 || n > DV_AHEAD_PARTS) return greedy ? walk(false_type{}, true_type{}) : walk(false_type{}, false_type{});
   draft_verify_parts<T><<<(int)((n + 3) / 4), 256, 0, s>>>(a, parts, a.T_rows * (a.draft ? 2 : 1), Divisor(cut.count));
   DIPACO_LAUNCH_CHECK();
-  return walk(std::true_type{});
+  return greedy ? walk(true_type{}, true_type{}) : walk(true_type{}, false_type{});
 }
 template dipaco_status launch_draft_verify<float>(const VerifyArgs<float>&, hipStream_t);
 template dipaco_status launch_draft_verify<bf16>(const VerifyArgs<bf16>&, hipStream_t);
