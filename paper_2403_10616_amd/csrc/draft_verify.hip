@@ -1,7 +1,7 @@
 // Which drafted tokens stay, and the token behind them (include/dipaco_kernels.h has the rule): a workgroup walks a document's tree from row 0.
 //
 // A token hangs on a border (u q < r, a running sum above v times the whole), so exponentials, sums and what is left of the target are 64-bit numbers: then
-// neither the order of a sum nor an exponential's last digits (2^-42 here) decide more than one draw in 10^10.
+// neither the order of a sum nor an exponential's last digits (2^-37 here) decide more than one draw in 10^10.
 //
 // A row of scores is cut into up to 32 parts of whole 1024 scores, a wave each: largest score, sum of exponentials against it.  From these the row's
 // sum is formed, and the part that a drawn token lies in is found without reading the others again; only parts that hold refused tokens are summed anew.
@@ -17,12 +17,11 @@ namespace {
 
 constexpr int DV_THREADS = 1024, DV_WAVES = DV_THREADS / 64, DV_PARTS = 32, DV_CHUNK = 1024;
 
-// 2^t for t <= 0, to 2^-42 of it: 2^f = sum of (f ln 2)^k / k! for |f| <= 1/2, up to k = 10 (the next term is below 2^-42)
+// 2^t for t <= 0, to 2^-37 of it: 2^f = sum of (f ln 2)^k / k! for |f| <= 1/2, up to k = 9 (the next term is below 2^-37)
 __device__ __forceinline__ double power_of_two(double t) {
   t = fmax(t, -1100.0);   // what is far below, -inf and NaN: 0 in 64 bits
   const double n = rint(t), f = t - n;
-  double p = 7.054911620801121e-09;
-  p = fma(p, f, 1.0178086009239696e-07);
+  double p = 1.0178086009239696e-07;
   p = fma(p, f, 1.3215486790144305e-06);
   p = fma(p, f, 1.5252733804059838e-05);
   p = fma(p, f, 1.5403530393381606e-04);
@@ -86,43 +85,53 @@ struct Cut {
   __host__ __device__ explicit Cut(int V) : len(((V + DV_PARTS - 1) / DV_PARTS + DV_CHUNK - 1) / DV_CHUNK * DV_CHUNK), count((V + len - 1) / len) {}
 };
 
-// A wave takes a part of a row: 16 scores a lane at a time
-template <typename T> __device__ __forceinline__ PartStat part_stat(const T* row, int lo, int hi, double rate, int lane) {
-  constexpr int VEC = Vec16<T>::N;
+// 1024 scores of a row in a wave, 16 a lane
+template <typename T> struct Scores {
+  static constexpr int VEC = Vec16<T>::N;
+  float x[16];
+  __device__ __forceinline__ void load(const T* row, int base, int hi, int lane) {
+#pragma unroll
+    for (int i = 0; i < 16; i += VEC) load_scores(row, base + 64 * i + lane * VEC, hi, x + i);
+  }
+  static __device__ __forceinline__ int place(int base, int i, int lane) { return base + 64 * (i / VEC * VEC) + lane * VEC + i % VEC; }
+};
+// A part of a row, by a wave.  x: its first scores
+template <typename T> __device__ __forceinline__ PartStat part_stat(const T* row, int lo, int hi, double rate, Scores<T>& x, int lane) {
   float top = -INFINITY;
   int at = 0x7fffffff;
   bool nan = false;
   double sum = 0.0;
-  for (int base = lo; base < hi; base += DV_CHUNK) {
-    float x[16], most = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < 16; i += VEC) load_scores(row, base + 64 * i + lane * VEC, hi, x + i);
+  for (int base = lo;;) {
+    float most = -INFINITY;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      most = fmaxf(most, x[i]);
-      nan |= x[i] != x[i];
+      most = fmaxf(most, x.x[i]);
+      nan |= x.x[i] != x.x[i];
     }
     if (rate == 0.0) {
       if (most > top) {
 #pragma unroll
         for (int i = 15; i >= 0; --i)
-          if (x[i] == most) at = base + 64 * (i / VEC * VEC) + lane * VEC + i % VEC;
+          if (x.x[i] == most) at = Scores<T>::place(base, i, lane);
       }
       top = fmaxf(top, most);
-      continue;
-    }
-    if (most > top) {
-      sum *= power_of_two(fma((double)top, rate, -(double)most * rate));
-      top = most;
-    }
-    const double shift = -(double)top * rate;
-    double s0 = 0.0, s1 = 0.0;
+    } else {
+      if (most > top) {
+        sum *= power_of_two(fma((double)top, rate, -(double)most * rate));
+        top = most;
+      }
+      const double shift = -(double)top * rate;
+      double s0 = 0.0, s1 = 0.0;
 #pragma unroll
-    for (int i = 0; i < 16; i += 2) {
-      s0 += power_of_two(fma((double)x[i], rate, shift));
-      s1 += power_of_two(fma((double)x[i + 1], rate, shift));
+      for (int i = 0; i < 16; i += 2) {
+        s0 += power_of_two(fma((double)x.x[i], rate, shift));
+        s1 += power_of_two(fma((double)x.x[i + 1], rate, shift));
+      }
+      sum += s0 + s1;
     }
-    sum += s0 + s1;
+    base += DV_CHUNK;
+    if (base >= hi) break;
+    x.load(row, base, hi, lane);
   }
   PartStat p;
   p.top = wave_max(top);
@@ -140,30 +149,36 @@ template <typename T> __device__ __forceinline__ PartStat part_stat(const T* row
   return p;
 }
 
-// A row, from its parts: ok where it is a distribution
+// A row, from its parts
 struct RowStat {
   float top;
   int at;
-  double total;
-  __device__ __forceinline__ bool ok() const { return total > 0.0; }
+  double inv;   // one over the sum; 0 where the row is no distribution
 };
 // of a part's sum against the row's largest score
 __device__ __forceinline__ double part_total(const PartStat& p, float top, double rate) {
   return rate != 0.0 ? p.total * power_of_two(fma((double)p.top, rate, -(double)top * rate)) : p.total;
 }
-// a part a lane, by a whole wave
-__device__ __forceinline__ RowStat join(const PartStat* parts, int n, double rate, int lane) {
-  PartStat p{-INFINITY, -1, 0.0};
-  if (lane < n) p = parts[lane];
+// Two rows by a wave, a part a lane: lanes 0 .. 31 hold `p` and `rate` of one, lanes 32 .. 63 of the other (no part: top -inf, total 0).  Every lane gets its half's.
+__device__ __forceinline__ RowStat join(const PartStat& p, double rate, int lane) {
   RowStat r;
-  r.top = wave_max(p.top);
-  r.total = wave_total(lane < n ? part_total(p, r.top, rate) : 0.0);   // NaN stays
-  if (r.top == -INFINITY) r.total = 0.0;
-  r.at = -1;
-  if (rate == 0.0) {
-    r.at = __builtin_amdgcn_readlane(p.at, __builtin_ctzll(__builtin_amdgcn_ballot_w64(p.top == r.top) | 1ull << 63));
-    if (r.total > 0.0) r.total = 1.0;
-  }
+  float top = p.top;
+  top = fmaxf(top, dpp_fetch<0xb1, 0xf>(top, -INFINITY));
+  top = fmaxf(top, dpp_fetch<0x4e, 0xf>(top, -INFINITY));
+  top = fmaxf(top, dpp_fetch<0x141, 0xf>(top, -INFINITY));
+  top = fmaxf(top, dpp_fetch<0x140, 0xf>(top, -INFINITY));
+  top = fmaxf(top, dpp_fetch<0x142, 0xa>(top, -INFINITY));
+  r.top = __shfl(top, lane | 31, WAVE);
+  double total = p.total == 0.0 ? 0.0 : part_total(p, r.top, rate);
+  total += dpp_fetch64<0x111, 0xf>(total);
+  total += dpp_fetch64<0x112, 0xf>(total);
+  total += dpp_fetch64<0x114, 0xf>(total);
+  total += dpp_fetch64<0x118, 0xf>(total);
+  total += dpp_fetch64<0x142, 0xa>(total);
+  total = __shfl(total, lane | 31, WAVE);   // NaN stays
+  const unsigned long long first = __builtin_amdgcn_ballot_w64(p.top == r.top) & (lane < 32 ? 0xffffffffull : 0xffffffffull << 32);
+  r.at = __shfl(p.at, first ? __builtin_ctzll(first) : lane, WAVE);
+  r.inv = total > 0.0 && r.top > -INFINITY ? rate != 0.0 ? 1.0 / total : 1.0 : 0.0;
   return r;
 }
 
@@ -174,24 +189,29 @@ template <typename T> __global__ void __launch_bounds__(256) draft_verify_parts(
   if (r >= n_rows) return;
   const bool of_draft = r >= a.T_rows;
   const T* const row = of_draft ? a.draft + (long)(r - a.T_rows) * a.V : a.target + (long)r * a.V;
-  const PartStat p = part_stat(row, part * cut.len, min((part + 1) * cut.len, a.V), of_draft ? a.draft_rate : a.rate, threadIdx.x & 63);
-  if ((threadIdx.x & 63) == 0) parts[item] = p;
+  const int lane = threadIdx.x & 63, lo = part * cut.len, hi = min(lo + cut.len, a.V);
+  Scores<T> x;
+  x.load(row, lo, hi, lane);
+  const PartStat p = part_stat(row, lo, hi, of_draft ? a.draft_rate : a.rate, x, lane);
+  if (lane == 0) parts[item] = p;
 }
 
 // LDS of a walk: per row, then the bits of refused tokens
 struct WalkRow {
   int parent, token;
-  double target, draft;   // weights of the row's token in its parent's distributions (AHEAD)
+  double target, draft;   // probabilities of the row's token behind its parent (AHEAD)
   RowStat p, q;           // the row's own distributions (AHEAD)
   float u;
 };
 
 // AHEAD: the parts of all rows have been formed by another launch; else a row's are formed when the walk comes to it.  GREEDY: temperature 0.  Both are the
 // kernel's because a branch at every score keeps the compiler from holding the series' coefficients: two copies a score where there is one now.
-template <typename T, bool AHEAD, bool GREEDY> __global__ void __launch_bounds__(DV_THREADS) __attribute__((amdgpu_waves_per_eu(4, 4))) draft_verify_walk(VerifyArgs<T> a, const PartStat* parts, int b0) {
+template <typename T, bool AHEAD, bool GREEDY>
+__global__ void __launch_bounds__(DV_THREADS) __attribute__((amdgpu_waves_per_eu(4, 4))) draft_verify_walk(VerifyArgs<T> a, const PartStat* parts, int b0) {
   constexpr int VEC = Vec16<T>::N;
   __shared__ PartStat stats[2][DV_PARTS];   // of the walk's row: target, draft
   __shared__ double sums[DV_PARTS];
+  __shared__ int drawn;
   extern __shared__ __attribute__((aligned(16))) char dv_smem[];
   WalkRow* const rows = reinterpret_cast<WalkRow*>(dv_smem);
   uint32_t* const refused = reinterpret_cast<uint32_t*>(rows + a.max_new);
@@ -201,57 +221,62 @@ template <typename T, bool AHEAD, bool GREEDY> __global__ void __launch_bounds__
   const int n = min(r.count, a.max_new);
   int* const path = a.path + (long)b * a.max_new;
   const double rate = GREEDY ? 0.0 : a.rate, draft_rate = a.draft_rate;
-  if (tid < n) {
-    WalkRow& x = rows[tid];
-    x.parent = draft_parent(a.parent[r.first + tid], tid);
-    x.token = a.tokens[r.first + tid];
-    x.u = a.u[r.first + tid];
-    if (AHEAD) {
-      const bool known = x.parent >= 0 && x.token >= 0 && x.token < a.V;
-      const long at = (long)(r.first + x.parent) * a.V + x.token;
-      x.target = known ? to_f32(a.target[at]) : 0.f;
-      x.draft = known && a.draft ? to_f32(a.draft[at]) : 0.f;
-    }
-  }
+  const PartStat nothing{-INFINITY, -1, 0.0};
   if (AHEAD) {
-    const long of_draft = (long)a.T_rows * cut.count;
+    const bool of_draft = lane >= 32;
+    const int part = lane & 31;
+    const PartStat* const at = parts + (long)(r.first + (of_draft ? a.T_rows : 0)) * cut.count + part;
+    const bool held = part < cut.count && (a.draft || !of_draft);
 #pragma unroll 2
     for (int i = wave; i < n; i += DV_WAVES) {
-      const PartStat* const at = parts + (long)(r.first + i) * cut.count;
-      const RowStat p = join(at, cut.count, rate, lane);
-      RowStat q{-INFINITY, -1, 0.0};
-      if (a.draft) q = join(at + of_draft, cut.count, draft_rate, lane);
-      if (lane == 0) {
-        rows[i].p = p;
-        rows[i].q = q;
-      }
+      const RowStat x = join(held ? at[(long)i * cut.count] : nothing, of_draft ? draft_rate : rate, lane);
+      if (lane == 0) rows[i].p = x;
+      if (lane == 32) rows[i].q = x;
+    }
+  }
+  float t_score = 0.f, d_score = 0.f;
+  if (tid < n) {
+    WalkRow& x = rows[tid];
+    const int parent = draft_parent(a.parent[r.first + tid], tid), token = a.tokens[r.first + tid];
+    x.parent = parent;
+    x.token = token;
+    x.u = a.u[r.first + tid];
+    if (AHEAD && parent >= 0 && token >= 0 && token < a.V) {
+      const long at = (long)(r.first + parent) * a.V + token;
+      t_score = to_f32(a.target[at]);
+      if (a.draft) d_score = to_f32(a.draft[at]);
     }
   }
   for (int i = tid; i < (a.V + 31) / 32; i += DV_THREADS) refused[i] = 0;
   __syncthreads();
   if (AHEAD && tid < n && rows[tid].parent >= 0) {
     WalkRow& x = rows[tid];
-    const RowStat p = rows[x.parent].p;
-    x.target = weight(rate, p.top, p.at, (float)x.target, x.token);
-    if (a.draft) {
-      const RowStat q = rows[x.parent].q;
-      x.draft = weight(draft_rate, q.top, q.at, (float)x.draft, x.token);
-    }
+    const RowStat p = rows[x.parent].p, q = rows[x.parent].q;
+    x.target = weight(rate, p.top, p.at, t_score, x.token) * p.inv;
+    x.draft = a.draft ? weight(draft_rate, q.top, q.at, d_score, x.token) * q.inv : 0.0;
   }
   if (AHEAD) __syncthreads();
   auto is_refused = [&](int y) { return (refused[y >> 5] >> (y & 31)) & 1; };
-  // a row's distribution, its parts left in stats[which]
-  auto stat = [&](const T* row, double row_rate, int which) {
-    __syncthreads();
-    for (int part = wave; part < cut.count; part += DV_WAVES) {
-      const PartStat p = part_stat(row, part * cut.len, min((part + 1) * cut.len, a.V), row_rate, lane);
-      if (lane == 0) stats[which][part] = p;
-    }
-    __syncthreads();
-    return join(stats[which], cut.count, row_rate, lane);
-  };
   // bit i: token y0 + i has been refused; y0 is a multiple of VEC
   auto refused_from = [&](int y0) { return refused[y0 >> 5] >> (y0 & 31); };
+  auto part_end = [&](int part) { return min((part + 1) * cut.len, a.V); };
+  // a row's distribution, its parts left in stats[which]
+  auto stat = [&](const T* row, double row_rate, int which) {
+    Scores<T> x, then;
+    if (wave < cut.count) x.load(row, wave * cut.len, part_end(wave), lane);
+    if (wave + DV_WAVES < cut.count) then.load(row, (wave + DV_WAVES) * cut.len, part_end(wave + DV_WAVES), lane);
+    __syncthreads();
+    if (wave < cut.count) {
+      const PartStat p = part_stat(row, wave * cut.len, part_end(wave), row_rate, x, lane);
+      if (lane == 0) stats[which][wave] = p;
+    }
+    if (wave + DV_WAVES < cut.count) {
+      const PartStat p = part_stat(row, (wave + DV_WAVES) * cut.len, part_end(wave + DV_WAVES), row_rate, then, lane);
+      if (lane == 0) stats[which][wave + DV_WAVES] = p;
+    }
+    __syncthreads();
+    return join((lane & 31) < cut.count ? stats[which][lane & 31] : nothing, row_rate, lane);   // the same in both halves
+  };
   double* const rest = a.rest + (long)b * a.V;
   int node = 0, kept = n > 0 ? 1 : 0, next = -1;
   if (tid == 0 && n > 0) path[0] = 0;
@@ -259,15 +284,16 @@ template <typename T, bool AHEAD, bool GREEDY> __global__ void __launch_bounds__
     const T* const target = a.target + (long)(r.first + node) * a.V;
     const T* const draft = a.draft ? a.draft + (long)(r.first + node) * a.V : nullptr;
     const RowStat P = AHEAD ? rows[node].p : stat(target, rate, 0);
-    if (!P.ok()) break;   // no next token
+    if (P.inv == 0.0) break;   // no next token
     RowStat Q{-INFINITY, -1, 0.0};
     if (AHEAD && draft) Q = rows[node].q;
     bool have_q = AHEAD;
     int child = node, taken = -1, tried = 0;
-    double left = 1.0, q_left = Q.total, r_inv = 1.0;   // what the refused tokens have left of the target (no draft scores), of the draft; of `rest`
-    bool dead = false;                                  // the target has nothing left
+    // One over what the refused tokens have left: of the target (no draft scores), of the draft; of `rest`
+    double left = 1.0, left_inv = 1.0, q_scale = 1.0, r_inv = 1.0;
+    bool dead = false;   // the target has nothing left
     while (!dead) {
-      int found = n;   // the next child
+      int found = n;     // the next child
       for (int i0 = (child + 1) & ~63; i0 < n && found == n; i0 += 64) {
         const int i = i0 + lane;
         const unsigned long long m = __builtin_amdgcn_ballot_w64(i < n && i > child && rows[i].parent == node);
@@ -277,22 +303,21 @@ template <typename T, bool AHEAD, bool GREEDY> __global__ void __launch_bounds__
       if (child >= n) break;
       if (draft && !have_q) {
         Q = stat(draft, draft_rate, 1);
-        q_left = Q.total;
         have_q = true;
       }
-      if (draft && !Q.ok()) break;   // what was drawn from no distribution is not taken
+      if (draft && Q.inv == 0.0) break;   // what was drawn from no distribution is not taken
       const int x = rows[child].token;
       if (x < 0 || x >= a.V) continue;
       const bool before = tried && is_refused(x);
-      const double wx = AHEAD ? rows[child].target : weight(rate, P.top, P.at, to_f32(target[x]), x);
+      const double px = AHEAD ? rows[child].target : weight(rate, P.top, P.at, to_f32(target[x]), x) * P.inv;
       double q = 1.0, rx;
       if (draft) {
-        const double w = AHEAD ? rows[child].draft : weight(draft_rate, Q.top, Q.at, to_f32(draft[x]), x);
-        q = before && a.distinct ? 0.0 : w / q_left;
+        const double qx = AHEAD ? rows[child].draft : weight(draft_rate, Q.top, Q.at, to_f32(draft[x]), x) * Q.inv;
+        q = before && a.distinct ? 0.0 : qx * q_scale;
         if (!(q > 0.0)) continue;
-        rx = tried ? rest[x] * r_inv : wx / P.total;
+        rx = tried ? rest[x] * r_inv : px;
       } else {
-        rx = before ? 0.0 : wx / P.total / left;
+        rx = before ? 0.0 : px * left_inv;
       }
       if ((double)rows[child].u * q < rx) {
         taken = child;
@@ -302,38 +327,36 @@ template <typename T, bool AHEAD, bool GREEDY> __global__ void __launch_bounds__
       if (tid == 0) refused[x >> 5] |= 1u << (x & 31);
       __syncthreads();
       if (!draft) {
-        if (!before) left -= wx / P.total;
+        if (!before) left -= px;
+        left_inv = 1.0 / left;
         dead = !(left > 0.0);
       } else {
         // rest <- max(what is left of the target - the draft, 0), and the sums of both
-        const double p_inv = 1.0 / P.total, q_inv = 1.0 / q_left, p_shift = -(double)P.top * rate, q_shift = -(double)Q.top * draft_rate;
+        const double q_inv = Q.inv * q_scale, p_shift = -(double)P.top * rate, q_shift = -(double)Q.top * draft_rate;
         auto refuse = [&](auto FIRSTc, auto DISTINCTc) {
           constexpr bool FIRST = decltype(FIRSTc)::value, DISTINCT = decltype(DISTINCTc)::value;
           for (int part = wave; part < cut.count; part += DV_WAVES) {
-            const int lo = part * cut.len, hi = min(lo + cut.len, a.V);
+            const int lo = part * cut.len, hi = part_end(part);
             double all = 0.0, q_all = 0.0;
-            for (int base = lo + lane * VEC; base < hi; base += DV_CHUNK) {
-              float xt[16], xd[16];
+            for (int base = lo; base < hi; base += DV_CHUNK) {
+              Scores<T> xd, xt;
               double before[16];
+              xd.load(draft, base, hi, lane);
+              if (FIRST) xt.load(target, base, hi, lane);
+              else
+#pragma unroll
+                for (int i = 0; i < 16; ++i) before[i] = rest[min(Scores<T>::place(base, i, lane), hi - 1)];
 #pragma unroll
               for (int j = 0; j < 16; j += VEC) {
-                load_scores(draft, base + 64 * j, hi, xd + j);
-                if (FIRST) load_scores(target, base + 64 * j, hi, xt + j);
-                else
-#pragma unroll
-                  for (int i = 0; i < VEC; ++i) before[j + i] = rest[min(base + 64 * j + i, hi - 1)];
-              }
-#pragma unroll
-              for (int j = 0; j < 16; j += VEC) {
-                const int y0 = base + 64 * j;
+                const int y0 = Scores<T>::place(base, j, lane);
                 const uint32_t gone = DISTINCT && y0 < hi ? refused_from(y0) : 0;
                 double now[VEC];
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) {   // a score of -inf behind the part's end: 0
-                  double w = power_of_two(fma((double)xd[j + i], draft_rate, q_shift)), p;
+                  double w = power_of_two(fma((double)xd.x[j + i], draft_rate, q_shift)), p;
                   if (!FIRST) p = before[j + i] * r_inv;
                   else if (GREEDY) p = y0 + i == P.at ? 1.0 : 0.0;
-                  else p = power_of_two(fma((double)xt[j + i], rate, p_shift)) * p_inv;
+                  else p = power_of_two(fma((double)xt.x[j + i], rate, p_shift)) * P.inv;
                   if (DISTINCT) {   // of the tokens refused before this one the draft has nothing left, and the target neither
                     const bool is_gone = gone & (1u << i);
                     q_all += is_gone ? 0.0 : w;
@@ -367,7 +390,7 @@ template <typename T, bool AHEAD, bool GREEDY> __global__ void __launch_bounds__
         else a.distinct ? refuse(std::true_type{}, std::true_type{}) : refuse(std::true_type{}, std::false_type{});
         __syncthreads();
         const double all = wave_total(lane < cut.count ? sums[lane] : 0.0);
-        if (a.distinct) q_left = wave_total(lane < cut.count ? stats[1][lane].total : 0.0);
+        if (a.distinct) q_scale = 1.0 / (wave_total(lane < cut.count ? stats[1][lane].total : 0.0) * Q.inv);   // inf: the draft has nothing left
         dead = !(all > 0.0);
         r_inv = 1.0 / all;
       }
@@ -382,21 +405,23 @@ template <typename T, bool AHEAD, bool GREEDY> __global__ void __launch_bounds__
       // sum over lo .. hi - 1, by a wave; lo is a multiple of VEC
       auto weights = [&](int lo, int hi) {
         double e = 0.0;
-        for (int base = lo + lane * VEC; base < hi; base += DV_CHUNK) {
+        for (int base = lo; base < hi; base += DV_CHUNK) {
           if (from_rest) {
 #pragma unroll
-            for (int j = 0; j < 16; j += VEC)
-#pragma unroll
-              for (int i = 0; i < VEC; ++i) e += base + 64 * j + i < hi ? rest[base + 64 * j + i] : 0.0;
+            for (int i = 0; i < 16; ++i) {
+              const int y = Scores<T>::place(base, i, lane);
+              const double w = rest[min(y, hi - 1)];
+              e += y < hi ? w : 0.0;
+            }
           } else {
-            float x[16];
-#pragma unroll
-            for (int j = 0; j < 16; j += VEC) load_scores(target, base + 64 * j, hi, x + j);
+            Scores<T> x;
+            x.load(target, base, hi, lane);
 #pragma unroll
             for (int j = 0; j < 16; j += VEC) {
-              const uint32_t gone = without && base + 64 * j < hi ? refused_from(base + 64 * j) : 0;
+              const int y0 = Scores<T>::place(base, j, lane);
+              const uint32_t gone = without && y0 < hi ? refused_from(y0) : 0;
 #pragma unroll
-              for (int i = 0; i < VEC; ++i) e += of_target(x[j + i], base + 64 * j + i, gone >> i);
+              for (int i = 0; i < VEC; ++i) e += of_target(x.x[j + i], y0 + i, gone >> i);
             }
           }
         }
@@ -405,17 +430,24 @@ template <typename T, bool AHEAD, bool GREEDY> __global__ void __launch_bounds__
       double all = 0.0;
       for (;;) {
         if (!from_rest) {
-          __syncthreads();
-          for (int part = wave; part < cut.count; part += DV_WAVES) {
-            const int lo = part * cut.len, hi = min(lo + cut.len, a.V);
-            bool anew = false;
-            if (without)
-              for (int w = (lo >> 5) + lane; w < (hi + 31) >> 5; w += 64) anew |= refused[w] != 0;
+          const int part = wave + DV_WAVES * (lane & 1);   // a lane each of the wave's two parts
+          double of_part = 0.0;
+          if (part < cut.count) {
             const PartStat p = AHEAD ? parts[(long)(r.first + node) * cut.count + part] : stats[0][part];
-            double of_part = rate != 0.0 ? part_total(p, P.top, rate) : P.at >= lo && P.at < hi ? 1.0 : 0.0;
-            if (__any(anew)) of_part = weights(lo, hi);
-            if (lane == 0) sums[part] = of_part;
+            of_part = rate != 0.0 ? part_total(p, P.top, rate) : P.at >= part * cut.len && P.at < part_end(part) ? 1.0 : 0.0;
           }
+          if (without)
+            for (int i = 0; i < 2 && wave + DV_WAVES * i < cut.count; ++i) {
+              const int lo = (wave + DV_WAVES * i) * cut.len, hi = part_end(wave + DV_WAVES * i);
+              bool anew = false;
+              for (int w = (lo >> 5) + lane; w < (hi + 31) >> 5; w += 64) anew |= refused[w] != 0;
+              if (__any(anew)) {
+                const double e = weights(lo, hi);
+                if ((lane & 1) == i) of_part = e;
+              }
+            }
+          __syncthreads();
+          if (lane < 2 && part < cut.count) sums[part] = of_part;
           __syncthreads();
         }
         all = wave_total(lane < cut.count ? sums[lane] : 0.0);
@@ -426,34 +458,40 @@ template <typename T, bool AHEAD, bool GREEDY> __global__ void __launch_bounds__
       // the first part whose running sum is above the aim; rounding may leave it above them all: the last that holds any
       int lo = 0, len = a.V;
       double before = 0.0;
-      auto first_above = [&](double mine, double& base) {   // a lane each; -1: none holds any
-        const double upto = before + wave_upto(mine);
+      auto first_above = [&](double mine, double upto) {   // a lane each; -1: none holds any
         const unsigned long long any = __builtin_amdgcn_ballot_w64(mine > 0.0), over = __builtin_amdgcn_ballot_w64(mine > 0.0 && upto > aim);
-        const int at = any == 0 ? -1 : over ? __builtin_ctzll(over) : 63 - __builtin_clzll(any);
-        base = at > 0 ? lane_value(upto, at - 1) : before;
-        return at;
+        return any == 0 ? -1 : over ? __builtin_ctzll(over) : 63 - __builtin_clzll(any);
       };
-      auto choose = [&](int n_parts, int part_len) {
-        double base;
-        const int at = max(first_above(lane < n_parts ? sums[lane] : 0.0, base), 0);
+      auto choose = [&](int n_parts, int part_len) {   // of sums[0 .. n_parts - 1]
+        const double mine = lane < n_parts ? sums[lane] : 0.0, upto = before + wave_upto(mine);
+        const int at = max(first_above(mine, upto), 0);
+        if (at > 0) before = lane_value(upto, at - 1);
         lo += at * part_len;
         len = min(part_len, len - at * part_len);
-        before = base;
+        return at;
       };
       choose(cut.count, cut.len);
-      while (len > 64) {   // then sixteenths of it
-        const int part_len = ((len + DV_WAVES - 1) / DV_WAVES + VEC - 1) / VEC * VEC, from = lo + wave * part_len;
-        const double e = weights(from, min(from + part_len, lo + len));
+      if (len > DV_CHUNK) {   // then 1024 of it: cut.len is at most 8192
+        const double e = lo + DV_CHUNK * wave < lo + len ? weights(lo + DV_CHUNK * wave, min(lo + DV_CHUNK * (wave + 1), lo + len)) : 0.0;
         __syncthreads();
         if (lane == 0) sums[wave] = e;
         __syncthreads();
-        choose(DV_WAVES, part_len);
+        choose(DV_WAVES, DV_CHUNK);
       }
-      double base;   // a score a lane
-      const int y = min(lo + lane, lo + len - 1);
-      const double mine = from_rest ? rest[y] : of_target(to_f32(target[y]), y, without ? is_refused(y) : 0);
-      const int at = first_above(lane < len ? mine : 0.0, base);
-      next = at < 0 ? -1 : lo + at;
+      // then a score a thread
+      const int y = min(lo + tid, lo + len - 1);
+      const double w = from_rest ? rest[y] : of_target(to_f32(target[y]), y, without ? is_refused(y) : 0), mine = tid < len ? w : 0.0, upto = wave_upto(mine);
+      __syncthreads();
+      if (lane == 63) sums[wave] = upto;
+      if (tid == 0) drawn = -1;
+      __syncthreads();
+      const int of_wave = choose(DV_WAVES, 64);
+      if (wave == of_wave) {
+        const int at = first_above(mine, before + upto);
+        if (lane == 0 && at >= 0) drawn = lo + at;
+      }
+      __syncthreads();
+      next = drawn;
       break;
     }
     if (tried) {   // tokens refused here are children of this row
