@@ -262,17 +262,12 @@ __global__ void __launch_bounds__(DV_THREADS) __attribute__((amdgpu_waves_per_eu
   auto part_end = [&](int part) { return min((part + 1) * cut.len, a.V); };
   // a row's distribution, its parts left in stats[which]
   auto stat = [&](const T* row, double row_rate, int which) {
-    Scores<T> x, then;
-    if (wave < cut.count) x.load(row, wave * cut.len, part_end(wave), lane);
-    if (wave + DV_WAVES < cut.count) then.load(row, (wave + DV_WAVES) * cut.len, part_end(wave + DV_WAVES), lane);
     __syncthreads();
-    if (wave < cut.count) {
-      const PartStat p = part_stat(row, wave * cut.len, part_end(wave), row_rate, x, lane);
-      if (lane == 0) stats[which][wave] = p;
-    }
-    if (wave + DV_WAVES < cut.count) {
-      const PartStat p = part_stat(row, (wave + DV_WAVES) * cut.len, part_end(wave + DV_WAVES), row_rate, then, lane);
-      if (lane == 0) stats[which][wave + DV_WAVES] = p;
+    for (int part = wave; part < cut.count; part += DV_WAVES) {
+      Scores<T> x;
+      x.load(row, part * cut.len, part_end(part), lane);
+      const PartStat p = part_stat(row, part * cut.len, part_end(part), row_rate, x, lane);
+      if (lane == 0) stats[which][part] = p;
     }
     __syncthreads();
     return join((lane & 31) < cut.count ? stats[which][lane & 31] : nothing, row_rate, lane);   // the same in both halves
