@@ -2,7 +2,7 @@
 // of slot L + path[i], in every layer and head.
 //
 // In place: path rises strictly, so a row's place lies in front of its source, and no place of an earlier row is the source of a later one.  A wave moves
-// the rows of one layer, document and head in order, as many at a time as its lanes hold; those it has read before it writes may be the places of others.
+// the rows of one layer, document and head in order, four loads of them ahead of their stores; those it has read before it writes may be the places of others.
 #include <algorithm>
 
 #include "draft.h"
@@ -12,6 +12,8 @@ namespace dipaco {
 
 namespace {
 
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));   // an array of HIP's own uint4 is kept in LDS
+
 __global__ void __launch_bounds__(256) cache_keep_rows(KeepArgs a, int first) {
   const int lane = threadIdx.x & 63, kh = blockIdx.y * 4 + (threadIdx.x >> 6), layer = blockIdx.z;
   const int b = first + blockIdx.x;
@@ -19,33 +21,44 @@ __global__ void __launch_bounds__(256) cache_keep_rows(KeepArgs a, int first) {
   const int* const path = a.path + (long)b * a.max_new;
   const int kept = min(max(a.kept[b], 0), a.max_new), cached = min(max(a.cache_len[b], 0), 0x7f000000);
   const int* const pages = a.pages + (long)b * a.pages_per_doc;
-  uint4* const cache = a.cache[layer];
-  auto row_of = [&](int pos) -> long {   // where the row of a position begins, -1 where the table has no page for it
-    const int at = pos >> a.page_shift;
-    const int page = at < a.pages_per_doc ? pages[at] : -1;
-    if ((unsigned)page >= (unsigned)a.n_pages) return -1;
-    return ((((long)page * 2 * a.H_kv + kh) << a.page_shift) + (pos & ((1 << a.page_shift) - 1))) * a.row_vecs;
+  u32x4* const cache = reinterpret_cast<u32x4*>(a.cache[layer]);
+  // Where the row of a position begins, -1 where the table has no page for it.  No load hangs on a branch: behind one the compiler waits for each by itself.
+  auto page_of = [&](int pos) { return pages[min(pos >> a.page_shift, a.pages_per_doc - 1)]; };
+  auto row_of = [&](int pos, int page) -> long {
+    const long row = ((((long)page * 2 * a.H_kv + kh) << a.page_shift) + (pos & ((1 << a.page_shift) - 1))) * a.row_vecs;
+    return (unsigned)page < (unsigned)a.n_pages && pos >> a.page_shift < a.pages_per_doc ? row : -1;
   };
-  const int rows = 64 / a.row_vecs;   // at a time
-  const int sub = lane / a.row_vecs, col = lane % a.row_vecs;
-  int before = -1;                    // the path's last row so far
-  for (int i0 = 0; i0 < kept; i0 += rows) {
-    const int i = i0 + sub;
-    const int from = i < kept && sub < rows ? path[i] : -1;
-    int left = __shfl_up(from, a.row_vecs, WAVE);
-    if (sub == 0) left = before;
-    const bool rises = from > left && from < a.max_new;
-    // rows from the first one on that does not rise are no path
-    const unsigned long long bad = __builtin_amdgcn_ballot_w64(!rises && i < kept && sub < rows);
-    const int good = bad ? __builtin_ctzll(bad) / a.row_vecs : rows;
-    long to = -1, src = -1;
-    if (sub < good && i < kept && from != i) {
-      to = row_of(cached + i);
-      src = row_of(cached + from);
+  constexpr int AHEAD = 4;
+  const int rows = 64 / a.row_vecs, sub = lane / a.row_vecs, col = lane % a.row_vecs;   // rows a load or store
+  int before = -1;                                                                    // the path's last row so far
+  for (int i0 = 0; i0 < kept; i0 += 64) {
+    // a row a lane: where it is and where it goes
+    const int i = i0 + lane, from = i < kept ? path[i] : -1;
+    int left = __shfl_up(from, 1, WAVE);
+    if (lane == 0) left = before;
+    const unsigned long long bad = __builtin_amdgcn_ballot_w64(i < kept && (from <= left || from >= a.max_new));
+    const int n = min(bad ? __builtin_ctzll(bad) : 64, kept - i0);   // rows from the first one on that does not rise are no path
+    const int to_page = page_of(cached + i), src_page = page_of(cached + max(from, 0));
+    long to = row_of(cached + i, to_page), src = row_of(cached + max(from, 0), src_page);
+    if (lane >= n || from == i || src < 0) to = -1;
+    if (to < 0) src = 0;
+    for (int r0 = 0; r0 < n; r0 += AHEAD * rows) {
+      u32x4 v[AHEAD];
+      long at[AHEAD];
+#pragma unroll
+      for (int j = 0; j < AHEAD; ++j) {
+        const int r = r0 + j * rows + sub;
+        at[j] = __shfl(to, r & 63, WAVE);
+        const long s = __shfl(src, r & 63, WAVE);   // 0 where nothing moves
+        if (r >= n) at[j] = -1;
+        v[j] = cache[s + col];
+      }
+#pragma unroll
+      for (int j = 0; j < AHEAD; ++j)
+        if (at[j] >= 0) cache[at[j] + col] = v[j];
     }
-    if (to >= 0 && src >= 0) cache[to + col] = cache[src + col];   // the wave's reads come first: the store waits for them
     if (bad) break;
-    before = __shfl(from, (rows - 1) * a.row_vecs, WAVE);
+    before = __shfl(from, 63, WAVE);
   }
 }
 

@@ -9,35 +9,42 @@ namespace dipaco {
 
 namespace {
 
+// An odd number of words from row to row: neighbours' words lie in other banks
+template <int WORDS> constexpr int row_words() { return WORDS | 1; }
+
 template <int WORDS>
 __global__ void __launch_bounds__(DRAFT_MOST_ROWS) draft_tree_rows(const int* parent, const int* row_start, int* depth, uint64_t* seen, int T_rows, int max_new, int words,
                                                                    int b0) {
-  extern __shared__ __attribute__((aligned(16))) uint64_t dt_smem[];   // [rows][WORDS] bits, then [rows] how far up they reach: the row, or -1
-  const int i = threadIdx.x;
+  constexpr int LD = row_words<WORDS>();
+  extern __shared__ __attribute__((aligned(16))) uint64_t dt_smem[];   // [rows][LD] bits, then [rows] how far up they reach: the row, or -1
+  const int i = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(i >> 6);   // rows of a wave see no row of a later one: words up to its own
   const RowRange r = ragged_rows(row_start, b0 + blockIdx.x, T_rows);
   const int n = min(r.count, max_new);
-  int* const reach = reinterpret_cast<int*>(dt_smem + (size_t)max_new * WORDS);
+  int* const reach = reinterpret_cast<int*>(dt_smem + (size_t)max_new * LD);
   uint64_t mine[WORDS];
 #pragma unroll
-  for (int w = 0; w < WORDS; ++w) mine[w] = i >> 6 == w ? 1ull << (i & 63) : 0;
+  for (int w = 0; w < WORDS; ++w) mine[w] = wave == w ? 1ull << (i & 63) : 0;
   int up = -1;
   if (i < n) {
     up = draft_parent(parent[r.first + i], i);
 #pragma unroll
-    for (int w = 0; w < WORDS; ++w) dt_smem[i * WORDS + w] = mine[w];
+    for (int w = 0; w < WORDS; ++w)
+      if (w <= wave) dt_smem[i * LD + w] = mine[w];
     reach[i] = up;
   }
   while (__syncthreads_or(up >= 0)) {
     int next = -1;
     if (up >= 0) {
 #pragma unroll
-      for (int w = 0; w < WORDS; ++w) mine[w] |= dt_smem[up * WORDS + w];
+      for (int w = 0; w < WORDS; ++w)   // the row's own wave is an earlier one, or this: it may hold fewer words
+        if (w <= wave) mine[w] |= w <= up >> 6 ? dt_smem[up * LD + w] : 0;
       next = reach[up];
     }
     __syncthreads();
     if (up >= 0) {
 #pragma unroll
-      for (int w = 0; w < WORDS; ++w) dt_smem[i * WORDS + w] = mine[w];
+      for (int w = 0; w < WORDS; ++w)
+        if (w <= wave) dt_smem[i * LD + w] = mine[w];
       reach[i] = next;
     }
     up = next;
@@ -59,9 +66,9 @@ dipaco_status launch_draft_tree(const int* parent, const int* row_start, int* de
   auto run = [&](auto Wc) -> dipaco_status {
     constexpr int WORDS = decltype(Wc)::value;
     static std::atomic<unsigned long long> lds_set{0};
-    if (dipaco_status st = ensure_dynamic_lds(reinterpret_cast<const void*>(draft_tree_rows<WORDS>), DRAFT_MOST_ROWS * (8 * WORDS + 4), lds_set)) return st;
+    if (dipaco_status st = ensure_dynamic_lds(reinterpret_cast<const void*>(draft_tree_rows<WORDS>), DRAFT_MOST_ROWS * (8 * row_words<WORDS>() + 4), lds_set)) return st;
     launch_parts(B, [&](long long first, unsigned count) {
-      draft_tree_rows<WORDS><<<count, (max_new + 63) / 64 * 64, (size_t)max_new * (8 * WORDS + 4), s>>>(parent, row_start, depth, seen, T_rows, max_new, words, (int)first);
+      draft_tree_rows<WORDS><<<count, (max_new + 63) / 64 * 64, (size_t)max_new * (8 * row_words<WORDS>() + 4), s>>>(parent, row_start, depth, seen, T_rows, max_new, words, (int)first);
     });
     DIPACO_LAUNCH_CHECK();
     return DIPACO_OK;
