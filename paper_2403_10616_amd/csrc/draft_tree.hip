@@ -14,7 +14,7 @@ template <int WORDS> constexpr int row_words() { return WORDS | 1; }
 
 template <int WORDS>
 __global__ void __launch_bounds__(DRAFT_MOST_ROWS) draft_tree_rows(const int* parent, const int* row_start, int* depth, uint64_t* seen, int T_rows, int max_new, int words,
-                                                                   int b0) {
+                                                                   Divisor per_row, int b0) {
   constexpr int LD = row_words<WORDS>();
   extern __shared__ __attribute__((aligned(16))) uint64_t dt_smem[];   // [rows][LD] bits, then [rows] how far up they reach: the row, or -1
   const int i = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(i >> 6);   // rows of a wave see no row of a later one: words up to its own
@@ -49,14 +49,22 @@ __global__ void __launch_bounds__(DRAFT_MOST_ROWS) draft_tree_rows(const int* pa
     }
     up = next;
   }
-  if (i >= n) return;
-  int count = 0;
+  if (i < n) {
+    int count = 0;
 #pragma unroll
-  for (int w = 0; w < WORDS; ++w) count += __builtin_popcountll(mine[w]);
-  depth[r.first + i] = count - 1;
-#pragma unroll
-  for (int w = 0; w < WORDS; ++w)
-    if (w < words) seen[(long)(r.first + i) * words + w] = mine[w];
+    for (int w = 0; w < WORDS; ++w) count += __builtin_popcountll(mine[w]);
+    depth[r.first + i] = count - 1;
+  }
+  if (WORDS == 1) {
+    if (i < n) seen[r.first + i] = mine[0];
+    return;
+  }
+  // the rows' words lie one behind the other: from LDS, where a wave's rows hold words up to their own
+  uint64_t* const out = seen + (long)r.first * words;
+  for (int at = i; at < n * words; at += blockDim.x) {
+    const int row = per_row(at), w = at - row * words;
+    out[at] = w <= row >> 6 ? dt_smem[row * LD + w] : 0;
+  }
 }
 
 }  // namespace
@@ -68,7 +76,7 @@ dipaco_status launch_draft_tree(const int* parent, const int* row_start, int* de
     static std::atomic<unsigned long long> lds_set{0};
     if (dipaco_status st = ensure_dynamic_lds(reinterpret_cast<const void*>(draft_tree_rows<WORDS>), DRAFT_MOST_ROWS * (8 * row_words<WORDS>() + 4), lds_set)) return st;
     launch_parts(B, [&](long long first, unsigned count) {
-      draft_tree_rows<WORDS><<<count, (max_new + 63) / 64 * 64, (size_t)max_new * (8 * row_words<WORDS>() + 4), s>>>(parent, row_start, depth, seen, T_rows, max_new, words, (int)first);
+      draft_tree_rows<WORDS><<<count, (max_new + 63) / 64 * 64, (size_t)max_new * (8 * row_words<WORDS>() + 4), s>>>(parent, row_start, depth, seen, T_rows, max_new, words, Divisor(words), (int)first);
     });
     DIPACO_LAUNCH_CHECK();
     return DIPACO_OK;
