@@ -158,7 +158,7 @@ constexpr size_t PAGED_GROUP_ROWS = std::max(PAGED_WIDE_GROUPS * PagedCut<bf16>:
 inline size_t partial_rows(int T_rows, int H, int64_t capacity) {
   return std::min((size_t)most_splits(capacity, PagedCut<float>::LEAST_KEYS) * T_rows, (size_t)T_rows + (PAGED_GROUP_ROWS + H - 1) / H);
 }
-template <typename T> PagedPlan plan(const PagedArgs<T>& a) {
+template <typename T> PagedPlan plan(const PagedArgs<T>& a, int dh, bool tree) {
   constexpr int NARROW_ROWS = PagedCut<T>::NARROW_ROWS, WIDE_ROWS = PagedCut<T>::WIDE_ROWS;
   const int G = a.H / a.H_kv, page_size = 1 << a.page_shift;
   const int64_t seen = std::min<int64_t>((int64_t)page_size * a.pages_per_doc, (int64_t)a.w.window + a.w.sinks + WIDE_ROWS);   // keys of a block, about
@@ -171,6 +171,13 @@ template <typename T> PagedPlan plan(const PagedArgs<T>& a) {
   if (const int64_t half = (p.narrow_splits + 1) / 2; std::is_same<T, bf16>::value && heads * half <= 256 && longest <= NARROW_ROWS) {   // twice the waves a workgroup
     p.narrow_splits = (int)half;
     p.narrow_keys = 2 * PagedCut<T>::LEAST_KEYS;
+    // Rows of a tree: one split where its waves (eight, four for wide heads) have at most 256 keys each, without a launch that joins splits.  Us, two splits | one:
+    // 16 rows, 14 heads of 64, over 1000 12.0 | 9.6, over 2000 12.2 | 12.2, over 3000 12.4 | 15.9; 8 documents of these over 2000 17.5 | 15.1.
+    const int one = (dh == 128 ? 1 : 2) * p.narrow_keys;
+    if (tree && seen <= one) {
+      p.narrow_splits = 1;
+      p.narrow_keys = one;
+    }
   }
   p.wide_blocks = longest <= NARROW_ROWS ? 0 : (int)(packed / WIDE_ROWS + std::min<int64_t>(a.B, packed / (NARROW_ROWS + 1)));
   const int64_t wide = std::max<int64_t>(1, p.wide_blocks) * a.H_kv;
@@ -194,7 +201,7 @@ size_t paged_workspace_bytes(int T_rows, int H, int dh, int page_size, int pages
   return 256 + partial_rows(T_rows, H, (int64_t)page_size * pages_per_doc) * H * (dh + 2) * sizeof(float);
 }
 template <typename T, template <typename> class Args> static dipaco_status launch_paged(Args<T> a, int dh, void* workspace, hipStream_t s) {
-  const PagedPlan p = plan<T>(a);
+  const PagedPlan p = plan<T>(a, dh, Args<T>::TREE);
   a.narrow_splits = Divisor(p.narrow_splits);
   a.narrow_keys = p.narrow_keys;
   a.narrow_turn = 3 - std::min(3, __builtin_ctz(p.narrow_splits));   // n splits begin at 8 / gcd(8, n) places by themselves
