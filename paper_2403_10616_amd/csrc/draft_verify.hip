@@ -15,7 +15,7 @@ namespace dipaco {
 
 namespace {
 
-constexpr int DV_THREADS = 1024, DV_WAVES = DV_THREADS / 64, DV_PARTS = 32, DV_CHUNK = 1024;
+constexpr int DV_THREADS = 512, DV_WAVES = DV_THREADS / 64, DV_PARTS = 32, DV_CHUNK = 1024;
 
 // 2^t for t <= 0, to 2^-37 of it: 2^f = sum of (f ln 2)^k / k! for |f| <= 1/2, up to k = 9 (the next term is below 2^-37)
 __device__ __forceinline__ double power_of_two(double t) {
@@ -182,39 +182,70 @@ __device__ __forceinline__ RowStat join(const PartStat& p, double rate, int lane
   return r;
 }
 
-// The parts of all rows of the call: [T rows][parts] of the target, then of the draft
-template <typename T> __global__ void __launch_bounds__(256) draft_verify_parts(VerifyArgs<T> a, PartStat* parts, int n_rows, Divisor count) {
-  const Cut cut(a.V);
-  const int item = blockIdx.x * 4 + (threadIdx.x >> 6), r = count(item), part = item - r * (int)count.d;
-  if (r >= n_rows) return;
-  const bool of_draft = r >= a.T_rows;
-  const T* const row = of_draft ? a.draft + (long)(r - a.T_rows) * a.V : a.target + (long)r * a.V;
-  const int lane = threadIdx.x & 63, lo = part * cut.len, hi = min(lo + cut.len, a.V);
+// Which rows' parts are formed ahead of the walks, by a launch of their own: [T rows][parts] of the target, then of the draft
+enum Ahead { NO_ROWS, PARENTS, ALL_ROWS };
+
+template <typename T> __device__ __forceinline__ void form_part(const VerifyArgs<T>& a, const Cut& cut, PartStat* parts, int row, int part, int lane) {
+  const bool of_draft = row >= a.T_rows;
+  const T* const scores = of_draft ? a.draft + (long)(row - a.T_rows) * a.V : a.target + (long)row * a.V;
+  const int lo = part * cut.len, hi = min(lo + cut.len, a.V);
   Scores<T> x;
-  x.load(row, lo, hi, lane);
-  const PartStat p = part_stat(row, lo, hi, of_draft ? a.draft_rate : a.rate, x, lane);
-  if (lane == 0) parts[item] = p;
+  x.load(scores, lo, hi, lane);
+  const PartStat p = part_stat(scores, lo, hi, of_draft ? a.draft_rate : a.rate, x, lane);
+  if (lane == 0) parts[(long)row * cut.count + part] = p;
+}
+// A part a wave
+template <typename T> __global__ void __launch_bounds__(256) draft_verify_parts(VerifyArgs<T> a, PartStat* parts, int n_rows, Divisor count) {
+  const int item = blockIdx.x * 4 + (threadIdx.x >> 6), row = count(item), part = item - row * (int)count.d;
+  if (row < n_rows) form_part(a, Cut(a.V), parts, row, part, threadIdx.x & 63);
+}
+// Parts of rows that have children, DV_PARENT_PARTS of a row a wave: two thirds or so of a tree's rows are leaves, of which a walk ends at one at most
+constexpr int DV_PARENT_PARTS = 4;
+template <typename T> __global__ void __launch_bounds__(256) draft_verify_parents(VerifyArgs<T> a, PartStat* parts, int n_rows, Divisor groups) {
+  const int lane = threadIdx.x & 63, item = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)), row = groups(item);
+  if (row >= n_rows) return;
+  const int at = row >= a.T_rows ? row - a.T_rows : row, b = __builtin_amdgcn_readfirstlane(find_document(a.row_start, a.B, at, lane));
+  const RowRange r = ragged_rows(a.row_start, b, a.T_rows);
+  const int n = min(r.count, a.max_new), i = at - r.first;
+  bool has_child = false;
+  for (int c = i + 1 + lane; c < n; c += 64) has_child |= draft_parent(a.parent[r.first + c], c) == i;
+  if (i < 0 || i >= n || !__any(has_child)) return;
+  const Cut cut(a.V);
+  const int first = (item - row * (int)groups.d) * DV_PARENT_PARTS;
+  for (int part = first; part < min(first + DV_PARENT_PARTS, cut.count); ++part) form_part(a, cut, parts, row, part, lane);
 }
 
-// LDS of a walk: per row, then the bits of refused tokens
-struct WalkRow {
-  int parent, token;
-  double target, draft;   // probabilities of the row's token behind its parent (AHEAD)
-  RowStat p, q;           // the row's own distributions (AHEAD)
-  float u;
+// LDS of a walk: arrays of `rows`, then the bits of refused tokens
+struct WalkRows {
+  RowStat *p, *q;           // the row's own distributions (formed ahead, PARENTS: of rows that are)
+  double *target, *draft;   // probabilities of the row's token behind its parent (formed ahead)
+  float* u;
+  int *parent, *token;
+  uint32_t* refused;
+  static constexpr int ROW_BYTES = 2 * (int)sizeof(RowStat) + 2 * 8 + 4 + 2 * 4;
+  __device__ __forceinline__ WalkRows(char* at, int rows) {
+    p = reinterpret_cast<RowStat*>(at);
+    q = p + rows;
+    target = reinterpret_cast<double*>(q + rows);
+    draft = target + rows;
+    u = reinterpret_cast<float*>(draft + rows);
+    parent = reinterpret_cast<int*>(u + rows);
+    token = parent + rows;
+    refused = reinterpret_cast<uint32_t*>(token + rows);
+  }
 };
 
-// AHEAD: the parts of all rows have been formed by another launch; else a row's are formed when the walk comes to it.  GREEDY: temperature 0.  Both are the
+// AHEAD: whose parts have been formed; another row's are formed when the walk comes to it.  GREEDY: temperature 0.  Both are the
 // kernel's because a branch at every score keeps the compiler from holding the series' coefficients: two copies a score where there is one now.
-template <typename T, bool AHEAD, bool GREEDY>
-__global__ void __launch_bounds__(DV_THREADS) __attribute__((amdgpu_waves_per_eu(4, 4))) draft_verify_walk(VerifyArgs<T> a, const PartStat* parts, int b0) {
+template <typename T, Ahead AHEAD, bool GREEDY>
+__global__ void __launch_bounds__(DV_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2))) draft_verify_walk(VerifyArgs<T> a, const PartStat* parts, int b0) {
   constexpr int VEC = Vec16<T>::N;
   __shared__ PartStat stats[2][DV_PARTS];   // of the walk's row: target, draft
   __shared__ double sums[DV_PARTS];
   __shared__ int drawn;
   extern __shared__ __attribute__((aligned(16))) char dv_smem[];
-  WalkRow* const rows = reinterpret_cast<WalkRow*>(dv_smem);
-  uint32_t* const refused = reinterpret_cast<uint32_t*>(rows + a.max_new);
+  const WalkRows rows(dv_smem, a.max_new);
+  uint32_t* const refused = rows.refused;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), b = b0 + blockIdx.x;
   const Cut cut(a.V);
   const RowRange r = ragged_rows(a.row_start, b, a.T_rows);
@@ -230,31 +261,31 @@ __global__ void __launch_bounds__(DV_THREADS) __attribute__((amdgpu_waves_per_eu
 #pragma unroll 2
     for (int i = wave; i < n; i += DV_WAVES) {
       const RowStat x = join(held ? at[(long)i * cut.count] : nothing, of_draft ? draft_rate : rate, lane);
-      if (lane == 0) rows[i].p = x;
-      if (lane == 32) rows[i].q = x;
+      if (lane == 0) rows.p[i] = x;
+      if (lane == 32) rows.q[i] = x;
     }
   }
-  float t_score = 0.f, d_score = 0.f;
-  if (tid < n) {
-    WalkRow& x = rows[tid];
-    const int parent = draft_parent(a.parent[r.first + tid], tid), token = a.tokens[r.first + tid];
-    x.parent = parent;
-    x.token = token;
-    x.u = a.u[r.first + tid];
-    if (AHEAD && parent >= 0 && token >= 0 && token < a.V) {
+  for (int i = tid; i < n; i += DV_THREADS) {
+    const int parent = draft_parent(a.parent[r.first + i], i), token = a.tokens[r.first + i];
+    rows.parent[i] = parent;
+    rows.token[i] = token;
+    rows.u[i] = a.u[r.first + i];
+    if (AHEAD && parent >= 0 && token >= 0 && token < a.V) {   // scores, until all rows' sums are in LDS
       const long at = (long)(r.first + parent) * a.V + token;
-      t_score = to_f32(a.target[at]);
-      if (a.draft) d_score = to_f32(a.draft[at]);
+      rows.target[i] = to_f32(a.target[at]);
+      if (a.draft) rows.draft[i] = to_f32(a.draft[at]);
     }
   }
   for (int i = tid; i < (a.V + 31) / 32; i += DV_THREADS) refused[i] = 0;
   __syncthreads();
-  if (AHEAD && tid < n && rows[tid].parent >= 0) {
-    WalkRow& x = rows[tid];
-    const RowStat p = rows[x.parent].p, q = rows[x.parent].q;
-    x.target = weight(rate, p.top, p.at, t_score, x.token) * p.inv;
-    x.draft = a.draft ? weight(draft_rate, q.top, q.at, d_score, x.token) * q.inv : 0.0;
-  }
+  if (AHEAD)
+    for (int i = tid; i < n; i += DV_THREADS) {
+      const int parent = rows.parent[i], token = rows.token[i];
+      if (parent < 0 || token < 0 || token >= a.V) continue;
+      const RowStat p = rows.p[parent], q = rows.q[parent];
+      rows.target[i] = weight(rate, p.top, p.at, (float)rows.target[i], token) * p.inv;
+      if (a.draft) rows.draft[i] = weight(draft_rate, q.top, q.at, (float)rows.draft[i], token) * q.inv;
+    }
   if (AHEAD) __syncthreads();
   auto is_refused = [&](int y) { return (refused[y >> 5] >> (y & 31)) & 1; };
   // bit i: token y0 + i has been refused; y0 is a multiple of VEC
@@ -278,43 +309,47 @@ __global__ void __launch_bounds__(DV_THREADS) __attribute__((amdgpu_waves_per_eu
   while (n > 0) {
     const T* const target = a.target + (long)(r.first + node) * a.V;
     const T* const draft = a.draft ? a.draft + (long)(r.first + node) * a.V : nullptr;
-    const RowStat P = AHEAD ? rows[node].p : stat(target, rate, 0);
+    auto next_child = [&](int after) {
+      for (int i0 = (after + 1) & ~63; i0 < n; i0 += 64) {
+        const int i = i0 + lane;
+        const unsigned long long m = __builtin_amdgcn_ballot_w64(i < n && i > after && rows.parent[i] == node);
+        if (m) return i0 + __builtin_ctzll(m);
+      }
+      return n;
+    };
+    int child = next_child(node);
+    const bool formed = AHEAD == ALL_ROWS || (AHEAD == PARENTS && child < n);
+    RowStat P;
+    if (AHEAD != ALL_ROWS && !formed) P = stat(target, rate, 0);
+    else P = rows.p[node];
     if (P.inv == 0.0) break;   // no next token
     RowStat Q{-INFINITY, -1, 0.0};
-    if (AHEAD && draft) Q = rows[node].q;
-    bool have_q = AHEAD;
-    int child = node, taken = -1, tried = 0;
+    if (AHEAD && draft) Q = rows.q[node];
+    bool have_q = AHEAD != NO_ROWS;
+    int taken = -1, tried = 0;
     // One over what the refused tokens have left: of the target (no draft scores), of the draft; of `rest`
     double left = 1.0, left_inv = 1.0, q_scale = 1.0, r_inv = 1.0;
     bool dead = false;   // the target has nothing left
-    while (!dead) {
-      int found = n;     // the next child
-      for (int i0 = (child + 1) & ~63; i0 < n && found == n; i0 += 64) {
-        const int i = i0 + lane;
-        const unsigned long long m = __builtin_amdgcn_ballot_w64(i < n && i > child && rows[i].parent == node);
-        if (m) found = i0 + __builtin_ctzll(m);
-      }
-      child = found;
-      if (child >= n) break;
+    for (; !dead && child < n; child = next_child(child)) {
       if (draft && !have_q) {
         Q = stat(draft, draft_rate, 1);
         have_q = true;
       }
       if (draft && Q.inv == 0.0) break;   // what was drawn from no distribution is not taken
-      const int x = rows[child].token;
+      const int x = rows.token[child];
       if (x < 0 || x >= a.V) continue;
       const bool before = tried && is_refused(x);
-      const double px = AHEAD ? rows[child].target : weight(rate, P.top, P.at, to_f32(target[x]), x) * P.inv;
+      const double px = AHEAD ? rows.target[child] : weight(rate, P.top, P.at, to_f32(target[x]), x) * P.inv;
       double q = 1.0, rx;
       if (draft) {
-        const double qx = AHEAD ? rows[child].draft : weight(draft_rate, Q.top, Q.at, to_f32(draft[x]), x) * Q.inv;
+        const double qx = AHEAD ? rows.draft[child] : weight(draft_rate, Q.top, Q.at, to_f32(draft[x]), x) * Q.inv;
         q = before && a.distinct ? 0.0 : qx * q_scale;
         if (!(q > 0.0)) continue;
         rx = tried ? rest[x] * r_inv : px;
       } else {
         rx = before ? 0.0 : px * left_inv;
       }
-      if ((double)rows[child].u * q < rx) {
+      if ((double)rows.u[child] * q < rx) {
         taken = child;
         break;
       }
@@ -425,24 +460,25 @@ __global__ void __launch_bounds__(DV_THREADS) __attribute__((amdgpu_waves_per_eu
       double all = 0.0;
       for (;;) {
         if (!from_rest) {
-          const int part = wave + DV_WAVES * (lane & 1);   // a lane each of the wave's two parts
+          constexpr int PER = DV_PARTS / DV_WAVES;
+          const int part = wave + DV_WAVES * (lane % PER);   // a lane each of the wave's parts
           double of_part = 0.0;
           if (part < cut.count) {
-            const PartStat p = AHEAD ? parts[(long)(r.first + node) * cut.count + part] : stats[0][part];
+            const PartStat p = formed ? parts[(long)(r.first + node) * cut.count + part] : stats[0][part];
             of_part = rate != 0.0 ? part_total(p, P.top, rate) : P.at >= part * cut.len && P.at < part_end(part) ? 1.0 : 0.0;
           }
           if (without)
-            for (int i = 0; i < 2 && wave + DV_WAVES * i < cut.count; ++i) {
+            for (int i = 0; i < PER && wave + DV_WAVES * i < cut.count; ++i) {
               const int lo = (wave + DV_WAVES * i) * cut.len, hi = part_end(wave + DV_WAVES * i);
               bool anew = false;
               for (int w = (lo >> 5) + lane; w < (hi + 31) >> 5; w += 64) anew |= refused[w] != 0;
               if (__any(anew)) {
                 const double e = weights(lo, hi);
-                if ((lane & 1) == i) of_part = e;
+                if (lane % PER == i) of_part = e;
               }
             }
           __syncthreads();
-          if (lane < 2 && part < cut.count) sums[part] = of_part;
+          if (lane < PER && part < cut.count) sums[part] = of_part;
           __syncthreads();
         }
         all = wave_total(lane < cut.count ? sums[lane] : 0.0);
@@ -473,17 +509,24 @@ __global__ void __launch_bounds__(DV_THREADS) __attribute__((amdgpu_waves_per_eu
         __syncthreads();
         choose(DV_WAVES, DV_CHUNK);
       }
-      // then a score a thread
-      const int y = min(lo + tid, lo + len - 1);
-      const double w = from_rest ? rest[y] : of_target(to_f32(target[y]), y, without ? is_refused(y) : 0), mine = tid < len ? w : 0.0, upto = wave_upto(mine);
+      // then two scores a thread
+      static_assert(2 * DV_THREADS >= DV_CHUNK, "");
+      double two[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int y = lo + 2 * tid + i, at = min(y, lo + len - 1);
+        const double w = from_rest ? rest[at] : of_target(to_f32(target[at]), at, without ? is_refused(at) : 0);
+        two[i] = y < lo + len ? w : 0.0;
+      }
+      const double both = two[0] + two[1], upto = wave_upto(both);
       __syncthreads();
       if (lane == 63) sums[wave] = upto;
       if (tid == 0) drawn = -1;
       __syncthreads();
-      const int of_wave = choose(DV_WAVES, 64);
+      const int of_wave = choose(DV_WAVES, 128);
       if (wave == of_wave) {
-        const int at = first_above(mine, before + upto);
-        if (lane == 0 && at >= 0) drawn = lo + at;
+        const int at = first_above(both, before + upto);
+        if (lane == at) drawn = lo + 2 * lane + (two[0] > 0.0 && (before + (upto - both) + two[0] > aim || !(two[1] > 0.0)) ? 0 : 1);
       }
       __syncthreads();
       next = drawn;
@@ -491,7 +534,8 @@ __global__ void __launch_bounds__(DV_THREADS) __attribute__((amdgpu_waves_per_eu
     }
     if (tried) {   // tokens refused here are children of this row
       __syncthreads();
-      if (tid < n && rows[tid].parent == node && rows[tid].token >= 0 && rows[tid].token < a.V) refused[rows[tid].token >> 5] = 0;
+      for (int i = tid; i < n; i += DV_THREADS)
+        if (rows.parent[i] == node && rows.token[i] >= 0 && rows.token[i] < a.V) refused[rows.token[i] >> 5] = 0;
       __syncthreads();
     }
     node = taken;
@@ -505,34 +549,43 @@ __global__ void __launch_bounds__(DV_THREADS) __attribute__((amdgpu_waves_per_eu
   }
 }
 
-constexpr int64_t DV_AHEAD_PARTS = 1 << 15;   // parts that are formed ahead of the walks
+// Parts that are formed ahead of the walks: all rows' up to DV_ALL_PARTS, then parents' up to DV_MOST_PARTS
+constexpr int64_t DV_ALL_PARTS = 1 << 12, DV_MOST_PARTS = 1 << 17;
 
 }  // namespace
 
 // [documents][V] of what the target has left, then the parts
 size_t draft_verify_workspace_bytes(int T_rows, int B, int V) {
-  return (size_t)B * V * sizeof(double) + 16 + (size_t)std::min<int64_t>(2 * (int64_t)T_rows * Cut(V).count, DV_AHEAD_PARTS) * sizeof(PartStat);
+  return (size_t)B * V * sizeof(double) + 16 + (size_t)std::min<int64_t>(2 * (int64_t)T_rows * Cut(V).count, DV_MOST_PARTS) * sizeof(PartStat);
 }
 template <typename T> dipaco_status launch_draft_verify(const VerifyArgs<T>& a, hipStream_t s) {
   const Cut cut(a.V);
-  const int64_t n = (int64_t)a.T_rows * cut.count * (a.draft ? 2 : 1);
-  const int lds = a.max_new * (int)sizeof(WalkRow) + (a.V + 31) / 32 * 4;
+  const int n_rows = a.T_rows * (a.draft ? 2 : 1), lds = a.max_new * WalkRows::ROW_BYTES + (a.V + 31) / 32 * 4;
+  const int64_t n = (int64_t)n_rows * cut.count;
   PartStat* const parts = reinterpret_cast<PartStat*>((reinterpret_cast<uintptr_t>(a.rest + (size_t)a.B * a.V) + 15) & ~(uintptr_t)15);
-  auto walk = [&](auto AHEADc, auto GREEDYc) -> dipaco_status {
-    constexpr bool AHEAD = decltype(AHEADc)::value, GREEDY = decltype(GREEDYc)::value;
-    static std::atomic<unsigned long long> lds_set{0};
-    if (dipaco_status st = ensure_dynamic_lds(reinterpret_cast<const void*>(draft_verify_walk<T, AHEAD, GREEDY>), 128 << 10, lds_set)) return st;
-    launch_parts(a.B, [&](long long first, unsigned count) { draft_verify_walk<T, AHEAD, GREEDY><<<count, DV_THREADS, lds, s>>>(a, parts, (int)first); });
-    DIPACO_LAUNCH_CHECK();
-    return DIPACO_OK;
+  auto walk = [&](auto AHEADc) -> dipaco_status {
+    auto run = [&](auto GREEDYc) -> dipaco_status {
+      constexpr Ahead AHEAD = decltype(AHEADc)::value;
+      constexpr bool GREEDY = decltype(GREEDYc)::value;
+      static std::atomic<unsigned long long> lds_set{0};
+      if (dipaco_status st = ensure_dynamic_lds(reinterpret_cast<const void*>(draft_verify_walk<T, AHEAD, GREEDY>), 128 << 10, lds_set)) return st;
+      launch_parts(a.B, [&](long long first, unsigned count) { draft_verify_walk<T, AHEAD, GREEDY><<<count, DV_THREADS, lds, s>>>(a, parts, (int)first); });
+      DIPACO_LAUNCH_CHECK();
+      return DIPACO_OK;
+    };
+    return a.rate == 0.0 ? run(std::true_type{}) : run(std::false_type{});
   };
-  using std::false_type;
-  using std::true_type;
-  const bool greedy = a.rate == 0.0;
-  if (n == 0 || n > DV_AHEAD_PARTS) return greedy ? walk(false_type{}, true_type{}) : walk(false_type{}, false_type{});
-  draft_verify_parts<T><<<(int)((n + 3) / 4), 256, 0, s>>>(a, parts, a.T_rows * (a.draft ? 2 : 1), Divisor(cut.count));
+  using std::integral_constant;
+  if (n == 0 || n > DV_MOST_PARTS) return walk(integral_constant<Ahead, NO_ROWS>{});
+  if (n <= DV_ALL_PARTS) {
+    draft_verify_parts<T><<<(int)((n + 3) / 4), 256, 0, s>>>(a, parts, n_rows, Divisor(cut.count));
+    DIPACO_LAUNCH_CHECK();
+    return walk(integral_constant<Ahead, ALL_ROWS>{});
+  }
+  const int groups = (cut.count + DV_PARENT_PARTS - 1) / DV_PARENT_PARTS;
+  draft_verify_parents<T><<<(n_rows * groups + 3) / 4, 256, 0, s>>>(a, parts, n_rows, Divisor(groups));
   DIPACO_LAUNCH_CHECK();
-  return greedy ? walk(true_type{}, true_type{}) : walk(true_type{}, false_type{});
+  return walk(integral_constant<Ahead, PARENTS>{});
 }
 template dipaco_status launch_draft_verify<float>(const VerifyArgs<float>&, hipStream_t);
 template dipaco_status launch_draft_verify<bf16>(const VerifyArgs<bf16>&, hipStream_t);
