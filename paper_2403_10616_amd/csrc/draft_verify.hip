@@ -199,10 +199,9 @@ template <typename T> __global__ void __launch_bounds__(256) draft_verify_parts(
   const int item = blockIdx.x * 4 + (threadIdx.x >> 6), row = count(item), part = item - row * (int)count.d;
   if (row < n_rows) form_part(a, Cut(a.V), parts, row, part, threadIdx.x & 63);
 }
-// Parts of rows that have children, DV_PARENT_PARTS of a row a wave: two thirds or so of a tree's rows are leaves, of which a walk ends at one at most
-constexpr int DV_PARENT_PARTS = 4;
-template <typename T> __global__ void __launch_bounds__(256) draft_verify_parents(VerifyArgs<T> a, PartStat* parts, int n_rows, Divisor groups) {
-  const int lane = threadIdx.x & 63, item = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)), row = groups(item);
+// Only parts of rows that have children: two thirds or so of a tree's rows are leaves, of which a walk ends at one at most
+template <typename T> __global__ void __launch_bounds__(256) draft_verify_parents(VerifyArgs<T> a, PartStat* parts, int n_rows, Divisor count) {
+  const int lane = threadIdx.x & 63, item = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)), row = count(item);
   if (row >= n_rows) return;
   const int at = row >= a.T_rows ? row - a.T_rows : row, b = __builtin_amdgcn_readfirstlane(find_document(a.row_start, a.B, at, lane));
   const RowRange r = ragged_rows(a.row_start, b, a.T_rows);
@@ -210,9 +209,7 @@ template <typename T> __global__ void __launch_bounds__(256) draft_verify_parent
   bool has_child = false;
   for (int c = i + 1 + lane; c < n; c += 64) has_child |= draft_parent(a.parent[r.first + c], c) == i;
   if (i < 0 || i >= n || !__any(has_child)) return;
-  const Cut cut(a.V);
-  const int first = (item - row * (int)groups.d) * DV_PARENT_PARTS;
-  for (int part = first; part < min(first + DV_PARENT_PARTS, cut.count); ++part) form_part(a, cut, parts, row, part, lane);
+  form_part(a, Cut(a.V), parts, row, item - row * (int)count.d, lane);
 }
 
 // LDS of a walk: arrays of `rows`, then the bits of refused tokens
@@ -365,15 +362,21 @@ __global__ void __launch_bounds__(DV_THREADS) __attribute__((amdgpu_waves_per_eu
         const double q_inv = Q.inv * q_scale, p_shift = -(double)P.top * rate, q_shift = -(double)Q.top * draft_rate;
         auto refuse = [&](auto FIRSTc, auto DISTINCTc) {
           constexpr bool FIRST = decltype(FIRSTc)::value, DISTINCT = decltype(DISTINCTc)::value;
+          Scores<T> xd, xt, then_d, then_t;   // a 1024 of scores, and the next, on their way meanwhile
+          if (wave < cut.count) {
+            xd.load(draft, wave * cut.len, part_end(wave), lane);
+            if (FIRST) xt.load(target, wave * cut.len, part_end(wave), lane);
+          }
           for (int part = wave; part < cut.count; part += DV_WAVES) {
             const int lo = part * cut.len, hi = part_end(part);
             double all = 0.0, q_all = 0.0;
             for (int base = lo; base < hi; base += DV_CHUNK) {
-              Scores<T> xd, xt;
+              const bool same = base + DV_CHUNK < hi;
+              const int then_part = same ? part : min(part + DV_WAVES, cut.count - 1), then_base = same ? base + DV_CHUNK : then_part * cut.len;
+              then_d.load(draft, then_base, part_end(then_part), lane);
+              if (FIRST) then_t.load(target, then_base, part_end(then_part), lane);
               double before[16];
-              xd.load(draft, base, hi, lane);
-              if (FIRST) xt.load(target, base, hi, lane);
-              else
+              if (!FIRST)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) before[i] = rest[min(Scores<T>::place(base, i, lane), hi - 1)];
 #pragma unroll
@@ -407,6 +410,8 @@ __global__ void __launch_bounds__(DV_THREADS) __attribute__((amdgpu_waves_per_eu
                     }
                 }
               }
+              xd = then_d;
+              if (FIRST) xt = then_t;
             }
             all = wave_total(all);
             if (DISTINCT) q_all = wave_total(q_all);
@@ -550,7 +555,7 @@ __global__ void __launch_bounds__(DV_THREADS) __attribute__((amdgpu_waves_per_eu
 }
 
 // Parts that are formed ahead of the walks: all rows' up to DV_ALL_PARTS, then parents' up to DV_MOST_PARTS
-constexpr int64_t DV_ALL_PARTS = 1 << 12, DV_MOST_PARTS = 1 << 17;
+constexpr int64_t DV_ALL_PARTS = 1 << 12, DV_MOST_PARTS = 1 << 14;
 
 }  // namespace
 
@@ -582,8 +587,7 @@ template <typename T> dipaco_status launch_draft_verify(const VerifyArgs<T>& a, 
     DIPACO_LAUNCH_CHECK();
     return walk(integral_constant<Ahead, ALL_ROWS>{});
   }
-  const int groups = (cut.count + DV_PARENT_PARTS - 1) / DV_PARENT_PARTS;
-  draft_verify_parents<T><<<(n_rows * groups + 3) / 4, 256, 0, s>>>(a, parts, n_rows, Divisor(groups));
+  draft_verify_parents<T><<<(int)((n + 3) / 4), 256, 0, s>>>(a, parts, n_rows, Divisor(cut.count));
   DIPACO_LAUNCH_CHECK();
   return walk(integral_constant<Ahead, PARENTS>{});
 }
