@@ -3,8 +3,8 @@
  *
  * Most expose single kernels of the path step (Algorithm 1 inner loop of arXiv 2403.10616: the pieces of
  * f(x, theta_i) and its gradient) so that each can be checked against its plain definition and timed against
- * its own roofline.  Attention with a window and over a paged cache stands beside them for programs that score or continue
- * text piece by piece; no step calls it.  They follow the conventions of dipaco.h: caller-owned device pointers, 16-byte aligned,
+ * its own roofline.  Attention with a window and over a paged cache, and a step of drafted decoding over that cache, stand beside them
+ * for programs that score or continue text piece by piece; no step calls them.  They follow the conventions of dipaco.h: caller-owned device pointers, 16-byte aligned,
  * work enqueued on `stream`, non-zero status = nothing enqueued.  dtype is a dipaco_dtype: the element type of
  * every `void*` operand (fp32 or bf16); accumulation is always fp32.
  */
@@ -196,7 +196,7 @@ dipaco_status dipaco_k_draft_verify(int32_t dtype, const void* target, const voi
                                     int32_t distinct, void* workspace, size_t workspace_bytes, void* stream);
 
 /* The rows that stay move to their places: in every cache slot cache_len[b] + i takes the keys and values of slot cache_len[b] + path[b, i],
- * i < kept[b].  caches: host array of n_layers device pointers, caches of the same pages.  path [B, max_new] and kept as
+ * i < kept[b].  caches: host array of n_layers device pointers, each another layer's cache, of the same pages.  path [B, max_new] and kept as
  * dipaco_k_draft_verify writes them; kept is taken as the nearest in 0 .. max_new, and a path ends at the first entry that does not rise or is
  * not in 0 .. max_new - 1.  A row whose slot, the old one or the new, has no page stays where it is.  */
 dipaco_status dipaco_k_cache_keep(int32_t dtype, const int32_t* path, const int32_t* kept, const int32_t* cache_len, const int32_t* pages,

@@ -3,6 +3,9 @@
 //
 // In place: path rises strictly, so a row's place lies in front of its source, and no place of an earlier row is the source of a later one.  A wave moves
 // the rows of one layer, document and head in order, four loads of them ahead of their stores; those it has read before it writes may be the places of others.
+//
+// Bound by latency (kept, the path, pages, rows) and, with more waves than the chip holds, by how often that is paid: 12 layers of one document, 14 heads of 64, 6 rows,
+// 3.5 us; 24 layers of 64 documents of up to 60 rows, 8 heads of 128, 57 MB read and written, 16 us (28 with one load at a time).
 #include <algorithm>
 
 #include "draft.h"

@@ -2,6 +2,8 @@
 //
 // A thread holds a row; its bits and the row that they reach up to lie in LDS.  A round joins to a row's bits those of the row that they reach, which
 // doubles their reach: ceil(log2(depth + 1)) rounds whatever the tree's shape, where following parents one by one takes a chain's length.
+// Bound by latency: the rows' bounds, the parents, then rounds of an LDS read, two barriers and a write.  One document of 16 rows 1.8 us, 256 of up to 500, chains
+// among them, 12 (13.8 with every word of every row and stores a row a lane).
 #include "draft.h"
 #include "kernels.h"
 

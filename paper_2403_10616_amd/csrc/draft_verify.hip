@@ -1,10 +1,15 @@
 // Which drafted tokens stay, and the token behind them (include/dipaco_kernels.h has the rule): a workgroup walks a document's tree from row 0.
 //
 // A token hangs on a border (u q < r, a running sum above v times the whole), so exponentials, sums and what is left of the target are 64-bit numbers: then
-// neither the order of a sum nor an exponential's last digits (2^-37 here) decide more than one draw in 10^10.
+// neither the order of a sum nor an exponential's last digits (2^-37 here) decide more than one draw in a million.
 //
 // A row of scores is cut into up to 32 parts of whole 1024 scores, a wave each: largest score, sum of exponentials against it.  From these the row's
 // sum is formed, and the part that a drawn token lies in is found without reading the others again; only parts that hold refused tokens are summed anew.
+//
+// Bound: a document's walk is a chain of decisions in one compute unit.  There a row of 32000 scores takes 10 us, of which its 64-bit exponentials, 17 instructions
+// each, are most, and a refusal by draft scores, which forms two of them for every token, 15.  So few rows' sums are formed by a launch of the whole chip ahead
+// of the walks, whose decisions then cost 1.3 us each, reads of LDS one behind the other.  Us, 32000 tokens: one chain of 6, bf16, 4 + 11; 64 chains of up to 8,
+// fp32, draft scores, 16 + 29; 32 trees of 64, bf16, 45; 24 trees of up to 40 with distinct siblings, 20011 tokens fp32, 67.
 #include <algorithm>
 #include <type_traits>
 
@@ -554,14 +559,17 @@ __global__ void __launch_bounds__(DV_THREADS) __attribute__((amdgpu_waves_per_eu
   }
 }
 
-// Parts that are formed ahead of the walks: all rows' up to DV_ALL_PARTS, then parents' up to DV_MOST_PARTS
-constexpr int64_t DV_ALL_PARTS = 1 << 12, DV_MOST_PARTS = 1 << 14;
+// Parts that are formed ahead of the walks: all rows' up to DV_ALL_PARTS; then parents' up to DV_MOST_PARTS, and up to DV_FEW_PARTS where documents have
+// DV_FEW_ROWS rows or fewer, of which a walk visits a large share.  Us, in the walk | parents ahead (both launches): 14656 parts (64 chains of up to 8) 150 | 45;
+// 19080 (24 trees of up to 40) 66 | 64; 65536 (32 trees of 64) 45 | 59.  A parent is found by loads of 2 us, which a call of few parts does without.
+constexpr int64_t DV_ALL_PARTS = 1 << 12, DV_MOST_PARTS = 1 << 14, DV_FEW_PARTS = 1 << 16;
+constexpr int DV_FEW_ROWS = 16;
 
 }  // namespace
 
 // [documents][V] of what the target has left, then the parts
 size_t draft_verify_workspace_bytes(int T_rows, int B, int V) {
-  return (size_t)B * V * sizeof(double) + 16 + (size_t)std::min<int64_t>(2 * (int64_t)T_rows * Cut(V).count, DV_MOST_PARTS) * sizeof(PartStat);
+  return (size_t)B * V * sizeof(double) + 16 + (size_t)std::min<int64_t>(2 * (int64_t)T_rows * Cut(V).count, DV_FEW_PARTS) * sizeof(PartStat);
 }
 template <typename T> dipaco_status launch_draft_verify(const VerifyArgs<T>& a, hipStream_t s) {
   const Cut cut(a.V);
@@ -581,7 +589,7 @@ template <typename T> dipaco_status launch_draft_verify(const VerifyArgs<T>& a, 
     return a.rate == 0.0 ? run(std::true_type{}) : run(std::false_type{});
   };
   using std::integral_constant;
-  if (n == 0 || n > DV_MOST_PARTS) return walk(integral_constant<Ahead, NO_ROWS>{});
+  if (n == 0 || n > (a.T_rows <= (int64_t)DV_FEW_ROWS * a.B ? DV_FEW_PARTS : DV_MOST_PARTS)) return walk(integral_constant<Ahead, NO_ROWS>{});
   if (n <= DV_ALL_PARTS) {
     draft_verify_parts<T><<<(int)((n + 3) / 4), 256, 0, s>>>(a, parts, n_rows, Divisor(cut.count));
     DIPACO_LAUNCH_CHECK();

@@ -10,6 +10,8 @@
 // Every eighth workgroup of a launch goes to the same eighth of the chip.  So workgroups that find nothing to do must not come at a fixed pace: wide
 // blocks that a call does not have are its last workgroups (128 tokens over 16000 positions: 25 us, 32 with every other workgroup idle), and the narrow
 // splits of a document, of which a short one leaves some idle, begin at another one of the eight each time.
+// Rows of a tree (TreeArgs) are cut the same way; any of them may see any slot of the document's new rows, so that all blocks of a document have the same tiles,
+// and in the tiles that hold such slots a row's bits are the mask (TreeView), two words a lane for 32 keys.
 // A split's sums go to the workspace, and paged_join adds them; a block whose keys are one split's writes its rows itself.
 #pragma once
 #include "visible.h"
