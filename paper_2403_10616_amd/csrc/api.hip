@@ -1165,7 +1165,7 @@ dipaco_status dipaco_k_cache_append(int32_t dtype, const void* qkv, const int32_
 size_t dipaco_k_attention_paged_workspace_bytes(int32_t T, int32_t B, int32_t max_new, int32_t H, int32_t H_kv, int32_t dh, int32_t page_size,
                                                 int32_t pages_per_doc) {
   if (check_heads(DIPACO_F32, H, H_kv, dh) != DIPACO_OK || check_cache(T, B, H, 1, page_size, pages_per_doc) != DIPACO_OK || max_new < 0) return 0;
-  return paged_workspace_bytes(T, H, dh, page_size, pages_per_doc);
+  return paged_workspace_bytes(T, H, dh, page_size, pages_per_doc, false);
 }
 
 dipaco_status dipaco_k_attention_paged(int32_t dtype, const void* qkv, const int32_t* row_start, const int32_t* cache_len, const int32_t* pages,
@@ -1180,7 +1180,7 @@ dipaco_status dipaco_k_attention_paged(int32_t dtype, const void* qkv, const int
   TRY(check_ptr(qkv, "qkv")); TRY(check_ptr(row_start, "row_start")); TRY(check_ptr(cache_len, "cache_len")); TRY(check_ptr(pages, "pages"));
   TRY(check_ptr(cache, "cache")); TRY(check_ptr(o, "o")); TRY(check_ptr(workspace, "workspace"));
   if (lse) TRY(check_ptr(lse, "lse"));
-  if (workspace_bytes < paged_workspace_bytes(T, H, dh, page_size, pages_per_doc))
+  if (workspace_bytes < paged_workspace_bytes(T, H, dh, page_size, pages_per_doc, false))
     return fail(DIPACO_EWORKSPACE, "workspace smaller than dipaco_k_attention_paged_workspace_bytes");
   hipStream_t st = static_cast<hipStream_t>(stream);
   const Window w{window, sinks};   // whole: positions may lie beyond the table
@@ -1204,7 +1204,7 @@ size_t dipaco_k_attention_tree_workspace_bytes(int32_t T, int32_t B, int32_t max
                                                int32_t pages_per_doc) {
   if (check_heads(DIPACO_F32, H, H_kv, dh) != DIPACO_OK || check_cache(T, B, H, 1, page_size, pages_per_doc) != DIPACO_OK || check_drafts(T, B, max_new) != DIPACO_OK)
     return 0;
-  return paged_workspace_bytes(T, H, dh, page_size, pages_per_doc);
+  return paged_workspace_bytes(T, H, dh, page_size, pages_per_doc, true);
 }
 
 dipaco_status dipaco_k_attention_tree(int32_t dtype, const void* qkv, const int32_t* row_start, const int32_t* cache_len, const int32_t* depth,
@@ -1220,7 +1220,7 @@ dipaco_status dipaco_k_attention_tree(int32_t dtype, const void* qkv, const int3
   TRY(check_ptr(qkv, "qkv")); TRY(check_ptr(row_start, "row_start")); TRY(check_ptr(cache_len, "cache_len")); TRY(check_ptr(depth, "depth"));
   TRY(check_ptr(seen, "seen")); TRY(check_ptr(pages, "pages")); TRY(check_ptr(cache, "cache")); TRY(check_ptr(o, "o")); TRY(check_ptr(workspace, "workspace"));
   if (lse) TRY(check_ptr(lse, "lse"));
-  if (workspace_bytes < paged_workspace_bytes(T, H, dh, page_size, pages_per_doc))
+  if (workspace_bytes < paged_workspace_bytes(T, H, dh, page_size, pages_per_doc, true))
     return fail(DIPACO_EWORKSPACE, "workspace smaller than dipaco_k_attention_tree_workspace_bytes");
   hipStream_t st = static_cast<hipStream_t>(stream);
   const Window w{window, sinks};

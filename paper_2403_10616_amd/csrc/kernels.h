@@ -326,7 +326,7 @@ dipaco_status launch_window_bwd_f32(const float* qkv, const int* lengths, const 
 
 // ---- paged.hip ---------------------------------------------------------------------------------------
 template <typename T> dipaco_status launch_cache_append(const PagedArgs<T>& a, int dh, hipStream_t s);
-size_t paged_workspace_bytes(int T_rows, int H, int dh, int page_size, int pages_per_doc);
+size_t paged_workspace_bytes(int T_rows, int H, int dh, int page_size, int pages_per_doc, bool tree);
 template <typename T> dipaco_status launch_attention_paged(PagedArgs<T> a, int dh, void* workspace, hipStream_t s);
 template <typename T> dipaco_status launch_attention_tree(const PagedArgs<T>& a, const int* depth, const uint64_t* seen, int dh, void* workspace, hipStream_t s);
 // paged_mfma.hip (bf16), paged_f32.hip.  Args: PagedArgs or TreeArgs

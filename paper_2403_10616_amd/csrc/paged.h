@@ -144,11 +144,83 @@ template <typename T> struct TreeArgs : PagedArgs<T> {
   const int* depth;          // [T rows]
   const uint32_t* seen;      // [T rows, words]
   int words;
+  int* plan;                 // null, or tiles a split, which the launch's first workgroup leaves for the join
+  int most_items;            // with a plan: items of a key head that the launch has workgroups for
   __device__ __forceinline__ TreeView view(int row0, int rows, int pos0, int last, int token) const {
     token = min(token, rows - 1);
     const long row = row0 + token;
     const int pos = pos0 + min(max(depth[row], 0), token);
     return {seen + row * words, words, pos0, last, min(this->w.near_from(pos), pos0), this->w.sinks, false};
+  }
+};
+
+template <typename T> __host__ __device__ __forceinline__ bool has_plan(const PagedArgs<T>&) { return false; }
+template <typename T> __host__ __device__ __forceinline__ bool has_plan(const TreeArgs<T>& a) { return a.plan != nullptr; }
+template <typename T> __device__ __forceinline__ int* plan_of(const PagedArgs<T>&) { return nullptr; }
+template <typename T> __device__ __forceinline__ int* plan_of(const TreeArgs<T>& a) { return a.plan; }
+
+// The item-th part of the wide blocks of trees (a block's tiles, cut into splits), for a key head.  Documents' lengths are known on the device alone, and a split of
+// equal share of its document would take as long as the longest one: so here a split is so many tiles, the same for all documents, of which the workgroups at hand
+// (`slots` are resident at once, one to TREE_ROUNDS rounds of them) end soonest; a workgroup's start and end take as long as TREE_START tiles.  Every wave reads the
+// documents (64 at most), a lane each, and comes to the same end.
+constexpr int TREE_DOCUMENTS = 64, TREE_ROUNDS = 3, TREE_START = 4;
+__device__ __forceinline__ int lanes_upto(int v) {   // lane i: the sum of lanes 0 .. i
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);   // row_shr 1, 2, 4, 8
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);   // row_bcast15 into rows 1 and 3
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);   // row_bcast31 into rows 2 and 3
+  return v;
+}
+struct TreeItem {
+  int b, block, split, per, cached;   // b: -1 where there are fewer items
+  RowRange rows;
+  template <typename T> __device__ __forceinline__ TreeItem(const TreeArgs<T>& a, int item, int slots, int lane) : b(-1), block(0), split(0), per(0), cached(0), rows{0, 0} {
+    using Cut = PagedCut<T>;
+    int blocks = 0, tiles = 0, mine = 0;
+    RowRange r{0, 0};
+    if (lane < a.B) {
+      r = ragged_rows(a.row_start, lane, a.T_rows);
+      mine = a.cached(lane);
+      const int n = min(r.count, a.max_new), packed = n * (int)a.group.d, last = min(mine + n, a.capacity()) - 1;
+      if (packed > Cut::NARROW_ROWS) {
+        blocks = (packed + Cut::WIDE_ROWS - 1) / Cut::WIDE_ROWS;
+        tiles = last < 0 ? 1 : max(TileList<Cut::WIDE_SHIFT>(a.w, mine, last).count, 1);
+      }
+    }
+    const int n_blocks = __builtin_amdgcn_readlane(lanes_upto(blocks), 63), longest = (int)wave_max((float)tiles) + 1;
+    const float work = wave_sum((float)blocks * (float)tiles);
+    const int least = max((longest + (int)a.wide_splits.d - 1) / (int)a.wide_splits.d, Cut::LEAST_KEYS >> Cut::WIDE_SHIFT);
+    // splits of p tiles: at most work / p, and one a block for what is left over
+    per = longest;
+    float best = INFINITY;
+#pragma unroll
+    for (int k = 1; k <= TREE_ROUNDS; ++k) {
+      const int room = k * slots / a.H_kv - n_blocks;
+      const int p = max((int)(work * __builtin_amdgcn_rcpf((float)max(room, 1)) * 1.00001f) + 1, least);
+      const float rounds = ceilf((work * __builtin_amdgcn_rcpf((float)p) + (float)n_blocks) * (float)a.H_kv / (float)slots), end = rounds * (float)(p + TREE_START);
+      if (room >= 1 && end < best) {
+        best = end;
+        per = p;
+      }
+    }
+    auto splits_of = [&](int p) {   // or one more, which finds nothing to do
+      return (int)((float)(tiles + p - 1) * __builtin_amdgcn_rcpf((float)p) * 1.00001f);
+    };
+    int upto = lanes_upto(blocks * splits_of(per));
+    if (__builtin_amdgcn_readlane(upto, 63) > a.most_items) {   // rounding may leave more than the launch holds
+      per = longest;
+      upto = lanes_upto(blocks);
+    }
+    if (item >= __builtin_amdgcn_readlane(upto, 63)) return;
+    const int at = __builtin_popcountll(__builtin_amdgcn_ballot_w64(upto <= item));
+    b = at;
+    const int i = item - (at ? __builtin_amdgcn_readlane(upto, at - 1) : 0), n = __builtin_amdgcn_readlane(blocks, at);
+    split = i / n;
+    block = i - split * n;
+    cached = __builtin_amdgcn_readlane(mine, at);
+    rows = {__builtin_amdgcn_readlane(r.first, at), __builtin_amdgcn_readlane(r.count, at)};
   }
 };
 

@@ -74,7 +74,7 @@ __global__ void __launch_bounds__(256) paged_join(Args<T> a, Divisor waves) {   
   } else {
     const PagedBlock<Cut::WIDE_SHIFT> blk(a, b, ((row - r.first) * G + head - a.group(head) * G) / Cut::WIDE_ROWS, Cut::WIDE_ROWS, a.wide_splits, Cut::LEAST_KEYS);
     tiles = blk.tiles.count;
-    per = blk.per;
+    per = has_plan(a) ? *plan_of(a) : blk.per;
   }
   if (head_of >= a.H || tiles <= per) tiles = 0;   // a block of one split has been written by its workgroup
   if (!__any(tiles > 0)) return;
@@ -151,12 +151,13 @@ __global__ void __launch_bounds__(256) paged_join(Args<T> a, Divisor waves) {   
 }
 
 // How often a call's keys are cut: enough workgroups for the chip, none with less than LEAST_KEYS keys however long the documents are
-struct PagedPlan { int narrow_splits, narrow_keys, wide_blocks, wide_splits; };
+struct PagedPlan { int narrow_splits, narrow_keys, wide_blocks, wide_splits; bool balanced; };   // balanced: wide splits are TreeItem's, wide_splits of a block at most
 inline int most_splits(int64_t keys, int least) { return (int)std::min<int64_t>(PAGED_MOST_SPLITS, (keys + least - 1) / least); }
 // Rows of partial sums that a workspace holds: `most` splits of every row, or as many as the workgroups that splits are made for have rows
 constexpr size_t PAGED_GROUP_ROWS = std::max(PAGED_WIDE_GROUPS * PagedCut<bf16>::WIDE_ROWS, PAGED_NARROW_GROUPS * PagedCut<bf16>::NARROW_ROWS);
-inline size_t partial_rows(int T_rows, int H, int64_t capacity) {
-  return std::min((size_t)most_splits(capacity, PagedCut<float>::LEAST_KEYS) * T_rows, (size_t)T_rows + (PAGED_GROUP_ROWS + H - 1) / H);
+// (of trees: twice that, for documents far longer than the others, whose splits are no longer than theirs)
+inline size_t partial_rows(int T_rows, int H, int64_t capacity, bool tree) {
+  return std::min((size_t)most_splits(capacity, PagedCut<float>::LEAST_KEYS) * T_rows, (size_t)T_rows + ((tree ? 2 : 1) * PAGED_GROUP_ROWS + H - 1) / H);
 }
 template <typename T> PagedPlan plan(const PagedArgs<T>& a, int dh, bool tree) {
   constexpr int NARROW_ROWS = PagedCut<T>::NARROW_ROWS, WIDE_ROWS = PagedCut<T>::WIDE_ROWS;
@@ -183,9 +184,13 @@ template <typename T> PagedPlan plan(const PagedArgs<T>& a, int dh, bool tree) {
   const int64_t wide = std::max<int64_t>(1, p.wide_blocks) * a.H_kv;
   p.wide_splits = (int)std::min<int64_t>(most, (PAGED_WIDE_GROUPS + wide - 1) / wide);
   // a call of narrow documents beside long chunks: the splits of the one have room for all rows of the other
-  const int room = (int)std::min<size_t>(PAGED_MOST_SPLITS, partial_rows(a.T_rows, a.H, (int64_t)page_size * a.pages_per_doc) / a.T_rows);
+  const int room = (int)std::min<size_t>(PAGED_MOST_SPLITS, partial_rows(a.T_rows, a.H, (int64_t)page_size * a.pages_per_doc, tree) / a.T_rows);
   p.narrow_splits = std::min(p.narrow_splits, room);
-  p.wide_splits = std::min(p.wide_splits, room);
+  // Documents of up to 4096 keys and more may differ by as much as a launch takes.  Us, splits of equal shares of their documents | of equal length: 32 documents of up to 64
+  // rows over up to 16000, 16 heads of 128 on 4, 201 | 173; 16 x 32 over 8000 each 79 | 83; 8 x 64 over 4000 each, 14 heads of 64, 37 | 34; 2 x 400 over 2048 of
+  // 12000 34 | 38, one of 64 over 16000 23 | 24.5: a plan costs each workgroup's start and the join a microsecond.
+  p.balanced = tree && std::is_same<T, bf16>::value && a.B > 1 && a.B <= TREE_DOCUMENTS && seen >= 4096 && p.wide_blocks > 0;
+  p.wide_splits = p.balanced ? room : std::min(p.wide_splits, room);
   return p;
 }
 
@@ -197,8 +202,8 @@ template <typename T> dipaco_status launch_cache_append(const PagedArgs<T>& a, i
   return DIPACO_OK;
 }
 // Non-decreasing in every size but the heads'
-size_t paged_workspace_bytes(int T_rows, int H, int dh, int page_size, int pages_per_doc) {
-  return 256 + partial_rows(T_rows, H, (int64_t)page_size * pages_per_doc) * H * (dh + 2) * sizeof(float);
+size_t paged_workspace_bytes(int T_rows, int H, int dh, int page_size, int pages_per_doc, bool tree) {
+  return 256 + partial_rows(T_rows, H, (int64_t)page_size * pages_per_doc, tree) * H * (dh + 2) * sizeof(float);
 }
 template <typename T, template <typename> class Args> static dipaco_status launch_paged(Args<T> a, int dh, void* workspace, hipStream_t s) {
   const PagedPlan p = plan<T>(a, dh, Args<T>::TREE);
@@ -206,9 +211,15 @@ template <typename T, template <typename> class Args> static dipaco_status launc
   a.narrow_keys = p.narrow_keys;
   a.narrow_turn = 3 - std::min(3, __builtin_ctz(p.narrow_splits));   // n splits begin at 8 / gcd(8, n) places by themselves
   a.wide_splits = Divisor(p.wide_splits);
-  a.state = static_cast<float2*>(workspace);
+  if constexpr (Args<T>::TREE) {
+    a.plan = p.balanced ? static_cast<int*>(workspace) : nullptr;
+    // keys of a document: the table's, or a window's and the sinks' with a tile more at each end; a split more than these make by rounding
+    const int64_t keys = std::min<int64_t>((int64_t)a.pages_per_doc << a.page_shift, (int64_t)a.w.window + a.w.sinks + a.max_new + 3 * 64);
+    a.most_items = (int)std::min<int64_t>(1 << 20, p.wide_blocks * (keys / PagedCut<T>::LEAST_KEYS + 2));
+  }
+  a.state = reinterpret_cast<float2*>(static_cast<char*>(workspace) + 64);
   const size_t states = (size_t)std::max(p.narrow_splits, p.wide_splits) * a.T_rows * a.H;
-  a.part = static_cast<float*>(workspace) + (2 * states + 3) / 4 * 4;
+  a.part = reinterpret_cast<float*>(a.state) + (2 * states + 3) / 4 * 4;
   auto run = [&](auto DHc) -> dipaco_status {
     constexpr int DH = decltype(DHc)::value;
     if (dipaco_status st = p.wide_blocks ? launch_paged_both<DH>(a, p.wide_blocks, s) : launch_paged_narrow<DH>(a, s)) return st;

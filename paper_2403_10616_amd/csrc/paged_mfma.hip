@@ -87,13 +87,37 @@ __device__ __forceinline__ void note_seen(SoftmaxRow<DH>& x, const PagedArgs<bf1
 
 // ---- wide ----------------------------------------------------------------------------------------------------------
 // pw_smem: [stage][K | V]
+template <int DH> constexpr int wide_slots() { return 256 * (DH == 32 ? 4 : DH == 64 ? 3 : 2); }   // workgroups that are resident at once: registers
+// block: the wide block; a tree's launch with a plan (TreeItem): the item, whatever `split` is
 template <int DH, typename A> __device__ __forceinline__ void wide_block(const A& a, int hk, int split, int block, char* pw_smem) {
   constexpr int KS = DH / 16, NP = panels<DH>(), TILE_BYTES = tile_bytes<DH>();
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, h = lane >> 5;
-  const WideBlock at_block(a, block, lane);
-  const int b = at_block.b;
+  int b, cached, per = 0;
+  RowRange of_document;
+  bool found = false;
+  if constexpr (A::TREE) {
+    if (has_plan(a)) {
+      const TreeItem item(a, block, wide_slots<DH>(), lane);
+      b = item.b;
+      cached = item.cached;
+      of_document = item.rows;
+      split = item.split;
+      per = item.per;
+      if (block == 0 && hk == 0 && threadIdx.x == 0) *plan_of(a) = per;
+      block = item.block;
+      found = true;
+    }
+  }
+  if (!found) {
+    const WideBlock at_block(a, block, lane);
+    b = at_block.b;
+    cached = at_block.cached;
+    of_document = at_block.rows;
+    block = at_block.block;
+  }
   if (b < 0) return;
-  const PagedBlock<Cut::WIDE_SHIFT> blk(a, b, at_block.rows, at_block.cached, at_block.block, Cut::WIDE_ROWS, a.wide_splits, Cut::LEAST_KEYS);
+  PagedBlock<Cut::WIDE_SHIFT> blk(a, b, of_document, cached, block, Cut::WIDE_ROWS, a.wide_splits, Cut::LEAST_KEYS);
+  if (A::TREE && per) blk.per = per;
   const int t0 = split * blk.per, n_tiles = min(blk.tiles.count - t0, blk.per);
   if (!blk.has(split)) return;
   const int r0 = blk.packed0 + 32 * wave;
@@ -349,6 +373,11 @@ template <int DH, template <typename> class Args> __global__ void __launch_bound
   extern __shared__ __attribute__((aligned(16))) char pb_smem[];
   int i = blockIdx.x;
   if (i < order.n_wide) {
+    if (Args<bf16>::TREE && has_plan(a)) {
+      const int item = order.heads(i);
+      wide_block<DH>(a, i - item * a.H_kv, 0, item, pb_smem);
+      return;
+    }
     const int block = order.head_splits(i), j = i - block * (int)order.head_splits.d, split = order.heads(j);
     wide_block<DH>(a, j - split * a.H_kv, split, block, pb_smem);
     return;
@@ -381,8 +410,17 @@ template <int DH, template <typename> class Args> dipaco_status launch_paged_bot
   static std::atomic<unsigned long long> lds_set{0};
   if (dipaco_status st = ensure_dynamic_lds(reinterpret_cast<const void*>(paged_both_mfma<DH, Args>), LDS, lds_set)) return st;
   const int wide = a.H_kv * (int)a.wide_splits.d;
-  const PagedOrder order{Divisor(a.H_kv), Divisor(wide), blocks * wide};
-  paged_both_mfma<DH, Args><<<order.n_wide + a.B * a.H_kv * (int)a.narrow_splits.d, AT_THREADS, LDS, s>>>(a, order);
+  auto launch = [&](const Args<bf16>& args, int n_wide) {
+    const PagedOrder order{Divisor(a.H_kv), Divisor(wide), n_wide};
+    paged_both_mfma<DH, Args><<<n_wide + a.B * a.H_kv * (int)a.narrow_splits.d, AT_THREADS, LDS, s>>>(args, order);
+  };
+  if constexpr (Args<bf16>::TREE) {
+    Args<bf16> t = a;   // rounds of what is resident, and room for a split a block
+    t.most_items = std::max(std::min(TREE_ROUNDS * wide_slots<DH>() / a.H_kv, a.most_items), blocks);
+    launch(t, has_plan(a) ? t.most_items * a.H_kv : blocks * wide);
+  } else {
+    launch(a, blocks * wide);
+  }
   DIPACO_LAUNCH_CHECK();
   return DIPACO_OK;
 }

@@ -96,6 +96,53 @@ def test_long_caches_and_large_trees(dtype, cached, counts, shape, H, Hkv, dh, p
     check(dtype, cached, counts, shape, H, Hkv, dh, page, window, sinks, seed=6)
 
 
+def lengths(seed, n, most):
+    """documents of lengths apart: most of them short, a few of `most`, some empty"""
+    rng = random.Random(seed)
+    return [rng.choice([0, rng.randint(0, 200), rng.randint(0, most), most]) for _ in range(n)]
+
+
+@TYPES
+@pytest.mark.parametrize("cached,counts,H,Hkv,dh,page,window,sinks", [
+    ([5000, 10], [40, 70], 2, 1, 32, 16, ALL, 0), ([0, 9000, 30, 4500], [64, 33, 0, 200], 4, 2, 64, 64, ALL, 0), ([20000, 5], [64, 64], 4, 4, 32, 32, ALL, 0),
+    ([6000, 5900, 6100], [150, 1, 90], 2, 2, 128, 64, 5000, 70), (lengths(1, 64, 4200), [36] * 64, 2, 1, 32, 64, ALL, 0),
+    (lengths(2, 65, 4200), [36] * 65, 2, 1, 32, 64, ALL, 0), (lengths(3, 30, 4300), [k % 45 for k in range(30)], 16, 16, 32, 16, ALL, 3),
+    ([4200, 4200], [1024, 1000], 1, 1, 64, 32, ALL, 0), ([4500] * 5, [9, 10, 33, 34, 8], 8, 2, 128, 32, ALL, 0)])
+def test_long_documents_of_lengths_apart(dtype, cached, counts, H, Hkv, dh, page, window, sinks):
+    """splits of equal length for all documents: one document far longer than the others, as many documents as a wave has lanes and one more,
+    documents without rows, with few rows and with several blocks of them"""
+    check(dtype, cached, counts, "level", H, Hkv, dh, page, window, sinks, seed=12)
+
+
+def test_long_documents_that_have_outgrown_their_table_or_lost_pages():
+    dtype, H, Hkv, dh, page = dp.BF16, 4, 2, 64, 64
+    cached, counts = [4400, 4400, 100, 4000], [60, 50, 70, 64]
+    c, x, st = filled(dtype, cached, counts, H, Hkv, dh, page, 5)
+    for b, gone in enumerate([range(10, 50), range(0, c.per_doc), [0], [60, 62]]):
+        for at in gone:
+            if c.table[b][at] >= 0:
+                c.data[c.table[b][at]] = float("nan")
+            c.table[b][at] = -1
+    c.pages = i32(c.table)
+    depth, seen = tree([ref.random_parents(random.Random(b), k, "deep") for b, k in enumerate(counts)])
+    lens = [4400, 4400, 100, 1 << 29]                            # the last one's rows see none of its table, nor each other
+    parents = [ref.random_parents(random.Random(b), k, "deep") for b, k in enumerate(counts)]
+    o, lse = attend(c, x.to(DEV), st, lens, depth, seen, H, max(counts), 4200, 0)
+    for b, (m, k) in enumerate(zip(cached, counts)):
+        at = slice(st[b], st[b + 1])
+        if b == 3:
+            assert not o[at].any() and bool((lse[at] == -INF).all())
+            continue
+        rows = ref.seen_rows(parents[b])
+        held = torch.tensor([c.table[b][p // page] >= 0 for p in range(m + k)])
+        mask = mask_of(m, rows, [len(r) - 1 for r in rows], 4200, 0, m + k) & held
+        kv, q = c.kv[b].double(), heads_of(x[at], k, H, Hkv, dh)[0]
+        wo, wl = aref.definition(q, kv[:, 0], kv[:, 1], mask)
+        _, _, eo, el = aref.forward(q, kv[:, 0], kv[:, 1], mask, TDT[dtype])
+        aref.inside(o[at].reshape(k, H, dh), wo, eo, f"o[{b}]")
+        aref.inside(lse[at], wl, el.nan_to_num(), f"lse[{b}]")
+
+
 @TYPES
 def test_peaked_rows(dtype):
     check(dtype, [400, 30], [30, 3], "level", 4, 2, 64, 16, ALL, 0, seed=8, scale=8.0)
@@ -241,7 +288,7 @@ def test_rows_of_nobody_stay_as_they_were(dtype):
 
 
 @TYPES
-@pytest.mark.parametrize("cached,counts,H,Hkv,dh", [([6000, 2000, 50], [1, 300, 400], 8, 1, 64), ([4000], [7], 8, 8, 128), ([9000, 9000], [1, 2], 4, 1, 32), ([700], [200], 2, 2, 64)])
+@pytest.mark.parametrize("cached,counts,H,Hkv,dh", [([6000, 2000, 50], [1, 300, 400], 8, 1, 64), ([30000, 5, 700], [64, 40, 64], 2, 1, 32), ([4000], [7], 8, 8, 128), ([9000, 9000], [1, 2], 4, 1, 32), ([700], [200], 2, 2, 64)])
 def test_the_workspace_is_as_large_as_it_is_said_to_be(dtype, cached, counts, H, Hkv, dh):
     page = 32
     c = Cache(dtype, [a + b for a, b in zip(cached, counts)], Hkv, dh, page, 3)
