@@ -139,6 +139,18 @@ def test_a_vocabulary_of_many_parts(dtype, mode):
     check_verify(dtype, [9, 4], "deep", 50001, mode, 1.0, seed=4)
 
 
+@TYPES
+@MODES
+@pytest.mark.parametrize("counts,shape,V,temperature", [
+    ([8, 0, 5, 8] * 10, "chain", 20000, 1.0), ([16, 3, 0, 16] * 8, "level", 20011, 0.7), ([7, 16] * 16, "forest", 17001, 0.0), ([40, 0, 33] * 9, "level", 20011, 0.8),
+    ([64, 50] * 6, "deep", 30001, 0.0)])
+def test_sums_formed_ahead_and_in_the_walk(dtype, mode, counts, shape, V, temperature):
+    """more parts of rows than all are formed of ahead of the walks: of rows with children (documents of few rows), of none (of many); documents without
+    rows among them, walks that end at leaves"""
+    lengths = check_verify(dtype, counts, shape, V, mode, temperature, near=0.3, seed=11)
+    assert max(lengths) > 1
+
+
 @MODES
 def test_many_siblings(mode):
     """a row with more siblings than a wave has lanes, most of them refused; one with as many rows as a document may have"""

@@ -528,6 +528,36 @@ def test_a_step_captured_and_replayed_beside_eager_work(dtype):
                 assert torch.equal(a, b), (k, step, i)
 
 
+def test_long_documents_captured_and_replayed_beside_eager_work():
+    """lengths and trees change between replays, and with them how the call is cut"""
+    dtype, H, Hkv, dh, page, B, n = dp.BF16, 4, 2, 64, 64, 3, 40
+    c = Cache(dtype, [6000] * B, Hkv, dh, page, 2)
+    c.data.normal_()
+    T, words = B * n, 1
+    x = torch.zeros((T, (H + 2 * Hkv) * dh), dtype=TDT[dtype], device=DEV)
+    st, lens, depth, seen = i32([n * b for b in range(B + 1)]), i32([0] * B), i32([0] * T), torch.zeros((T, words), dtype=torch.int64, device=DEV)
+    o, lse = torch.zeros((T, H * dh), dtype=TDT[dtype], device=DEV), torch.zeros((T, H), device=DEV)
+    ws = torch.empty(dp.dipaco_k_attention_tree_workspace_bytes(T, B, n, H, Hkv, dh, page, c.per_doc), dtype=torch.uint8, device=DEV)
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=side):
+        dp.dipaco_k_attention_tree(dtype, x, st, lens, depth, seen, c.pages, c.data, o, lse, T, B, n, H, Hkv, dh, c.n_pages, page, c.per_doc, ALL, 0, ws)
+    for k in range(4):
+        rng = random.Random(k)
+        counts, at = [[40, 40, 40], [1, 40, 30], [0, 0, 5], [40, 9, 17]][k], [[5900, 10, 3000], [0, 5000, 5900], [0, 0, 4000], [200, 5900, 5800]][k]
+        starts = starts_of(counts)
+        d, m = tree([ref.random_parents(rng, a, "level") for a in counts], max_new=n, rows=T, starts=starts)
+        x.copy_(draw((T, (H + 2 * Hkv) * dh), 90 + k, dtype))
+        for to, frm in ((depth, d), (seen, m), (st, i32(starts)), (lens, i32(at))):
+            to.copy_(frm)
+        graph.replay()
+        torch.cuda.synchronize()
+        eo, el = attend(c, x, starts, at, d, m, H, n, ALL, 0, rows=T)
+        torch.cuda.synchronize()
+        rows = starts[-1]
+        assert torch.equal(eo[:rows], o[:rows]) and torch.equal(el[:rows], lse[:rows]) and bool(torch.isfinite(el[:rows]).all())
+
+
 def test_on_another_stream():
     s, t = Step(dp.BF16, 3, 9), Step(dp.BF16, 3, 9)
     fill(s, 5)
