@@ -6,7 +6,7 @@
 // A row of scores is cut into up to 32 parts of whole 1024 scores, a wave each: largest score, sum of exponentials against it.  From these the row's
 // sum is formed, and the part that a drawn token lies in is found without reading the others again; only parts that hold refused tokens are summed anew.
 //
-// Bound: a document's walk is a chain of decisions in one compute unit.  There a row of 32000 scores takes 10 us, of which its 64-bit exponentials, 17 instructions
+// Bound: a document's walk is a chain of decisions in one compute unit.  There a row of 32000 scores takes 10 us, of which its 64-bit exponentials, 18 instructions
 // each, are most, and a refusal by draft scores, which forms two of them for every token, 15.  So few rows' sums are formed by a launch of the whole chip ahead
 // of the walks, whose decisions then cost 1.3 us each, reads of LDS one behind the other.  Us, 32000 tokens: one chain of 6, bf16, 4 + 11; 64 chains of up to 8,
 // fp32, draft scores, 16 + 29; 32 trees of 64, bf16, 45; 24 trees of up to 40 with distinct siblings, 20011 tokens fp32, 67.
@@ -75,9 +75,13 @@ template <typename T> __device__ __forceinline__ void load_scores(const T* row, 
   }
 }
 
+// 2^((x - top) rate), 0 where x is -inf.  The difference first: it is 0 for x = top, and else off by 2^-53 of itself, however large both are (a mask's lowest value) and
+// however large the rate.  x rate - top rate in one fma saves an instruction, and leaves the rounding of top rate, which passes 2^10 where that passes 2^63.
+__device__ __forceinline__ double exponential(float x, double top, double rate) { return power_of_two(((double)x - top) * rate); }
+
 // rate: log2(e) / temperature; 0: all probability at the first maximum
 __device__ __forceinline__ double weight(double rate, float top, int at, float x, int y) {
-  return rate != 0.0 ? power_of_two(fma((double)x, rate, -(double)top * rate)) : y == at ? 1.0 : 0.0;
+  return rate != 0.0 ? exponential(x, top, rate) : y == at ? 1.0 : 0.0;
 }
 
 struct PartStat {
@@ -122,15 +126,15 @@ template <typename T> __device__ __forceinline__ PartStat part_stat(const T* row
       top = fmaxf(top, most);
     } else {
       if (most > top) {
-        sum *= power_of_two(fma((double)top, rate, -(double)most * rate));
+        sum *= exponential(top, most, rate);
         top = most;
       }
-      const double shift = -(double)top * rate;
+      const double from = top;
       double s0 = 0.0, s1 = 0.0;
 #pragma unroll
       for (int i = 0; i < 16; i += 2) {
-        s0 += power_of_two(fma((double)x.x[i], rate, shift));
-        s1 += power_of_two(fma((double)x.x[i + 1], rate, shift));
+        s0 += exponential(x.x[i], from, rate);
+        s1 += exponential(x.x[i + 1], from, rate);
       }
       sum += s0 + s1;
     }
@@ -148,7 +152,7 @@ template <typename T> __device__ __forceinline__ PartStat part_stat(const T* row
     p.at = at;
     p.total = 1.0;
   } else {
-    p.total = wave_total(sum * power_of_two(fma((double)top, rate, -(double)p.top * rate)));
+    p.total = wave_total(sum * exponential(top, p.top, rate));
   }
   if (__any(nan) || p.top == INFINITY) p.total = NAN;
   return p;
@@ -162,7 +166,7 @@ struct RowStat {
 };
 // of a part's sum against the row's largest score
 __device__ __forceinline__ double part_total(const PartStat& p, float top, double rate) {
-  return rate != 0.0 ? p.total * power_of_two(fma((double)p.top, rate, -(double)top * rate)) : p.total;
+  return rate != 0.0 ? p.total * exponential(p.top, top, rate) : p.total;
 }
 // Two rows by a wave, a part a lane: lanes 0 .. 31 hold `p` and `rate` of one, lanes 32 .. 63 of the other (no part: top -inf, total 0).  Every lane gets its half's.
 __device__ __forceinline__ RowStat join(const PartStat& p, double rate, int lane) {
@@ -364,7 +368,7 @@ __global__ void __launch_bounds__(DV_THREADS) __attribute__((amdgpu_waves_per_eu
         dead = !(left > 0.0);
       } else {
         // rest <- max(what is left of the target - the draft, 0), and the sums of both
-        const double q_inv = Q.inv * q_scale, p_shift = -(double)P.top * rate, q_shift = -(double)Q.top * draft_rate;
+        const double q_inv = Q.inv * q_scale, p_top = P.top, q_top = Q.top;
         auto refuse = [&](auto FIRSTc, auto DISTINCTc) {
           constexpr bool FIRST = decltype(FIRSTc)::value, DISTINCT = decltype(DISTINCTc)::value;
           Scores<T> xd, xt, then_d, then_t;   // a 1024 of scores, and the next, on their way meanwhile
@@ -391,10 +395,10 @@ __global__ void __launch_bounds__(DV_THREADS) __attribute__((amdgpu_waves_per_eu
                 double now[VEC];
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) {   // a score of -inf behind the part's end: 0
-                  double w = power_of_two(fma((double)xd.x[j + i], draft_rate, q_shift)), p;
+                  double w = exponential(xd.x[j + i], q_top, draft_rate), p;
                   if (!FIRST) p = before[j + i] * r_inv;
                   else if (GREEDY) p = y0 + i == P.at ? 1.0 : 0.0;
-                  else p = power_of_two(fma((double)xt.x[j + i], rate, p_shift)) * P.inv;
+                  else p = exponential(xt.x[j + i], p_top, rate) * P.inv;
                   if (DISTINCT) {   // of the tokens refused before this one the draft has nothing left, and the target neither
                     const bool is_gone = gone & (1u << i);
                     q_all += is_gone ? 0.0 : w;
@@ -440,8 +444,8 @@ __global__ void __launch_bounds__(DV_THREADS) __attribute__((amdgpu_waves_per_eu
       // The next token: from `rest`, whose parts' sums are in place, or from the target's row without the refused tokens, or from all of it
       const bool from_rest = draft && tried && !dead;
       bool without = !draft && tried && !dead;
-      const double shift = -(double)P.top * rate;
-      auto of_target = [&](float x, int y, uint32_t gone) { return gone & 1 ? 0.0 : GREEDY ? (y == P.at && x > -INFINITY ? 1.0 : 0.0) : power_of_two(fma((double)x, rate, shift)); };   // x = -inf: behind what is summed
+      const double top = P.top;
+      auto of_target = [&](float x, int y, uint32_t gone) { return gone & 1 ? 0.0 : GREEDY ? (y == P.at && x > -INFINITY ? 1.0 : 0.0) : exponential(x, top, rate); };   // x = -inf: behind what is summed
       // sum over lo .. hi - 1, by a wave; lo is a multiple of VEC
       auto weights = [&](int lo, int hi) {
         double e = 0.0;
