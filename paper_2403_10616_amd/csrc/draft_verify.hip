@@ -571,9 +571,10 @@ constexpr int DV_FEW_ROWS = 16;
 
 }  // namespace
 
-// [documents][V] of what the target has left, then the parts
+// [documents][V] of what the target has left, then the parts: as many as a row of V scores or fewer may have (their number falls where they get longer)
 size_t draft_verify_workspace_bytes(int T_rows, int B, int V) {
-  return (size_t)B * V * sizeof(double) + 16 + (size_t)std::min<int64_t>(2 * (int64_t)T_rows * Cut(V).count, DV_FEW_PARTS) * sizeof(PartStat);
+  const int most = std::min(DV_PARTS, (V + DV_CHUNK - 1) / DV_CHUNK);
+  return (size_t)B * V * sizeof(double) + 16 + (size_t)std::min<int64_t>(2 * (int64_t)T_rows * most, DV_FEW_PARTS) * sizeof(PartStat);
 }
 template <typename T> dipaco_status launch_draft_verify(const VerifyArgs<T>& a, hipStream_t s) {
   const Cut cut(a.V);

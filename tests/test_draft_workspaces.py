@@ -1,0 +1,22 @@
+"""Workspaces of drafted decoding never shrink with a size of the call: one made for the largest call serves the smaller ones."""
+import pytest
+
+import paper_2403_10616_amd as dp
+
+MOST_V = 1 << 18
+# both sides of every multiple of 1024 tokens, where the number of a row's parts or their length may change
+VOCABULARIES = sorted({v for k in range(0, MOST_V + 1, 1024) for v in (k - 1, k, k + 1) if 1 <= v <= MOST_V})
+
+
+@pytest.mark.parametrize("B", [1, 4, 64])
+@pytest.mark.parametrize("T", [1, 64, 1000, 1 << 20])
+def test_verification_with_the_vocabulary(T, B):
+    sizes = [dp.dipaco_k_draft_verify_workspace_bytes(T, B, v) for v in VOCABULARIES]
+    assert sizes[0] > 0 and sizes == sorted(sizes), [(v, a, b) for v, a, b in zip(VOCABULARIES, sizes, sizes[1:]) if a > b][:3]
+
+
+@pytest.mark.parametrize("V", [1, 1001, 32000, 32768, 32769, 36000, 65536, 65537, MOST_V])
+def test_verification_with_rows_and_documents(V):
+    rows = [dp.dipaco_k_draft_verify_workspace_bytes(t, 3, V) for t in range(0, 4000, 37)]
+    documents = [dp.dipaco_k_draft_verify_workspace_bytes(500, b, V) for b in range(1, 400, 7)]
+    assert rows == sorted(rows) and documents == sorted(documents)
