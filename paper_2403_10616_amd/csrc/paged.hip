@@ -201,9 +201,10 @@ template <typename T> dipaco_status launch_cache_append(const PagedArgs<T>& a, i
   DIPACO_LAUNCH_CHECK();
   return DIPACO_OK;
 }
-// Non-decreasing in every size but the heads'
+// Non-decreasing in every size.  In heads of rows: partial_rows' H times as many or, for its second term is rounded up to whole rows, up to H - 1 more
 size_t paged_workspace_bytes(int T_rows, int H, int dh, int page_size, int pages_per_doc, bool tree) {
-  return 256 + partial_rows(T_rows, H, (int64_t)page_size * pages_per_doc, tree) * H * (dh + 2) * sizeof(float);
+  const size_t heads = (size_t)T_rows * H, most = most_splits((int64_t)page_size * pages_per_doc, PagedCut<float>::LEAST_KEYS);
+  return 256 + std::min(most * heads, heads + (tree ? 2 : 1) * PAGED_GROUP_ROWS + H - 1) * (dh + 2) * sizeof(float);
 }
 template <typename T, template <typename> class Args> static dipaco_status launch_paged(Args<T> a, int dh, void* workspace, hipStream_t s) {
   const PagedPlan p = plan<T>(a, dh, Args<T>::TREE);

@@ -20,3 +20,18 @@ def test_verification_with_rows_and_documents(V):
     rows = [dp.dipaco_k_draft_verify_workspace_bytes(t, 3, V) for t in range(0, 4000, 37)]
     documents = [dp.dipaco_k_draft_verify_workspace_bytes(500, b, V) for b in range(1, 400, 7)]
     assert rows == sorted(rows) and documents == sorted(documents)
+
+
+HEADS = list(range(1, 130)) + [x for k in (8, 16) for x in range((1 << k) - 2, (1 << k) + 3)] + list(range(900, 1100))
+
+
+@pytest.mark.parametrize("name", ["tree", "paged"])
+@pytest.mark.parametrize("T", [1, 2, 5, 64, 300, 5000])
+@pytest.mark.parametrize("pages_per_doc", [1, 40, 3000])
+def test_attention_with_the_heads(name, T, pages_per_doc):
+    size = getattr(dp, f"dipaco_k_attention_{name}_workspace_bytes")
+    heads = [h for h in HEADS if T * h <= 1 << 25 and (h + 2) * 32 <= 1 << 20]
+    sizes = [size(T, 4, 8, h, 1, 32, 64, pages_per_doc) for h in heads]
+    got = [(h, s) for h, s in zip(heads, sizes) if s]
+    assert len(got) > 100
+    assert [s for _, s in got] == sorted(s for _, s in got), [(a, b) for a, b in zip(got, got[1:]) if a[1] > b[1]][:3]
