@@ -196,8 +196,8 @@ dipaco_status dipaco_k_draft_verify(int32_t dtype, const void* target, const voi
                                     int32_t distinct, void* workspace, size_t workspace_bytes, void* stream);
 
 /* The rows that stay move to their places: in every cache slot cache_len[b] + i takes the keys and values of slot cache_len[b] + path[b, i],
- * i < kept[b].  caches: host array of n_layers device pointers, each another layer's cache, of the same pages.  path [B, max_new] and kept as
- * dipaco_k_draft_verify writes them; kept is taken as the nearest in 0 .. max_new, and a path ends at the first entry that does not rise or is
+ * i < kept[b].  caches: host array of n_layers device pointers, each another layer's cache (the same one twice is
+ * refused), of the same pages.  path [B, max_new] and kept as dipaco_k_draft_verify writes them; kept is taken as the nearest in 0 .. max_new, and a path ends at the first entry that does not rise or is
  * not in 0 .. max_new - 1.  A row whose slot, the old one or the new, has no page stays where it is.  */
 dipaco_status dipaco_k_cache_keep(int32_t dtype, const int32_t* path, const int32_t* kept, const int32_t* cache_len, const int32_t* pages,
                                   void* const* caches, int32_t n_layers, int32_t B, int32_t max_new, int32_t H_kv, int32_t dh,

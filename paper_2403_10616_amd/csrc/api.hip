@@ -1274,7 +1274,11 @@ dipaco_status dipaco_k_cache_keep(int32_t dtype, const int32_t* path, const int3
   if (n_layers == 0 || max_new == 0) return DIPACO_OK;
   TRY(check_ptr(path, "path")); TRY(check_ptr(kept, "kept")); TRY(check_ptr(cache_len, "cache_len")); TRY(check_ptr(pages, "pages"));
   if (!caches) return fail(DIPACO_EINVAL, "caches is NULL");
-  for (int l = 0; l < n_layers; ++l) TRY(check_ptr(caches[l], "a cache"));
+  for (int l = 0; l < n_layers; ++l) {   // the rows of a cache that is given twice would move twice, and lose what they hold
+    TRY(check_ptr(caches[l], "a cache"));
+    for (int k = 0; k < l; ++k)
+      if (caches[k] == caches[l]) return fail(DIPACO_EINVAL, "each cache must be another layer's");
+  }
   int shift = 4;
   while ((1 << shift) < page_size) ++shift;
   const KeepArgs a{path, kept, cache_len, pages, B, max_new, H_kv, n_pages, shift, pages_per_doc, dh * (dtype == DIPACO_BF16 ? 2 : 4) / 16, {}};
