@@ -21,6 +21,7 @@ namespace dipaco {
 namespace {
 
 constexpr int DV_THREADS = 512, DV_WAVES = DV_THREADS / 64, DV_PARTS = 32, DV_CHUNK = 1024;
+constexpr double DV_LEAST_LEFT = 1.0 / 1024;   // of a row: what differences of probabilities, right to 2^-36 of the row, may leave, to 2^-26 of itself
 
 // 2^t for t <= 0, to 2^-37 of it: 2^f = sum of (f ln 2)^k / k! for |f| <= 1/2, up to k = 9 (the next term is below 2^-37)
 __device__ __forceinline__ double power_of_two(double t) {
@@ -364,6 +365,16 @@ __global__ void __launch_bounds__(DV_THREADS) __attribute__((amdgpu_waves_per_eu
       __syncthreads();
       if (!draft) {
         if (!before) left -= px;
+        // What is left after large shares is lost in their roundings: its own tokens' sum then.  A row comes to that once in 1/LEAST_LEFT times, and the sum's cost is no matter
+        if (!GREEDY && left < DV_LEAST_LEFT) {
+          const double top = P.top;
+          double e = 0.0;
+          for (int y = tid; y < a.V; y += DV_THREADS) e += is_refused(y) ? 0.0 : exponential(to_f32(target[y]), top, rate);
+          e = wave_total(e);
+          if (lane == 0) sums[wave] = e;
+          __syncthreads();
+          left = wave_total(lane < DV_WAVES ? sums[lane] : 0.0) * P.inv;
+        }
         left_inv = 1.0 / left;
         dead = !(left > 0.0);
       } else {

@@ -2,8 +2,9 @@
 import pytest
 import torch
 
+import draft_reference as ref
 import paper_2403_10616_amd as dp
-from test_gpu_drafts import MODES, TYPES, check_verify
+from test_gpu_drafts import MODES, TYPES, check_verify, verify
 from test_gpu_window import TDT
 
 pytestmark = pytest.mark.gpu
@@ -65,3 +66,47 @@ def test_temperatures_near_zero(dtype, mode, temperature, V, counts):
     for draft_temperature in (1.0, temperature):
         check_verify(dtype, counts, "level", V, mode, temperature, draft_temperature=draft_temperature, special=special, seed=23)
     check_verify(dtype, counts, "level", V, mode, 1.0, draft_temperature=temperature, special=special, seed=24)
+
+
+# documents of 65 rows in vocabularies of many parts, as AHEAD: all rows' sums ahead, those of rows with children, none
+PICKED = pytest.mark.parametrize("B,V", [(1, 60), (1, 32000), (4, 32000), (8, 32000)])
+
+
+def picked(dtype, B, V, scores, tokens, u, v):
+    """every document: a root with children of these tokens, each with u; its row's scores, the other rows' and tokens' far below"""
+    n = len(tokens) + 1
+    target = torch.full((B * n, V), -300.0)
+    target[:, :len(scores)] = torch.tensor(scores)
+    target = target.to(TDT[dtype])
+    given = [0] + tokens
+    path, kept, token = verify(dtype, target, None, given * B, [[-1] + [0] * (n - 1)] * B, torch.tensor(([0.0] + u) * B), torch.tensor(v))
+    for b in range(B):
+        want, last = ref.walk(target[:n], None, given, [-1] + [0] * (n - 1), torch.tensor([0.0] + u), v[b], 1.0)
+        assert path[b] == want + [-1] * (n - len(want)) and kept[b] == len(want) and token[b] == last, (b, path[b], want, token[b], last)
+    return kept, token
+
+
+@TYPES
+@PICKED
+@pytest.mark.parametrize("refused", [20, 40, 50, 64])
+def test_many_picked_tokens_are_refused(dtype, B, V, refused):
+    """each holds half of what the ones before it have left, down to 2^-64 of the row: what is then left decides about the next, and is what is drawn from"""
+    step = 0.6875                                                   # a token's share of what is left: 1 - e^-0.6875 = 0.497
+    scores = [-step * k for k in range(V if V < 100 else 200)]
+    v = [(0.3, 0.7, 0.95, 0.1, 0.55, 0.8, 0.2, 0.9)[b] for b in range(B)]
+    tokens = [min(k, len(scores) - 1) for k in range(64)]
+    kept, token = picked(dtype, B, V, scores, tokens, [0.75 if k < refused else 0.25 for k in range(64)], v)
+    if refused < min(len(scores) - 4, 64):
+        assert kept == [2] * B                                      # the first that is not refused is taken
+    if refused == 64 and V > 100:
+        assert min(token) >= 64
+
+
+@TYPES
+@PICKED
+def test_picked_tokens_of_almost_all_probability_are_refused(dtype, B, V):
+    """random numbers just below 1: of the row 1e-7, 1e-14 and 1e-21 are left"""
+    top = 1 - 2.0 ** -24
+    for u, want in (([top, top, top, 0.5], [0, 4]), ([top, top, top, top], None)):
+        kept, token = picked(dtype, B, V, [0.0, -16.0, -32.0, -48.0, -64.0, -64.0], [0, 1, 2, 3] + [-1] * 60, u + [0.0] * 60, [0.75] * B)
+        assert kept == [2 if want else 1] * B and (want or token == [5] * B)
