@@ -152,8 +152,12 @@ def _ptr(t) -> Optional[int]:
 def _stream(stream) -> Optional[int]:
     if stream is None:
         import torch
-        # the handle alone: torch.cuda.current_stream() makes an object of it, 2.7 us of a call's host time beside 0.4
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) or None
+        # the handle alone: torch.cuda.current_stream() makes an object of it, 2.7 us of a call's host time beside 0.4.  The function is torch's own
+        # affair: a torch that lacks it has the object
+        handle = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        if handle is not None:
+            return handle(torch.cuda.current_device()) or None
+        stream = torch.cuda.current_stream()
     return stream.cuda_stream or None
 
 
