@@ -162,7 +162,7 @@ dipaco_status dipaco_k_draft_tree(const int32_t* parent, const int32_t* row_star
  * its bit of `seen` is set; window >= max_new, so that no row's ancestor lies in front of its window.
  *   depth, seen  as dipaco_k_draft_tree writes them for the same max_new.  Others may be given: a depth is taken as the nearest in 0 .. i, bits
  *                of rows that the document does not have are ignored, and a row may see any others, or none.
- * Everything else, the workspace included, as in dipaco_k_attention_paged. */
+ * bf16: probabilities enter their product with 16 bits for every dh.  Everything else, the workspace included, as in dipaco_k_attention_paged. */
 size_t dipaco_k_attention_tree_workspace_bytes(int32_t T, int32_t B, int32_t max_new, int32_t H, int32_t H_kv, int32_t dh,
                                                int32_t page_size, int32_t pages_per_doc);
 dipaco_status dipaco_k_attention_tree(int32_t dtype, const void* qkv, const int32_t* row_start, const int32_t* cache_len, const int32_t* depth,

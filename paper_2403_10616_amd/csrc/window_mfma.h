@@ -13,7 +13,8 @@
 // in the same run 119), of 64 50 (51).
 //
 // Probabilities enter the second product as in attention_mfma.h: as two bf16 numbers, 16 bits in all, for head sizes 32 and 128 (the output's own rounding hides
-// the rest), rounded to bf16 for head size 64 (off by at most 2^-8 of each, as the output is).  Their sum is taken in fp32 before that, so
+// the rest), rounded to bf16 for head size 64 (off by at most 2^-8 of each, as the output is); as two for rows of a tree, whatever the head size (2 x 400 rows over 12000, window
+// 2048, 14 heads of 64, 33 -> 38 us, 1 x 16 over 1000 8.7 -> 9.5).  Their sum is taken in fp32 before that, so
 // that lse keeps fp32's digits.  Two numbers cost head size 128 a quarter to a third: 2 x up to 32768 positions, 16 heads on 4, window 4096, 1800 -> 2300 - 2450 us,
 // the gradient on 4 x up to 8000, window 1000, 945 -> 1130 - 1190; what splits a pair of them by a dot product instruction saved 2 % and was left out.
 #pragma once
@@ -148,7 +149,8 @@ __device__ __forceinline__ void attend_half(SoftmaxRow<DH>& x, const uint4 (&qf)
 #pragma unroll
   for (int e = 0; e < 16; e += 2) { s0 += st[e]; s1 += st[e + 1]; }
   x.l += s0 + s1;
-  const auto p0 = p_frag<split_p<DH>(), 0>(st), p1 = p_frag<split_p<DH>(), 8>(st);
+  constexpr bool SPLIT = split_p<DH>() || std::is_same<View, TreeView>::value;
+  const auto p0 = p_frag<SPLIT, 0>(st), p1 = p_frag<SPLIT, 8>(st);
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) {
     x.o[dt] = mfma_p(vf[dt][0], p0, x.o[dt]);
