@@ -182,7 +182,8 @@ dipaco_status dipaco_k_attention_tree(int32_t dtype, const void* qkv, const int3
  *     u q(x) < r(x): taken, and the walk goes on from there;
  *     else r <- max(r - q, 0) over its sum, and for distinct = 1 q(x) <- 0 and q <- q over its sum.
  *   draft = NULL: q is 1 at x and 0 elsewhere.  Where no child is taken the next token is the first y with r(0) + .. + r(y) > v; an r
- *   whose sum is 0 is softmax(target_node / temperature) again.  Decided in 64 bits.
+ *   whose sum is 0 is softmax(target_node / temperature) again.  Decided with 64-bit numbers, whose exponentials
+ *   are right to 2^-36 of themselves.
  *   path   device int32 [B, max_new]: row 0 and the rows taken, in order, then -1.   kept device int32 [B]: their number, 0 for a document
  *          without rows.   next device int32 [B]: the next token; -1 for a document without rows, and where the target's logits are no
  *          distribution (a NaN, a +inf, or nothing above -inf), where the walk ends.  Draft logits that are none: no child is taken.

@@ -1,7 +1,7 @@
 // Which drafted tokens stay, and the token behind them (include/dipaco_kernels.h has the rule): a workgroup walks a document's tree from row 0.
 //
 // A token hangs on a border (u q < r, a running sum above v times the whole), so exponentials, sums and what is left of the target are 64-bit numbers: then
-// neither the order of a sum nor an exponential's last digits (2^-37 here) decide more than one draw in a million.
+// neither the order of a sum nor an exponential's last digits (2^-36 here) decide more than one draw in a million.
 //
 // A row of scores is cut into up to 32 parts of whole 1024 scores, a wave each: largest score, sum of exponentials against it.  From these the row's
 // sum is formed, and the part that a drawn token lies in is found without reading the others again; only parts that hold refused tokens are summed anew.
@@ -23,7 +23,8 @@ namespace {
 constexpr int DV_THREADS = 512, DV_WAVES = DV_THREADS / 64, DV_PARTS = 32, DV_CHUNK = 1024;
 constexpr double DV_LEAST_LEFT = 1.0 / 1024;   // of a row: what differences of probabilities, right to 2^-36 of the row, may leave, to 2^-26 of itself
 
-// 2^t for t <= 0, to 2^-37 of it: 2^f = sum of (f ln 2)^k / k! for |f| <= 1/2, up to k = 9 (the next term is below 2^-37)
+// 2^t for t <= 0, to 2^-36 of it: 2^f = sum of (f ln 2)^k / k! for |f| <= 1/2, up to k = 9 (those left out are below 2^-37 together, 2^-36.6 of the least 2^f; each
+// further one, 2^-5 of that, is an instruction more of 18)
 __device__ __forceinline__ double power_of_two(double t) {
   t = fmax(t, -1100.0);   // what is far below, -inf and NaN: 0 in 64 bits
   const double n = rint(t), f = t - n;
