@@ -575,18 +575,22 @@ __global__ void __launch_bounds__(DV_THREADS) __attribute__((amdgpu_waves_per_eu
   }
 }
 
-// Parts that are formed ahead of the walks: all rows' up to DV_ALL_PARTS; then parents' up to DV_MOST_PARTS, and up to DV_FEW_PARTS where documents have
-// DV_FEW_ROWS rows or fewer, of which a walk visits a large share.  Us, in the walk | parents ahead (both launches): 14656 parts (64 chains of up to 8) 150 | 45;
-// 19080 (24 trees of up to 40) 66 | 64; 65536 (32 trees of 64) 45 | 59.  A parent is found by loads of 2 us, which a call of few parts does without.
-constexpr int64_t DV_ALL_PARTS = 1 << 12, DV_MOST_PARTS = 1 << 14, DV_FEW_PARTS = 1 << 16;
-constexpr int DV_FEW_ROWS = 16;
+// Parts that are formed ahead of the walks: all rows' up to DV_ALL_PARTS, then parents' up to DV_DRAWN_PARTS, or DV_PICKED_PARTS where there are no draft scores: a
+// walk then forms a row once, not twice, and has no pass at a refusal, so that there is less to gain.  A parent is found by loads of 2 us.  32000 tokens, bf16 (f: fp32), chains or
+// trees ("level"), us in the walk | parents ahead | all ahead, both launches:
+//   draft scores, chains: 8 x 6, 3072 parts, 116 | 33.5 | 32.2;  16 x 8, 8192, 149 | 40.4 | 38.6;  8 x 40, 20480, 172 | 59 | 57;  64 x 8 f, 32768, 157 | 64 | 61;
+//     16 x 40, 40960, 230 | 84 | 78;  128 x 8, 65536, 168 | 99 | 90;  256 x 8, 131072, 171 | 163 | 151;  512 x 4, 131072, 174 | 185 | 174
+//   draft scores, trees: 24 x up to 40 f, distinct, 20011 tokens, 19080, 67 | 63 | 70;  8 x 64, 32768, 164 | 155 | 169;  32 x 16, 32768, 146 | 151 | 164;  16 x 64, 65536, 147 | 153 | 177
+//   picked, trees: 2 x 64, 4096, 58 | 33.5 | 25.4;  4 x 64, 8192, 32 | 28 | 31;  8 x 64, 16384, 46 | 34 | 41;  16 x 64, 32768, 53 | 43 | 55;  64 x 16, 32768, 39 | 41 | 52;
+//     32 x 64, 65536, 45 | 57 | 81;  128 x 16, 65536, 42 | 57 | 78
+constexpr int64_t DV_ALL_PARTS = 1 << 12, DV_PICKED_PARTS = 1 << 15, DV_DRAWN_PARTS = 1 << 16;
 
 }  // namespace
 
 // [documents][V] of what the target has left, then the parts: as many as a row of V scores or fewer may have (their number falls where they get longer)
 size_t draft_verify_workspace_bytes(int T_rows, int B, int V) {
   const int most = std::min(DV_PARTS, (V + DV_CHUNK - 1) / DV_CHUNK);
-  return (size_t)B * V * sizeof(double) + 16 + (size_t)std::min<int64_t>(2 * (int64_t)T_rows * most, DV_FEW_PARTS) * sizeof(PartStat);
+  return (size_t)B * V * sizeof(double) + 16 + (size_t)std::min<int64_t>(2 * (int64_t)T_rows * most, DV_DRAWN_PARTS) * sizeof(PartStat);
 }
 template <typename T> dipaco_status launch_draft_verify(const VerifyArgs<T>& a, hipStream_t s) {
   const Cut cut(a.V);
@@ -606,7 +610,7 @@ template <typename T> dipaco_status launch_draft_verify(const VerifyArgs<T>& a, 
     return a.rate == 0.0 ? run(std::true_type{}) : run(std::false_type{});
   };
   using std::integral_constant;
-  if (n == 0 || n > (a.T_rows <= (int64_t)DV_FEW_ROWS * a.B ? DV_FEW_PARTS : DV_MOST_PARTS)) return walk(integral_constant<Ahead, NO_ROWS>{});
+  if (n == 0 || n > (a.draft ? DV_DRAWN_PARTS : DV_PICKED_PARTS)) return walk(integral_constant<Ahead, NO_ROWS>{});
   if (n <= DV_ALL_PARTS) {
     draft_verify_parts<T><<<(int)((n + 3) / 4), 256, 0, s>>>(a, parts, n_rows, Divisor(cut.count));
     DIPACO_LAUNCH_CHECK();

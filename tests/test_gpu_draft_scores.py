@@ -9,15 +9,32 @@ from test_gpu_window import TDT
 
 pytestmark = pytest.mark.gpu
 
-# Documents whose rows' sums are formed ahead of the walks: all rows', those of rows with children (documents of few rows, more than 4096 parts of a
-# thousand scores), none (documents of many rows, more than 16384 parts)
-AHEAD = pytest.mark.parametrize("counts", [[6, 3, 0, 9], [7, 16, 0, 12] * 8, [40, 33, 37] * 7])
+# Documents whose rows' sums are formed ahead of the walks, at 32000 tokens: all rows', those of rows with children (more than 4096 parts of a thousand scores),
+# none (more than 65536, without draft scores 32768)
+MANY = [40, 33, 37] * 10
+AHEAD = pytest.mark.parametrize("counts", [[6, 3, 0, 9], [7, 16, 0, 12] * 8, MANY])
 
 
 def keep_top(scores, k, value):
     """all but the k largest scores of each row are `value`"""
     least = torch.topk(scores.float(), k, 1).values[:, -1:]
     scores[scores.float() < least] = value
+
+
+@TYPES
+@MODES
+@pytest.mark.parametrize("shape,temperature", [("level", 0.8), ("deep", 0.0), ("chain", 1.0)])
+def test_many_rows_whose_sums_are_formed_in_the_walk(dtype, mode, shape, temperature):
+    lengths = check_verify(dtype, MANY, shape, 32000, mode, temperature, near=0.3, seed=25)
+    assert mode == "picked" or max(lengths) > 1                     # drawn drafts do stay
+
+
+@TYPES
+@MODES
+@pytest.mark.parametrize("counts,shape", [([40] * 8, "chain"), ([40, 64, 0, 33] * 3, "deep")])
+def test_long_chains_whose_sums_are_formed_ahead(dtype, mode, counts, shape):
+    """more than 16 rows a document, up to 65536 parts"""
+    check_verify(dtype, counts, shape, 32000, mode, 0.9, near=0.3, seed=26)
 
 
 @TYPES
@@ -47,14 +64,14 @@ def test_rows_of_one_value(dtype, mode, counts, value, temperature):
         target[0::3] = value
         draft[0::2] = value
 
-    check_verify(dtype, counts, "level", 25001, mode, temperature, draft_temperature=temperature, special=special, seed=22)
+    check_verify(dtype, counts, "level", 32000, mode, temperature, draft_temperature=temperature, special=special, seed=22)
 
 
 @TYPES
 @MODES
-@pytest.mark.parametrize("temperature", [1e-5, 1e-12, 1e-20, 1e-38, 1e-45])
-@pytest.mark.parametrize("V,counts", [(300, [6, 3, 20]), (32000, [6, 3]), (32000, [40, 33, 37] * 7)])
-def test_temperatures_near_zero(dtype, mode, temperature, V, counts):
+@pytest.mark.parametrize("V,counts,temperature", [(V, c, t) for t in (1e-5, 1e-12, 1e-20, 1e-38, 1e-45) for V, c in ((300, [6, 3, 20]), (32000, [6, 3]))] +
+                         [(32000, [16, 9, 12] * 8, 1e-12), (32000, MANY, 1e-20)])
+def test_temperatures_near_zero(dtype, mode, V, counts, temperature):
     """of the target and of the draft: all probability at the largest score, shared by those that equal it"""
     def special(target, draft):
         draft += 9.1
@@ -69,7 +86,7 @@ def test_temperatures_near_zero(dtype, mode, temperature, V, counts):
 
 
 # documents of 65 rows in vocabularies of many parts, as AHEAD: all rows' sums ahead, those of rows with children, none
-PICKED = pytest.mark.parametrize("B,V", [(1, 60), (1, 32000), (4, 32000), (8, 32000)])
+PICKED = pytest.mark.parametrize("B,V", [(1, 60), (1, 32000), (4, 32000), (16, 32000)])
 
 
 def picked(dtype, B, V, scores, tokens, u, v):
@@ -93,7 +110,7 @@ def test_many_picked_tokens_are_refused(dtype, B, V, refused):
     """each holds half of what the ones before it have left, down to 2^-64 of the row: what is then left decides about the next, and is what is drawn from"""
     step = 0.6875                                                   # a token's share of what is left: 1 - e^-0.6875 = 0.497
     scores = [-step * k for k in range(V if V < 100 else 200)]
-    v = [(0.3, 0.7, 0.95, 0.1, 0.55, 0.8, 0.2, 0.9)[b] for b in range(B)]
+    v = [(0.3, 0.7, 0.95, 0.1, 0.55, 0.8, 0.2, 0.9)[b % 8] for b in range(B)]
     tokens = [min(k, len(scores) - 1) for k in range(64)]
     kept, token = picked(dtype, B, V, scores, tokens, [0.75 if k < refused else 0.25 for k in range(64)], v)
     if refused < min(len(scores) - 4, 64):
