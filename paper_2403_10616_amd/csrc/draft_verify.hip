@@ -8,8 +8,8 @@
 //
 // Bound: a document's walk is a chain of decisions in one compute unit.  There a row of 32000 scores takes 10 us, of which its 64-bit exponentials, 18 instructions
 // each, are most, and a refusal by draft scores, which forms two of them for every token, 15.  So few rows' sums are formed by a launch of the whole chip ahead
-// of the walks, whose decisions then cost 1.3 us each, reads of LDS one behind the other.  Us, 32000 tokens: one chain of 6, bf16, 4 + 11; 64 chains of up to 8,
-// fp32, draft scores, 16 + 29; 32 trees of 64, bf16, 45; 24 trees of up to 40 with distinct siblings, 20011 tokens fp32, 67.
+// of the walks, whose decisions then cost 1.3 us each, reads of LDS one behind the other.  Us, 32000 tokens: one chain of 6, bf16, 4 + 12; 64 chains of up to 8,
+// fp32, draft scores, 16 + 28; 32 trees of 64, bf16, 46; 24 trees of up to 40 with distinct siblings, 20011 tokens fp32, 13 + 51.
 #include <algorithm>
 #include <type_traits>
 

@@ -173,7 +173,7 @@ template <typename T> PagedPlan plan(const PagedArgs<T>& a, int dh, bool tree) {
     p.narrow_splits = (int)half;
     p.narrow_keys = 2 * PagedCut<T>::LEAST_KEYS;
     // Rows of a tree: one split where its waves (eight, four for wide heads) have at most 256 keys each, without a launch that joins splits.  Us, two splits | one:
-    // 16 rows, 14 heads of 64, over 1000 12.0 | 9.6, over 2000 12.2 | 12.2, over 3000 12.4 | 15.9; 8 documents of these over 2000 17.5 | 15.1.
+    // 16 rows, 14 heads of 64, over 1000 11.5 | 9.7, over 2000 12.9 | 13.7, over 3000 13.1 | 18.1; 8 documents of these over 1000 12.8 | 10.8, over 2000 18.0 | 15.9.
     const int one = (dh == 128 ? 1 : 2) * p.narrow_keys;
     if (tree && seen <= one) {
       p.narrow_splits = 1;
@@ -187,8 +187,8 @@ template <typename T> PagedPlan plan(const PagedArgs<T>& a, int dh, bool tree) {
   const int room = (int)std::min<size_t>(PAGED_MOST_SPLITS, partial_rows(a.T_rows, a.H, (int64_t)page_size * a.pages_per_doc, tree) / a.T_rows);
   p.narrow_splits = std::min(p.narrow_splits, room);
   // Documents of up to 4096 keys and more may differ by as much as a launch takes.  Us, splits of equal shares of their documents | of equal length: 32 documents of up to 64
-  // rows over up to 16000, 16 heads of 128 on 4, 201 | 173; 16 x 32 over 8000 each 79 | 83; 8 x 64 over 4000 each, 14 heads of 64, 37 | 34; 2 x 400 over 2048 of
-  // 12000 34 | 38, one of 64 over 16000 23 | 24.5: a plan costs each workgroup's start and the join a microsecond.
+  // rows over up to 16000, 16 heads of 128 on 4, 209 | 165; 16 x 32 over 8000 each 78 | 79; 8 x 64 over 4200 each, 14 heads of 64, 42 | 37; 16 x up to 64 over up to 16000 128 | 109;
+  // 2 x 400 over 2048 of 12000 38.5 | 41, one of 64 over 16000 26.6 | 28: a plan costs each workgroup's start and the join a microsecond.
   p.balanced = tree && std::is_same<T, bf16>::value && a.B > 1 && a.B <= TREE_DOCUMENTS && seen >= 4096 && p.wide_blocks > 0;
   p.wide_splits = p.balanced ? room : std::min(p.wide_splits, room);
   return p;

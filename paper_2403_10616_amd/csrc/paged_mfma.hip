@@ -9,8 +9,8 @@
 // for few keys, latency (one document of 1000, 14 heads of 64: 9 us, a microsecond each for the document's rows and length, the pages, the first keys, the
 // join).  Chunks: as window_mfma.h, and a workgroup's start and end (6000 and 3500 cycles beside 2250 a tile of head size 64): 1 x 512 tokens over 8000, 16
 // heads of 128 on 4, 76 us with the join (455 TFLOP/s); 4 x up to 512 (1253 in all) over up to 12000, 14 heads of 64, window 2048, 28 without it.  Trees: 1 x 16 rows
-// over 1000, 14 heads of 64, 9.5; 32 x up to 64 over up to 16000, 16 heads of 128 on 4, 151 - 173 and the join's 13 (matrix cores 0.38 and vector ALU 0.35 of the cycles
-// of the units at work; blocks of 128 rows are two thirds full); 2 x 400 over 12000, window 2048, 14 heads of 64, 29 and 6.
+// over 1000, 14 heads of 64, 10; 32 x up to 64 over up to 16000, 16 heads of 128 on 4, 152 - 165 and the join's 13 (matrix cores 0.38 and vector ALU 0.35 of the cycles
+// of the units at work; blocks of 128 rows are two thirds full); 2 x 400 over 12000, window 2048, 14 heads of 64, 35 and 6.
 #include "kernels.h"
 #include "window_mfma.h"
 
