@@ -5,6 +5,7 @@ import torch
 import draft_reference as ref
 import paper_2403_10616_amd as dp
 from test_gpu_drafts import MODES, TYPES, check_verify, verify
+from test_gpu_paged import guarded_workspace
 from test_gpu_window import TDT
 
 pytestmark = pytest.mark.gpu
@@ -127,3 +128,18 @@ def test_picked_tokens_of_almost_all_probability_are_refused(dtype, B, V):
     for u, want in (([top, top, top, 0.5], [0, 4]), ([top, top, top, top], None)):
         kept, token = picked(dtype, B, V, [0.0, -16.0, -32.0, -48.0, -64.0, -64.0], [0, 1, 2, 3] + [-1] * 60, u + [0.0] * 60, [0.75] * B)
         assert kept == [2 if want else 1] * B and (want or token == [5] * B)
+
+
+@pytest.mark.parametrize("draft,rows", [(True, 32), (False, 33), (False, 32)])
+def test_the_workspace_of_many_parts_is_as_large_as_it_is_said_to_be(draft, rows):
+    """65536 parts of rows with draft scores, the most that are formed ahead, and a few more and a few less than the most without"""
+    B, V, g = 32, 32000, torch.Generator().manual_seed(5)
+    T = B * rows
+    target = 8 * torch.randn(T, V, generator=g)
+    scores = target + 0.3 * torch.randn(T, V, generator=g) if draft else None
+    args = (dp.F32, target, scores, target.argmax(1).roll(1).tolist(), [list(range(-1, rows - 1))] * B, torch.rand(T, generator=g), torch.rand(B, generator=g))
+    n = dp.dipaco_k_draft_verify_workspace_bytes(T, B, V)
+    whole, ws = guarded_workspace(n)
+    got = verify(*args, ws=ws)
+    assert got == verify(*args) and max(got[1]) > 2
+    assert bool((whole[:4096] == 170).all()) and bool((whole[4096 + n:] == 170).all())
