@@ -578,7 +578,7 @@ __global__ void __launch_bounds__(DV_THREADS) __attribute__((amdgpu_waves_per_eu
 // Parts that are formed ahead of the walks: all rows' up to DV_ALL_PARTS, then parents' up to DV_DRAWN_PARTS, or DV_PICKED_PARTS where there are no draft scores: a
 // walk then forms a row once, not twice, and has no pass at a refusal, so that there is less to gain.  A parent is found by loads of 2 us.  32000 tokens, bf16 (f: fp32), chains or
 // trees ("level"), us in the walk | parents ahead | all ahead, both launches:
-//   draft scores, chains: 8 x 6, 3072 parts, 116 | 33.5 | 32.2;  16 x 8, 8192, 149 | 40.4 | 38.6;  8 x 40, 20480, 172 | 59 | 57;  64 x 8 f, 32768, 157 | 64 | 61;
+//   draft scores, chains: 8 x 6, 116 | 33.5 | 32.2;  16 x 8, 8192 parts, 149 | 40.4 | 38.6;  8 x 40, 20480, 172 | 59 | 57;  64 x 8 f, 32768, 157 | 64 | 61;
 //     16 x 40, 40960, 230 | 84 | 78;  128 x 8, 65536, 168 | 99 | 90;  256 x 8, 131072, 171 | 163 | 151;  512 x 4, 131072, 174 | 185 | 174
 //   draft scores, trees: 24 x up to 40 f, distinct, 20011 tokens, 19080, 67 | 63 | 70;  8 x 64, 32768, 164 | 155 | 169;  32 x 16, 32768, 146 | 151 | 164;  16 x 64, 65536, 147 | 153 | 177
 //   picked, trees: 2 x 64, 4096, 58 | 33.5 | 25.4;  4 x 64, 8192, 32 | 28 | 31;  8 x 64, 16384, 46 | 34 | 41;  16 x 64, 32768, 53 | 43 | 55;  64 x 16, 32768, 39 | 41 | 52;
